@@ -889,6 +889,160 @@ int asym_mla_set_workgroup_form(int level);
 int asym_mla_decode_plan(const asym_topology* topo, int B, int H_q, int S_k, int split_tokens,
                          int mapping, uint32_t xcd_mask, void* stream, asym_mla_plan_info* out);
 
+/* ---- prompt attention ----------------------------------------------------- */
+/* Attention of whole prompts, or of chunks of them behind a cached prefix, over
+ * packed sequences with grouped key/value heads: sequence b has the query rows
+ * cu_q[b] .. cu_q[b + 1] - 1 of q and the key rows cu_k[b] .. cu_k[b + 1] - 1 of K
+ * and V; for its row i and query head h, with g = h / (H_q / H_kv),
+ *   O[i][h] = softmax_j(scale * q[i][h] . K[j][g]) . V[j][g]
+ *   lse[i][h] = log sum_j exp(scale * q[i][h] . K[j][g])   (nullable output)
+ * over all keys j of the sequence, or, if causal is not 0, over j <= i + L_k - L_q
+ * (the last query sees the last key).  A row that sees no key has O = 0 and
+ * lse = -infinity.  What a row does not see (later keys, other sequences' rows)
+ * does not reach it, whatever it holds, infinities and NaN included.
+ * Layout (caller-owned device memory): q [T_q][H_q][128], K and V [T_k][H_kv][128],
+ * bf16, with the given strides in values between tokens and between heads
+ * (multiples of 8; K's and V's token strides 128 to 2^23), so that the parts of
+ * a fused projection's output are taken as they lie; O [T_q][H_q][128] bf16 and
+ * lse [T_q][H_q] fp32 contiguous.  cu_q and cu_k: device int32 [B + 1], not
+ * falling; held within [0, T_q] and [0, T_k] whatever they say.  Rows of O and lse
+ * outside every sequence are left as they are.  D must be 128; q, K, V and O
+ * 16-byte aligned.  H_q / H_kv may be any whole number.
+ * One launch, no workspace, no host synchronisation; may be captured.  mapping:
+ * AWARE keeps the tiles that read one key/value head on one XCD where the head
+ * count divides by the XCDs or the other way round (its keys and values cross
+ * into one L2); the oblivious mappings number them head by head.  Longest tiles
+ * first in every mapping, and every mapping gives the same bits.  Runs on the
+ * stream's CU set; asynchronous.
+ * Errors: ASYM_EINVAL, ASYM_EUNSUPPORTED, ASYM_EHIP. */
+int asym_attn_prefill_bf16(int B, int H_q, int H_kv, int D, int T_q, int T_k,
+                           const void* q, int64_t q_token, int64_t q_head,
+                           const void* k, int64_t k_token, int64_t k_head,
+                           const void* v, int64_t v_token, int64_t v_head,
+                           void* o, float* lse, const int32_t* cu_q, const int32_t* cu_k,
+                           float scale, int causal, int mapping, void* stream);
+
+/* ---- paged cache in microscaled 4-bit floating point ---------------------- */
+/* A page (ASYM_FP4_PAGE_BYTES) holds 32 consecutive tokens of one head, keys or
+ * values, in 4.25 bits a value.  Format: a block is 32 consecutive channels of one
+ * token; with e the bf16 exponent field of its largest magnitude, its scale byte
+ * is s = max(e, 4) - 2, for 2^(s - 127), and each value is held as the 4-bit float
+ * (0, 0.5, 1, 1.5, 2, 3, 4, 6 and their negatives; code = 8 * sign + index)
+ * nearest to value / 2^(s - 127), ties to the even code, saturated at 6.  A block
+ * that holds an infinity or a NaN has s = 255 and codes 0, and reads as NaN.
+ * Layout of a page, token t, channel c, block b = c / 32:
+ *   keys:   code in nibble c % 2 (0 the low one) of byte 64 t + c / 2;
+ *           scale in byte 2048 + 2 (t % 16 + 16 b) + t / 16;
+ *   values: with q = t % 16 / 4 and j = t % 4 + 4 (t / 16), code in nibble j % 2 of
+ *           byte 1024 (c / 64) + 16 (c % 16 + 16 q) + 4 (c / 16 % 4) + j / 2;
+ *           scale in byte 2048 + 32 q + 4 j + b.
+ * Pools: [pool_pages][ASYM_FP4_PAGE_BYTES], 16-byte aligned, any size.  Tables:
+ * device int32 [B][H_kv][pages_per_head], the page of each (request, head, 32
+ * tokens); k_pages and v_pages may be one table.  An entry outside [0, pool_pages)
+ * is not written, and reads as zeros. */
+#define ASYM_FP4_PAGE_BYTES 2176
+
+/* Quantise tokens into the cache: request b's n = cu[b + 1] - cu[b] tokens, rows
+ * cu[b] .. of K and V [T][H_kv][128] bf16 (strides as in asym_attn_prefill_bf16),
+ * become its positions start[b] .. start[b] + n - 1.  cu: device int32 [B + 1], held
+ * within [0, T]; start: device int32 [B], >= 0 (a request with a negative one is
+ * left out; positions behind the table too).  Everything else that the pages hold
+ * stays.  A page that two requests of one call write (shared pages) ends up with
+ * bytes of both: fork first.  One launch, asynchronous, may be captured.
+ * Errors: ASYM_EINVAL, ASYM_EUNSUPPORTED, ASYM_EHIP. */
+int asym_kv_write_fp4(int B, int H_kv, int T, const void* k, int64_t k_token, int64_t k_head,
+                      const void* v, int64_t v_token, int64_t v_head,
+                      void* k_pool, void* v_pool, size_t pool_pages,
+                      const int32_t* k_pages, const int32_t* v_pages, int pages_per_head,
+                      const int32_t* cu, const int32_t* start, void* stream);
+
+/* The reverse: positions start[b] .. of request b, as bf16 (exact), into rows cu[b]
+ * .. of K and V [T][H_kv][128] contiguous: what a chunk's asym_attn_prefill_bf16
+ * needs of the prefix before it.  Rows outside every request, and positions
+ * behind the table, are left as they are.  Errors: as asym_kv_write_fp4. */
+int asym_kv_read_fp4(int B, int H_kv, int T, const void* k_pool, const void* v_pool, size_t pool_pages,
+                     const int32_t* k_pages, const int32_t* v_pages, int pages_per_head,
+                     const int32_t* cu, const int32_t* start, void* k, void* v, void* stream);
+
+/* Decode attention over the 4-bit cache, a length per request: for request b and
+ * query head h, with g = h / (H_q / H_kv) and t < lens[b],
+ *   O[b][h] = softmax_t(scale * q[b][h] . K[b][g][t]) . V[b][g][t]
+ *   lse[b][h] = log sum_t exp(scale * q[b][h] . K[b][g][t])   (nullable output)
+ * K and V the values that the pages hold.  q and O [B][H_q][128] bf16 contiguous,
+ * 16-byte aligned, lse fp32 [B][H_q]; lens: device int32 [B], held within [0,
+ * S_max]; S_max at most 32 * pages_per_head.  A request of length 0 has O = 0 and
+ * lse = -infinity.  Nothing at or behind a request's length reaches its result.
+ * D must be 128, H_q / H_kv any whole number up to 16.
+ * The sequence is cut into splits of split_tokens tokens (a multiple of 32 up to
+ * 2048; 0: automatic, from B, H_kv and S_max); a second launch joins the splits
+ * that a request's length reaches, in an order fixed by it.  The fp32 partials lie in the
+ * caller's workspace (16-byte aligned; asym_attn_decode_paged_fp4_plan's
+ * workspace_bytes, 0 with one split), which calls that may overlap must not share.
+ * No host synchronisation; may be captured.  Runs on the stream's CU set;
+ * asynchronous.  Errors: ASYM_EINVAL, ASYM_EUNSUPPORTED, ASYM_EHIP. */
+int asym_attn_decode_paged_fp4(int B, int H_q, int H_kv, int S_max, int D, const void* q,
+                               const void* k_pool, const void* v_pool, size_t pool_pages,
+                               const int32_t* k_pages, const int32_t* v_pages, int pages_per_head,
+                               const int32_t* lens, void* o, float* lse, float scale, int split_tokens,
+                               void* workspace, size_t workspace_bytes, void* stream);
+
+/* What asym_attn_decode_paged_fp4 would launch (host only; n_xcds, tasks_per_xcd
+ * and dense_static are 0). */
+int asym_attn_decode_paged_fp4_plan(int B, int H_q, int H_kv, int S_max, int D, int split_tokens,
+                                    asym_attn_plan_info* out);
+
+/* ---- pages of a paged cache ------------------------------------------------ */
+/* Taking, sharing, copying and giving up the pages of a cache on the device, for
+ * caches of either page size (8 KiB pages of asym_attn_decode_paged_bf16,
+ * ASYM_FP4_PAGE_BYTES).  State, all caller-owned device int32:
+ *   table [R][H][pages_per_head]: the page of each (row, head, 32 tokens), -1 where
+ *     there is none; lens [R]: tokens of each row; refs [pool_pages]: how many table
+ *     entries name a page (0: it is free).
+ * A row is a request's; the pages of lens[r] tokens are the first ceil(lens[r] / 32)
+ * entries of each head.  A cache whose keys and values share a table has one
+ * state and two pools; with a table each it has two states.  Requests of a call
+ * (n, device int32 arrays) that name a row outside [0, R), or one that an earlier
+ * request of the call names (as a target), are left out.
+ * status (device int32 [2], nullable): see each call.  Results do not depend on
+ * timing.  No host synchronisation; may be captured; asynchronous.  The workspace
+ * (asym_kv_pages_workspace bytes, 16-byte aligned) must not be shared by calls that
+ * may overlap; it need not be kept or cleared between them.
+ * Errors: ASYM_EINVAL, ASYM_EUNSUPPORTED, ASYM_EHIP. */
+enum asym_kv_op { ASYM_KV_EXTEND = 0, ASYM_KV_FORK = 1, ASYM_KV_COMPACT = 2 };
+int asym_kv_pages_workspace(int op, int R, int H, int pages_per_head, size_t pool_pages, int n,
+                            size_t* bytes);
+
+/* Rows grow: row rows[i] gets pages up to new_lens[i] tokens, the lowest free ones in
+ * the order of requests, heads, tokens.  A new length that is no longer than the row's,
+ * or does not fit the table, leaves it as it is.  status: pages taken, 0; if there are
+ * too few free pages nothing changes and status is 0, the number lacking. */
+int asym_kv_extend(int R, int H, int pages_per_head, int32_t* table, int32_t* lens, int32_t* refs,
+                   size_t pool_pages, int n, const int32_t* rows, const int32_t* new_lens,
+                   int32_t* status, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Row dst[i] becomes a copy of row src[i] as it was before the call (so rows may
+ * change places in one call): whole pages are shared, a part page at the end is
+ * copied into the lowest free page (in the order of requests, heads), so that both
+ * rows can grow; what row dst[i] held is given up afterwards.  src[i] = dst[i] is left
+ * as it is.  v_pool nullable.  Pages of page_bytes (a multiple of 16).  status: pages
+ * taken, 0; if there are too few free pages nothing changes and status is 0, the
+ * number lacking (pages that the call itself gives up do not count as free). */
+int asym_kv_fork(int R, int H, int pages_per_head, int32_t* table, int32_t* lens, int32_t* refs,
+                 void* k_pool, void* v_pool, size_t page_bytes, size_t pool_pages, int n,
+                 const int32_t* src, const int32_t* dst, int32_t* status, void* workspace,
+                 size_t workspace_bytes, void* stream);
+
+/* Rows end: their references are given up, their entries become -1, lens 0. */
+int asym_kv_free(int R, int H, int pages_per_head, int32_t* table, int32_t* lens, int32_t* refs,
+                 size_t pool_pages, int n, const int32_t* rows, void* stream);
+
+/* With n pages in use, those at or above n move, in order, into the free ones below n, in
+ * order; counts and table entries follow.  v_pool nullable.  Pages given up keep
+ * their bytes.  status: pages moved, pages in use (all below it now). */
+int asym_kv_compact(int R, int H, int pages_per_head, int32_t* table, int32_t* refs,
+                    void* k_pool, void* v_pool, size_t page_bytes, size_t pool_pages,
+                    int32_t* status, void* workspace, size_t workspace_bytes, void* stream);
+
 /* ---- streaming copy and co-run (Sections 7.2, 7.3) ---------------------- */
 /* The bandwidth-bound tenant of the co-location study (Section 7.3 runs a
  * second tenant on the complementary units): dst[i] = src[i] for n_bytes

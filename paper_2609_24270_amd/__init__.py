@@ -46,6 +46,9 @@ EXPORTS = (
     "asym_gemm_bf16_trace",
     "asym_gemm_plan", "asym_gemm_set_small_m",
     "asym_attn_decode_bf16", "asym_attn_decode_plan", "asym_attn_decode_paged_bf16", "asym_attn_pages_place", "asym_mla_decode_bf16", "asym_mla_decode_plan", "asym_mla_set_workgroup_form",
+    "asym_attn_prefill_bf16", "asym_kv_write_fp4", "asym_kv_read_fp4", "asym_attn_decode_paged_fp4",
+    "asym_attn_decode_paged_fp4_plan", "asym_kv_pages_workspace", "asym_kv_extend", "asym_kv_fork", "asym_kv_free",
+    "asym_kv_compact",
     "asym_copy_bf16", "asym_corun", "asym_last_error", "asym_version",
 )
 
@@ -217,6 +220,7 @@ def load_library(path: str = LIB_PATH):
     ip = ctypes.POINTER(ctypes.c_int)
     u32p = ctypes.POINTER(ctypes.c_uint32)
     topo_p = ctypes.c_void_p
+    i64, sz, f32 = ctypes.c_int64, ctypes.c_size_t, ctypes.c_float
     sig = {
         "asym_device_query": (i, [i, ctypes.POINTER(DeviceInfo)]),
         "asym_topology_cache_key": (i, [i, cp, ctypes.c_size_t, ctypes.POINTER(ctypes.c_size_t)]),
@@ -277,6 +281,16 @@ def load_library(path: str = LIB_PATH):
                                       ctypes.c_size_t, ip, i, ctypes.POINTER(ctypes.c_int32)]),
         "asym_mla_decode_bf16": (i, [topo_p, i, i, i, vp, vp, vp, vp, ctypes.c_float, i, i, u32, vp]),
         "asym_mla_decode_plan": (i, [topo_p, i, i, i, i, i, u32, vp, ctypes.POINTER(MlaPlanInfo)]),
+        "asym_attn_prefill_bf16": (i, [i] * 6 + [vp, i64, i64] * 3 + [vp] * 4 + [f32, i, i, vp]),
+        "asym_kv_write_fp4": (i, [i, i, i] + [vp, i64, i64] * 2 + [vp, vp, sz, vp, vp, i, vp, vp, vp]),
+        "asym_kv_read_fp4": (i, [i, i, i, vp, vp, sz, vp, vp, i, vp, vp, vp, vp, vp]),
+        "asym_attn_decode_paged_fp4": (i, [i] * 5 + [vp, vp, vp, sz, vp, vp, i, vp, vp, vp, f32, i, vp, sz, vp]),
+        "asym_attn_decode_paged_fp4_plan": (i, [i] * 6 + [ctypes.POINTER(AttnPlanInfo)]),
+        "asym_kv_pages_workspace": (i, [i, i, i, i, sz, i, ctypes.POINTER(sz)]),
+        "asym_kv_extend": (i, [i, i, i, vp, vp, vp, sz, i, vp, vp, vp, vp, sz, vp]),
+        "asym_kv_fork": (i, [i, i, i, vp, vp, vp, vp, vp, sz, sz, i, vp, vp, vp, vp, sz, vp]),
+        "asym_kv_free": (i, [i, i, i, vp, vp, vp, sz, i, vp, vp]),
+        "asym_kv_compact": (i, [i, i, i, vp, vp, vp, vp, sz, sz, vp, vp, sz, vp]),
         "asym_copy_bf16": (i, [topo_p, vp, vp, ctypes.c_size_t, i, vp, u32, vp]),
         "asym_corun": (i, [topo_p, ctypes.POINTER(Task), i, ctypes.POINTER(TaskResult)]),
         "asym_last_error": (cp, []),
@@ -1041,6 +1055,308 @@ def mla_decode_plan(B: int, Hq: int, S: int, split_tokens: int = 0, mapping="awa
     _check(load_library().asym_mla_decode_plan(topo.handle if topo else None, B, Hq, S, split_tokens, mp,
                                                xcd_mask, _stream_ptr(stream), ctypes.byref(out)))
     return out.to_dict()
+
+
+# ---- prompt attention, the 4-bit paged cache, its pages ---------------------------------
+
+FP4_PAGE_BYTES = 2176  # a page of 32 tokens of one head in microscaled 4-bit floating point
+KV_EXTEND, KV_FORK, KV_COMPACT = 0, 1, 2
+
+
+class _On:
+    """The device of a call's tensors as the current one, and the stream as torch's
+    current one (its allocations then belong to it); nothing where they are already."""
+
+    def __init__(self, device, stream):
+        import torch
+        self.stack = []
+        if device.index is not None and device.index != torch.cuda.current_device():
+            self.stack.append(torch.cuda.device(device))
+        if stream is not None:
+            self.stack.append(torch.cuda.stream(stream))
+
+    def __enter__(self):
+        for c in self.stack:
+            c.__enter__()
+
+    def __exit__(self, *e):
+        for c in reversed(self.stack):
+            c.__exit__(*e)
+
+
+def _on_gpu(what, first, *rest):
+    if not first.is_cuda or any(t.device != first.device for t in rest):
+        raise ValueError(f"{what}: the tensors must be on one GPU")
+
+
+def _index(t, what, shape=None):
+    import torch
+    if t.dtype != torch.int32:
+        raise TypeError(f"{what} must be int32")
+    if not t.is_contiguous() or (shape is not None and tuple(t.shape) != tuple(shape)):
+        raise ValueError(f"{what} must be contiguous" + (f" {list(shape)}" if shape is not None else ""))
+
+
+def _rows128(t, what):
+    """[T, H, 128] bf16 with unit stride in its last dimension: its strides."""
+    import torch
+    if t.dtype != torch.bfloat16:
+        raise TypeError(f"{what} must be bfloat16")
+    if t.dim() != 3 or t.shape[2] != 128 or t.stride(2) != 1:
+        raise ValueError(f"{what} must be [tokens, heads, 128] with unit stride in its last dimension")
+    T, H, _ = t.shape
+    # (a dimension of one has no stride to keep to)
+    return (t.stride(0) if T > 1 else H * 128), (t.stride(1) if H > 1 else 128)
+
+
+def _workspace(nbytes, device):
+    import torch
+    return torch.empty(max(nbytes, 16), dtype=torch.uint8, device=device)
+
+
+def attn_prefill(q, k, v, cu_q, cu_k=None, o=None, lse=None, scale: Optional[float] = None, causal: bool = True,
+                 mapping="aware", stream=None):
+    """Attention of packed prompts (or chunks of them behind a prefix): q
+    [T_q, H_q, 128], k and v [T_k, H_kv, 128] bf16 CUDA tensors, strided in their
+    first two dimensions as they like (views of a fused projection's output);
+    cu_q and cu_k int32 [B + 1] CUDA tensors, the sequences' first rows (cu_k
+    defaults to cu_q).  causal: row i of a sequence sees keys j <= i + L_k - L_q.
+    Returns O [T_q, H_q, 128] bf16 (and fills lse [T_q, H_q] fp32 when given); rows
+    outside every sequence are not written.  scale defaults to 1 / sqrt(128)."""
+    import math
+
+    import torch
+    if cu_k is None:
+        cu_k = cu_q
+    qt, qh = _rows128(q, "q")
+    kt, kh = _rows128(k, "k")
+    vt, vh = _rows128(v, "v")
+    if v.shape != k.shape:
+        raise ValueError("k and v must have one shape")
+    _index(cu_q, "cu_q")
+    _index(cu_k, "cu_k", cu_q.shape)
+    if cu_q.dim() != 1 or cu_q.numel() < 1:
+        raise ValueError("cu_q must be [B + 1]")
+    Tq, Hq, D = q.shape
+    Tk, Hkv, _ = k.shape
+    _on_gpu("attn_prefill", q, k, v, cu_q, cu_k, *(t for t in (o, lse) if t is not None))
+    if o is not None and (o.dtype != torch.bfloat16 or tuple(o.shape) != (Tq, Hq, D) or not o.is_contiguous()):
+        raise ValueError("o must be a contiguous bf16 [T_q, H_q, 128] tensor")
+    if lse is not None and (lse.dtype != torch.float32 or tuple(lse.shape) != (Tq, Hq) or not lse.is_contiguous()):
+        raise ValueError("lse must be a contiguous fp32 [T_q, H_q] tensor")
+    sc = 1.0 / math.sqrt(D) if scale is None else float(scale)
+    mp = MAPPINGS[mapping] if isinstance(mapping, str) else int(mapping)
+    with _On(q.device, stream):
+        if o is None:
+            o = torch.empty((Tq, Hq, D), dtype=torch.bfloat16, device=q.device)
+        _check(load_library().asym_attn_prefill_bf16(
+            cu_q.numel() - 1, Hq, Hkv, D, Tq, Tk, q.data_ptr(), qt, qh, k.data_ptr(), kt, kh, v.data_ptr(), vt, vh,
+            o.data_ptr(), lse.data_ptr() if lse is not None else None, cu_q.data_ptr(), cu_k.data_ptr(), sc,
+            1 if causal else 0, mp, _stream_ptr(stream)))
+    return o
+
+
+def _fp4_cache(k_pool, v_pool, k_pages, v_pages):
+    """Checks a 4-bit cache's pools and tables; (B, H_kv, pages per head)."""
+    import torch
+    if k_pool.dtype != torch.uint8 or v_pool.dtype != torch.uint8:
+        raise TypeError("pools must be uint8")
+    if k_pool.dim() != 2 or k_pool.shape[1] != FP4_PAGE_BYTES or v_pool.shape != k_pool.shape \
+            or not k_pool.is_contiguous() or not v_pool.is_contiguous():
+        raise ValueError("pools must be contiguous [pool_pages, 2176]")
+    _index(k_pages, "k_pages")
+    if k_pages.dim() != 3:
+        raise ValueError("page tables must be [B, H_kv, pages]")
+    _index(v_pages, "v_pages", k_pages.shape)
+    return tuple(k_pages.shape)
+
+
+def kv_write_fp4(k, v, k_pool, v_pool, k_pages, v_pages, cu, start, stream=None) -> None:
+    """Quantise tokens into a 4-bit paged cache: rows cu[b] .. cu[b + 1] - 1 of k and v
+    [T, H_kv, 128] (bf16, strided as in attn_prefill) become request b's positions
+    start[b] onwards.  Pools uint8 [pool_pages, 2176]; tables int32 [B, H_kv, pages];
+    cu int32 [B + 1], start int32 [B].  Pages must not be shared between requests."""
+    kt, kh = _rows128(k, "k")
+    vt, vh = _rows128(v, "v")
+    B, H, pph = _fp4_cache(k_pool, v_pool, k_pages, v_pages)
+    if k.shape != v.shape or k.shape[1] != H:
+        raise ValueError("k and v must be [T, H_kv, 128], H_kv as in the tables")
+    _index(cu, "cu", (B + 1,))
+    _index(start, "start", (B,))
+    _on_gpu("kv_write_fp4", k, v, k_pool, v_pool, k_pages, v_pages, cu, start)
+    with _On(k.device, stream):
+        _check(load_library().asym_kv_write_fp4(
+            B, H, k.shape[0], k.data_ptr(), kt, kh, v.data_ptr(), vt, vh, k_pool.data_ptr(), v_pool.data_ptr(),
+            k_pool.shape[0], k_pages.data_ptr(), v_pages.data_ptr(), pph, cu.data_ptr(), start.data_ptr(),
+            _stream_ptr(stream)))
+
+
+def kv_read_fp4(k_pool, v_pool, k_pages, v_pages, cu, start, k, v, stream=None):
+    """Read tokens of a 4-bit paged cache back as bf16 (exact): request b's positions
+    start[b] onwards into rows cu[b] .. cu[b + 1] - 1 of k and v [T, H_kv, 128]
+    (contiguous); returns (k, v)."""
+    import torch
+    B, H, pph = _fp4_cache(k_pool, v_pool, k_pages, v_pages)
+    for t, what in ((k, "k"), (v, "v")):
+        if t.dtype != torch.bfloat16:
+            raise TypeError(f"{what} must be bfloat16")
+        if t.dim() != 3 or tuple(t.shape[1:]) != (H, 128) or t.shape != k.shape or not t.is_contiguous():
+            raise ValueError("k and v must be contiguous [T, H_kv, 128]")
+    _index(cu, "cu", (B + 1,))
+    _index(start, "start", (B,))
+    _on_gpu("kv_read_fp4", k, v, k_pool, v_pool, k_pages, v_pages, cu, start)
+    with _On(k.device, stream):
+        _check(load_library().asym_kv_read_fp4(
+            B, H, k.shape[0], k_pool.data_ptr(), v_pool.data_ptr(), k_pool.shape[0], k_pages.data_ptr(),
+            v_pages.data_ptr(), pph, cu.data_ptr(), start.data_ptr(), k.data_ptr(), v.data_ptr(), _stream_ptr(stream)))
+    return k, v
+
+
+def attn_decode_paged_fp4(q, k_pool, v_pool, k_pages, v_pages, lens, S: Optional[int] = None, o=None, lse=None,
+                          scale: Optional[float] = None, split_tokens: int = 0, stream=None):
+    """Decode attention over a 4-bit paged cache: q [B, H_q, 128] bf16; pools uint8
+    [pool_pages, 2176]; tables int32 [B, H_kv, pages]; lens int32 [B], each request's
+    tokens, at most S (default: what the tables hold).  Returns O [B, H_q, 128] bf16
+    (and fills lse [B, H_q] fp32 when given)."""
+    import math
+
+    import torch
+    if q.dtype != torch.bfloat16:
+        raise TypeError("q must be bfloat16")
+    if q.dim() != 3 or q.shape[2] != 128 or not q.is_contiguous():
+        raise ValueError("q must be contiguous [B, H_q, 128]")
+    B, H, pph = _fp4_cache(k_pool, v_pool, k_pages, v_pages)
+    if q.shape[0] != B:
+        raise ValueError("q and the tables disagree on B")
+    Hq = q.shape[1]
+    _index(lens, "lens", (B,))
+    if S is None:
+        S = pph * PAGE_TOKENS
+    _on_gpu("attn_decode_paged_fp4", q, k_pool, v_pool, k_pages, v_pages, lens, *(t for t in (o, lse) if t is not None))
+    if o is not None and (o.dtype != torch.bfloat16 or tuple(o.shape) != (B, Hq, 128) or not o.is_contiguous()):
+        raise ValueError("o must be a contiguous bf16 [B, H_q, 128] tensor")
+    if lse is not None and (lse.dtype != torch.float32 or tuple(lse.shape) != (B, Hq) or not lse.is_contiguous()):
+        raise ValueError("lse must be a contiguous fp32 [B, H_q] tensor")
+    sc = 1.0 / math.sqrt(128) if scale is None else float(scale)
+    plan = AttnPlanInfo()
+    lib = load_library()
+    _check(lib.asym_attn_decode_paged_fp4_plan(B, Hq, H, S, 128, split_tokens, ctypes.byref(plan)))
+    nbytes = plan.workspace_bytes
+    with _On(q.device, stream):
+        if o is None:
+            o = torch.empty((B, Hq, 128), dtype=torch.bfloat16, device=q.device)
+        ws = _workspace(nbytes, q.device) if nbytes else None
+        _check(lib.asym_attn_decode_paged_fp4(
+            B, Hq, H, S, 128, q.data_ptr(), k_pool.data_ptr(), v_pool.data_ptr(), k_pool.shape[0], k_pages.data_ptr(),
+            v_pages.data_ptr(), pph, lens.data_ptr(), o.data_ptr(), lse.data_ptr() if lse is not None else None, sc,
+            split_tokens, ws.data_ptr() if nbytes else None, nbytes, _stream_ptr(stream)))
+    return o
+
+
+def attn_decode_paged_fp4_plan(B: int, Hq: int, Hkv: int, S: int, D: int = 128, split_tokens: int = 0) -> dict:
+    out = AttnPlanInfo()
+    _check(load_library().asym_attn_decode_paged_fp4_plan(B, Hq, Hkv, S, D, split_tokens, ctypes.byref(out)))
+    return out.to_dict()
+
+
+def _pages_state(what, table, lens, refs, *lists):
+    """Checks a paged cache's state and a call's request lists; (R, H, pages per head)."""
+    _index(table, "table")
+    if table.dim() != 3:
+        raise ValueError("table must be [R, H, pages]")
+    R, H, pph = table.shape
+    if lens is not None:
+        _index(lens, "lens", (R,))
+    _index(refs, "refs")
+    if refs.dim() != 1:
+        raise ValueError("refs must be [pool_pages]")
+    for t in lists:
+        if t is not None:
+            _index(t, "request lists and status")
+            if t.dim() != 1:
+                raise ValueError("request lists and status must have one dimension")
+    _on_gpu(what, table, refs, *(t for t in (lens, *lists) if t is not None))
+    return R, H, pph
+
+
+def _pools(what, k_pool, v_pool, refs):
+    """Checks the pools that a call moves pages of; (k pointer, v pointer, page bytes)."""
+    pools = [k_pool] if v_pool is None else [k_pool, v_pool]
+    _on_gpu(what, refs, *pools)
+    n = refs.shape[0]
+    for t in pools:
+        if t.dim() < 2 or t.shape[0] != n or not t.is_contiguous() or t.shape != k_pool.shape or t.dtype != k_pool.dtype:
+            raise ValueError("pools must be contiguous [pool_pages, ...], of one shape and type, pool_pages as in refs")
+    return k_pool.data_ptr(), (v_pool.data_ptr() if v_pool is not None else None), \
+        k_pool.numel() // max(n, 1) * k_pool.element_size()
+
+
+def _status(status):
+    if status is not None and status.numel() != 2:
+        raise ValueError("status must have 2 entries")
+    return status.data_ptr() if status is not None else None
+
+
+def _pages_workspace(op, R, H, pph, pool_pages, n, device):
+    nbytes = ctypes.c_size_t()
+    _check(load_library().asym_kv_pages_workspace(op, R, H, pph, pool_pages, n, ctypes.byref(nbytes)))
+    return _workspace(nbytes.value, device), nbytes.value
+
+
+def kv_extend(table, lens, refs, rows, new_lens, status=None, stream=None) -> None:
+    """Rows of a paged cache grow: row rows[i] of table [R, H, pages] gets the lowest free
+    pages up to new_lens[i] tokens; refs [pool_pages] and lens [R] follow.  All int32
+    CUDA tensors.  status [2]: pages taken and 0, or 0 and the number of pages lacking
+    (then nothing changes)."""
+    R, H, pph = _pages_state("kv_extend", table, lens, refs, rows, new_lens, status)
+    if rows.shape != new_lens.shape:
+        raise ValueError("rows and new_lens must have one shape")
+    st = _status(status)
+    with _On(table.device, stream):
+        ws, nbytes = _pages_workspace(KV_EXTEND, R, H, pph, refs.shape[0], rows.numel(), table.device)
+        _check(load_library().asym_kv_extend(
+            R, H, pph, table.data_ptr(), lens.data_ptr(), refs.data_ptr(), refs.shape[0], rows.numel(), rows.data_ptr(),
+            new_lens.data_ptr(), st, ws.data_ptr(), nbytes, _stream_ptr(stream)))
+
+
+def kv_fork(k_pool, v_pool, table, lens, refs, src, dst, status=None, stream=None) -> None:
+    """Row dst[i] of a paged cache becomes a copy of row src[i] as it was before the call:
+    whole pages shared, a part page at the end copied into the lowest free page; what
+    row dst[i] held is given up.  Pools [pool_pages, ...] (v_pool None: only one); the
+    rest as kv_extend."""
+    R, H, pph = _pages_state("kv_fork", table, lens, refs, src, dst, status)
+    if src.shape != dst.shape:
+        raise ValueError("src and dst must have one shape")
+    kp, vp, page = _pools("kv_fork", k_pool, v_pool, refs)
+    st = _status(status)
+    with _On(table.device, stream):
+        ws, nbytes = _pages_workspace(KV_FORK, R, H, pph, refs.shape[0], src.numel(), table.device)
+        _check(load_library().asym_kv_fork(
+            R, H, pph, table.data_ptr(), lens.data_ptr(), refs.data_ptr(), kp, vp, page, refs.shape[0], src.numel(),
+            src.data_ptr(), dst.data_ptr(), st, ws.data_ptr(), nbytes, _stream_ptr(stream)))
+
+
+def kv_free(table, lens, refs, rows, stream=None) -> None:
+    """Rows of a paged cache end: their pages' counts fall, their entries become -1."""
+    R, H, pph = _pages_state("kv_free", table, lens, refs, rows)
+    with _On(table.device, stream):
+        _check(load_library().asym_kv_free(
+            R, H, pph, table.data_ptr(), lens.data_ptr(), refs.data_ptr(), refs.shape[0], rows.numel(), rows.data_ptr(),
+            _stream_ptr(stream)))
+
+
+def kv_compact(k_pool, v_pool, table, lens, refs, status=None, stream=None) -> None:
+    """The n pages in use of a paged cache become pages 0 .. n - 1: those at or above n
+    move, in order, into the free ones below; refs and table follow (lens does not
+    change).  status [2]: pages moved, n."""
+    R, H, pph = _pages_state("kv_compact", table, lens, refs, status)
+    kp, vp, page = _pools("kv_compact", k_pool, v_pool, refs)
+    st = _status(status)
+    with _On(table.device, stream):
+        ws, nbytes = _pages_workspace(KV_COMPACT, R, H, pph, refs.shape[0], 0, table.device)
+        _check(load_library().asym_kv_compact(
+            R, H, pph, table.data_ptr(), refs.data_ptr(), kp, vp, page, refs.shape[0], st, ws.data_ptr(), nbytes,
+            _stream_ptr(stream)))
 
 
 # ---- copy and co-run --------------------------------------------------------------

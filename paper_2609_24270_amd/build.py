@@ -22,7 +22,8 @@ ARCH = "gfx950"
 SOURCES = ["capi.cpp", "topology.cpp", "topology_cache.cpp", "schedule.cpp", "corun.cpp", "affinity.cpp",
            "interleave.cpp", "kv_place.cpp", "numa_host.cpp",
            "gemm.hip", "gemm_skinny.hip", "attn_decode.hip", "probe.hip", "latency.hip", "copy.hip", "numa.hip",
-           "transpose.hip", "noalloc.hip", "mla_decode.hip"]
+           "transpose.hip", "noalloc.hip", "mla_decode.hip",
+           "attn_prefill.hip", "kv_fp4.hip", "attn_decode_fp4.hip", "kv_pages.hip"]
 
 COMMON = ["-O3", "-std=c++17", "-fPIC", f"--offload-arch={ARCH}",
           "-I", os.path.join(ROOT, "include"), "-Wall", "-Wno-unused-function"]
@@ -34,9 +35,11 @@ DEVICE_ONLY = ["-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]
 # mla_decode.hip: in the AGPR form the 128 output accumulators, which the
 # online softmax rescales with vector instructions, were copied between AGPRs
 # and VGPRs every 16-token block (256 moves per block); in the VGPR form they
-# stay put.  attn_decode.hip: the same, 8 moves per task.
+# stay put.  attn_decode.hip: the same, 8 moves per task.  attn_prefill.hip and
+# attn_decode_fp4.hip: their outputs are rescaled in the same way.
 _VGPR_FORM = ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]
-EXTRA = {"gemm.hip": _VGPR_FORM, "mla_decode.hip": _VGPR_FORM, "attn_decode.hip": _VGPR_FORM}
+EXTRA = {"gemm.hip": _VGPR_FORM, "mla_decode.hip": _VGPR_FORM, "attn_decode.hip": _VGPR_FORM,
+         "attn_prefill.hip": _VGPR_FORM, "attn_decode_fp4.hip": _VGPR_FORM}
 
 
 def hipcc() -> str:

@@ -1,0 +1,289 @@
+// Writing tokens into, and reading them back from, a paged cache in microscaled
+// 4-bit floating point (format and page layout: kv_fp4.h).
+//
+// A wave has one page of one head: the tokens of the call that fall into it.  A page
+// is written by one wave only, so that tokens that share a byte (values: two tokens
+// a byte) need no atomics; what a page holds of other tokens stays.
+#include <hip/hip_runtime.h>
+
+#include "internal.h"
+#include "kv_fp4.h"
+
+namespace asym {
+namespace {
+
+constexpr int kWaves = 4;
+
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+struct KvParams {
+  const uint16_t *k, *v;       // write: tokens [T][H][128], strides below
+  uint16_t *ko, *vo;           // read: [T][H][128]
+  int64_t k_tok, k_head, v_tok, v_head;
+  uint8_t *k_pool, *v_pool;
+  const int *k_pages, *v_pages;  // [B][H][pph]
+  const int *cu, *start;
+  int B, H, T, pph, pool_pages, ranks;
+};
+
+// The rank-th page that the call touches, over the sequences in order: its sequence,
+// its place in the sequence's tables, the sequence's first row and position, and its
+// tokens [lo, hi) of the page.  One wave.
+__device__ bool find_page(const KvParams& p, int rank, int& seq, int& page, int& row, int& lo, int& hi) {
+  const int lane = threadIdx.x & 63;
+  for (int c = 0; 64 * c < p.B; ++c) {
+    const int b = 64 * c + lane;
+    int s = 0, n = 0, at = 0, pages = 0;
+    if (b < p.B) {
+      packed_rows(p.cu, b, p.T, s, n);
+      at = p.start[b];
+      // positions before 0 or behind the tables have no page
+      const int64_t cap = (int64_t)p.pph * kKvPageTokens;
+      if (at < 0 || n < 1 || at >= cap) n = 0;
+      n = (int)min((int64_t)n, cap - at);
+      if (n > 0) pages = (at + n - 1) / kKvPageTokens - at / kKvPageTokens + 1;
+    }
+    const int upto = wave_scan_add(pages);
+    const unsigned long long in = __ballot(rank < upto);
+    if (in) {
+      const int l = __builtin_ctzll(in);
+      seq = 64 * c + l;
+      const int first = __builtin_amdgcn_readlane(upto - pages, l);
+      at = __builtin_amdgcn_readlane(at, l);
+      n = __builtin_amdgcn_readlane(n, l);
+      s = __builtin_amdgcn_readlane(s, l);
+      page = at / kKvPageTokens + (rank - first);
+      lo = max(at - page * kKvPageTokens, 0);
+      hi = min(at + n - page * kKvPageTokens, kKvPageTokens);
+      row = s + page * kKvPageTokens - at;  // of the page's token 0
+      return true;
+    }
+    rank -= __builtin_amdgcn_readlane(upto, 63);
+  }
+  return false;
+}
+
+// largest magnitude's bits over a group of 4 lanes; an infinity or a NaN stays the largest
+__device__ __forceinline__ uint32_t max4(uint32_t x) {
+  x = max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0xB1, 0xF, 0xF, true));  // quad_perm 1 0 3 2
+  return max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x4E, 0xF, 0xF, true));  // quad_perm 2 3 0 1
+}
+
+__device__ __forceinline__ uint32_t scale_byte(uint32_t top) {  // of a block's largest magnitude (bf16 bits)
+  const uint32_t e = top >> 7;
+  return e == 255u ? 255u : max(e, 4u) - 2u;
+}
+
+// two bf16 -> two codes in byte `sel` of a word (the hardware rounds to nearest even
+// and saturates, as the format says)
+template <int SEL>
+__device__ __forceinline__ uint32_t codes2(uint32_t old, uint32_t pair, float scale) {
+  return __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(old, __builtin_bit_cast(bf16x2, pair), scale, SEL);
+}
+__device__ __forceinline__ uint32_t codes8(u32x4 x, uint32_t s) {
+  if (s == 255u) return 0u;
+  const float f = __uint_as_float(s << 23);
+  uint32_t w = codes2<0>(0u, x[0], f);
+  w = codes2<1>(w, x[1], f);
+  w = codes2<2>(w, x[2], f);
+  return codes2<3>(w, x[3], f);
+}
+
+__global__ void __launch_bounds__(64 * kWaves) kv_write_kernel(KvParams p) {
+  __shared__ uint32_t tile[kWaves][kKvPageTokens][17];  // codes of 32 tokens (16 words each, one of padding)
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int item = blockIdx.x * kWaves + wave;
+  const int head = item % p.H;
+  int seq, page, row, lo, hi;
+  const bool any = item / p.H < p.ranks && find_page(p, item / p.H, seq, page, row, lo, hi);
+  if (!any) return;  // (no barriers below: LDS is the wave's own)
+  const size_t entry = ((size_t)seq * p.H + head) * p.pph + page;
+  const int kp = __builtin_amdgcn_readfirstlane(p.k_pages[entry]), vp = __builtin_amdgcn_readfirstlane(p.v_pages[entry]);
+  const int c16 = lane & 15, t4 = lane >> 4;  // 8 channels, one of four tokens
+  if (kp >= 0 && kp < p.pool_pages) {
+    uint8_t* dst = p.k_pool + (size_t)kp * kFp4PageBytes;
+    for (int t = t4; t < kKvPageTokens; t += 4) {
+      const bool on = t >= lo && t < hi;
+      u32x4 x = {};
+      if (on)
+        x = *reinterpret_cast<const u32x4*>(p.k + (int64_t)(row + t) * p.k_tok + (int64_t)head * p.k_head + 8 * c16);
+      uint32_t top = 0;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) top = max(top, max(x[e] & 0x7FFFu, (x[e] >> 16) & 0x7FFFu));
+      const uint32_t s = scale_byte(max4(top));
+      if (on) {
+        *reinterpret_cast<uint32_t*>(dst + 64 * t + 4 * c16) = codes8(x, s);
+        if ((c16 & 3) == 0) dst[kFp4ScaleOff + 2 * ((t & 15) + 16 * (c16 >> 2)) + (t >> 4)] = (uint8_t)s;
+      }
+    }
+  }
+  if (vp >= 0 && vp < p.pool_pages) {
+    uint8_t* dst = p.v_pool + (size_t)vp * kFp4PageBytes;
+    for (int t = t4; t < kKvPageTokens; t += 4) {
+      const bool on = t >= lo && t < hi;
+      u32x4 x = {};
+      if (on)
+        x = *reinterpret_cast<const u32x4*>(p.v + (int64_t)(row + t) * p.v_tok + (int64_t)head * p.v_head + 8 * c16);
+      uint32_t top = 0;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) top = max(top, max(x[e] & 0x7FFFu, (x[e] >> 16) & 0x7FFFu));
+      const uint32_t s = scale_byte(max4(top));
+      tile[wave][t][c16] = codes8(x, s);
+      if (on && (c16 & 3) == 0)
+        dst[kFp4ScaleOff + 32 * ((t & 15) >> 2) + 4 * ((t & 3) + 4 * (t >> 4)) + (c16 >> 2)] = (uint8_t)s;
+    }
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+    // lane (m, q): 8 words, of channels 16 g + m, tokens 4 q + 0 .. 3 and 16 + 4 q + 0 .. 3
+    const int m = lane & 15, q = lane >> 4;
+    uint32_t keep = 0;  // nibbles of tokens that are not written
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const int t = 4 * q + (j & 3) + 16 * (j >> 2);
+      if (t < lo || t >= hi) keep |= 0xFu << (4 * j);
+    }
+    if (keep != 0xFFFFFFFFu) {
+#pragma unroll
+      for (int g = 0; g < 8; ++g) {
+        uint32_t w = 0;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const int t = 4 * q + (j & 3) + 16 * (j >> 2), c = 16 * g + m;
+          w |= ((tile[wave][t][c >> 3] >> (4 * (c & 7))) & 0xFu) << (4 * j);
+        }
+        uint32_t* at = reinterpret_cast<uint32_t*>(dst + 1024 * (g >> 2) + 16 * lane + 4 * (g & 3));
+        if (keep) w = (w & ~keep) | (*at & keep);
+        *at = w;
+      }
+    }
+  }
+}
+
+// 8 codes of one scale -> 8 bf16
+__device__ __forceinline__ u32x4 values8(uint32_t w, uint32_t s) {
+  const float f = __uint_as_float(s == 255u ? 0x7FC00000u : s << 23);
+  u32x4 x;
+  x[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, f, 0));
+  x[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, f, 1));
+  x[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, f, 2));
+  x[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, f, 3));
+  return x;
+}
+
+__global__ void __launch_bounds__(64 * kWaves) kv_read_kernel(KvParams p) {
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int item = blockIdx.x * kWaves + wave;
+  const int head = item % p.H;
+  int seq, page, row, lo, hi;
+  if (item / p.H >= p.ranks || !find_page(p, item / p.H, seq, page, row, lo, hi)) return;
+  const size_t entry = ((size_t)seq * p.H + head) * p.pph + page;
+  const int kp = __builtin_amdgcn_readfirstlane(p.k_pages[entry]), vp = __builtin_amdgcn_readfirstlane(p.v_pages[entry]);
+  const bool k_in = kp >= 0 && kp < p.pool_pages, v_in = vp >= 0 && vp < p.pool_pages;  // else zeros
+  const uint8_t* ks = p.k_pool + (size_t)(k_in ? kp : 0) * kFp4PageBytes;
+  const uint8_t* vs = p.v_pool + (size_t)(v_in ? vp : 0) * kFp4PageBytes;
+  const int c16 = lane & 15, b = c16 >> 2;
+  for (int t = lane >> 4; t < kKvPageTokens; t += 4) {
+    if (t < lo || t >= hi) continue;
+    const int64_t out = ((int64_t)(row + t) * p.H + head) * kKvD + 8 * c16;
+    u32x4 x = {}, y = {};
+    if (k_in)
+      x = values8(*reinterpret_cast<const uint32_t*>(ks + 64 * t + 4 * c16),
+                  ks[kFp4ScaleOff + 2 * ((t & 15) + 16 * b) + (t >> 4)]);
+    if (v_in) {
+      const int q = (t & 15) >> 2, j = (t & 3) + 4 * (t >> 4);
+      uint32_t w = 0;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const int c = 8 * c16 + e;
+        const uint32_t byte = vs[1024 * (c >> 6) + 16 * ((c & 15) + 16 * q) + 4 * ((c >> 4) & 3) + (j >> 1)];
+        w |= ((byte >> (4 * (j & 1))) & 0xFu) << (4 * e);
+      }
+      y = values8(w, vs[kFp4ScaleOff + 32 * q + 4 * j + b]);
+    }
+    *reinterpret_cast<u32x4*>(p.ko + out) = x;
+    *reinterpret_cast<u32x4*>(p.vo + out) = y;
+  }
+}
+
+int kv_check(const char* what, int B, int H, int T, int pph, size_t pool_pages, const void* k_pool, const void* v_pool,
+             const void* k_pages, const void* v_pages, const void* cu, const void* start) {
+  const std::string w(what);
+  if (B < 0 || T < 0 || H < 1 || pph < 1) return fail(ASYM_EINVAL, w + ": B and T must be >= 0, H and pages_per_head >= 1");
+  if (pool_pages < 1 || pool_pages > 0x7FFFFFFFu) return fail(ASYM_EINVAL, w + ": pool_pages must be in [1, 2^31)");
+  if (pph > (1 << 25)) return fail(ASYM_EUNSUPPORTED, w + ": more than 2^30 tokens a request");
+  if (B == 0 || T == 0) return ASYM_OK;
+  if (!k_pool || !v_pool || !k_pages || !v_pages || !cu || !start) return fail(ASYM_EINVAL, w + ": null pointer");
+  if (((uintptr_t)k_pool | (uintptr_t)v_pool) & 15u) return fail(ASYM_EINVAL, w + ": pools must be 16-byte aligned");
+  if (((uintptr_t)k_pages | (uintptr_t)v_pages | (uintptr_t)cu | (uintptr_t)start) & 3u)
+    return fail(ASYM_EINVAL, w + ": tables, offsets and positions must be 4-byte aligned");
+  return ASYM_OK;
+}
+
+// n tokens from any position touch at most n / 32 + 2 pages: ranks, and the grid of a
+// wave per (rank, head)
+int kv_grid(const char* what, KvParams& p, unsigned* grid) {
+  const int64_t ranks = (int64_t)p.T / kKvPageTokens + 2ll * p.B;
+  const int64_t items = ranks * p.H;
+  if (items > (1 << 26) - kWaves) return  // (threads of a launch are counted in 32 bits)
+    fail(ASYM_EUNSUPPORTED, std::string(what) + ": too many pages");
+  p.ranks = (int)ranks;
+  *grid = (unsigned)((items + kWaves - 1) / kWaves);
+  return ASYM_OK;
+}
+
+}  // namespace
+}  // namespace asym
+
+extern "C" int asym_kv_write_fp4(int B, int H_kv, int T, const void* k, int64_t k_token, int64_t k_head, const void* v,
+                                 int64_t v_token, int64_t v_head, void* k_pool, void* v_pool, size_t pool_pages,
+                                 const int32_t* k_pages, const int32_t* v_pages, int pages_per_head, const int32_t* cu,
+                                 const int32_t* start, void* stream) {
+  using namespace asym;
+  int rc = kv_check("kv write", B, H_kv, T, pages_per_head, pool_pages, k_pool, v_pool, k_pages, v_pages, cu, start);
+  if (rc != ASYM_OK) return rc;
+  if (B == 0 || T == 0) return ASYM_OK;
+  if (!k || !v) return fail(ASYM_EINVAL, "kv write: null pointer");
+  if (((uintptr_t)k | (uintptr_t)v) & 15u) return fail(ASYM_EINVAL, "kv write: K and V must be 16-byte aligned");
+  for (int64_t s : {k_token, k_head, v_token, v_head})
+    if (s < 0 || s % 8) return fail(ASYM_EINVAL, "kv write: strides must be multiples of 8 values and not negative");
+  KvParams p = {};
+  p.k = static_cast<const uint16_t*>(k);
+  p.v = static_cast<const uint16_t*>(v);
+  p.k_tok = k_token; p.k_head = k_head; p.v_tok = v_token; p.v_head = v_head;
+  p.k_pool = static_cast<uint8_t*>(k_pool);
+  p.v_pool = static_cast<uint8_t*>(v_pool);
+  p.k_pages = k_pages; p.v_pages = v_pages; p.cu = cu; p.start = start;
+  p.B = B; p.H = H_kv; p.T = T; p.pph = pages_per_head; p.pool_pages = (int)pool_pages;
+  unsigned grid;
+  rc = kv_grid("kv write", p, &grid);
+  if (rc != ASYM_OK) return rc;
+  hipLaunchKernelGGL(kv_write_kernel, dim3(grid), dim3(64 * kWaves), 0, static_cast<hipStream_t>(stream), p);
+  ASYM_HIP(hipGetLastError());
+  return ASYM_OK;
+}
+
+extern "C" int asym_kv_read_fp4(int B, int H_kv, int T, const void* k_pool, const void* v_pool, size_t pool_pages,
+                                const int32_t* k_pages, const int32_t* v_pages, int pages_per_head, const int32_t* cu,
+                                const int32_t* start, void* k, void* v, void* stream) {
+  using namespace asym;
+  int rc = kv_check("kv read", B, H_kv, T, pages_per_head, pool_pages, k_pool, v_pool, k_pages, v_pages, cu, start);
+  if (rc != ASYM_OK) return rc;
+  if (B == 0 || T == 0) return ASYM_OK;
+  if (!k || !v) return fail(ASYM_EINVAL, "kv read: null pointer");
+  if (((uintptr_t)k | (uintptr_t)v) & 15u) return fail(ASYM_EINVAL, "kv read: K and V must be 16-byte aligned");
+  KvParams p = {};
+  p.ko = static_cast<uint16_t*>(k);
+  p.vo = static_cast<uint16_t*>(v);
+  p.k_pool = static_cast<uint8_t*>(const_cast<void*>(k_pool));
+  p.v_pool = static_cast<uint8_t*>(const_cast<void*>(v_pool));
+  p.k_pages = k_pages; p.v_pages = v_pages; p.cu = cu; p.start = start;
+  p.B = B; p.H = H_kv; p.T = T; p.pph = pages_per_head; p.pool_pages = (int)pool_pages;
+  unsigned grid;
+  rc = kv_grid("kv read", p, &grid);
+  if (rc != ASYM_OK) return rc;
+  hipLaunchKernelGGL(kv_read_kernel, dim3(grid), dim3(64 * kWaves), 0, static_cast<hipStream_t>(stream), p);
+  ASYM_HIP(hipGetLastError());
+  return ASYM_OK;
+}

@@ -1,0 +1,455 @@
+// The pages of a paged key/value cache, managed on the device: rows of a table
+// take, share, copy and give up pages of a pool without the host knowing which.
+//
+// State: table [R][H][pph] (page of each (row, head, 32-token page), -1 where there is
+// none), lens [R] (tokens of each row), refs [pool_pages] (table entries that name a
+// page; 0: the page is free).  Pages are taken lowest first, in an order fixed by the
+// arguments, so that the result never depends on timing; refs is changed with integer
+// atomics, whose order does not matter.
+//
+// A call is a few short launches, since each step needs the whole of the one before:
+//   1. segments of 4096 pages are counted (free or live); beside them one workgroup lays
+//      out what the call needs (a prefix over its requests);
+//   2. each segment adds up the counts before it and writes its pages' numbers to their
+//      places in a list;
+//   3. the tables, the counts and the pages themselves are changed.
+// They are bound by launches and, for large calls, by the copies (read and written once).
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+
+#include "internal.h"
+#include "kv_fp4.h"
+
+namespace asym {
+namespace {
+
+constexpr int kSeg = 4096;     // pages counted by a workgroup
+constexpr int kThreads = 256;
+constexpr int kPer = kSeg / kThreads;
+
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+// Words of the workspace, in order: the header; counts [segments]; first [n] (place of a
+// request's first page in the list); flag [n]; list [pool_pages]; then rows [n][H][pph]
+// and new_len [n] (fork) or holes [pool_pages] and where [pool_pages] (compact).
+enum { kNeed = 0, kTotal = 1, kHoles = 2, kHeader = 16 };
+
+struct PagesParams {
+  int* table;
+  int* lens;
+  int* refs;
+  const int *a, *b;  // extend: rows, new lengths; fork: sources, targets; free: rows
+  int* status;       // [2], nullable
+  uint8_t *k_pool, *v_pool;
+  int64_t page_bytes;
+  int R, H, pph, pool, n, segs;
+  int *head, *counts, *first, *flag, *list, *rows, *new_len, *holes, *where;
+};
+
+__device__ __forceinline__ int pages_of(int len, int pph) {
+  return min((int)(((int64_t)max(len, 0) + kKvPageTokens - 1) / kKvPageTokens), pph);
+}
+
+// Sum over the workgroup's threads before this one, and over all of them.
+__device__ int block_scan(int x, int* red, int& all) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int upto = wave_scan_add(x);
+  __syncthreads();  // (red may still be read from the call before)
+  if (lane == 63) red[wave] = upto;
+  __syncthreads();
+  int before = 0;
+  all = 0;
+#pragma unroll
+  for (int w = 0; w < kThreads / 64; ++w) {
+    if (w < wave) before += red[w];
+    all += red[w];
+  }
+  return before + upto - x;
+}
+
+// Whether request i names a row that no earlier request of the call names.
+__device__ __forceinline__ bool first_of_its_row(const int* __restrict__ rows, int i) {
+  const int r = rows[i];
+  bool seen = false;
+  for (int j = 0; j < i; ++j) seen |= rows[j] == r;
+  return !seen;
+}
+
+enum { kExtend, kFork, kCompact };
+
+// 1. counts[s]: free pages (extend, fork) or live ones (compact) of segment s; the last
+// workgroup: what the requests need.
+template <int OP>
+__global__ void __launch_bounds__(kThreads) pages_count(PagesParams p) {
+  __shared__ int red[kThreads / 64];
+  const int seg = blockIdx.x;
+  if (seg < p.segs) {
+    int c = 0;
+    for (int i = 0; i < kPer; ++i) {
+      const int64_t page = (int64_t)seg * kSeg + i * kThreads + threadIdx.x;
+      if (page < p.pool) c += (p.refs[page] > 0) == (OP == kCompact);
+    }
+    int all;
+    block_scan(c, red, all);
+    if (threadIdx.x == 0) p.counts[seg] = all;
+    return;
+  }
+  if constexpr (OP != kCompact) {
+    int base = 0;
+    for (int i0 = 0; i0 < p.n; i0 += kThreads) {
+      const int i = i0 + threadIdx.x;
+      int need = 0, ok = 0;
+      if (i < p.n) {
+        if constexpr (OP == kExtend) {
+          const int r = p.a[i], to = p.b[i];
+          // (a row outside the table, a length that is no longer or does not fit: left as it is)
+          if (r >= 0 && r < p.R && to > p.lens[r] && (int64_t)to <= (int64_t)p.pph * kKvPageTokens &&
+              first_of_its_row(p.a, i)) {
+            ok = 1;
+            need = (pages_of(to, p.pph) - pages_of(p.lens[r], p.pph)) * p.H;
+          }
+        } else {
+          const int s = p.a[i], d = p.b[i];
+          if (s >= 0 && s < p.R && d >= 0 && d < p.R && s != d && first_of_its_row(p.b, i)) {
+            ok = 1;
+            const int len = min(max(p.lens[s], 0), p.pph * kKvPageTokens);
+            need = len % kKvPageTokens ? p.H : 0;
+          }
+        }
+      }
+      int all;
+      const int before = block_scan(need, red, all);
+      if (i < p.n) {
+        p.first[i] = base + before;
+        p.flag[i] = ok;
+      }
+      base += all;
+    }
+    if (threadIdx.x == 0) p.head[kNeed] = base;
+  }
+}
+
+// 2. list[r]: the r-th free page (as many as are needed), or the r-th live one; compact:
+// holes[r], the r-th free page below the number of live ones, and where[page] = page.
+template <int OP>
+__global__ void __launch_bounds__(kThreads) pages_list(PagesParams p) {
+  __shared__ int red[kThreads / 64];
+  const int seg = blockIdx.x;
+  int mine = 0, tot = 0;
+  for (int s = threadIdx.x; s < p.segs; s += kThreads) {
+    const int c = p.counts[s];
+    tot += c;
+    if (s < seg) mine += c;
+  }
+  int base, total;
+  block_scan(mine, red, base);
+  block_scan(tot, red, total);
+  if (seg == 0 && threadIdx.x == 0) {
+    p.head[kTotal] = total;
+    if (OP == kCompact && total == 0) p.head[kHoles] = 0;
+  }
+  const int need = OP == kCompact ? 0 : p.head[kNeed];
+  if (OP != kCompact && base >= need) return;  // (the whole workgroup)
+  for (int i = 0; i < kPer; ++i) {
+    const int64_t page = (int64_t)seg * kSeg + i * kThreads + threadIdx.x;
+    const bool in = page < p.pool;
+    const bool live = in && p.refs[page] > 0;
+    const int x = in && live == (OP == kCompact);
+    int all;
+    const int r = base + block_scan(x, red, all);
+    base += all;
+    if constexpr (OP == kCompact) {
+      if (live) p.list[r] = (int)page;
+      if (in) p.where[page] = (int)page;
+      if (in && !live && page < total) p.holes[page - r] = (int)page;
+      if (page == total - 1) p.head[kHoles] = total - r - (live ? 1 : 0);  // free pages below `total`
+    } else {
+      if (x && r < need) p.list[r] = (int)page;
+    }
+  }
+}
+
+__device__ __forceinline__ void copy_page(uint8_t* pool, int64_t bytes, int64_t to, int64_t from, int thread, int threads) {
+  const u32x4* s = reinterpret_cast<const u32x4*>(pool + from * bytes);
+  u32x4* d = reinterpret_cast<u32x4*>(pool + to * bytes);
+  for (int i = thread; i < bytes / 16; i += threads) d[i] = s[i];
+}
+
+// 3. extend: a workgroup a request
+__global__ void __launch_bounds__(kThreads) pages_extend(PagesParams p) {
+  const int need = p.head[kNeed], total = p.head[kTotal];
+  const int i = blockIdx.x;
+  const bool enough = need <= total;
+  if (i == 0 && threadIdx.x == 0 && p.status) {
+    p.status[0] = enough ? need : 0;
+    p.status[1] = enough ? 0 : need - total;
+  }
+  if (!enough || i >= p.n || !p.flag[i]) return;
+  const int r = p.a[i], to = p.b[i];
+  const int had = pages_of(p.lens[r], p.pph), add = pages_of(to, p.pph) - had;
+  for (int x = threadIdx.x; x < add * p.H; x += kThreads) {
+    const int h = x / add, c = x - h * add;
+    const int page = p.list[p.first[i] + x];
+    p.table[((int64_t)r * p.H + h) * p.pph + had + c] = page;
+    p.refs[page] = 1;
+  }
+  __syncthreads();  // (every thread has read the old length)
+  if (threadIdx.x == 0) p.lens[r] = to;
+}
+
+// 3. fork: a workgroup a (request, head) lays out the new row beside the table, takes
+// its references, and copies the part page
+__global__ void __launch_bounds__(kThreads) pages_fork(PagesParams p) {
+  const int need = p.head[kNeed], total = p.head[kTotal];
+  const bool enough = need <= total;
+  const int i = blockIdx.x / p.H, h = blockIdx.x - i * p.H;
+  if (blockIdx.x == 0 && threadIdx.x == 0 && p.status) {
+    p.status[0] = enough ? need : 0;
+    p.status[1] = enough ? 0 : need - total;
+  }
+  if (!enough || i >= p.n || !p.flag[i]) return;
+  const int s = p.a[i];
+  const int len = min(max(p.lens[s], 0), p.pph * kKvPageTokens), whole = len / kKvPageTokens;
+  const int* from = p.table + ((int64_t)s * p.H + h) * p.pph;
+  int* to = p.rows + ((int64_t)i * p.H + h) * p.pph;
+  for (int c = threadIdx.x; c < p.pph; c += kThreads) {
+    const int page = c < whole ? from[c] : -1;
+    to[c] = page;
+    if (page >= 0 && page < p.pool) atomicAdd(&p.refs[page], 1);
+  }
+  if (h == 0 && threadIdx.x == 0) p.new_len[i] = len;
+  if (len % kKvPageTokens == 0) return;
+  const int page = p.list[p.first[i] + h], old = from[whole];
+  __syncthreads();  // (the row's entry was -1 until here)
+  if (threadIdx.x == 0) {
+    to[whole] = page;
+    p.refs[page] = 1;
+  }
+  if (old < 0 || old >= p.pool) return;
+  copy_page(p.k_pool, p.page_bytes, page, old, threadIdx.x, kThreads);
+  if (p.v_pool) copy_page(p.v_pool, p.page_bytes, page, old, threadIdx.x, kThreads);
+}
+
+__device__ void release_row(const PagesParams& p, int r) {
+  const int used = pages_of(p.lens[r], p.pph);
+  for (int x = threadIdx.x; x < used * p.H; x += kThreads) {
+    const int h = x / used, c = x - h * used;
+    const int page = p.table[((int64_t)r * p.H + h) * p.pph + c];
+    if (page >= 0 && page < p.pool) atomicSub(&p.refs[page], 1);
+  }
+  __syncthreads();
+}
+
+// 4. fork: the targets' old rows are given up, the new ones take their place
+__global__ void __launch_bounds__(kThreads) pages_fork_rows(PagesParams p) {
+  if (p.head[kNeed] > p.head[kTotal] || !p.flag[blockIdx.x]) return;
+  const int r = p.b[blockIdx.x];
+  release_row(p, r);
+  const int64_t row = (int64_t)p.H * p.pph;
+  for (int64_t x = threadIdx.x; x < row; x += kThreads) p.table[r * row + x] = p.rows[blockIdx.x * row + x];
+  if (threadIdx.x == 0) p.lens[r] = p.new_len[blockIdx.x];
+}
+
+__global__ void __launch_bounds__(kThreads) pages_free(PagesParams p) {
+  const int i = blockIdx.x, r = p.a[i];
+  if (r < 0 || r >= p.R) return;
+  bool seen = false;
+  for (int j = threadIdx.x; j < i; j += kThreads) seen |= p.a[j] == r;
+  if (__syncthreads_or(seen)) return;
+  release_row(p, r);
+  const int64_t row = (int64_t)p.H * p.pph;
+  for (int64_t x = threadIdx.x; x < row; x += kThreads) p.table[r * row + x] = -1;
+  if (threadIdx.x == 0) p.lens[r] = 0;
+}
+
+// 3. compact: the live pages at or above the number of live ones go, in order, into the
+// holes below it (sources and targets never meet)
+__global__ void __launch_bounds__(kThreads) pages_move(PagesParams p) {
+  const int total = p.head[kTotal], holes = p.head[kHoles];
+  if (blockIdx.x == 0 && threadIdx.x == 0 && p.status) {
+    p.status[0] = holes;
+    p.status[1] = total;
+  }
+  for (int j = blockIdx.x; j < holes; j += gridDim.x) {
+    const int from = p.list[total - holes + j], to = p.holes[j];
+    if (threadIdx.x == 0) {
+      p.where[from] = to;
+      p.refs[to] = p.refs[from];
+      p.refs[from] = 0;
+    }
+    copy_page(p.k_pool, p.page_bytes, to, from, threadIdx.x, kThreads);
+    if (p.v_pool) copy_page(p.v_pool, p.page_bytes, to, from, threadIdx.x, kThreads);
+  }
+}
+
+// 4. compact: the tables' entries follow
+__global__ void __launch_bounds__(kThreads) pages_rename(PagesParams p) {
+  if (p.head[kHoles] == 0) return;
+  const int64_t n = (int64_t)p.R * p.H * p.pph;
+  for (int64_t x = (int64_t)blockIdx.x * kThreads + threadIdx.x; x < n; x += (int64_t)gridDim.x * kThreads) {
+    const int page = p.table[x];
+    if (page >= 0 && page < p.pool) {
+      const int to = p.where[page];
+      if (to != page) p.table[x] = to;
+    }
+  }
+}
+
+// The checks that every call shares; lays the workspace out (words, counted in `words`).
+int pages_setup(const char* what, int op, int R, int H, int pph, int32_t* table, int32_t* lens, int32_t* refs,
+                size_t pool_pages, int n, void* workspace, size_t workspace_bytes, PagesParams* p) {
+  const std::string w(what);
+  if (R < 1 || H < 1 || pph < 1 || n < 0) return fail(ASYM_EINVAL, w + ": R, H and pages_per_head must be >= 1, n >= 0");
+  if (pph > (1 << 25)) return fail(ASYM_EUNSUPPORTED, w + ": more than 2^30 tokens a row");
+  if (pool_pages < 1 || pool_pages > 0x7FFFFFFFu) return fail(ASYM_EINVAL, w + ": pool_pages must be in [1, 2^31)");
+  if ((int64_t)n * H >= (1 << 24))  // (threads of a launch are counted in 32 bits)
+    return fail(ASYM_EUNSUPPORTED, w + ": too many requests");
+  if (!table || !lens || !refs) return fail(ASYM_EINVAL, w + ": null pointer");
+  if (((uintptr_t)table | (uintptr_t)lens | (uintptr_t)refs) & 3u)
+    return fail(ASYM_EINVAL, w + ": tables, lengths and counts must be 4-byte aligned");
+  *p = PagesParams{};
+  p->table = table; p->lens = lens; p->refs = refs;
+  p->R = R; p->H = H; p->pph = pph; p->pool = (int)pool_pages; p->n = n;
+  p->segs = (int)((pool_pages + kSeg - 1) / kSeg);
+  if (op < 0) return ASYM_OK;  // (free: no workspace)
+  size_t bytes = 0;
+  const int rc = asym_kv_pages_workspace(op, R, H, pph, pool_pages, n, &bytes);
+  if (rc != ASYM_OK) return rc;
+  if (!workspace || workspace_bytes < bytes || ((uintptr_t)workspace & 15u))
+    return fail(ASYM_EINVAL, w + ": the workspace must be 16-byte aligned and hold asym_kv_pages_workspace's bytes");
+  int* at = static_cast<int*>(workspace);
+  auto take = [&](size_t words) {
+    int* x = at;
+    at += words;
+    return x;
+  };
+  p->head = take(kHeader);
+  p->counts = take(p->segs);
+  p->list = take(pool_pages);
+  if (op == ASYM_KV_COMPACT) {
+    p->holes = take(pool_pages);
+    p->where = take(pool_pages);
+  } else {
+    p->first = take(n);
+    p->flag = take(n);
+    if (op == ASYM_KV_FORK) {
+      p->new_len = take(n);
+      p->rows = take((size_t)n * H * pph);
+    }
+  }
+  return ASYM_OK;
+}
+
+int pools_check(const char* what, const void* k_pool, const void* v_pool, size_t page_bytes) {
+  const std::string w(what);
+  if (!k_pool) return fail(ASYM_EINVAL, w + ": null pointer");
+  if (((uintptr_t)k_pool | (uintptr_t)v_pool) & 15u) return fail(ASYM_EINVAL, w + ": pools must be 16-byte aligned");
+  if (page_bytes < 16 || page_bytes % 16 || page_bytes > (1u << 30))
+    return fail(ASYM_EINVAL, w + ": page_bytes must be a multiple of 16, at most 2^30");
+  if (k_pool == v_pool) return fail(ASYM_EINVAL, w + ": one pool given twice (leave v_pool null)");
+  return ASYM_OK;
+}
+
+}  // namespace
+}  // namespace asym
+
+using namespace asym;
+
+extern "C" int asym_kv_pages_workspace(int op, int R, int H, int pages_per_head, size_t pool_pages, int n, size_t* bytes) {
+  if (!bytes) return fail(ASYM_EINVAL, "kv pages workspace: null output");
+  if (op != ASYM_KV_EXTEND && op != ASYM_KV_FORK && op != ASYM_KV_COMPACT)
+    return fail(ASYM_EINVAL, "kv pages workspace: unknown operation");
+  if (R < 1 || H < 1 || pages_per_head < 1 || n < 0 || pool_pages < 1 || pool_pages > 0x7FFFFFFFu)
+    return fail(ASYM_EINVAL, "kv pages workspace: bad sizes");
+  size_t words = kHeader + (pool_pages + kSeg - 1) / kSeg + pool_pages;
+  if (op == ASYM_KV_COMPACT)
+    words += 2 * pool_pages;
+  else
+    words += 2 * (size_t)n;
+  if (op == ASYM_KV_FORK) words += (size_t)n + (size_t)n * H * pages_per_head;
+  *bytes = words * sizeof(int);
+  return ASYM_OK;
+}
+
+extern "C" int asym_kv_extend(int R, int H, int pages_per_head, int32_t* table, int32_t* lens, int32_t* refs,
+                              size_t pool_pages, int n, const int32_t* rows, const int32_t* new_lens, int32_t* status,
+                              void* workspace, size_t workspace_bytes, void* stream) {
+  PagesParams p;
+  const int rc = pages_setup("kv extend", ASYM_KV_EXTEND, R, H, pages_per_head, table, lens, refs, pool_pages, n, workspace,
+                             workspace_bytes, &p);
+  if (rc != ASYM_OK) return rc;
+  if (n > 0 && (!rows || !new_lens)) return fail(ASYM_EINVAL, "kv extend: null pointer");
+  if (((uintptr_t)rows | (uintptr_t)new_lens | (uintptr_t)status) & 3u)
+    return fail(ASYM_EINVAL, "kv extend: rows, lengths and status must be 4-byte aligned");
+  p.a = rows; p.b = new_lens; p.status = status;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  hipLaunchKernelGGL((pages_count<kExtend>), dim3(p.segs + 1), dim3(kThreads), 0, s, p);
+  hipLaunchKernelGGL((pages_list<kExtend>), dim3(p.segs), dim3(kThreads), 0, s, p);
+  hipLaunchKernelGGL(pages_extend, dim3(std::max(n, 1)), dim3(kThreads), 0, s, p);  // (status with no request too)
+  ASYM_HIP(hipGetLastError());
+  return ASYM_OK;
+}
+
+extern "C" int asym_kv_fork(int R, int H, int pages_per_head, int32_t* table, int32_t* lens, int32_t* refs, void* k_pool,
+                            void* v_pool, size_t page_bytes, size_t pool_pages, int n, const int32_t* src,
+                            const int32_t* dst, int32_t* status, void* workspace, size_t workspace_bytes, void* stream) {
+  PagesParams p;
+  int rc = pages_setup("kv fork", ASYM_KV_FORK, R, H, pages_per_head, table, lens, refs, pool_pages, n, workspace,
+                       workspace_bytes, &p);
+  if (rc == ASYM_OK) rc = pools_check("kv fork", k_pool, v_pool, page_bytes);
+  if (rc != ASYM_OK) return rc;
+  if (n > 0 && (!src || !dst)) return fail(ASYM_EINVAL, "kv fork: null pointer");
+  if (((uintptr_t)src | (uintptr_t)dst | (uintptr_t)status) & 3u)
+    return fail(ASYM_EINVAL, "kv fork: sources, targets and status must be 4-byte aligned");
+  p.a = src; p.b = dst; p.status = status;
+  p.k_pool = static_cast<uint8_t*>(k_pool);
+  p.v_pool = static_cast<uint8_t*>(v_pool);
+  p.page_bytes = (int64_t)page_bytes;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  hipLaunchKernelGGL((pages_count<kFork>), dim3(p.segs + 1), dim3(kThreads), 0, s, p);
+  hipLaunchKernelGGL((pages_list<kFork>), dim3(p.segs), dim3(kThreads), 0, s, p);
+  hipLaunchKernelGGL(pages_fork, dim3(std::max(n * H, 1)), dim3(kThreads), 0, s, p);  // (status with no request too)
+  if (n > 0) hipLaunchKernelGGL(pages_fork_rows, dim3(n), dim3(kThreads), 0, s, p);
+  ASYM_HIP(hipGetLastError());
+  return ASYM_OK;
+}
+
+extern "C" int asym_kv_free(int R, int H, int pages_per_head, int32_t* table, int32_t* lens, int32_t* refs,
+                            size_t pool_pages, int n, const int32_t* rows, void* stream) {
+  PagesParams p;
+  const int rc = pages_setup("kv free", -1, R, H, pages_per_head, table, lens, refs, pool_pages, n, nullptr, 0, &p);
+  if (rc != ASYM_OK) return rc;
+  if (n == 0) return ASYM_OK;
+  if (!rows || ((uintptr_t)rows & 3u)) return fail(ASYM_EINVAL, "kv free: rows must be given, 4-byte aligned");
+  p.a = rows;
+  hipLaunchKernelGGL(pages_free, dim3(n), dim3(kThreads), 0, static_cast<hipStream_t>(stream), p);
+  ASYM_HIP(hipGetLastError());
+  return ASYM_OK;
+}
+
+extern "C" int asym_kv_compact(int R, int H, int pages_per_head, int32_t* table, int32_t* refs, void* k_pool, void* v_pool,
+                               size_t page_bytes, size_t pool_pages, int32_t* status, void* workspace,
+                               size_t workspace_bytes, void* stream) {
+  PagesParams p;
+  int32_t none = 0;
+  int rc = pages_setup("kv compact", ASYM_KV_COMPACT, R, H, pages_per_head, table, &none, refs, pool_pages, 0, workspace,
+                       workspace_bytes, &p);
+  if (rc == ASYM_OK) rc = pools_check("kv compact", k_pool, v_pool, page_bytes);
+  if (rc != ASYM_OK) return rc;
+  if ((uintptr_t)status & 3u) return fail(ASYM_EINVAL, "kv compact: status must be 4-byte aligned");
+  p.lens = nullptr;
+  p.status = status;
+  p.k_pool = static_cast<uint8_t*>(k_pool);
+  p.v_pool = static_cast<uint8_t*>(v_pool);
+  p.page_bytes = (int64_t)page_bytes;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  const int64_t entries = (int64_t)R * H * pages_per_head;
+  hipLaunchKernelGGL((pages_count<kCompact>), dim3(p.segs), dim3(kThreads), 0, s, p);
+  hipLaunchKernelGGL((pages_list<kCompact>), dim3(p.segs), dim3(kThreads), 0, s, p);
+  hipLaunchKernelGGL(pages_move, dim3((unsigned)std::min<size_t>(pool_pages, 4096)), dim3(kThreads), 0, s, p);
+  hipLaunchKernelGGL(pages_rename, dim3((unsigned)std::min<int64_t>((entries + kThreads - 1) / kThreads, 4096)),
+                     dim3(kThreads), 0, s, p);
+  ASYM_HIP(hipGetLastError());
+  return ASYM_OK;
+}
