@@ -24,6 +24,7 @@
 #include <hip/hip_runtime.h>
 
 #include <cmath>
+#include <type_traits>
 
 #include "internal.h"
 #include "kv_fp4.h"
@@ -154,25 +155,47 @@ __device__ __forceinline__ float sum_halves(float x) {
   return __uint_as_float(sw[0]) + __uint_as_float(sw[1]);
 }
 
-// Value bytes within a block's V tile: 16-byte chunk c of row r lies at chunk c ^ swz(r)
-__device__ __forceinline__ int swz_k(int row) { return row & 15; }
+// 16-byte chunk c of a tile's row r lies at chunk c ^ swz(r): the rows that one read
+// takes together then lie on different banks (K: 8 rows, one chunk of each; V: 4 rows,
+// two chunks of each).
+__device__ __forceinline__ int swz_k(int row) { return row & 7; }
 __device__ __forceinline__ int swz_v(int row) { return (row & 3) << 1; }
 
-// V^T operand of 32 channels (block cb) x 16 tokens (step ks of the block)
-__device__ __forceinline__ bf16x8 v_frag(const unsigned char* vt, int lane, int cb, int ks) {
-  const int i = lane & 15, half = (lane >> 4) & 1, h = lane >> 5;
+typedef __attribute__((address_space(3))) unsigned char lds_byte;
+
+// A lane's places in the K and V tiles (bytes from a tile's start).
+struct Places {
+  uint32_t k[4];  // row n, chunks 2 c + h of c = 0 .. 3 (c + 4: 128 bytes on; rows 32 + n: 32 rows on)
+  uint32_t v[2];  // channels of blocks cb = 0, 1 (cb + 2: 128 bytes on), tokens 4 h + (lane % 16) / 4
+};
+__device__ __forceinline__ Places places(int lane) {
+  Places p;
+  const int n = lane & 31, h = lane >> 5, i = lane & 15, half = (lane >> 4) & 1;
+#pragma unroll
+  for (int c = 0; c < 4; ++c) p.k[c] = (uint32_t)(n * kRowBytes + (((2 * c + h) ^ swz_k(n)) << 4));
+#pragma unroll
+  for (int cb = 0; cb < 2; ++cb) {
+    const int row = 4 * h + (i >> 2), chunk = 4 * cb + 2 * half + ((i & 3) >> 1);
+    p.v[cb] = (uint32_t)(row * kRowBytes + ((chunk ^ swz_v(row)) << 4) + ((i & 1) << 3));
+  }
+  return p;
+}
+
+// K operand: 32 keys (half t of the block) x 16 channels (step c)
+__device__ __forceinline__ bf16x8 k_frag(const lds_byte* kt, const Places& pl, int t, int c) {
+  return *(const __attribute__((address_space(3))) bf16x8*)(kt + pl.k[c & 3] + (c >> 2) * 128 + t * 32 * kRowBytes);
+}
+
+// V^T operand: 32 channels (block cb) x 16 tokens (step ks of the block)
+__device__ __forceinline__ bf16x8 v_frag(const lds_byte* vt, const Places& pl, int cb, int ks) {
   union {
     s16x4 s[2];
     bf16x8 b;
   } u;
 #pragma unroll
-  for (int part = 0; part < 2; ++part) {
-    const int row = 16 * ks + 8 * part + 4 * h + (i >> 2);
-    const int chunk = 4 * cb + 2 * half + ((i & 3) >> 1);
-    const unsigned char* a = vt + row * kRowBytes + ((chunk ^ swz_v(row)) << 4) + ((i & 1) << 3);
+  for (int part = 0; part < 2; ++part)
     u.s[part] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-        (__attribute__((address_space(3))) s16x4*)(a));
-  }
+        (__attribute__((address_space(3))) s16x4*)(vt + pl.v[cb & 1] + (cb >> 1) * 128 + (16 * ks + 8 * part) * kRowBytes));
   return u.b;
 }
 
@@ -182,14 +205,14 @@ __device__ __forceinline__ bf16x8 v_frag(const unsigned char* vt, int lane, int 
 // and what they do to the rows that see them is added by itself, counted by one
 // more product of small whole numbers (1 for inf, 128 for -inf, 16384 for NaN; 64
 // keys at most, exact in fp32).  Returns false where there are none.
-__device__ bool pv_guarded(const unsigned char* vt, int lane, int j, int lim, const bf16x8 (&pf)[4], f32x16 (&o)[4]) {
+__device__ __forceinline__ bool pv_guarded(const lds_byte* vt, const Places& pl, int lane, int j, int lim, const bf16x8 (&pf)[4], f32x16 (&o)[4]) {
   uint32_t bad = 0;
 #pragma unroll
   for (int kst = 0; kst < 4; ++kst)
 #pragma unroll
     for (int cb = 0; cb < 4; ++cb) {
       __builtin_amdgcn_sched_barrier(0);
-      const u32x4 w = __builtin_bit_cast(u32x4, v_frag(vt, lane, cb, kst));
+      const u32x4 w = __builtin_bit_cast(u32x4, v_frag(vt, pl, cb, kst));
 #pragma unroll
       for (int e = 0; e < 4; ++e) bad |= (w[e] & 0x7F807F80u) + 0x00800080u;  // an exponent of all ones carries
     }
@@ -201,7 +224,7 @@ __device__ bool pv_guarded(const unsigned char* vt, int lane, int j, int lim, co
 #pragma unroll
     for (int kst = 0; kst < 4; ++kst) {
       __builtin_amdgcn_sched_barrier(0);  // (one operand at a time: registers, not speed, count here)
-      const u32x4 f = __builtin_bit_cast(u32x4, v_frag(vt, lane, cb, kst));
+      const u32x4 f = __builtin_bit_cast(u32x4, v_frag(vt, pl, cb, kst));
       u32x4 fin, code, vis;
 #pragma unroll
       for (int e = 0; e < 4; ++e) {  // two values a word
@@ -263,12 +286,12 @@ __global__ void __launch_bounds__(64 * NW, 2) attn_prefill_kernel(PrefillParams 
   const int64_t row = min(row0 + n, rows - 1);
   const int tok = (int)(row / p.G), g = (int)(row - (int64_t)tok * p.G);
   const int64_t orow = (int64_t)(qs + tok) * p.Hq + (int64_t)hk * p.G + g;
-  // keys that the row sees, and the least and most over the wave and the workgroup
+  // keys that the row sees; the most over the wave, the least and most over the workgroup
   auto limit = [&](int64_t r) { return p.causal ? max(off + (int)(min(r, rows - 1) / p.G) + 1, 0) : Lk; };
   const int lim = p.causal ? max(off + tok + 1, 0) : Lk;
-  const int lim_lo = __builtin_amdgcn_readfirstlane(limit(row0));
   const int lim_hi = __builtin_amdgcn_readfirstlane(limit(row0 + 31));
   const int nblk = (__builtin_amdgcn_readfirstlane(limit((int64_t)tile * BM + BM - 1)) + PN - 1) / PN;
+  const int nfull = __builtin_amdgcn_readfirstlane(limit((int64_t)tile * BM)) / PN;  // blocks that every row sees whole
 
   bf16x8 qf[8];
   {
@@ -284,7 +307,8 @@ __global__ void __launch_bounds__(64 * NW, 2) attn_prefill_kernel(PrefillParams 
   const uint16_t* kb = p.k + (int64_t)ks * p.k_tok + (int64_t)hk * p.k_head;
   const uint16_t* vb = p.v + (int64_t)ks * p.v_tok + (int64_t)hk * p.v_head;
   const uint32_t lds0 = (uint32_t)(size_t)lds;
-  // 1 KiB is 4 rows of a block: lane -> row lane / 16, 16-byte place lane % 16
+  const Places pl = places(lane);
+  // 1 KiB is 4 rows of a tile: lane -> row lane / 16, 16-byte place lane % 16
   constexpr int PIECES = kTileBytes / 1024 / NW;
   auto load_block = [&](int j) {
     const int left = min(Lk - j * PN, PN);
@@ -304,31 +328,24 @@ __global__ void __launch_bounds__(64 * NW, 2) attn_prefill_kernel(PrefillParams 
 #pragma unroll
   for (int cb = 0; cb < 4; ++cb) o[cb] = f32x16{};
   float m = -INFINITY, l = 0.f;
-  if (nblk > 0) load_block(0);
-  for (int j = 0; j < nblk; ++j) {
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    __syncthreads();
-    if (j + 1 < nblk) load_block(j + 1);
-    if (j * PN >= lim_hi) continue;  // (the wave's rows see none of this block)
-    const unsigned char* kt = lds + (j & 1) * (2 * kTileBytes);
-    const unsigned char* vt = kt + kTileBytes;
 
+  // One block of keys; EDGE: some row of the workgroup does not see all of it
+  auto step = [&](int j, auto edge_c) {
+    constexpr bool EDGE = decltype(edge_c)::value;
+    const lds_byte* kt = (const lds_byte*)lds + (j & 1) * (2 * kTileBytes);
+    const lds_byte* vt = kt + kTileBytes;
     f32x16 s[2] = {f32x16{}, f32x16{}};
 #pragma unroll
     for (int c = 0; c < 8; ++c)
 #pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        const int r = 32 * t + n;
-        const bf16x8 kf = *reinterpret_cast<const bf16x8*>(kt + r * kRowBytes + (((2 * c + h) ^ swz_k(r)) << 4));
-        s[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[c], s[t], 0, 0, 0);
-      }
-    const bool edge = j * PN + PN > lim_lo;  // some row does not see all of this block
-    if (edge) {
+      for (int t = 0; t < 2; ++t) s[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k_frag(kt, pl, t, c), qf[c], s[t], 0, 0, 0);
+    if constexpr (EDGE) {
+      const int left = lim - j * PN - 4 * h;
 #pragma unroll
       for (int t = 0; t < 2; ++t)
 #pragma unroll
         for (int r = 0; r < 16; ++r)
-          if (j * PN + 32 * t + (r & 3) + 8 * (r >> 2) + 4 * h >= lim) s[t][r] = -INFINITY;
+          if (32 * t + (r & 3) + 8 * (r >> 2) >= left) s[t][r] = -INFINITY;
     }
     const float top = max_halves(fmaxf(max16(s[0]), max16(s[1])));
     if (__any((top - m) * p.c > 8.f)) {  // (a first finite max: inf; NaN never)
@@ -351,12 +368,29 @@ __global__ void __launch_bounds__(64 * NW, 2) attn_prefill_kernel(PrefillParams 
         l += e;
         pf[2 * t + (r >> 3)][r & 7] = (__bf16)e;
       }
-    if (edge && pv_guarded(vt, lane, j, lim, pf, o)) continue;
+    if constexpr (EDGE)
+      if (pv_guarded(vt, pl, lane, j, lim, pf, o)) return;
 #pragma unroll
     for (int kst = 0; kst < 4; ++kst)
 #pragma unroll
       for (int cb = 0; cb < 4; ++cb)
-        o[cb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v_frag(vt, lane, cb, kst), pf[kst], o[cb], 0, 0, 0);
+        o[cb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v_frag(vt, pl, cb, kst), pf[kst], o[cb], 0, 0, 0);
+  };
+
+  if (nblk > 0) load_block(0);
+  auto next = [&](int j) {  // block j is there, and block j + 1 on its way
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    if (j + 1 < nblk) load_block(j + 1);
+  };
+  int j = 0;
+  for (; j < nfull; ++j) {
+    next(j);
+    step(j, std::false_type{});
+  }
+  for (; j < nblk; ++j) {
+    next(j);
+    if (j * PN < lim_hi) step(j, std::true_type{});  // (else the wave's rows see none of it)
   }
 
   // a lane has 64 of the row's 128 channels: 4 of every 8, the other half's in lane ^ 32
