@@ -199,59 +199,10 @@ __device__ __forceinline__ bf16x8 v_frag(const lds_byte* vt, const Places& pl, i
   return u.b;
 }
 
-// O^T += V^T . P^T of a block that not every row sees whole.  A masked key's
-// probability is 0, but 0 times an infinity or a NaN among its values is NaN, in a
-// row that does not see it: where the block holds such values they are taken out,
-// and what they do to the rows that see them is added by itself, counted by one
-// more product of small whole numbers (1 for inf, 128 for -inf, 16384 for NaN; 64
-// keys at most, exact in fp32).  Returns false where there are none.
-__device__ __forceinline__ bool pv_guarded(const lds_byte* vt, const Places& pl, int lane, int j, int lim, const bf16x8 (&pf)[4], f32x16 (&o)[4]) {
-  uint32_t bad = 0;
-#pragma unroll
-  for (int kst = 0; kst < 4; ++kst)
-#pragma unroll
-    for (int cb = 0; cb < 4; ++cb) {
-      __builtin_amdgcn_sched_barrier(0);
-      const u32x4 w = __builtin_bit_cast(u32x4, v_frag(vt, pl, cb, kst));
-#pragma unroll
-      for (int e = 0; e < 4; ++e) bad |= (w[e] & 0x7F807F80u) + 0x00800080u;  // an exponent of all ones carries
-    }
-  if (!__any((bad & 0x80008000u) != 0)) return false;
-  const int h = lane >> 5;
-#pragma unroll
-  for (int cb = 0; cb < 4; ++cb) {
-    f32x16 seen = {};
-#pragma unroll
-    for (int kst = 0; kst < 4; ++kst) {
-      __builtin_amdgcn_sched_barrier(0);  // (one operand at a time: registers, not speed, count here)
-      const u32x4 f = __builtin_bit_cast(u32x4, v_frag(vt, pl, cb, kst));
-      u32x4 fin, code, vis;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {  // two values a word
-        const uint32_t mask = ((((f[e] & 0x7F807F80u) + 0x00800080u) >> 15) & 0x00010001u) * 0xFFFFu;
-        auto kind = [](uint32_t u) { return (u & 0x7Fu) ? 0x4680u : (u & 0x8000u) ? 0x4300u : 0x3F80u; };
-        fin[e] = f[e] & ~mask;
-        code[e] = (kind(f[e] & 0xFFFFu) | (kind(f[e] >> 16) << 16)) & mask;
-        const int r = 8 * (kst & 1) + 2 * e, key = j * PN + 32 * (kst >> 1) + (r & 3) + 8 * (r >> 2) + 4 * h;
-        vis[e] = (key < lim ? 0x3F80u : 0u) | (key + 1 < lim ? 0x3F800000u : 0u);
-      }
-      o[cb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, fin), pf[kst], o[cb], 0, 0, 0);
-      seen = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, code), __builtin_bit_cast(bf16x8, vis),
-                                                     seen, 0, 0, 0);
-    }
-#pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      const int k = (int)seen[r], up = k & 127, down = (k >> 7) & 127;
-      if (k) o[cb][r] += k >= 16384 || (up && down) ? NAN : up ? INFINITY : -INFINITY;
-    }
-  }
-  return true;
-}
-
 template <int NW>
 __global__ void __launch_bounds__(64 * NW, 2) attn_prefill_kernel(PrefillParams p) {
   constexpr int BM = 32 * NW;
-  __shared__ __attribute__((aligned(1024))) unsigned char lds[4 * kTileBytes];  // K, V of two blocks
+  __shared__ __attribute__((aligned(1024))) unsigned char lds[4 * kTileBytes];  // two K tiles, two V tiles
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int n = lane & 31, h = lane >> 5;
 
@@ -310,43 +261,43 @@ __global__ void __launch_bounds__(64 * NW, 2) attn_prefill_kernel(PrefillParams 
   const Places pl = places(lane);
   // 1 KiB is 4 rows of a tile: lane -> row lane / 16, 16-byte place lane % 16
   constexpr int PIECES = kTileBytes / 1024 / NW;
-  auto load_block = [&](int j) {
-    const int left = min(Lk - j * PN, PN);
-    const i32x4 rk = tile_rsrc(kb + (int64_t)j * PN * p.k_tok, p.k_tok, left);
-    const i32x4 rv = tile_rsrc(vb + (int64_t)j * PN * p.v_tok, p.v_tok, left);
-    const uint32_t dst = lds0 + (uint32_t)(j & 1) * (2 * kTileBytes);
+  auto load_k = [&](int j) {
+    const i32x4 rs = tile_rsrc(kb + (int64_t)j * PN * p.k_tok, p.k_tok, min(Lk - j * PN, PN));
+    const uint32_t dst = lds0 + (uint32_t)(j & 1) * kTileBytes;
 #pragma unroll
     for (int i = 0; i < PIECES; ++i) {
       const int piece = wave * PIECES + i, r = 4 * piece + (lane >> 4);
-      lds_load_1k(dst + piece * 1024, rk, (uint32_t)r * (uint32_t)p.k_tok * 2u + (((lane & 15) ^ swz_k(r)) << 4));
-      lds_load_1k(dst + kTileBytes + piece * 1024, rv,
-                  (uint32_t)r * (uint32_t)p.v_tok * 2u + (((lane & 15) ^ swz_v(r)) << 4));
+      lds_load_1k(dst + piece * 1024, rs, (uint32_t)r * (uint32_t)p.k_tok * 2u + (((lane & 15) ^ swz_k(r)) << 4));
     }
   };
+  auto load_v = [&](int j) {
+    const i32x4 rs = tile_rsrc(vb + (int64_t)j * PN * p.v_tok, p.v_tok, min(Lk - j * PN, PN));
+    const uint32_t dst = lds0 + (uint32_t)(2 + (j & 1)) * kTileBytes;
+#pragma unroll
+    for (int i = 0; i < PIECES; ++i) {
+      const int piece = wave * PIECES + i, r = 4 * piece + (lane >> 4);
+      lds_load_1k(dst + piece * 1024, rs, (uint32_t)r * (uint32_t)p.v_tok * 2u + (((lane & 15) ^ swz_v(r)) << 4));
+    }
+  };
+  auto k_tile = [&](int j) { return (lds_byte*)lds + (j & 1) * kTileBytes; };
+  auto v_tile = [&](int j) { return (lds_byte*)lds + (2 + (j & 1)) * kTileBytes; };
 
   f32x16 o[4];
 #pragma unroll
   for (int cb = 0; cb < 4; ++cb) o[cb] = f32x16{};
   float m = -INFINITY, l = 0.f;
+  f32x16 s[2];
+  bf16x8 pf[4];
 
-  // One block of keys; EDGE: some row of the workgroup does not see all of it
-  auto step = [&](int j, auto edge_c) {
-    constexpr bool EDGE = decltype(edge_c)::value;
-    const lds_byte* kt = (const lds_byte*)lds + (j & 1) * (2 * kTileBytes);
-    const lds_byte* vt = kt + kTileBytes;
-    f32x16 s[2] = {f32x16{}, f32x16{}};
+  auto scores = [&](int j) {
+    const lds_byte* kt = k_tile(j);
+    s[0] = s[1] = f32x16{};
 #pragma unroll
     for (int c = 0; c < 8; ++c)
 #pragma unroll
       for (int t = 0; t < 2; ++t) s[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k_frag(kt, pl, t, c), qf[c], s[t], 0, 0, 0);
-    if constexpr (EDGE) {
-      const int left = lim - j * PN - 4 * h;
-#pragma unroll
-      for (int t = 0; t < 2; ++t)
-#pragma unroll
-        for (int r = 0; r < 16; ++r)
-          if (32 * t + (r & 3) + 8 * (r >> 2) >= left) s[t][r] = -INFINITY;
-    }
+  };
+  auto softmax = [&] {
     const float top = max_halves(fmaxf(max16(s[0]), max16(s[1])));
     if (__any((top - m) * p.c > 8.f)) {  // (a first finite max: inf; NaN never)
       const float m_new = fmaxf(m, top);
@@ -359,7 +310,6 @@ __global__ void __launch_bounds__(64 * NW, 2) attn_prefill_kernel(PrefillParams 
       m = m_new;
     }
     const float ms = m == -INFINITY ? 0.f : m * p.c;
-    bf16x8 pf[4];
 #pragma unroll
     for (int t = 0; t < 2; ++t)
 #pragma unroll
@@ -368,29 +318,115 @@ __global__ void __launch_bounds__(64 * NW, 2) attn_prefill_kernel(PrefillParams 
         l += e;
         pf[2 * t + (r >> 3)][r & 7] = (__bf16)e;
       }
-    if constexpr (EDGE)
-      if (pv_guarded(vt, pl, lane, j, lim, pf, o)) return;
+  };
+  auto add_pv = [&](int j) {
+    const lds_byte* vt = v_tile(j);
 #pragma unroll
     for (int kst = 0; kst < 4; ++kst)
 #pragma unroll
       for (int cb = 0; cb < 4; ++cb)
         o[cb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v_frag(vt, pl, cb, kst), pf[kst], o[cb], 0, 0, 0);
   };
-
-  if (nblk > 0) load_block(0);
-  auto next = [&](int j) {  // block j is there, and block j + 1 on its way
+  auto arrived = [&] {  // this wave's loads, and with them everyone's
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
-    if (j + 1 < nblk) load_block(j + 1);
   };
-  int j = 0;
-  for (; j < nfull; ++j) {
-    next(j);
-    step(j, std::false_type{});
+
+  // Blocks that every row sees whole.
+  if (nfull > 0) {
+    load_k(0);
+    load_v(0);
   }
-  for (; j < nblk; ++j) {
-    next(j);
-    if (j * PN < lim_hi) step(j, std::true_type{});  // (else the wave's rows see none of it)
+  for (int j = 0; j < nfull; ++j) {
+    arrived();
+    if (j + 1 < nfull) {
+      load_k(j + 1);
+      load_v(j + 1);
+    }
+    scores(j);
+    softmax();
+    add_pv(j);
+  }
+  // The rest.  A masked key's probability is 0, but 0 times an infinity or a NaN among
+  // its values is NaN, in a row that does not see it.  Where a block holds such values
+  // they are taken out of the V tile and kept, as small whole numbers, in the K tile's
+  // place (1: inf, 128: -inf, 16384: NaN), and a product of their own with the rows' masks
+  // says what they do to the rows that see them (sums over 64 keys, exact in fp32).
+  if (nfull < nblk) {
+    __syncthreads();
+    load_k(nfull);
+    load_v(nfull);
+  }
+  for (int j = nfull; j < nblk; ++j) {
+    arrived();
+    if (j + 1 < nblk) {
+      load_k(j + 1);
+      load_v(j + 1);
+    }
+    const bool mine = j * PN < lim_hi;  // (else the wave's rows see none of it)
+    auto each_word = [&](auto f) {      // the thread's words of the V tile
+#pragma unroll
+      for (int i = 0; i < kTileBytes / 16 / (64 * NW); ++i) {
+        const uint32_t at = (uint32_t)(i * 64 * NW + (int)threadIdx.x) * 16;
+        f(at, *(__attribute__((address_space(3))) u32x4*)(v_tile(j) + at));
+      }
+    };
+    uint32_t bad = 0;
+    if (p.causal)
+      each_word([&](uint32_t, u32x4 w) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) bad |= (w[e] & 0x7F807F80u) + 0x00800080u;  // an exponent of all ones carries
+      });
+    const bool guard = p.causal && __syncthreads_or((bad & 0x80008000u) != 0);
+    if (mine) {
+      scores(j);
+      const int left = lim - j * PN - 4 * h;
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          if (32 * t + (r & 3) + 8 * (r >> 2) >= left) s[t][r] = -INFINITY;
+      softmax();
+    }
+    if (guard) {
+      __syncthreads();  // (the K tile has been read)
+      each_word([&](uint32_t at, u32x4 w) {
+        u32x4 fin, code;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {  // two values a word
+          const uint32_t mask = ((((w[e] & 0x7F807F80u) + 0x00800080u) >> 15) & 0x00010001u) * 0xFFFFu;
+          auto kind = [](uint32_t u) { return (u & 0x7Fu) ? 0x4680u : (u & 0x8000u) ? 0x4300u : 0x3F80u; };
+          fin[e] = w[e] & ~mask;
+          code[e] = (kind(w[e] & 0xFFFFu) | (kind(w[e] >> 16) << 16)) & mask;
+        }
+        *(__attribute__((address_space(3))) u32x4*)(v_tile(j) + at) = fin;
+        *(__attribute__((address_space(3))) u32x4*)(k_tile(j) + at) = code;
+      });
+      __syncthreads();
+      if (mine) {
+#pragma unroll
+        for (int cb = 0; cb < 4; ++cb) {
+          f32x16 seen = {};
+#pragma unroll
+          for (int kst = 0; kst < 4; ++kst) {
+            u32x4 vis;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const int r = 8 * (kst & 1) + 2 * e, key = j * PN + 32 * (kst >> 1) + (r & 3) + 8 * (r >> 2) + 4 * h;
+              vis[e] = (key < lim ? 0x3F80u : 0u) | (key + 1 < lim ? 0x3F800000u : 0u);
+            }
+            seen = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v_frag(k_tile(j), pl, cb, kst), __builtin_bit_cast(bf16x8, vis),
+                                                           seen, 0, 0, 0);
+          }
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            const int k = (int)seen[r];
+            o[cb][r] += ((k & 127) ? INFINITY : 0.f) + (((k >> 7) & 127) ? -INFINITY : 0.f) + (k >= 16384 ? NAN : 0.f);
+          }
+        }
+      }
+    }
+    if (mine) add_pv(j);
   }
 
   // a lane has 64 of the row's 128 channels: 4 of every 8, the other half's in lane ^ 32
@@ -461,18 +497,26 @@ extern "C" int asym_attn_prefill_bf16(int B, int H_q, int H_kv, int D, int T_q, 
   // score (minus infinity) to minus infinity
   p.c = std::fmax(p.scale * 1.4426950408889634f, 1.17549435e-38f);
   p.q_flip = scale < 0 ? 0x80008000u : 0u;
-  constexpr int NW = 4;
-  const int64_t tiles = (int64_t)T_q * p.G / (32 * NW) + B;  // sequences end in a part tile each
+  // Tiles of 256 rows read the keys half as often and are faster once there is one for
+  // every CU (us, 128 rows first: 16384 tokens, 32 / 8 heads 2031 1953, 4096 tokens 149 137,
+  // two of 4096 with 16 / 16 heads 149 138, eight chunks of 1000 tokens behind
+  // prefixes 329 329); with fewer, CUs would idle (1024 tokens, 32 / 8 heads 25 32).
+  auto count = [&](int rows) { return (int64_t)T_q * p.G / rows + B; };  // sequences end in a part tile each
+  const bool wide = count(256) * H_kv >= 256;
+  const int64_t tiles = count(wide ? 256 : 128);
   int64_t grid = tiles * H_kv;
   if (p.aware && kXcds % H_kv == 0) {
     const int share = kXcds / H_kv;
     grid = (tiles + share - 1) / share * kXcds;
   }
-  if (grid >= (1 << 24))  // (threads of a launch are counted in 32 bits)
+  if (grid >= (1 << 23))  // (threads of a launch are counted in 32 bits)
     return fail(ASYM_EUNSUPPORTED, "prefill: too many rows");
   p.tiles = (int)tiles;
-  hipLaunchKernelGGL((attn_prefill_kernel<NW>), dim3((unsigned)grid), dim3(64 * NW), 0, static_cast<hipStream_t>(stream),
-                     p);
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  if (wide)
+    hipLaunchKernelGGL((attn_prefill_kernel<8>), dim3((unsigned)grid), dim3(512), 0, s, p);
+  else
+    hipLaunchKernelGGL((attn_prefill_kernel<4>), dim3((unsigned)grid), dim3(256), 0, s, p);
   ASYM_HIP(hipGetLastError());
   return ASYM_OK;
 }
