@@ -9,6 +9,7 @@ or fails to load, every call raises.
 from __future__ import annotations
 
 import ctypes
+import functools
 import json
 import os
 from typing import Optional, Sequence
@@ -1061,57 +1062,72 @@ def mla_decode_plan(B: int, Hq: int, S: int, split_tokens: int = 0, mapping="awa
 
 FP4_PAGE_BYTES = 2176  # a page of 32 tokens of one head in microscaled 4-bit floating point
 KV_EXTEND, KV_FORK, KV_COMPACT = 0, 1, 2
+_SCALE_128 = 128 ** -0.5
 
 
-class _On:
-    """The device of a call's tensors as the current one, and the stream as torch's
-    current one (its allocations then belong to it); nothing where they are already."""
+# (These calls are short: what the binding does of each costs as much as their
+# kernels, so it looks at each tensor's properties once and compares whole shapes.)
 
-    def __init__(self, device, stream):
-        import torch
-        self.stack = []
-        if device.index is not None and device.index != torch.cuda.current_device():
-            self.stack.append(torch.cuda.device(device))
-        if stream is not None:
-            self.stack.append(torch.cuda.stream(stream))
-
-    def __enter__(self):
-        for c in self.stack:
-            c.__enter__()
-
-    def __exit__(self, *e):
-        for c in reversed(self.stack):
-            c.__exit__(*e)
+def _gpu_of(what, *tensors) -> int:
+    """The one GPU that the tensors are on."""
+    d = tensors[0].get_device()
+    for t in tensors:
+        if t.get_device() != d or d < 0:
+            raise ValueError(f"{what}: the tensors must be on one GPU")
+    return d
 
 
-def _on_gpu(what, first, *rest):
-    if not first.is_cuda or any(t.device != first.device for t in rest):
-        raise ValueError(f"{what}: the tensors must be on one GPU")
+def _on(device: int, stream, call):
+    """call(raw stream) with the tensors' device as the current one, on `stream` or
+    that device's current stream (what the call allocates then belongs to it)."""
+    import torch
+    if stream is None:
+        if device == torch.cuda.current_device():
+            return call(_stream_ptr(None))
+        with torch.cuda.device(device):
+            return call(_stream_ptr(None))
+    if stream.device.index != device:
+        raise ValueError("the stream and the tensors are on different GPUs")
+    with torch.cuda.device(device), torch.cuda.stream(stream):
+        return call(stream.cuda_stream)
 
 
 def _index(t, what, shape=None):
     import torch
-    if t.dtype != torch.int32:
+    if t.dtype is not torch.int32:
         raise TypeError(f"{what} must be int32")
-    if not t.is_contiguous() or (shape is not None and tuple(t.shape) != tuple(shape)):
+    if not t.is_contiguous() or (shape is not None and t.shape != shape):
         raise ValueError(f"{what} must be contiguous" + (f" {list(shape)}" if shape is not None else ""))
 
 
 def _rows128(t, what):
-    """[T, H, 128] bf16 with unit stride in its last dimension: its strides."""
+    """A bf16 [T, H, 128] tensor with unit stride in its last dimension: (T, H, token stride, head stride)."""
     import torch
-    if t.dtype != torch.bfloat16:
+    if t.dtype is not torch.bfloat16:
         raise TypeError(f"{what} must be bfloat16")
-    if t.dim() != 3 or t.shape[2] != 128 or t.stride(2) != 1:
+    shape, stride = t.shape, t.stride()
+    if len(shape) != 3 or shape[2] != 128 or stride[2] != 1:
         raise ValueError(f"{what} must be [tokens, heads, 128] with unit stride in its last dimension")
-    T, H, _ = t.shape
+    T, H, _ = shape
     # (a dimension of one has no stride to keep to)
-    return (t.stride(0) if T > 1 else H * 128), (t.stride(1) if H > 1 else 128)
+    return T, H, (stride[0] if T > 1 else H * 128), (stride[1] if H > 1 else 128)
+
+
+def _outputs(o, lse, shape, o_shape):
+    """Checks the given outputs of an attention call: (their addresses or None, the tensors given)."""
+    import torch
+    if o is not None and (o.dtype is not torch.bfloat16 or o.shape != shape or not o.is_contiguous()):
+        raise ValueError(f"o must be a contiguous bf16 {o_shape} tensor")
+    if lse is None:
+        return None, () if o is None else (o,)
+    if lse.dtype is not torch.float32 or lse.shape != shape[:2] or not lse.is_contiguous():
+        raise ValueError("lse must be contiguous fp32, o's shape without its last dimension")
+    return lse.data_ptr(), (lse,) if o is None else (o, lse)
 
 
 def _workspace(nbytes, device):
     import torch
-    return torch.empty(max(nbytes, 16), dtype=torch.uint8, device=device)
+    return torch.empty(nbytes, dtype=torch.uint8, device=device)
 
 
 def attn_prefill(q, k, v, cu_q, cu_k=None, o=None, lse=None, scale: Optional[float] = None, causal: bool = True,
@@ -1123,52 +1139,49 @@ def attn_prefill(q, k, v, cu_q, cu_k=None, o=None, lse=None, scale: Optional[flo
     defaults to cu_q).  causal: row i of a sequence sees keys j <= i + L_k - L_q.
     Returns O [T_q, H_q, 128] bf16 (and fills lse [T_q, H_q] fp32 when given); rows
     outside every sequence are not written.  scale defaults to 1 / sqrt(128)."""
-    import math
-
     import torch
     if cu_k is None:
         cu_k = cu_q
-    qt, qh = _rows128(q, "q")
-    kt, kh = _rows128(k, "k")
-    vt, vh = _rows128(v, "v")
-    if v.shape != k.shape:
+    Tq, Hq, qt, qh = _rows128(q, "q")
+    Tk, Hkv, kt, kh = _rows128(k, "k")
+    vT, vH, vt, vh = _rows128(v, "v")
+    if vT != Tk or vH != Hkv:
         raise ValueError("k and v must have one shape")
     _index(cu_q, "cu_q")
-    _index(cu_k, "cu_k", cu_q.shape)
-    if cu_q.dim() != 1 or cu_q.numel() < 1:
+    if cu_q.dim() != 1 or cu_q.shape[0] < 1:
         raise ValueError("cu_q must be [B + 1]")
-    Tq, Hq, D = q.shape
-    Tk, Hkv, _ = k.shape
-    _on_gpu("attn_prefill", q, k, v, cu_q, cu_k, *(t for t in (o, lse) if t is not None))
-    if o is not None and (o.dtype != torch.bfloat16 or tuple(o.shape) != (Tq, Hq, D) or not o.is_contiguous()):
-        raise ValueError("o must be a contiguous bf16 [T_q, H_q, 128] tensor")
-    if lse is not None and (lse.dtype != torch.float32 or tuple(lse.shape) != (Tq, Hq) or not lse.is_contiguous()):
-        raise ValueError("lse must be a contiguous fp32 [T_q, H_q] tensor")
-    sc = 1.0 / math.sqrt(D) if scale is None else float(scale)
+    if cu_k is not cu_q:
+        _index(cu_k, "cu_k", cu_q.shape)
+    lse_ptr, out = _outputs(o, lse, (Tq, Hq, 128), "[T_q, H_q, 128]")
+    device = _gpu_of("attn_prefill", q, k, v, cu_q, cu_k, *out)
+    sc = _SCALE_128 if scale is None else float(scale)
     mp = MAPPINGS[mapping] if isinstance(mapping, str) else int(mapping)
-    with _On(q.device, stream):
-        if o is None:
-            o = torch.empty((Tq, Hq, D), dtype=torch.bfloat16, device=q.device)
+
+    def call(raw):
+        r = torch.empty((Tq, Hq, 128), dtype=torch.bfloat16, device=q.device) if o is None else o
         _check(load_library().asym_attn_prefill_bf16(
-            cu_q.numel() - 1, Hq, Hkv, D, Tq, Tk, q.data_ptr(), qt, qh, k.data_ptr(), kt, kh, v.data_ptr(), vt, vh,
-            o.data_ptr(), lse.data_ptr() if lse is not None else None, cu_q.data_ptr(), cu_k.data_ptr(), sc,
-            1 if causal else 0, mp, _stream_ptr(stream)))
-    return o
+            cu_q.shape[0] - 1, Hq, Hkv, 128, Tq, Tk, q.data_ptr(), qt, qh, k.data_ptr(), kt, kh, v.data_ptr(), vt, vh,
+            r.data_ptr(), lse_ptr, cu_q.data_ptr(), cu_k.data_ptr(), sc, 1 if causal else 0, mp, raw))
+        return r
+    return _on(device, stream, call)
 
 
 def _fp4_cache(k_pool, v_pool, k_pages, v_pages):
-    """Checks a 4-bit cache's pools and tables; (B, H_kv, pages per head)."""
+    """Checks a 4-bit cache's pools and tables: (B, H_kv, pages per head)."""
     import torch
-    if k_pool.dtype != torch.uint8 or v_pool.dtype != torch.uint8:
+    if k_pool.dtype is not torch.uint8 or v_pool.dtype is not torch.uint8:
         raise TypeError("pools must be uint8")
-    if k_pool.dim() != 2 or k_pool.shape[1] != FP4_PAGE_BYTES or v_pool.shape != k_pool.shape \
-            or not k_pool.is_contiguous() or not v_pool.is_contiguous():
+    pool = k_pool.shape
+    if len(pool) != 2 or pool[1] != FP4_PAGE_BYTES or v_pool.shape != pool or not k_pool.is_contiguous() \
+            or not v_pool.is_contiguous():
         raise ValueError("pools must be contiguous [pool_pages, 2176]")
     _index(k_pages, "k_pages")
-    if k_pages.dim() != 3:
+    shape = k_pages.shape
+    if len(shape) != 3:
         raise ValueError("page tables must be [B, H_kv, pages]")
-    _index(v_pages, "v_pages", k_pages.shape)
-    return tuple(k_pages.shape)
+    if v_pages is not k_pages:
+        _index(v_pages, "v_pages", shape)
+    return shape
 
 
 def kv_write_fp4(k, v, k_pool, v_pool, k_pages, v_pages, cu, start, stream=None) -> None:
@@ -1176,19 +1189,17 @@ def kv_write_fp4(k, v, k_pool, v_pool, k_pages, v_pages, cu, start, stream=None)
     [T, H_kv, 128] (bf16, strided as in attn_prefill) become request b's positions
     start[b] onwards.  Pools uint8 [pool_pages, 2176]; tables int32 [B, H_kv, pages];
     cu int32 [B + 1], start int32 [B].  Pages must not be shared between requests."""
-    kt, kh = _rows128(k, "k")
-    vt, vh = _rows128(v, "v")
-    B, H, pph = _fp4_cache(k_pool, v_pool, k_pages, v_pages)
-    if k.shape != v.shape or k.shape[1] != H:
+    T, H, kt, kh = _rows128(k, "k")
+    vT, vH, vt, vh = _rows128(v, "v")
+    B, Hkv, pph = _fp4_cache(k_pool, v_pool, k_pages, v_pages)
+    if vT != T or vH != H or H != Hkv:
         raise ValueError("k and v must be [T, H_kv, 128], H_kv as in the tables")
     _index(cu, "cu", (B + 1,))
     _index(start, "start", (B,))
-    _on_gpu("kv_write_fp4", k, v, k_pool, v_pool, k_pages, v_pages, cu, start)
-    with _On(k.device, stream):
-        _check(load_library().asym_kv_write_fp4(
-            B, H, k.shape[0], k.data_ptr(), kt, kh, v.data_ptr(), vt, vh, k_pool.data_ptr(), v_pool.data_ptr(),
-            k_pool.shape[0], k_pages.data_ptr(), v_pages.data_ptr(), pph, cu.data_ptr(), start.data_ptr(),
-            _stream_ptr(stream)))
+    device = _gpu_of("kv_write_fp4", k, v, k_pool, v_pool, k_pages, v_pages, cu, start)
+    _on(device, stream, lambda raw: _check(load_library().asym_kv_write_fp4(
+        B, H, T, k.data_ptr(), kt, kh, v.data_ptr(), vt, vh, k_pool.data_ptr(), v_pool.data_ptr(), k_pool.shape[0],
+        k_pages.data_ptr(), v_pages.data_ptr(), pph, cu.data_ptr(), start.data_ptr(), raw)))
 
 
 def kv_read_fp4(k_pool, v_pool, k_pages, v_pages, cu, start, k, v, stream=None):
@@ -1197,19 +1208,27 @@ def kv_read_fp4(k_pool, v_pool, k_pages, v_pages, cu, start, k, v, stream=None):
     (contiguous); returns (k, v)."""
     import torch
     B, H, pph = _fp4_cache(k_pool, v_pool, k_pages, v_pages)
-    for t, what in ((k, "k"), (v, "v")):
-        if t.dtype != torch.bfloat16:
-            raise TypeError(f"{what} must be bfloat16")
-        if t.dim() != 3 or tuple(t.shape[1:]) != (H, 128) or t.shape != k.shape or not t.is_contiguous():
-            raise ValueError("k and v must be contiguous [T, H_kv, 128]")
+    if k.dtype is not torch.bfloat16 or v.dtype is not torch.bfloat16:
+        raise TypeError("k and v must be bfloat16")
+    shape = k.shape
+    if len(shape) != 3 or shape[1] != H or shape[2] != 128 or v.shape != shape or not k.is_contiguous() \
+            or not v.is_contiguous():
+        raise ValueError("k and v must be contiguous [T, H_kv, 128]")
     _index(cu, "cu", (B + 1,))
     _index(start, "start", (B,))
-    _on_gpu("kv_read_fp4", k, v, k_pool, v_pool, k_pages, v_pages, cu, start)
-    with _On(k.device, stream):
-        _check(load_library().asym_kv_read_fp4(
-            B, H, k.shape[0], k_pool.data_ptr(), v_pool.data_ptr(), k_pool.shape[0], k_pages.data_ptr(),
-            v_pages.data_ptr(), pph, cu.data_ptr(), start.data_ptr(), k.data_ptr(), v.data_ptr(), _stream_ptr(stream)))
+    device = _gpu_of("kv_read_fp4", k, v, k_pool, v_pool, k_pages, v_pages, cu, start)
+    _on(device, stream, lambda raw: _check(load_library().asym_kv_read_fp4(
+        B, H, shape[0], k_pool.data_ptr(), v_pool.data_ptr(), k_pool.shape[0], k_pages.data_ptr(), v_pages.data_ptr(), pph,
+        cu.data_ptr(), start.data_ptr(), k.data_ptr(), v.data_ptr(), raw)))
     return k, v
+
+
+@functools.lru_cache(maxsize=256)
+def _fp4_plan_workspace(B, Hq, Hkv, S, split_tokens) -> int:
+    """The plan's workspace bytes (a function of the sizes alone)."""
+    plan = AttnPlanInfo()
+    _check(load_library().asym_attn_decode_paged_fp4_plan(B, Hq, Hkv, S, 128, split_tokens, ctypes.byref(plan)))
+    return plan.workspace_bytes
 
 
 def attn_decode_paged_fp4(q, k_pool, v_pool, k_pages, v_pages, lens, S: Optional[int] = None, o=None, lse=None,
@@ -1218,39 +1237,33 @@ def attn_decode_paged_fp4(q, k_pool, v_pool, k_pages, v_pages, lens, S: Optional
     [pool_pages, 2176]; tables int32 [B, H_kv, pages]; lens int32 [B], each request's
     tokens, at most S (default: what the tables hold).  Returns O [B, H_q, 128] bf16
     (and fills lse [B, H_q] fp32 when given)."""
-    import math
-
     import torch
-    if q.dtype != torch.bfloat16:
+    if q.dtype is not torch.bfloat16:
         raise TypeError("q must be bfloat16")
-    if q.dim() != 3 or q.shape[2] != 128 or not q.is_contiguous():
+    shape = q.shape
+    if len(shape) != 3 or shape[2] != 128 or not q.is_contiguous():
         raise ValueError("q must be contiguous [B, H_q, 128]")
     B, H, pph = _fp4_cache(k_pool, v_pool, k_pages, v_pages)
-    if q.shape[0] != B:
+    if shape[0] != B:
         raise ValueError("q and the tables disagree on B")
-    Hq = q.shape[1]
+    Hq = shape[1]
     _index(lens, "lens", (B,))
     if S is None:
         S = pph * PAGE_TOKENS
-    _on_gpu("attn_decode_paged_fp4", q, k_pool, v_pool, k_pages, v_pages, lens, *(t for t in (o, lse) if t is not None))
-    if o is not None and (o.dtype != torch.bfloat16 or tuple(o.shape) != (B, Hq, 128) or not o.is_contiguous()):
-        raise ValueError("o must be a contiguous bf16 [B, H_q, 128] tensor")
-    if lse is not None and (lse.dtype != torch.float32 or tuple(lse.shape) != (B, Hq) or not lse.is_contiguous()):
-        raise ValueError("lse must be a contiguous fp32 [B, H_q] tensor")
-    sc = 1.0 / math.sqrt(128) if scale is None else float(scale)
-    plan = AttnPlanInfo()
-    lib = load_library()
-    _check(lib.asym_attn_decode_paged_fp4_plan(B, Hq, H, S, 128, split_tokens, ctypes.byref(plan)))
-    nbytes = plan.workspace_bytes
-    with _On(q.device, stream):
-        if o is None:
-            o = torch.empty((B, Hq, 128), dtype=torch.bfloat16, device=q.device)
+    lse_ptr, out = _outputs(o, lse, shape, "[B, H_q, 128]")
+    device = _gpu_of("attn_decode_paged_fp4", q, k_pool, v_pool, k_pages, v_pages, lens, *out)
+    sc = _SCALE_128 if scale is None else float(scale)
+    nbytes = _fp4_plan_workspace(B, Hq, H, S, split_tokens)
+
+    def call(raw):
+        r = torch.empty(shape, dtype=torch.bfloat16, device=q.device) if o is None else o
         ws = _workspace(nbytes, q.device) if nbytes else None
-        _check(lib.asym_attn_decode_paged_fp4(
+        _check(load_library().asym_attn_decode_paged_fp4(
             B, Hq, H, S, 128, q.data_ptr(), k_pool.data_ptr(), v_pool.data_ptr(), k_pool.shape[0], k_pages.data_ptr(),
-            v_pages.data_ptr(), pph, lens.data_ptr(), o.data_ptr(), lse.data_ptr() if lse is not None else None, sc,
-            split_tokens, ws.data_ptr() if nbytes else None, nbytes, _stream_ptr(stream)))
-    return o
+            v_pages.data_ptr(), pph, lens.data_ptr(), r.data_ptr(), lse_ptr, sc, split_tokens,
+            ws.data_ptr() if nbytes else None, nbytes, raw))
+        return r
+    return _on(device, stream, call)
 
 
 def attn_decode_paged_fp4_plan(B: int, Hq: int, Hkv: int, S: int, D: int = 128, split_tokens: int = 0) -> dict:
@@ -1259,48 +1272,50 @@ def attn_decode_paged_fp4_plan(B: int, Hq: int, Hkv: int, S: int, D: int = 128, 
     return out.to_dict()
 
 
-def _pages_state(what, table, lens, refs, *lists):
-    """Checks a paged cache's state and a call's request lists; (R, H, pages per head)."""
+def _pages_state(table, lens, refs):
+    """Checks a paged cache's state: (R, H, pages per head, pool pages)."""
     _index(table, "table")
-    if table.dim() != 3:
+    shape = table.shape
+    if len(shape) != 3:
         raise ValueError("table must be [R, H, pages]")
-    R, H, pph = table.shape
-    if lens is not None:
-        _index(lens, "lens", (R,))
+    _index(lens, "lens", shape[:1])
     _index(refs, "refs")
     if refs.dim() != 1:
         raise ValueError("refs must be [pool_pages]")
-    for t in lists:
-        if t is not None:
-            _index(t, "request lists and status")
-            if t.dim() != 1:
-                raise ValueError("request lists and status must have one dimension")
-    _on_gpu(what, table, refs, *(t for t in (lens, *lists) if t is not None))
-    return R, H, pph
+    return *shape, refs.shape[0]
 
 
-def _pools(what, k_pool, v_pool, refs):
-    """Checks the pools that a call moves pages of; (k pointer, v pointer, page bytes)."""
-    pools = [k_pool] if v_pool is None else [k_pool, v_pool]
-    _on_gpu(what, refs, *pools)
-    n = refs.shape[0]
-    for t in pools:
-        if t.dim() < 2 or t.shape[0] != n or not t.is_contiguous() or t.shape != k_pool.shape or t.dtype != k_pool.dtype:
-            raise ValueError("pools must be contiguous [pool_pages, ...], of one shape and type, pool_pages as in refs")
-    return k_pool.data_ptr(), (v_pool.data_ptr() if v_pool is not None else None), \
-        k_pool.numel() // max(n, 1) * k_pool.element_size()
+def _requests(a, b=None) -> int:
+    """Checks a call's request lists: their length."""
+    _index(a, "request lists")
+    if a.dim() != 1:
+        raise ValueError("request lists must have one dimension")
+    if b is not None:
+        _index(b, "request lists", a.shape)
+    return a.shape[0]
+
+
+def _pools(k_pool, v_pool, pool_pages) -> int:
+    """Checks the pools that a call moves pages of: the page's bytes."""
+    shape, dtype = k_pool.shape, k_pool.dtype
+    if len(shape) < 2 or shape[0] != pool_pages or not k_pool.is_contiguous() or (v_pool is not None and (
+            v_pool.shape != shape or v_pool.dtype is not dtype or not v_pool.is_contiguous())):
+        raise ValueError("pools must be contiguous [pool_pages, ...], of one shape and type, pool_pages as in refs")
+    return k_pool.numel() // max(pool_pages, 1) * k_pool.element_size()
 
 
 def _status(status):
-    if status is not None and status.numel() != 2:
-        raise ValueError("status must have 2 entries")
-    return status.data_ptr() if status is not None else None
+    if status is None:
+        return None
+    _index(status, "status", (2,))
+    return status.data_ptr()
 
 
-def _pages_workspace(op, R, H, pph, pool_pages, n, device):
+@functools.lru_cache(maxsize=256)
+def _pages_workspace(op, R, H, pph, pool_pages, n) -> int:
     nbytes = ctypes.c_size_t()
     _check(load_library().asym_kv_pages_workspace(op, R, H, pph, pool_pages, n, ctypes.byref(nbytes)))
-    return _workspace(nbytes.value, device), nbytes.value
+    return nbytes.value
 
 
 def kv_extend(table, lens, refs, rows, new_lens, status=None, stream=None) -> None:
@@ -1308,15 +1323,18 @@ def kv_extend(table, lens, refs, rows, new_lens, status=None, stream=None) -> No
     pages up to new_lens[i] tokens; refs [pool_pages] and lens [R] follow.  All int32
     CUDA tensors.  status [2]: pages taken and 0, or 0 and the number of pages lacking
     (then nothing changes)."""
-    R, H, pph = _pages_state("kv_extend", table, lens, refs, rows, new_lens, status)
-    if rows.shape != new_lens.shape:
-        raise ValueError("rows and new_lens must have one shape")
+    R, H, pph, pool = _pages_state(table, lens, refs)
+    n = _requests(rows, new_lens)
     st = _status(status)
-    with _On(table.device, stream):
-        ws, nbytes = _pages_workspace(KV_EXTEND, R, H, pph, refs.shape[0], rows.numel(), table.device)
+    device = _gpu_of("kv_extend", table, lens, refs, rows, new_lens, *(() if status is None else (status,)))
+    nbytes = _pages_workspace(KV_EXTEND, R, H, pph, pool, n)
+
+    def call(raw):
+        ws = _workspace(nbytes, table.device)
         _check(load_library().asym_kv_extend(
-            R, H, pph, table.data_ptr(), lens.data_ptr(), refs.data_ptr(), refs.shape[0], rows.numel(), rows.data_ptr(),
-            new_lens.data_ptr(), st, ws.data_ptr(), nbytes, _stream_ptr(stream)))
+            R, H, pph, table.data_ptr(), lens.data_ptr(), refs.data_ptr(), pool, n, rows.data_ptr(), new_lens.data_ptr(),
+            st, ws.data_ptr(), nbytes, raw))
+    _on(device, stream, call)
 
 
 def kv_fork(k_pool, v_pool, table, lens, refs, src, dst, status=None, stream=None) -> None:
@@ -1324,39 +1342,49 @@ def kv_fork(k_pool, v_pool, table, lens, refs, src, dst, status=None, stream=Non
     whole pages shared, a part page at the end copied into the lowest free page; what
     row dst[i] held is given up.  Pools [pool_pages, ...] (v_pool None: only one); the
     rest as kv_extend."""
-    R, H, pph = _pages_state("kv_fork", table, lens, refs, src, dst, status)
-    if src.shape != dst.shape:
-        raise ValueError("src and dst must have one shape")
-    kp, vp, page = _pools("kv_fork", k_pool, v_pool, refs)
+    R, H, pph, pool = _pages_state(table, lens, refs)
+    n = _requests(src, dst)
+    page = _pools(k_pool, v_pool, pool)
     st = _status(status)
-    with _On(table.device, stream):
-        ws, nbytes = _pages_workspace(KV_FORK, R, H, pph, refs.shape[0], src.numel(), table.device)
+    device = _gpu_of("kv_fork", table, lens, refs, src, dst, k_pool, k_pool if v_pool is None else v_pool,
+                     *(() if status is None else (status,)))
+    nbytes = _pages_workspace(KV_FORK, R, H, pph, pool, n)
+
+    def call(raw):
+        ws = _workspace(nbytes, table.device)
         _check(load_library().asym_kv_fork(
-            R, H, pph, table.data_ptr(), lens.data_ptr(), refs.data_ptr(), kp, vp, page, refs.shape[0], src.numel(),
-            src.data_ptr(), dst.data_ptr(), st, ws.data_ptr(), nbytes, _stream_ptr(stream)))
+            R, H, pph, table.data_ptr(), lens.data_ptr(), refs.data_ptr(), k_pool.data_ptr(),
+            None if v_pool is None else v_pool.data_ptr(), page, pool, n, src.data_ptr(), dst.data_ptr(), st,
+            ws.data_ptr(), nbytes, raw))
+    _on(device, stream, call)
 
 
 def kv_free(table, lens, refs, rows, stream=None) -> None:
     """Rows of a paged cache end: their pages' counts fall, their entries become -1."""
-    R, H, pph = _pages_state("kv_free", table, lens, refs, rows)
-    with _On(table.device, stream):
-        _check(load_library().asym_kv_free(
-            R, H, pph, table.data_ptr(), lens.data_ptr(), refs.data_ptr(), refs.shape[0], rows.numel(), rows.data_ptr(),
-            _stream_ptr(stream)))
+    R, H, pph, pool = _pages_state(table, lens, refs)
+    n = _requests(rows)
+    device = _gpu_of("kv_free", table, lens, refs, rows)
+    _on(device, stream, lambda raw: _check(load_library().asym_kv_free(
+        R, H, pph, table.data_ptr(), lens.data_ptr(), refs.data_ptr(), pool, n, rows.data_ptr(), raw)))
 
 
 def kv_compact(k_pool, v_pool, table, lens, refs, status=None, stream=None) -> None:
     """The n pages in use of a paged cache become pages 0 .. n - 1: those at or above n
     move, in order, into the free ones below; refs and table follow (lens does not
     change).  status [2]: pages moved, n."""
-    R, H, pph = _pages_state("kv_compact", table, lens, refs, status)
-    kp, vp, page = _pools("kv_compact", k_pool, v_pool, refs)
+    R, H, pph, pool = _pages_state(table, lens, refs)
+    page = _pools(k_pool, v_pool, pool)
     st = _status(status)
-    with _On(table.device, stream):
-        ws, nbytes = _pages_workspace(KV_COMPACT, R, H, pph, refs.shape[0], 0, table.device)
+    device = _gpu_of("kv_compact", table, lens, refs, k_pool, k_pool if v_pool is None else v_pool,
+                     *(() if status is None else (status,)))
+    nbytes = _pages_workspace(KV_COMPACT, R, H, pph, pool, 0)
+
+    def call(raw):
+        ws = _workspace(nbytes, table.device)
         _check(load_library().asym_kv_compact(
-            R, H, pph, table.data_ptr(), refs.data_ptr(), kp, vp, page, refs.shape[0], st, ws.data_ptr(), nbytes,
-            _stream_ptr(stream)))
+            R, H, pph, table.data_ptr(), refs.data_ptr(), k_pool.data_ptr(), None if v_pool is None else v_pool.data_ptr(),
+            page, pool, st, ws.data_ptr(), nbytes, raw))
+    _on(device, stream, call)
 
 
 # ---- copy and co-run --------------------------------------------------------------

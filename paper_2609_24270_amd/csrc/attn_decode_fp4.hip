@@ -54,13 +54,6 @@ struct Fp4DecodeParams {
   uint32_t q_flip;
 };
 
-__device__ __forceinline__ __amdgpu_buffer_rsrc_t page_rsrc(const uint8_t* pool, int page, int pool_pages) {
-  // a page outside the pool reads as zeros
-  const bool in = page >= 0 && page < pool_pages;
-  const uint64_t a = (uint64_t)pool + (uint64_t)(uint32_t)(in ? page : 0) * kFp4PageBytes;
-  return __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void*>(a), (short)0, in ? kFp4PageBytes : 0, 0x00020000);
-}
-
 __device__ __forceinline__ float max_quarters(float x) {
   x = fmaxf(x, __shfl_xor(x, 16));
   return fmaxf(x, __shfl_xor(x, 32));

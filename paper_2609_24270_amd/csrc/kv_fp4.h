@@ -35,6 +35,13 @@ constexpr int kFp4ScaleOff = 2048;
 constexpr int kKvPageTokens = 32;
 constexpr int kKvD = 128;
 
+// The bytes of one page; a page outside the pool reads as zeros.
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t page_rsrc(const uint8_t* pool, int page, int pool_pages) {
+  const bool in = page >= 0 && page < pool_pages;
+  const uint64_t a = (uint64_t)pool + (uint64_t)(uint32_t)(in ? page : 0) * kFp4PageBytes;
+  return __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void*>(a), (short)0, in ? kFp4PageBytes : 0, 0x00020000);
+}
+
 // Sum over the lanes up to and including this one (64 lanes; every lane on).
 __device__ __forceinline__ int wave_scan_add(int x) {
   x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xF, 0xF, true);  // row_shr 1, 2, 4, 8

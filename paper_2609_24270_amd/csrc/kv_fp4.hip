@@ -15,6 +15,8 @@ namespace {
 constexpr int kWaves = 4;
 
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 struct KvParams {
@@ -180,30 +182,54 @@ __global__ void __launch_bounds__(64 * kWaves) kv_read_kernel(KvParams p) {
   if (item / p.H >= p.ranks || !find_page(p, item / p.H, seq, page, row, lo, hi)) return;
   const size_t entry = ((size_t)seq * p.H + head) * p.pph + page;
   const int kp = __builtin_amdgcn_readfirstlane(p.k_pages[entry]), vp = __builtin_amdgcn_readfirstlane(p.v_pages[entry]);
-  const bool k_in = kp >= 0 && kp < p.pool_pages, v_in = vp >= 0 && vp < p.pool_pages;  // else zeros
-  const uint8_t* ks = p.k_pool + (size_t)(k_in ? kp : 0) * kFp4PageBytes;
-  const uint8_t* vs = p.v_pool + (size_t)(v_in ? vp : 0) * kFp4PageBytes;
-  const int c16 = lane & 15, b = c16 >> 2;
-  for (int t = lane >> 4; t < kKvPageTokens; t += 4) {
-    if (t < lo || t >= hi) continue;
-    const int64_t out = ((int64_t)(row + t) * p.H + head) * kKvD + 8 * c16;
-    u32x4 x = {}, y = {};
-    if (k_in)
-      x = values8(*reinterpret_cast<const uint32_t*>(ks + 64 * t + 4 * c16),
-                  ks[kFp4ScaleOff + 2 * ((t & 15) + 16 * b) + (t >> 4)]);
-    if (v_in) {
-      const int q = (t & 15) >> 2, j = (t & 3) + 4 * (t >> 4);
-      uint32_t w = 0;
+  const __amdgpu_buffer_rsrc_t rk = page_rsrc(p.k_pool, kp, p.pool_pages), rv = page_rsrc(p.v_pool, vp, p.pool_pages);
+  const int n = lane & 15, q = lane >> 4;
+  // keys: lane (token n of either half, block q) has 32 channels
+  u32x4 kc[2], vc[2];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const int c = 8 * c16 + e;
-        const uint32_t byte = vs[1024 * (c >> 6) + 16 * ((c & 15) + 16 * q) + 4 * ((c >> 4) & 3) + (j >> 1)];
-        w |= ((byte >> (4 * (j & 1))) & 0xFu) << (4 * e);
+  for (int t = 0; t < 2; ++t) {
+    kc[t] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rk, 1024 * t + 64 * n + 16 * q, 0, 0));
+    vc[t] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rv, 1024 * t + 16 * lane, 0, 0));
+  }
+  const uint32_t kscale = __builtin_amdgcn_raw_buffer_load_b16(rk, kFp4ScaleOff + 2 * lane, 0, 0);
+  uint32_t vscale[2];  // of token n of either half: 4 blocks, one a byte
+#pragma unroll
+  for (int t = 0; t < 2; ++t)
+    vscale[t] = __builtin_amdgcn_raw_buffer_load_b32(rv, kFp4ScaleOff + 32 * (n >> 2) + 4 * ((n & 3) + 4 * t), 0, 0);
+#pragma unroll
+  for (int t = 0; t < 2; ++t) {
+    const int tok = 16 * t + n;
+    if (tok < lo || tok >= hi) continue;
+    u32x4* dst = reinterpret_cast<u32x4*>(p.ko + ((int64_t)(row + tok) * p.H + head) * kKvD + 32 * q);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) dst[i] = values8(kc[t][i], (kscale >> (8 * t)) & 0xFFu);
+  }
+  // values: the page has them channel by channel; a matrix product with the tokens' scales
+  // on a diagonal turns them (exact: every sum has one term).  Column n is token 16 t + n,
+  // which lies in slot (n % 4) + 4 t of quarter n / 4.
+#pragma unroll
+  for (int t = 0; t < 2; ++t) {
+    const int tok = 16 * t + n;
+    const bool on = tok >= lo && tok < hi;
+    uint2* dst = reinterpret_cast<uint2*>(p.vo + ((int64_t)(row + tok) * p.H + head) * kKvD + 4 * q);
+#pragma unroll
+    for (int blk = 0; blk < 4; ++blk) {
+      const uint32_t sb = (vscale[t] >> (8 * blk)) & 0xFFu;
+      // (a power of two, or NaN, as bf16)
+      const uint32_t h = q == (n >> 2) ? (sb == 255u ? 0x7FC0u : sb << 7) : 0u;
+      u32x4 d = {};
+#pragma unroll
+      for (int w = 0; w < 2; ++w)
+        d[2 * t + w] = (n & 3) >> 1 == w ? ((n & 1) ? h << 16 : h) : 0u;
+#pragma unroll
+      for (int g2 = 0; g2 < 2; ++g2) {
+        const int g = 2 * blk + g2;
+        const f32x4 x = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+            __builtin_bit_cast(bf16x8, values8(vc[g >> 2][g & 3], 127u)), __builtin_bit_cast(bf16x8, d), f32x4{}, 0, 0, 0);
+        const bf16x2 y0 = {(__bf16)x[0], (__bf16)x[1]}, y1 = {(__bf16)x[2], (__bf16)x[3]};
+        if (on) dst[4 * g] = uint2{__builtin_bit_cast(uint32_t, y0), __builtin_bit_cast(uint32_t, y1)};
       }
-      y = values8(w, vs[kFp4ScaleOff + 32 * q + 4 * j + b]);
     }
-    *reinterpret_cast<u32x4*>(p.ko + out) = x;
-    *reinterpret_cast<u32x4*>(p.vo + out) = y;
   }
 }
 

@@ -13,7 +13,9 @@
 //   2. each segment adds up the counts before it and writes its pages' numbers to their
 //      places in a list;
 //   3. the tables, the counts and the pages themselves are changed.
-// They are bound by launches and, for large calls, by the copies (read and written once).
+// Up to 16384 pages and 1024 requests one workgroup does 1 and 2, and all of an extend:
+// short calls are bound by their launches.  Large ones are bound by the copies (each page
+// read and written once).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -26,13 +28,15 @@ namespace {
 
 constexpr int kSeg = 4096;     // pages counted by a workgroup
 constexpr int kThreads = 256;
-constexpr int kPer = kSeg / kThreads;
+constexpr int kPer = kSeg / kThreads;  // pages of a thread
+constexpr int kSmallThreads = 1024;    // of the one workgroup of a small call
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
-// Words of the workspace, in order: the header; counts [segments]; first [n] (place of a
-// request's first page in the list); flag [n]; list [pool_pages]; then rows [n][H][pph]
-// and new_len [n] (fork) or holes [pool_pages] and where [pool_pages] (compact).
+// Words of the workspace, in order: the header; counts [segments]; list [pool_pages]; then
+// holes [pool_pages] and where [pool_pages] (compact), or first [n] (place of a request's
+// first page in the list), flag [n] and claim [R] (the first request that names a row), and
+// new_len [n] and rows [n][H][pph] (fork).
 enum { kNeed = 0, kTotal = 1, kHoles = 2, kHeader = 16 };
 
 struct PagesParams {
@@ -44,7 +48,7 @@ struct PagesParams {
   uint8_t *k_pool, *v_pool;
   int64_t page_bytes;
   int R, H, pph, pool, n, segs;
-  int *head, *counts, *first, *flag, *list, *rows, *new_len, *holes, *where;
+  int *head, *counts, *first, *flag, *claim, *list, *rows, *new_len, *holes, *where;
 };
 
 __device__ __forceinline__ int pages_of(int len, int pph) {
@@ -52,7 +56,8 @@ __device__ __forceinline__ int pages_of(int len, int pph) {
 }
 
 // Sum over the workgroup's threads before this one, and over all of them.
-__device__ int block_scan(int x, int* red, int& all) {
+template <int THREADS>
+__device__ __forceinline__ int block_scan(int x, int* red, int& all) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int upto = wave_scan_add(x);
   __syncthreads();  // (red may still be read from the call before)
@@ -61,22 +66,64 @@ __device__ int block_scan(int x, int* red, int& all) {
   int before = 0;
   all = 0;
 #pragma unroll
-  for (int w = 0; w < kThreads / 64; ++w) {
+  for (int w = 0; w < THREADS / 64; ++w) {
     if (w < wave) before += red[w];
     all += red[w];
   }
   return before + upto - x;
 }
 
-// Whether request i names a row that no earlier request of the call names.
-__device__ __forceinline__ bool first_of_its_row(const int* __restrict__ rows, int i) {
-  const int r = rows[i];
-  bool seen = false;
-  for (int j = 0; j < i; ++j) seen |= rows[j] == r;
-  return !seen;
+enum { kExtend, kFork, kCompact };
+
+// Pages that request i needs (-1: it is left out, `first`: no earlier request names its row).
+template <int OP>
+__device__ __forceinline__ int request_needs(const PagesParams& p, int i, bool first) {
+  if constexpr (OP == kExtend) {
+    const int r = p.a[i], to = p.b[i];
+    // (a row outside the table, a length that is no longer or does not fit: left as it is)
+    if (!first || r < 0 || r >= p.R || to <= p.lens[r] || (int64_t)to > (int64_t)p.pph * kKvPageTokens) return -1;
+    return (pages_of(to, p.pph) - pages_of(p.lens[r], p.pph)) * p.H;
+  } else {
+    const int s = p.a[i], d = p.b[i];
+    if (!first || s < 0 || s >= p.R || d < 0 || d >= p.R || s == d) return -1;
+    return min(max(p.lens[s], 0), p.pph * kKvPageTokens) % kKvPageTokens ? p.H : 0;
+  }
 }
 
-enum { kExtend, kFork, kCompact };
+// A thread's kPer pages: bit i says whether page first + i is live (compact) or free.
+template <int OP>
+__device__ __forceinline__ uint32_t page_bits(const PagesParams& p, int64_t first) {
+  uint32_t bits = 0;
+  int r[kPer];
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) r[i] = first + i < p.pool ? p.refs[first + i] : OP == kCompact ? 0 : 1;
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) bits |= (uint32_t)((r[i] > 0) == (OP == kCompact)) << i;
+  return bits;
+}
+
+// 2. list[r]: the r-th free page (as many as are needed), or the r-th live one; compact:
+// holes[r], the r-th free page below the number of live ones, and where[page] = page.
+// `rank`: of the thread's first page.
+template <int OP>
+__device__ __forceinline__ void place_pages(const PagesParams& p, int64_t first, uint32_t bits, int rank, int need,
+                                            int total) {
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) {
+    const int64_t page = first + i;
+    const bool x = (bits >> i) & 1;
+    if (page >= p.pool) break;
+    if constexpr (OP == kCompact) {
+      if (x) p.list[rank] = (int)page;
+      p.where[page] = (int)page;
+      if (!x && page < total) p.holes[page - rank] = (int)page;
+      if (page == total - 1) p.head[kHoles] = total - rank - (x ? 1 : 0);  // free pages below `total`
+    } else {
+      if (x && rank < need) p.list[rank] = (int)page;
+    }
+    rank += x;
+  }
+}
 
 // 1. counts[s]: free pages (extend, fork) or live ones (compact) of segment s; the last
 // workgroup: what the requests need.
@@ -85,44 +132,33 @@ __global__ void __launch_bounds__(kThreads) pages_count(PagesParams p) {
   __shared__ int red[kThreads / 64];
   const int seg = blockIdx.x;
   if (seg < p.segs) {
-    int c = 0;
-    for (int i = 0; i < kPer; ++i) {
-      const int64_t page = (int64_t)seg * kSeg + i * kThreads + threadIdx.x;
-      if (page < p.pool) c += (p.refs[page] > 0) == (OP == kCompact);
-    }
     int all;
-    block_scan(c, red, all);
+    block_scan<kThreads>(__popc(page_bits<OP>(p, (int64_t)seg * kSeg + (int)threadIdx.x * kPer)), red, all);
     if (threadIdx.x == 0) p.counts[seg] = all;
     return;
   }
   if constexpr (OP != kCompact) {
+    const int* row_of = OP == kExtend ? p.a : p.b;  // the row that a request changes
+    for (int r = threadIdx.x; r < p.R; r += kThreads) p.claim[r] = 0x7FFFFFFF;
+    __syncthreads();
+    for (int i = threadIdx.x; i < p.n; i += kThreads)
+      if (row_of[i] >= 0 && row_of[i] < p.R) atomicMin(&p.claim[row_of[i]], i);
+    __syncthreads();
     int base = 0;
     for (int i0 = 0; i0 < p.n; i0 += kThreads) {
       const int i = i0 + threadIdx.x;
-      int need = 0, ok = 0;
+      int need = -1;
       if (i < p.n) {
-        if constexpr (OP == kExtend) {
-          const int r = p.a[i], to = p.b[i];
-          // (a row outside the table, a length that is no longer or does not fit: left as it is)
-          if (r >= 0 && r < p.R && to > p.lens[r] && (int64_t)to <= (int64_t)p.pph * kKvPageTokens &&
-              first_of_its_row(p.a, i)) {
-            ok = 1;
-            need = (pages_of(to, p.pph) - pages_of(p.lens[r], p.pph)) * p.H;
-          }
-        } else {
-          const int s = p.a[i], d = p.b[i];
-          if (s >= 0 && s < p.R && d >= 0 && d < p.R && s != d && first_of_its_row(p.b, i)) {
-            ok = 1;
-            const int len = min(max(p.lens[s], 0), p.pph * kKvPageTokens);
-            need = len % kKvPageTokens ? p.H : 0;
-          }
-        }
+        const int r = row_of[i];
+        const bool first = r >= 0 && r < p.R &&
+                           __hip_atomic_load(&p.claim[r], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == i;
+        need = request_needs<OP>(p, i, first);
       }
       int all;
-      const int before = block_scan(need, red, all);
+      const int before = block_scan<kThreads>(max(need, 0), red, all);
       if (i < p.n) {
         p.first[i] = base + before;
-        p.flag[i] = ok;
+        p.flag[i] = need >= 0;
       }
       base += all;
     }
@@ -130,50 +166,112 @@ __global__ void __launch_bounds__(kThreads) pages_count(PagesParams p) {
   }
 }
 
-// 2. list[r]: the r-th free page (as many as are needed), or the r-th live one; compact:
-// holes[r], the r-th free page below the number of live ones, and where[page] = page.
+// 2.
 template <int OP>
 __global__ void __launch_bounds__(kThreads) pages_list(PagesParams p) {
   __shared__ int red[kThreads / 64];
   const int seg = blockIdx.x;
+  const int64_t first = (int64_t)seg * kSeg + (int)threadIdx.x * kPer;
+  const uint32_t bits = page_bits<OP>(p, first);
   int mine = 0, tot = 0;
   for (int s = threadIdx.x; s < p.segs; s += kThreads) {
     const int c = p.counts[s];
     tot += c;
     if (s < seg) mine += c;
   }
-  int base, total;
-  block_scan(mine, red, base);
-  block_scan(tot, red, total);
+  int base, total, all;
+  block_scan<kThreads>(mine, red, base);
+  block_scan<kThreads>(tot, red, total);
   if (seg == 0 && threadIdx.x == 0) {
     p.head[kTotal] = total;
     if (OP == kCompact && total == 0) p.head[kHoles] = 0;
   }
   const int need = OP == kCompact ? 0 : p.head[kNeed];
   if (OP != kCompact && base >= need) return;  // (the whole workgroup)
-  for (int i = 0; i < kPer; ++i) {
-    const int64_t page = (int64_t)seg * kSeg + i * kThreads + threadIdx.x;
-    const bool in = page < p.pool;
-    const bool live = in && p.refs[page] > 0;
-    const int x = in && live == (OP == kCompact);
-    int all;
-    const int r = base + block_scan(x, red, all);
-    base += all;
-    if constexpr (OP == kCompact) {
-      if (live) p.list[r] = (int)page;
-      if (in) p.where[page] = (int)page;
-      if (in && !live && page < total) p.holes[page - r] = (int)page;
-      if (page == total - 1) p.head[kHoles] = total - r - (live ? 1 : 0);  // free pages below `total`
-    } else {
-      if (x && r < need) p.list[r] = (int)page;
+  const int rank = base + block_scan<kThreads>(__popc(bits), red, all);
+  place_pages<OP>(p, first, bits, rank, need, total);
+}
+
+__device__ __forceinline__ void write_status(const PagesParams& p, int need, int total) {
+  if (!p.status) return;
+  p.status[0] = need <= total ? need : 0;
+  p.status[1] = need <= total ? 0 : need - total;
+}
+
+// 1 and 2 of a small call, and 3 of an extend.
+template <int OP>
+__global__ void __launch_bounds__(kSmallThreads) pages_small(PagesParams p) {
+  __shared__ int red[kSmallThreads / 64];
+  __shared__ int row_of[kSmallThreads], start[kSmallThreads];
+  const int i = threadIdx.x;
+  const uint32_t bits = page_bits<OP>(p, (int64_t)i * kPer);
+  int need = 0, total;
+  if constexpr (OP != kCompact) {
+    const int row = i < p.n ? (OP == kExtend ? p.a : p.b)[i] : -1;
+    row_of[i] = row;
+    __syncthreads();
+    bool first = i < p.n;
+    for (int j = 0; j < i && j < p.n; ++j) first &= row_of[j] != row;
+    const int x = i < p.n ? request_needs<OP>(p, i, first) : -1;
+    start[i] = block_scan<kSmallThreads>(max(x, 0), red, need);
+    if (i < p.n) {
+      p.first[i] = start[i];
+      p.flag[i] = x >= 0;
     }
+    if (x < 0) row_of[i] = -1;  // (each thread's own; read after the next barrier)
+  }
+  const int rank = block_scan<kSmallThreads>(__popc(bits), red, total);
+  place_pages<OP>(p, (int64_t)i * kPer, bits, rank, need, total);
+  if (i == 0) {
+    p.head[kNeed] = need;
+    p.head[kTotal] = total;
+    if (OP == kCompact && total == 0) p.head[kHoles] = 0;
+  }
+  if constexpr (OP == kExtend) {
+    if (i == 0) write_status(p, need, total);
+    if (need > total) return;
+    __syncthreads();  // (the list is there)
+    for (int x = i; x < need; x += kSmallThreads) {
+      int lo = 0, hi = p.n;  // the last request whose pages begin at or before x (those that take none are passed over)
+      while (hi - lo > 1) {
+        const int mid = (lo + hi) / 2;
+        if (start[mid] <= x)
+          lo = mid;
+        else
+          hi = mid;
+      }
+      const int r = row_of[lo], had = pages_of(p.lens[r], p.pph), add = pages_of(p.b[lo], p.pph) - had;
+      const int at = x - start[lo], h = at / add, page = p.list[x];
+      p.table[((int64_t)r * p.H + h) * p.pph + had + (at - h * add)] = page;
+      p.refs[page] = 1;
+    }
+    __syncthreads();  // (every thread has read the old lengths)
+    if (i < p.n && row_of[i] >= 0) p.lens[row_of[i]] = p.b[i];
   }
 }
 
-__device__ __forceinline__ void copy_page(uint8_t* pool, int64_t bytes, int64_t to, int64_t from, int thread, int threads) {
-  const u32x4* s = reinterpret_cast<const u32x4*>(pool + from * bytes);
-  u32x4* d = reinterpret_cast<u32x4*>(pool + to * bytes);
-  for (int i = thread; i < bytes / 16; i += threads) d[i] = s[i];
+// Page `to` of both pools := page `from`.  Eight loads a thread are on their way before the
+// first of them is stored: one at a time, a compaction moved 3.8 TB/s.
+__device__ __forceinline__ void copy_pages(const PagesParams& p, int64_t to, int64_t from) {
+  const int words = (int)(p.page_bytes / 16), pools = p.v_pool ? 2 : 1;
+  const u32x4* ks = reinterpret_cast<const u32x4*>(p.k_pool + from * p.page_bytes);
+  const u32x4* vs = reinterpret_cast<const u32x4*>(p.v_pool + from * p.page_bytes);
+  u32x4* kd = reinterpret_cast<u32x4*>(p.k_pool + to * p.page_bytes);
+  u32x4* vd = reinterpret_cast<u32x4*>(p.v_pool + to * p.page_bytes);
+  const int all = words * pools;
+  for (int w0 = threadIdx.x; w0 < all; w0 += 8 * kThreads) {
+    u32x4 x[8];
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+      const int w = w0 + u * kThreads;
+      if (w < all) x[u] = __builtin_nontemporal_load(w < words ? ks + w : vs + (w - words));
+    }
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+      const int w = w0 + u * kThreads;
+      if (w < all) __builtin_nontemporal_store(x[u], w < words ? kd + w : vd + (w - words));
+    }
+  }
 }
 
 // 3. extend: a workgroup a request
@@ -181,10 +279,7 @@ __global__ void __launch_bounds__(kThreads) pages_extend(PagesParams p) {
   const int need = p.head[kNeed], total = p.head[kTotal];
   const int i = blockIdx.x;
   const bool enough = need <= total;
-  if (i == 0 && threadIdx.x == 0 && p.status) {
-    p.status[0] = enough ? need : 0;
-    p.status[1] = enough ? 0 : need - total;
-  }
+  if (i == 0 && threadIdx.x == 0) write_status(p, need, total);
   if (!enough || i >= p.n || !p.flag[i]) return;
   const int r = p.a[i], to = p.b[i];
   const int had = pages_of(p.lens[r], p.pph), add = pages_of(to, p.pph) - had;
@@ -204,10 +299,7 @@ __global__ void __launch_bounds__(kThreads) pages_fork(PagesParams p) {
   const int need = p.head[kNeed], total = p.head[kTotal];
   const bool enough = need <= total;
   const int i = blockIdx.x / p.H, h = blockIdx.x - i * p.H;
-  if (blockIdx.x == 0 && threadIdx.x == 0 && p.status) {
-    p.status[0] = enough ? need : 0;
-    p.status[1] = enough ? 0 : need - total;
-  }
+  if (blockIdx.x == 0 && threadIdx.x == 0) write_status(p, need, total);
   if (!enough || i >= p.n || !p.flag[i]) return;
   const int s = p.a[i];
   const int len = min(max(p.lens[s], 0), p.pph * kKvPageTokens), whole = len / kKvPageTokens;
@@ -227,8 +319,7 @@ __global__ void __launch_bounds__(kThreads) pages_fork(PagesParams p) {
     p.refs[page] = 1;
   }
   if (old < 0 || old >= p.pool) return;
-  copy_page(p.k_pool, p.page_bytes, page, old, threadIdx.x, kThreads);
-  if (p.v_pool) copy_page(p.v_pool, p.page_bytes, page, old, threadIdx.x, kThreads);
+  copy_pages(p, page, old);
 }
 
 __device__ void release_row(const PagesParams& p, int r) {
@@ -278,8 +369,7 @@ __global__ void __launch_bounds__(kThreads) pages_move(PagesParams p) {
       p.refs[to] = p.refs[from];
       p.refs[from] = 0;
     }
-    copy_page(p.k_pool, p.page_bytes, to, from, threadIdx.x, kThreads);
-    if (p.v_pool) copy_page(p.v_pool, p.page_bytes, to, from, threadIdx.x, kThreads);
+    copy_pages(p, to, from);
   }
 }
 
@@ -333,6 +423,7 @@ int pages_setup(const char* what, int op, int R, int H, int pph, int32_t* table,
   } else {
     p->first = take(n);
     p->flag = take(n);
+    p->claim = take(R);
     if (op == ASYM_KV_FORK) {
       p->new_len = take(n);
       p->rows = take((size_t)n * H * pph);
@@ -340,6 +431,8 @@ int pages_setup(const char* what, int op, int R, int H, int pph, int32_t* table,
   }
   return ASYM_OK;
 }
+
+bool small_call(const PagesParams& p) { return p.pool <= kSmallThreads * kPer && p.n <= kSmallThreads; }
 
 int pools_check(const char* what, const void* k_pool, const void* v_pool, size_t page_bytes) {
   const std::string w(what);
@@ -366,7 +459,7 @@ extern "C" int asym_kv_pages_workspace(int op, int R, int H, int pages_per_head,
   if (op == ASYM_KV_COMPACT)
     words += 2 * pool_pages;
   else
-    words += 2 * (size_t)n;
+    words += 2 * (size_t)n + R;
   if (op == ASYM_KV_FORK) words += (size_t)n + (size_t)n * H * pages_per_head;
   *bytes = words * sizeof(int);
   return ASYM_OK;
@@ -384,6 +477,11 @@ extern "C" int asym_kv_extend(int R, int H, int pages_per_head, int32_t* table, 
     return fail(ASYM_EINVAL, "kv extend: rows, lengths and status must be 4-byte aligned");
   p.a = rows; p.b = new_lens; p.status = status;
   hipStream_t s = static_cast<hipStream_t>(stream);
+  if (small_call(p)) {
+    hipLaunchKernelGGL((pages_small<kExtend>), dim3(1), dim3(kSmallThreads), 0, s, p);
+    ASYM_HIP(hipGetLastError());
+    return ASYM_OK;
+  }
   hipLaunchKernelGGL((pages_count<kExtend>), dim3(p.segs + 1), dim3(kThreads), 0, s, p);
   hipLaunchKernelGGL((pages_list<kExtend>), dim3(p.segs), dim3(kThreads), 0, s, p);
   hipLaunchKernelGGL(pages_extend, dim3(std::max(n, 1)), dim3(kThreads), 0, s, p);  // (status with no request too)
@@ -407,8 +505,12 @@ extern "C" int asym_kv_fork(int R, int H, int pages_per_head, int32_t* table, in
   p.v_pool = static_cast<uint8_t*>(v_pool);
   p.page_bytes = (int64_t)page_bytes;
   hipStream_t s = static_cast<hipStream_t>(stream);
-  hipLaunchKernelGGL((pages_count<kFork>), dim3(p.segs + 1), dim3(kThreads), 0, s, p);
-  hipLaunchKernelGGL((pages_list<kFork>), dim3(p.segs), dim3(kThreads), 0, s, p);
+  if (small_call(p)) {
+    hipLaunchKernelGGL((pages_small<kFork>), dim3(1), dim3(kSmallThreads), 0, s, p);
+  } else {
+    hipLaunchKernelGGL((pages_count<kFork>), dim3(p.segs + 1), dim3(kThreads), 0, s, p);
+    hipLaunchKernelGGL((pages_list<kFork>), dim3(p.segs), dim3(kThreads), 0, s, p);
+  }
   hipLaunchKernelGGL(pages_fork, dim3(std::max(n * H, 1)), dim3(kThreads), 0, s, p);  // (status with no request too)
   if (n > 0) hipLaunchKernelGGL(pages_fork_rows, dim3(n), dim3(kThreads), 0, s, p);
   ASYM_HIP(hipGetLastError());
@@ -445,8 +547,12 @@ extern "C" int asym_kv_compact(int R, int H, int pages_per_head, int32_t* table,
   p.page_bytes = (int64_t)page_bytes;
   hipStream_t s = static_cast<hipStream_t>(stream);
   const int64_t entries = (int64_t)R * H * pages_per_head;
-  hipLaunchKernelGGL((pages_count<kCompact>), dim3(p.segs), dim3(kThreads), 0, s, p);
-  hipLaunchKernelGGL((pages_list<kCompact>), dim3(p.segs), dim3(kThreads), 0, s, p);
+  if (small_call(p)) {
+    hipLaunchKernelGGL((pages_small<kCompact>), dim3(1), dim3(kSmallThreads), 0, s, p);
+  } else {
+    hipLaunchKernelGGL((pages_count<kCompact>), dim3(p.segs), dim3(kThreads), 0, s, p);
+    hipLaunchKernelGGL((pages_list<kCompact>), dim3(p.segs), dim3(kThreads), 0, s, p);
+  }
   hipLaunchKernelGGL(pages_move, dim3((unsigned)std::min<size_t>(pool_pages, 4096)), dim3(kThreads), 0, s, p);
   hipLaunchKernelGGL(pages_rename, dim3((unsigned)std::min<int64_t>((entries + kThreads - 1) / kThreads, 4096)),
                      dim3(kThreads), 0, s, p);
