@@ -973,11 +973,13 @@ int asym_kv_read_fp4(int B, int H_kv, int T, const void* k_pool, const void* v_p
  * S_max]; S_max at most 32 * pages_per_head.  A request of length 0 has O = 0 and
  * lse = -infinity.  Nothing at or behind a request's length reaches its result.
  * D must be 128, H_q / H_kv any whole number up to 16.
- * The sequence is cut into splits of split_tokens tokens (a multiple of 32 up to
- * 2048; 0: automatic, from B, H_kv and S_max); a second launch joins the splits
- * that a request's length reaches, in an order fixed by it.  The fp32 partials lie in the
- * caller's workspace (16-byte aligned; asym_attn_decode_paged_fp4_plan's
- * workspace_bytes, 0 with one split), which calls that may overlap must not share.
+ * The batch's pages are cut into equal shares, one a wave (split_tokens tokens of one
+ * head, a multiple of 32 up to 2^20; 0: automatic, from the batch), and a second launch
+ * joins what was cut, in the order of the shares; many short requests take a wave a
+ * (request, key/value head) instead.  The results depend on the sizes and the lengths alone.
+ * The fp32 pieces lie in the caller's workspace (16-byte aligned;
+ * asym_attn_decode_paged_fp4_plan's workspace_bytes, which may be 0), which calls that may
+ * overlap must not share.
  * No host synchronisation; may be captured.  Runs on the stream's CU set;
  * asynchronous.  Errors: ASYM_EINVAL, ASYM_EUNSUPPORTED, ASYM_EHIP. */
 int asym_attn_decode_paged_fp4(int B, int H_q, int H_kv, int S_max, int D, const void* q,
@@ -986,8 +988,9 @@ int asym_attn_decode_paged_fp4(int B, int H_q, int H_kv, int S_max, int D, const
                                const int32_t* lens, void* o, float* lse, float scale, int split_tokens,
                                void* workspace, size_t workspace_bytes, void* stream);
 
-/* What asym_attn_decode_paged_fp4 would launch (host only; n_xcds, tasks_per_xcd
- * and dense_static are 0). */
+/* What asym_attn_decode_paged_fp4 would launch (host only): tasks shares, of
+ * split_tokens tokens if every request has S_max, the longest request in n_splits
+ * pieces at most; n_xcds, tasks_per_xcd and dense_static are 0. */
 int asym_attn_decode_paged_fp4_plan(int B, int H_q, int H_kv, int S_max, int D, int split_tokens,
                                     asym_attn_plan_info* out);
 

@@ -3,8 +3,11 @@
 //
 //   O[b, h] = softmax_t(scale * <q[b, h], K[b, g, t]>) . V[b, g, :],  t < lens[b], g = h / G
 //
-// The sequence is cut into splits; a wave has one (request, key/value head, split) and
-// serves the G <= 16 query heads that read that head, 32 tokens (a page) at a time:
+// The pages of the batch, request by request and head by head, are one list, cut into equal
+// shares, one a wave, whatever the requests' lengths (which only the device knows): a grid
+// of (request, head, split) tasks left waves idle behind the short ones (64 requests of up to
+// 32768 tokens, 1.42 GB: 319 us, in shares 229, 6.2 TB/s).  A wave walks its share; for each (request, key/value head) that it meets it serves the G <= 16
+// query heads that read that head, 32 tokens (a page) at a time:
 //   scores   two v_mfma_scale_f32_16x16x128_f8f6f4 a 16 tokens: the page's codes and scales
 //            are the operand as they lie, with no conversion at all.  The other operand
 //            takes 8 bits at most, so q, whose bf16 has 8 significant bits, goes in as
@@ -17,21 +20,28 @@
 //            probabilities: 4 operands (one per block of 32 channels) of
 //            bf16(p * X), rounded as p alone would be, since X is a power of two; the
 //            codes become bf16 by v_cvt_scalef32_pk_bf16_fp4 (exact), two an instruction.
-// No LDS, no barrier.  Each split leaves its unnormalised output, max and sum in fp32
-// for the second launch; with one split the wave writes the result itself.
+// No LDS, no barrier.  A (request, head) that lies in one share is written by its wave;
+// of one that is cut, each share leaves its unnormalised output, max and sum in fp32 (at
+// most two such pieces a wave: its first and its last), which a second launch joins in the
+// order of the shares.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cmath>
 
 #include "internal.h"
 #include "kv_fp4.h"
+#include "read_policy.h"
 
 namespace asym {
 namespace {
 
 constexpr int kWaves = 4;
 constexpr int kMaxG = 16;
-constexpr int kMaxSplitPages = 64;  // a lane holds the number of one page of the split
+constexpr int kShares = 2048;     // waves: 8 a CU of 256 (12 fit, and join more pieces: 64 requests of up to 1000
+                                  // tokens 20.1 us, with 8 a CU 18.1)
+constexpr int kMostPieces = 128;  // that the longest request is cut into
+constexpr int kJoinWaves = 16;
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
@@ -46,10 +56,12 @@ struct Fp4DecodeParams {
   const int* lens;
   uint16_t* o;                   // [B][Hq][128]
   float* lse;                    // [B][Hq], nullable
-  float* part_o;                 // [B][Hq][n_splits][128]
-  float* part_ml;                // [B][Hq][n_splits][2]: max (of the raw scores), sum
+  float* part_o;                 // [shares][2][G][128]
+  float* part_ml;                // [shares][2][G][2]: max (of the raw scores), sum
   int B, Hq, Hkv, G, S, pph, pool_pages;
-  int split_pages, n_splits, tasks;
+  int2* cut;                     // [B][Hkv]: of a (request, head) that was cut, 2 (its first share) + (1: that share's
+                                 // last piece), its last share; -1 of one that was not
+  int shares, share_pages, least;  // share_pages 0: the batch's pages over the shares, at least `least`
   float c, scale;                // |scale| * log2(e), |scale|
   uint32_t q_flip;
 };
@@ -103,206 +115,368 @@ struct PageRegs {
   uint32_t ks;
 };
 
+template <int POLICY>
 __device__ __forceinline__ void load_page(const Fp4DecodeParams& p, int kp, int vp, int lane, PageRegs& r) {
   const __amdgpu_buffer_rsrc_t rk = page_rsrc(p.k_pool, kp, p.pool_pages), rv = page_rsrc(p.v_pool, vp, p.pool_pages);
   const uint32_t ko = (uint32_t)((lane & 15) * 64 + (lane >> 4) * 16);
 #pragma unroll
-  for (int t = 0; t < 2; ++t) {
-    r.k[t] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rk, ko + 1024 * t, 0, 0));
-    r.v[t] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rv, (uint32_t)lane * 16 + 1024 * t, 0, 0));
+  for (int t = 0; t < 2; ++t) r.k[t] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rk, ko + 1024 * t, 0, POLICY));
+  r.ks = __builtin_amdgcn_raw_buffer_load_b16(rk, kFp4ScaleOff + (uint32_t)lane * 2, 0, POLICY);
+#pragma unroll
+  for (int t = 0; t < 2; ++t)
+    r.v[t] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rv, (uint32_t)lane * 16 + 1024 * t, 0, POLICY));
+#pragma unroll
+  for (int t = 0; t < 2; ++t)
     r.vs[t] = __builtin_bit_cast(
-        u32x4, __builtin_amdgcn_raw_buffer_load_b128(rv, kFp4ScaleOff + (uint32_t)(lane >> 4) * 32 + 16 * t, 0, 0));
-  }
-  r.ks = __builtin_amdgcn_raw_buffer_load_b16(rk, kFp4ScaleOff + (uint32_t)lane * 2, 0, 0);
+        u32x4, __builtin_amdgcn_raw_buffer_load_b128(rv, kFp4ScaleOff + (uint32_t)(lane >> 4) * 32 + 16 * t, 0, POLICY));
 }
 
-__global__ void __launch_bounds__(64 * kWaves) fp4_decode_split(Fp4DecodeParams p) {
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int task = blockIdx.x * kWaves + wave;
-  if (task >= p.tasks) return;
-  const int split = task % p.n_splits, bh = task / p.n_splits;
-  const int b = bh / p.Hkv, hk = bh - b * p.Hkv;
-  const int len = __builtin_amdgcn_readfirstlane(min(max(p.lens[b], 0), p.S));
-  const int pg0 = split * p.split_pages;
-  const int n_pg = min((len + kKvPageTokens - 1) / kKvPageTokens - pg0, p.split_pages);
-  if (n_pg <= 0 && (p.n_splits > 1 || split > 0)) return;  // (the merge knows the lengths)
-  const int n = lane & 15, quarter = lane >> 4;
-
-  int kpg = -1, vpg = -1;
-  if (lane < n_pg) {
-    const size_t e = (size_t)bh * p.pph + pg0 + lane;
-    kpg = p.k_pages[e];
-    vpg = p.v_pages[e];
-  }
-  i32x8 q_hi, q_lo;
-  int s_hi, s_lo;
-  const int head = hk * p.G + n;  // this lane's query head
-  load_q(p.q + ((size_t)b * p.Hq + (n < p.G ? head : 0)) * kKvD, n < p.G, quarter, p.q_flip, q_hi, q_lo, s_hi, s_lo);
-
+// One wave's running result for the G heads of its group: column lane % 16 is a head;
+// o[g] holds channels 16 g + 4 (lane / 16) + 0 .. 3.
+struct Running {
   f32x4 o[8];
+  float m, l;
+};
+
+// 32 tokens, of which `left` exist (32 or more: all)
+__device__ __forceinline__ void add_page(const Fp4DecodeParams& p, const PageRegs& cur, int left, int quarter,
+                                         const i32x8& q_hi, const i32x8& q_lo, int s_hi, int s_lo, Running& a) {
+  f32x4 s[2];  // scores: rows 4 quarter + r of tokens 16 t .., column n
 #pragma unroll
-  for (int g = 0; g < 8; ++g) o[g] = f32x4{};
-  float m = -INFINITY, l = 0.f;
-  PageRegs cur, nxt;
-  if (n_pg > 0)
-    load_page(p, __builtin_amdgcn_readlane(kpg, 0), __builtin_amdgcn_readlane(vpg, 0), lane, cur);
-  for (int i = 0; i < n_pg; ++i) {
-    const int ni = min(i + 1, n_pg - 1);  // (the last page again: no branch around the loads)
-    load_page(p, __builtin_amdgcn_readlane(kpg, ni), __builtin_amdgcn_readlane(vpg, ni), lane, nxt);
-    const int left = len - (pg0 + i) * kKvPageTokens;
-    // scores: rows 4 quarter + r of tokens 16 t .., column n
-    f32x4 s[2];
+  for (int t = 0; t < 2; ++t) {
+    const i32x8 k = {(int)cur.k[t][0], (int)cur.k[t][1], (int)cur.k[t][2], (int)cur.k[t][3], 0, 0, 0, 0};
+    const int ks = (int)(cur.ks >> (8 * t));
+    s[t] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(k, q_lo, f32x4{}, 4, 0, 0, ks, 0, s_lo);
+    s[t] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(k, q_hi, s[t], 4, 0, 0, ks, 0, s_hi);
+  }
+  uint32_t vs[8];
 #pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      const i32x8 a = {(int)cur.k[t][0], (int)cur.k[t][1], (int)cur.k[t][2], (int)cur.k[t][3], 0, 0, 0, 0};
-      const int ks = (int)(cur.ks >> (8 * t));
-      s[t] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, q_lo, f32x4{}, 4, 0, 0, ks, 0, s_lo);
-      s[t] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, q_hi, s[t], 4, 0, 0, ks, 0, s_hi);
-    }
-    uint32_t vs[8];
-#pragma unroll
-    for (int j = 0; j < 8; ++j) vs[j] = cur.vs[j >> 2][j & 3];
-    if (left < kKvPageTokens) {
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const bool on = 4 * quarter + (j & 3) + 16 * (j >> 2) < left;
-        if (!on) s[j >> 2][j & 3] = -INFINITY;
-        if (!on) vs[j] = 0;  // (as 0: whatever scale lies there cannot reach the sum)
-      }
-    }
-    float top = fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])),
-                      fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3])));
-    top = max_quarters(top);
-    if (__any((top - m) * p.c > 8.f)) {
-      const float m_new = fmaxf(m, top);
-      const float alpha = __builtin_amdgcn_exp2f((m - (m_new == -INFINITY ? 0.f : m_new)) * p.c);
-      l *= alpha;
-#pragma unroll
-      for (int g = 0; g < 8; ++g) o[g] *= alpha;
-      m = m_new;
-    }
-    const float ms = m == -INFINITY ? 0.f : m * p.c;
-    float e[8];
+  for (int j = 0; j < 8; ++j) vs[j] = cur.vs[j >> 2][j & 3];
+  if (left < kKvPageTokens) {
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      e[j] = __builtin_amdgcn_exp2f(fmaf(s[j >> 2][j & 3], p.c, -ms));
-      l += e[j];
+      const bool on = 4 * quarter + (j & 3) + 16 * (j >> 2) < left;
+      if (!on) s[j >> 2][j & 3] = -INFINITY;
+      if (!on) vs[j] = 0;  // (as 0: whatever scale lies there cannot reach the sum)
     }
-#pragma unroll
-    for (int blk = 0; blk < 4; ++blk) {
-      bf16x8 pf;
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const uint32_t x = blk == 0 ? vs[j] << 23 : blk == 1 ? vs[j] << 15 : blk == 2 ? vs[j] << 7 : vs[j] >> 1;
-        pf[j] = (__bf16)(e[j] * __uint_as_float(x & 0x7F800000u));
-      }
-#pragma unroll
-      for (int g2 = 0; g2 < 2; ++g2) {
-        const int g = 2 * blk + g2;
-        const uint32_t w = cur.v[g >> 2][g & 3];
-        union {
-          bf16x2 p[4];
-          bf16x8 v;
-        } f;
-        f.p[0] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, 1.f, 0);
-        f.p[1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, 1.f, 1);
-        f.p[2] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, 1.f, 2);
-        f.p[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, 1.f, 3);
-        o[g] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f.v, pf, o[g], 0, 0, 0);
-      }
-    }
-    cur = nxt;
   }
-  l += __shfl_xor(l, 16);
-  l += __shfl_xor(l, 32);
-  if (n >= p.G) return;
-  const size_t row = (size_t)b * p.Hq + head;
-  if (p.n_splits == 1) {
-    const float inv = l == 0.f ? 0.f : 1.f / l;
-    uint16_t* dst = p.o + row * kKvD + 4 * quarter;
+  float top = fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])),
+                    fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3])));
+  top = max_quarters(top);
+  if (__any((top - a.m) * p.c > 8.f)) {
+    const float m_new = fmaxf(a.m, top);
+    const float alpha = __builtin_amdgcn_exp2f((a.m - (m_new == -INFINITY ? 0.f : m_new)) * p.c);
+    a.l *= alpha;
 #pragma unroll
-    for (int g = 0; g < 8; ++g) {
-      const bf16x2 a = {(__bf16)(o[g][0] * inv), (__bf16)(o[g][1] * inv)}, c = {(__bf16)(o[g][2] * inv), (__bf16)(o[g][3] * inv)};
-      *reinterpret_cast<uint2*>(dst + 16 * g) = uint2{__builtin_bit_cast(uint32_t, a), __builtin_bit_cast(uint32_t, c)};
-    }
-    if (p.lse && quarter == 0) p.lse[row] = l == 0.f ? -INFINITY : m * p.scale + __logf(l);
-    return;
+    for (int g = 0; g < 8; ++g) a.o[g] *= alpha;
+    a.m = m_new;
   }
-  float* dst = p.part_o + (row * p.n_splits + split) * kKvD + 4 * quarter;
+  const float ms = a.m == -INFINITY ? 0.f : a.m * p.c;
+  float e[8];
 #pragma unroll
-  for (int g = 0; g < 8; ++g) *reinterpret_cast<f32x4*>(dst + 16 * g) = o[g];
-  if (quarter == 0) {
-    float* ml = p.part_ml + (row * p.n_splits + split) * 2;
-    ml[0] = m;
-    ml[1] = l;
+  for (int j = 0; j < 8; ++j) {
+    e[j] = __builtin_amdgcn_exp2f(fmaf(s[j >> 2][j & 3], p.c, -ms));
+    a.l += e[j];
+  }
+#pragma unroll
+  for (int blk = 0; blk < 4; ++blk) {
+    bf16x8 pf;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const uint32_t x = blk == 0 ? vs[j] << 23 : blk == 1 ? vs[j] << 15 : blk == 2 ? vs[j] << 7 : vs[j] >> 1;
+      pf[j] = (__bf16)(e[j] * __uint_as_float(x & 0x7F800000u));
+    }
+#pragma unroll
+    for (int g2 = 0; g2 < 2; ++g2) {
+      const int g = 2 * blk + g2;
+      const uint32_t w = cur.v[g >> 2][g & 3];
+      union {
+        bf16x2 p[4];
+        bf16x8 v;
+      } f;
+      f.p[0] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, 1.f, 0);
+      f.p[1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, 1.f, 1);
+      f.p[2] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, 1.f, 2);
+      f.p[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, 1.f, 3);
+      a.o[g] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f.v, pf, a.o[g], 0, 0, 0);
+    }
   }
 }
 
-// Merge: a workgroup has one (request, head) row; wave w takes splits w, w + 4, ... of
-// those that the request's length reaches, in an order fixed by the length.
-__global__ void __launch_bounds__(64 * kWaves) fp4_decode_merge(Fp4DecodeParams p) {
-  __shared__ float red[kWaves][kKvD], red_l[kWaves];
+// Where the requests' pages lie in the list, 256 requests at a time: lane l has requests
+// base + l, + 64, + 128 and + 192.  (Named members: the compiler would put an array that is
+// indexed at run time into LDS.)
+struct Requests {
+  int base;
+  int len0, len1, len2, len3;
+  int upto0, upto1, upto2, upto3;  // pages (of one head) of the batch up to and with the request
+
+  static __device__ __forceinline__ int pages_of(int len) { return (int)((uint32_t)(len + kKvPageTokens - 1) / kKvPageTokens); }
+  static __device__ __forceinline__ int pick(int i, int a, int b, int c, int d) { return i < 2 ? (i ? b : a) : (i == 2 ? c : d); }
+  __device__ __forceinline__ void load(const Fp4DecodeParams& p, int from, int before, int lane) {
+    base = from;
+    const int b = from + lane;
+    len0 = b < p.B ? p.lens[b] : 0;
+    len1 = b + 64 < p.B ? p.lens[b + 64] : 0;
+    len2 = b + 128 < p.B ? p.lens[b + 128] : 0;
+    len3 = b + 192 < p.B ? p.lens[b + 192] : 0;
+    auto held = [&](int x) { return min(max(x, 0), p.S); };
+    len0 = held(len0);
+    upto0 = before + wave_scan_add(pages_of(len0));
+    upto1 = upto2 = upto3 = before = __builtin_amdgcn_readlane(upto0, 63);
+    len1 = held(len1), len2 = held(len2), len3 = held(len3);
+    if (from + 64 < p.B) {
+      upto1 = before + wave_scan_add(pages_of(len1));
+      before = __builtin_amdgcn_readlane(upto1, 63);
+      upto2 = before + wave_scan_add(pages_of(len2));
+      before = __builtin_amdgcn_readlane(upto2, 63);
+      upto3 = before + wave_scan_add(pages_of(len3));
+    }
+  }
+  __device__ __forceinline__ int end() const { return __builtin_amdgcn_readlane(upto3, 63); }
+  __device__ __forceinline__ int len_of(int at) const {  // of request base + at
+    return __builtin_amdgcn_readlane(pick(at >> 6, len0, len1, len2, len3), at & 63);
+  }
+  // The request (at) whose pages hold the list's page f; returns the place of its first page
+  __device__ __forceinline__ int find(const Fp4DecodeParams& p, int f, int lane, int& at) {
+    while (end() * p.Hkv <= f) load(p, base + 256, end(), lane);
+    auto last = [&](int upto) { return __builtin_amdgcn_readlane(upto, 63) * p.Hkv <= f; };
+    const int i = last(upto0) + last(upto1) + last(upto2);
+    const int x = pick(i, upto0, upto1, upto2, upto3), l = __builtin_ctzll(__ballot(x * p.Hkv > f));
+    at = 64 * i + l;
+    return (__builtin_amdgcn_readlane(x, l) - pages_of(len_of(at))) * p.Hkv;
+  }
+};
+// The batch's pages (of one head)
+__device__ __forceinline__ int batch_pages(const Fp4DecodeParams& p, int lane, const Requests& r0) {
+  int sum = r0.end();
+  if (p.B > 256) {
+    int more = 0;
+    for (int b = 256 + lane; b < p.B; b += 64) more += Requests::pages_of(min(max(p.lens[b], 0), p.S));
+    sum += wave_sum(more);
+  }
+  return sum;
+}
+
+// ROWS: a wave has one (request, key/value head), whole.
+template <int POLICY, bool ROWS>
+__global__ void __launch_bounds__(64 * kWaves) fp4_decode_share(Fp4DecodeParams p) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const size_t row = blockIdx.x;
-  const int b = (int)(row / p.Hq);
-  const int len = min(max(p.lens[b], 0), p.S);
-  const int per = p.split_pages * kKvPageTokens, ns = (len + per - 1) / per;
-  const float* ml = p.part_ml + row * p.n_splits * 2;
-  const float* po = p.part_o + row * p.n_splits * kKvD + 2 * lane;
-  float M = -INFINITY;
-  for (int s = lane; s < ns; s += 64) M = fmaxf(M, ml[2 * s]);
+  const int w = blockIdx.x * kWaves + wave;
+  const int n = lane & 15, quarter = lane >> 4;
+  Requests rq;
+  int f, f1, at, len, pages, hk, pg, share = 0;  // pages f .. f1 - 1 of the list
+  if constexpr (ROWS) {
+    if (w >= p.B * p.Hkv) return;
+    at = w / p.Hkv;
+    hk = w - at * p.Hkv;
+    rq.base = 0;
+    len = __builtin_amdgcn_readfirstlane(min(max(p.lens[at], 0), p.S));
+    f = pg = 0;
+    f1 = pages = Requests::pages_of(len);  // (none: the result below is that of no token)
+  } else {
+    rq.load(p, 0, 0, lane);
+    const int total = batch_pages(p, lane, rq) * p.Hkv;
+    share = p.share_pages ? p.share_pages : max((total + p.shares - 1) / p.shares, p.least);
+    if ((int64_t)w * share >= total) return;
+    f = w * share;
+    f1 = min(f + share, total);
+    const int in = f - rq.find(p, f, lane, at);  // the page, over its request's heads
+    len = rq.len_of(at);
+    pages = Requests::pages_of(len);
+    hk = in / pages;
+    pg = in - hk * pages;
+  }
+
+  for (bool first = true;; first = false) {
+    const int b = rq.base + at, bh = b * p.Hkv + hk;
+    const int count = min(pages - pg, f1 - f);
+    // a lane holds the number of one page of 64, and of one of the next 64
+    const size_t row = (size_t)bh * p.pph + pg;
+    auto numbers = [&](int i, int& k, int& v) {
+      k = v = -1;
+      if (i + lane < count) {
+        k = p.k_pages[row + i + lane];
+        v = p.v_pages[row + i + lane];
+      }
+    };
+    int kpg, vpg, kpg2, vpg2;
+    numbers(0, kpg, vpg);
+    PageRegs cur, nxt;
+    load_page<POLICY>(p, __builtin_amdgcn_readlane(kpg, 0), __builtin_amdgcn_readlane(vpg, 0), lane, cur);
+    i32x8 q_hi, q_lo;
+    int s_hi, s_lo;
+    const int head = hk * p.G + n;  // this lane's query head
+    load_q(p.q + ((size_t)b * p.Hq + (n < p.G ? head : 0)) * kKvD, n < p.G, quarter, p.q_flip, q_hi, q_lo, s_hi, s_lo);
+    Running a;
 #pragma unroll
-  for (int d = 32; d >= 1; d >>= 1) M = fmaxf(M, __shfl_xor(M, d));
-  float a0 = 0.f, a1 = 0.f, L = 0.f;
-  for (int s = wave; s < ns; s += kWaves) {
-    const float w = M == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((ml[2 * s] - M) * p.c);  // (no finite score: NaN comes through)
-    const float2 x = *reinterpret_cast<const float2*>(po + (size_t)s * kKvD);
-    L = fmaf(ml[2 * s + 1], w, L);
-    a0 = fmaf(x.x, w, a0);
-    a1 = fmaf(x.y, w, a1);
+    for (int g = 0; g < 8; ++g) a.o[g] = f32x4{};
+    a.m = -INFINITY;
+    a.l = 0.f;
+    for (int i = 0; i < count; ++i) {
+      const int e = i & 63;
+      if (e == 0) numbers(i + 64, kpg2, vpg2);
+      if (e == 63) {
+        kpg = kpg2;
+        vpg = vpg2;
+      }
+      // (behind the last page: none, which loads nothing)
+      const int ne = (e + 1) & 63, kn = __builtin_amdgcn_readlane(kpg, ne), vn = __builtin_amdgcn_readlane(vpg, ne);
+      load_page<POLICY>(p, i + 1 < count ? kn : -1, i + 1 < count ? vn : -1, lane, nxt);
+      add_page(p, cur, len - (pg + i) * kKvPageTokens, quarter, q_hi, q_lo, s_hi, s_lo, a);
+      cur = nxt;
+    }
+    a.l += __shfl_xor(a.l, 16);
+    a.l += __shfl_xor(a.l, 32);
+    if (n < p.G) {
+      if (count == pages) {  // all of it
+        const size_t out = (size_t)b * p.Hq + head;
+        const float inv = a.l == 0.f ? 0.f : 1.f / a.l;
+        uint16_t* dst = p.o + out * kKvD + 4 * quarter;
+#pragma unroll
+        for (int g = 0; g < 8; ++g) {
+          const bf16x2 x = {(__bf16)(a.o[g][0] * inv), (__bf16)(a.o[g][1] * inv)};
+          const bf16x2 y = {(__bf16)(a.o[g][2] * inv), (__bf16)(a.o[g][3] * inv)};
+          *reinterpret_cast<uint2*>(dst + 16 * g) = uint2{__builtin_bit_cast(uint32_t, x), __builtin_bit_cast(uint32_t, y)};
+        }
+        if (p.lse && quarter == 0) p.lse[out] = a.l == 0.f ? -INFINITY : a.m * p.scale + __logf(a.l);
+      } else {
+        const size_t piece = ((size_t)w * 2 + (first ? 0 : 1)) * p.G + n;
+        float* dst = p.part_o + piece * kKvD + 4 * quarter;
+#pragma unroll
+        for (int g = 0; g < 8; ++g) *reinterpret_cast<f32x4*>(dst + 16 * g) = a.o[g];
+        if (quarter == 0) *reinterpret_cast<float2*>(p.part_ml + piece * 2) = float2{a.m, a.l};
+      }
+    }
+    // (for the join: which waves have a piece of it, and whether the first of them is its wave's second)
+    if (!ROWS && pg == 0 && lane == 0)
+      p.cut[bh] = count == pages ? int2{-1, 0} : int2{2 * w + (first ? 0 : 1), (f + pages - 1) / share};
+    f += count;
+    if (ROWS || f >= f1) return;
+    pg = 0;
+    if (++hk == p.Hkv) {  // the next request that has tokens (there is one)
+      hk = 0;
+      do {
+        if (++at == 256) {
+          rq.load(p, rq.base + 256, rq.end(), lane);
+          at = 0;
+        }
+        len = rq.len_of(at);
+      } while (len == 0);
+      pages = Requests::pages_of(len);
+    }
   }
-  red[wave][2 * lane] = a0;
-  red[wave][2 * lane + 1] = a1;
-  if (lane == 0) red_l[wave] = L;
-  __syncthreads();
-  if (wave) return;
-  for (int w = 1; w < kWaves; ++w) {
-    a0 += red[w][2 * lane];
-    a1 += red[w][2 * lane + 1];
-    L += red_l[w];
+}
+
+// A few waves (`per`, a power of two) a (request, query head): one without tokens is written,
+// one that was cut is joined.  Wave j takes pieces j, j + per, ..., eight loads at a time (the
+// first eight go out before the row's max is known); the waves' sums are added in order.
+__global__ void __launch_bounds__(64 * kJoinWaves) fp4_decode_join(Fp4DecodeParams p, int per) {
+  __shared__ float red[kJoinWaves][kKvD], red_l[kJoinWaves];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int sub = wave & (per - 1);
+  const int row = (int)(blockIdx.x * (blockDim.x >> 6) + wave) / per;
+  float a0 = 0.f, a1 = 0.f, L = 0.f, M = -INFINITY;
+  bool join = false;
+  if (row < p.B * p.Hq) {
+    const int b = row / p.Hq, h = row - b * p.Hq, hk = h / p.G, g = h - hk * p.G;
+    const int2 cut = p.cut[b * p.Hkv + hk];  // (of a request without tokens: not written, and not used)
+    if (min(p.lens[b], p.S) <= 0) {
+      if (sub == 0) {
+        *reinterpret_cast<uint32_t*>(p.o + (size_t)row * kKvD + 2 * lane) = 0;
+        if (p.lse && lane == 0) p.lse[row] = -INFINITY;
+      }
+    } else if (cut.x >= 0) {
+      join = true;
+      const int w0 = cut.x >> 1, w1 = cut.y;
+      auto piece = [&](int w) { return ((size_t)w * 2 + (w == w0 ? cut.x & 1 : 0)) * p.G + g; };
+      float2 x[8], q[8];
+      auto load = [&](int w) {
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+          const size_t e = piece(min(w + u * per, w1));
+          x[u] = *reinterpret_cast<const float2*>(p.part_o + e * kKvD + 2 * lane);
+          q[u] = *reinterpret_cast<const float2*>(p.part_ml + e * 2);
+        }
+      };
+      load(w0 + sub);
+      for (int w = w0 + lane; w <= w1; w += 64) M = fmaxf(M, p.part_ml[piece(w) * 2]);
+#pragma unroll
+      for (int d = 32; d >= 1; d >>= 1) M = fmaxf(M, __shfl_xor(M, d));
+      for (int w = w0 + sub; w <= w1; w += 8 * per) {
+        if (w != w0 + sub) load(w);
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+          if (w + u * per > w1) break;
+          // (M minus infinity: nothing but NaN, which goes on)
+          const float s = M == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((q[u].x - M) * p.c);
+          L = fmaf(q[u].y, s, L);
+          a0 = fmaf(x[u].x, s, a0);
+          a1 = fmaf(x[u].y, s, a1);
+        }
+      }
+    }
   }
+  if (per > 1) {
+    red[wave][2 * lane] = a0;
+    red[wave][2 * lane + 1] = a1;
+    if (lane == 0) red_l[wave] = L;
+    __syncthreads();
+    if (sub) return;
+    for (int j = 1; j < per; ++j) {
+      a0 += red[wave + j][2 * lane];
+      a1 += red[wave + j][2 * lane + 1];
+      L += red_l[wave + j];
+    }
+  }
+  if (!join || sub) return;
   const float inv = L == 0.f ? 0.f : 1.f / L;
   const bf16x2 r = {(__bf16)(a0 * inv), (__bf16)(a1 * inv)};
-  *reinterpret_cast<uint32_t*>(p.o + row * kKvD + 2 * lane) = __builtin_bit_cast(uint32_t, r);
+  *reinterpret_cast<uint32_t*>(p.o + (size_t)row * kKvD + 2 * lane) = __builtin_bit_cast(uint32_t, r);
   if (p.lse && lane == 0) p.lse[row] = L == 0.f ? -INFINITY : M * p.scale + __logf(L);
 }
 
-// The split: the longest power-of-two number of pages, up to 32, that still gives 2048
-// waves at the longest length.
-int fp4_plan(int B, int Hq, int Hkv, int S, int D, int split_tokens, asym_attn_plan_info* out) {
+struct Fp4Plan {
+  int shares = 0, share_pages = 0, least = 1, per = 1;
+  bool rows = false;
+};
+
+int fp4_plan(int B, int Hq, int Hkv, int S, int D, int split_tokens, asym_attn_plan_info* out, Fp4Plan* plan) {
   if (B < 0 || Hq < 1 || Hkv < 1 || S < 1) return fail(ASYM_EINVAL, "fp4 attention: B must be >= 0, H_q, H_kv and S_max >= 1");
   if (Hq % Hkv) return fail(ASYM_EINVAL, "fp4 attention: H_kv must divide H_q");
   if (Hq / Hkv > kMaxG) return fail(ASYM_EUNSUPPORTED, "fp4 attention: at most 16 query heads per key/value head");
   if (D != kKvD) return fail(ASYM_EUNSUPPORTED, "fp4 attention: the head dimension must be 128");
-  if (S > (1 << 30)) return fail(ASYM_EUNSUPPORTED, "fp4 attention: S_max above 2^30");
-  if (split_tokens < 0 || split_tokens % kKvPageTokens || split_tokens > kMaxSplitPages * kKvPageTokens)
-    return fail(ASYM_EINVAL, "fp4 attention: split_tokens must be 0 (automatic) or a multiple of 32 up to 2048");
-  const int64_t heads = (int64_t)B * Hkv;
-  int L = split_tokens;
-  if (!L) {
-    L = 1024;
-    while (L > kKvPageTokens && heads * ((S + L - 1) / L) < 2048) L /= 2;
-  }
-  const int64_t n = ((int64_t)S + L - 1) / L, tasks = heads * n;
-  if (tasks > (1 << 26) - kWaves || (int64_t)B * Hq >= (1 << 24))  // (threads of a launch are counted in 32 bits)
+  if (split_tokens < 0 || split_tokens % kKvPageTokens || split_tokens > (1 << 20))
+    return fail(ASYM_EINVAL, "fp4 attention: split_tokens must be 0 (automatic) or a multiple of 32 up to 2^20");
+  const int64_t pages = ((int64_t)S + kKvPageTokens - 1) / kKvPageTokens, heads = (int64_t)B * Hkv, most = heads * pages;
+  if (most > (1 << 30)) return fail(ASYM_EUNSUPPORTED, "fp4 attention: more than 2^30 pages");
+  Fp4Plan P;
+  // Enough heads for every wave, and short: a wave a head, whole.  Shares balance unequal
+  // lengths, but cost a search, pieces and their join.  8 key/value heads, lengths from a
+  // quarter of S_max on, us, shares first: 256 requests of up to 300 tokens 26.2 15.4, 600
+  // 37.6 27.1, 1200 58.9 51.5, 2400 85.4 95.5; 512 of 1200 93.8 98.6; 1024 of 600 112 95.
+  P.rows = !split_tokens && heads >= kShares && S <= 1024;
+  P.least = split_tokens ? split_tokens / kKvPageTokens : (int)std::max<int64_t>(1, (pages + kMostPieces - 1) / kMostPieces);
+  P.share_pages = split_tokens / kKvPageTokens;
+  int64_t shares = P.rows ? heads : (most + P.least - 1) / P.least;
+  if (!P.rows && !split_tokens) shares = std::min<int64_t>(shares, kShares);
+  if (shares > (1 << 26) - kWaves || (int64_t)B * Hq * kJoinWaves >= (1 << 26))  // (threads of a launch are counted in 32 bits)
     return fail(ASYM_EUNSUPPORTED, "fp4 attention: too many tasks");
+  P.shares = (int)shares;
+  const int64_t share = P.rows ? pages : std::max<int64_t>(P.least, shares ? (most + shares - 1) / shares : 0);
+  const int64_t pieces = P.rows ? 1 : std::min(shares, (pages + P.least - 2) / P.least + 1);
+  // the join's waves of a query head, by the pieces that it has if all requests are of S_max:
+  // about eight each
+  const int64_t usual = std::min(pieces, heads ? (shares + heads - 1) / heads : 0);
+  while (P.per < kJoinWaves && P.per * 8 < usual) P.per *= 2;
   *out = asym_attn_plan_info{};
-  out->split_tokens = L;
-  out->n_splits = (int)n;
-  out->tasks = (int)tasks;
-  out->grid = (int)((tasks + kWaves - 1) / kWaves);
+  out->split_tokens = (int)std::min<int64_t>(share * kKvPageTokens, 1 << 30);
+  out->n_splits = (int)pieces;
+  out->tasks = P.shares;
+  out->grid = (P.shares + kWaves - 1) / kWaves;
   out->tasks_per_workgroup = kWaves;
-  out->workspace_bytes = n > 1 ? (size_t)B * Hq * n * (kKvD + 2) * sizeof(float) : 0;
+  out->workspace_bytes = P.rows ? 0 : (size_t)shares * 2 * (Hq / Hkv) * (kKvD + 2) * sizeof(float) + heads * sizeof(int2);
+  *plan = P;
   return ASYM_OK;
 }
 
@@ -312,7 +486,8 @@ int fp4_plan(int B, int Hq, int Hkv, int S, int D, int split_tokens, asym_attn_p
 extern "C" int asym_attn_decode_paged_fp4_plan(int B, int H_q, int H_kv, int S_max, int D, int split_tokens,
                                                asym_attn_plan_info* out) {
   if (!out) return asym::fail(ASYM_EINVAL, "fp4 attention plan: null output");
-  return asym::fp4_plan(B, H_q, H_kv, S_max, D, split_tokens, out);
+  asym::Fp4Plan plan;
+  return asym::fp4_plan(B, H_q, H_kv, S_max, D, split_tokens, out, &plan);
 }
 
 extern "C" int asym_attn_decode_paged_fp4(int B, int H_q, int H_kv, int S_max, int D, const void* q, const void* k_pool,
@@ -322,7 +497,8 @@ extern "C" int asym_attn_decode_paged_fp4(int B, int H_q, int H_kv, int S_max, i
                                           size_t workspace_bytes, void* stream) {
   using namespace asym;
   asym_attn_plan_info plan;
-  int rc = fp4_plan(B, H_q, H_kv, S_max, D, split_tokens, &plan);
+  Fp4Plan P;
+  int rc = fp4_plan(B, H_q, H_kv, S_max, D, split_tokens, &plan, &P);
   if (rc != ASYM_OK) return rc;
   if (pages_per_head < 1 || (int64_t)pages_per_head * kKvPageTokens < S_max)
     return fail(ASYM_EINVAL, "fp4 attention: the page tables end before S_max");
@@ -344,20 +520,31 @@ extern "C" int asym_attn_decode_paged_fp4(int B, int H_q, int H_kv, int S_max, i
   p.o = static_cast<uint16_t*>(o);
   p.lse = lse;
   p.part_o = static_cast<float*>(workspace);
-  p.part_ml = p.part_o ? p.part_o + (size_t)B * H_q * plan.n_splits * kKvD : nullptr;
+  if (!P.rows) {
+    const size_t pieces = (size_t)P.shares * 2 * (H_q / H_kv);
+    p.part_ml = p.part_o + pieces * kKvD;
+    p.cut = reinterpret_cast<int2*>(p.part_ml + pieces * 2);
+  }
   p.B = B; p.Hq = H_q; p.Hkv = H_kv; p.G = H_q / H_kv; p.S = S_max; p.pph = pages_per_head;
   p.pool_pages = (int)pool_pages;
-  p.split_pages = plan.split_tokens / kKvPageTokens;
-  p.n_splits = plan.n_splits;
-  p.tasks = plan.tasks;
+  p.shares = P.shares;
+  p.share_pages = P.share_pages;
+  p.least = P.least;
   p.scale = std::fabs(scale);
   p.c = std::fmax(p.scale * 1.4426950408889634f, 1.17549435e-38f);  // (0 weighs all keys alike, a masked one not at all)
   p.q_flip = scale < 0 ? 0x80008000u : 0u;
   hipStream_t s = static_cast<hipStream_t>(stream);
-  hipLaunchKernelGGL(fp4_decode_split, dim3((unsigned)plan.grid), dim3(64 * kWaves), 0, s, p);
+  // (at most: the requests may be shorter than S_max)
+  const int64_t bytes = 2ll * B * H_kv * ((S_max + (int64_t)kKvPageTokens - 1) / kKvPageTokens) * kFp4PageBytes;
+  const bool once = attn_streams_kv(paged_kv_bytes(bytes, (int64_t)pool_pages * kFp4PageBytes, k_pool == v_pool));
+  auto kernel = P.rows ? (once ? fp4_decode_share<2, true> : fp4_decode_share<0, true>)
+                       : (once ? fp4_decode_share<2, false> : fp4_decode_share<0, false>);
+  hipLaunchKernelGGL(kernel, dim3((unsigned)plan.grid), dim3(64 * kWaves), 0, s, p);
   ASYM_HIP(hipGetLastError());
-  if (plan.n_splits > 1) {
-    hipLaunchKernelGGL(fp4_decode_merge, dim3((unsigned)((size_t)B * H_q)), dim3(64 * kWaves), 0, s, p);
+  if (!P.rows) {
+    const int waves = std::max(P.per, 4);
+    const int64_t all = (int64_t)B * H_q * P.per;
+    hipLaunchKernelGGL(fp4_decode_join, dim3((unsigned)((all + waves - 1) / waves)), dim3(64 * waves), 0, s, p, P.per);
     ASYM_HIP(hipGetLastError());
   }
   return ASYM_OK;

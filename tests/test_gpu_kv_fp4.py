@@ -217,7 +217,10 @@ def poison_behind(pool, table, lens, values):
 @pytest.mark.parametrize("lens,Hq,Hkv,pph,split", [
     ([1], 1, 1, 1, 0), ([31, 32, 33], 4, 2, 2, 0), ([0, 5, 0, 64], 8, 2, 2, 32), ([100, 7, 65], 16, 1, 4, 32),
     ([300, 1, 0, 257], 5, 1, 10, 64), ([96], 3, 3, 3, 96), ([500, 20], 12, 4, 16, 0), ([1000], 32, 8, 32, 128),
-    ([40] * 70, 2, 1, 2, 0), ([2049, 64], 7, 1, 65, 2048), ([640], 14, 2, 20, 32)])
+    ([40] * 70, 2, 1, 2, 0), ([2049, 64], 7, 1, 65, 2048), ([640], 14, 2, 20, 32),
+    # batches of more requests than a wave looks at once, requests without tokens between them
+    ([0, 33, 64] * 100 + [0] * 300 + [50, 0, 0], 2, 2, 2, 0), ([70] + [0] * 520 + [45], 4, 2, 3, 32),
+    ([3, 0, 40, 65] * 512, 1, 1, 3, 0), ([0] * 5, 4, 2, 2, 0), ([5000, 1, 0, 4097], 3, 1, 157, 0)])
 def test_decode_against_oracle(dev, lens, Hq, Hkv, pph, split):
     B = len(lens)
     (kp, vp), kt, vt = clean_cache(B, Hkv, pph, seed=sum(lens) + Hq)

@@ -163,7 +163,7 @@ DECODE = dict(B=2, Hq=8, Hkv=2, S=64, D=128, q=P, kp=P, vp=P, pool=4, kt=P, vt=P
 @pytest.mark.parametrize("change,want", [
     (dict(B=-1), asym.EINVAL), (dict(S=0), asym.EINVAL), (dict(S=65), asym.EINVAL), (dict(Hq=7), asym.EINVAL),
     (dict(Hq=34), asym.EUNSUPPORTED), (dict(D=64), asym.EUNSUPPORTED), (dict(split=33), asym.EINVAL),
-    (dict(split=2080), asym.EINVAL), (dict(split=-32), asym.EINVAL), (dict(pool=0), asym.EINVAL), (dict(q=None), asym.EINVAL),
+    (dict(split=(1 << 20) + 32), asym.EINVAL), (dict(split=-32), asym.EINVAL), (dict(pool=0), asym.EINVAL), (dict(q=None), asym.EINVAL),
     (dict(lens=None), asym.EINVAL), (dict(o=P + 4), asym.EINVAL), (dict(lens=P + 1), asym.EINVAL),
     (dict(scale=float("nan")), asym.EINVAL), (dict(split=32), asym.EINVAL), (dict(split=32, ws=P, wsb=16), asym.EINVAL),
     (dict(split=32, ws=P + 4, wsb=1 << 20), asym.EINVAL), (dict(B=1 << 20, S=1 << 30, pph=1 << 25), asym.EUNSUPPORTED)])
@@ -174,10 +174,14 @@ def test_decode_refusals(change, want):
 
 def test_decode_plan():
     p = asym.attn_decode_paged_fp4_plan(16, 32, 8, 8000)
-    assert p["tasks"] == 16 * 8 * p["n_splits"] and p["n_splits"] == -(-8000 // p["split_tokens"])
-    assert p["workspace_bytes"] == 16 * 32 * p["n_splits"] * 130 * 4
-    assert asym.attn_decode_paged_fp4_plan(1, 8, 8, 32)["workspace_bytes"] == 0
-    assert asym.attn_decode_paged_fp4_plan(1, 8, 8, 320, split_tokens=96)["n_splits"] == 4
+    assert p["tasks"] == 2048 and p["split_tokens"] == -(-16 * 8 * 250 // 2048) * 32
+    assert p["workspace_bytes"] >= 2048 * 2 * 4 * 130 * 4 + 16 * 8 * 8
+    assert p["n_splits"] == 126  # 250 pages in shares of two, which need not begin where they do
+    one = asym.attn_decode_paged_fp4_plan(1, 8, 8, 32)
+    assert one["tasks"] == 8 and one["n_splits"] == 1
+    assert asym.attn_decode_paged_fp4_plan(1, 8, 8, 320, split_tokens=96)["tasks"] == 27
+    short = asym.attn_decode_paged_fp4_plan(256, 32, 8, 300)  # a wave a head
+    assert short["tasks"] == 2048 and short["n_splits"] == 1 and short["workspace_bytes"] == 0
     with pytest.raises(asym.AsymError):
         asym.attn_decode_paged_fp4_plan(1, 8, 8, 0)
     assert code("asym_attn_decode_paged_fp4_plan", 1, 8, 8, 32, 128, 0, None) == asym.EINVAL
