@@ -680,6 +680,15 @@ def stream_destroy(stream) -> None:
     _check(load_library().asym_stream_destroy(ctypes.c_void_p(stream.cuda_stream)))
 
 
+def _raw_stream(device: int):
+    """The handle of torch's current stream on a device."""
+    import torch
+    try:
+        return torch._C._cuda_getCurrentRawStream(device)
+    except AttributeError:
+        return torch.cuda.current_stream(device).cuda_stream
+
+
 def _stream_ptr(stream):
     """The hipStream_t of a torch stream, or of torch's current one, as an int.
     (torch.cuda.current_stream() builds a Stream object for it, 2.6 us of a
@@ -1083,9 +1092,9 @@ def _on(device: int, stream, call):
     import torch
     if stream is None:
         if device == torch.cuda.current_device():
-            return call(_stream_ptr(None))
+            return call(_raw_stream(device))
         with torch.cuda.device(device):
-            return call(_stream_ptr(None))
+            return call(_raw_stream(device))
     if stream.device.index != device:
         raise ValueError("the stream and the tensors are on different GPUs")
     with torch.cuda.device(device), torch.cuda.stream(stream):
