@@ -8,11 +8,11 @@
 // A workgroup computes 32 * NW rows of one sequence and one key/value head; a row is
 // a (token, query head of the group) pair, token-major, so a tile of few tokens
 // serves all heads that read the same keys and the diagonal is 32 * NW / G tokens
-// wide.  Each wave has 32 rows.  Blocks of 64 keys and values stream through LDS
-// (buffer_load ... lds, two buffers); per block
-//   S^T = K . Q^T   (v_mfma_f32_32x32x16_bf16, K from LDS, Q in registers):
-//                   a lane holds 32 of the 64 scores of ONE row;
-//   softmax         over the lane's own registers and one exchange with lane ^ 32;
+// wide.  Each wave has two blocks of 16 rows.  Blocks of 64 keys and values stream
+// through LDS (buffer_load ... lds, two buffers); per block
+//   S^T = K . Q^T   (v_mfma_f32_16x16x32_bf16, K from LDS, Q in registers): a row's 64
+//                   scores lie in four lanes, 16 apart;
+//   softmax         over the lane's own registers and two exchanges between those four;
 //                   the running max is raised only when a row's grows by more than
 //                   2^8 (the sums stay in range, the output is rescaled rarely);
 //   O^T += V^T . P^T: the score registers, rounded to bf16 (the type of the products'
@@ -21,10 +21,18 @@
 //                   is free: V^T is read in that order with ds_read_b64_tr_b16, which
 //                   transposes 16-bit values on the way from LDS.
 // Scores, max, sum and output are fp32.
+//
+// What bounds it: the matrix cores, at the clock they are left.  16384 causal tokens, 32
+// query and 8 key heads, take 1910 us, 1150 TFLOP/s.  Over that time the clock is 2.1 GHz,
+// the matrix cores work in 51 % of the cycles, the vector units (softmax) in 45 %, LDS
+// reads in 25 % and without conflicts: what remains is the overlap of the first two,
+// which two waves a SIMD reach in part.  Blocks of 32 rows (v_mfma_f32_32x32x16_bf16)
+// took 1990 us; 48 rows a wave spill (2620); two groups of waves in turn on products and
+// softmax 1950 to 2280; no maximum at all in the usual block, for its sum tells when
+// one is needed, 1900: the vector work is not what bounds it.
 #include <hip/hip_runtime.h>
 
 #include <cmath>
-#include <type_traits>
 
 #include "internal.h"
 #include "kv_fp4.h"
@@ -34,6 +42,8 @@ namespace {
 
 constexpr int PD = 128;   // head dimension
 constexpr int PN = 64;    // keys per block
+constexpr int NT = PN / 16, NK = PN / 32;  // 16-key and 32-key steps of a block
+constexpr int NQ = 2;     // 16-row blocks of a wave
 constexpr int kXcds = 8;  // workgroup i is dealt to XCD i mod 8 (only speed depends on it)
 constexpr int kRowBytes = PD * 2;
 constexpr int kTileBytes = PN * kRowBytes;
@@ -41,7 +51,7 @@ constexpr int kTileBytes = PN * kRowBytes;
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
-typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 
@@ -136,58 +146,38 @@ __device__ __forceinline__ void lds_load_1k(uint32_t dst, i32x4 rs, uint32_t vof
                : "memory");
 }
 
-__device__ __forceinline__ float max16(const f32x16& s) {
-  float m = fmaxf(fmaxf(s[0], s[1]), s[2]);
-#pragma unroll
-  for (int i = 3; i < 15; i += 2) m = fmaxf(fmaxf(m, s[i]), s[i + 1]);
-  return fmaxf(m, s[15]);
-}
-
-// max over this lane and lane ^ 32
-__device__ __forceinline__ float max_halves(float x) {
-  const uint32_t u = __float_as_uint(x);
-  const auto sw = __builtin_amdgcn_permlane32_swap(u, u, false, false);
-  return fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1]));
-}
-__device__ __forceinline__ float sum_halves(float x) {
-  const uint32_t u = __float_as_uint(x);
-  const auto sw = __builtin_amdgcn_permlane32_swap(u, u, false, false);
-  return __uint_as_float(sw[0]) + __uint_as_float(sw[1]);
-}
-
 // 16-byte chunk c of a tile's row r lies at chunk c ^ swz(r): the rows that one read
-// takes together then lie on different banks (K: 8 rows, one chunk of each; V: 4 rows,
-// two chunks of each).
-__device__ __forceinline__ int swz_k(int row) { return row & 7; }
-__device__ __forceinline__ int swz_v(int row) { return (row & 3) << 1; }
+// takes together (K: 16 rows, one chunk of each; V: 8 rows, two chunks of each) then
+// lie on different ones of the 64 banks.  Rows are 256 bytes, all banks once.
+__device__ __forceinline__ int swz_k(int row) { return row & 15; }
+__device__ __forceinline__ int swz_v(int row) { return (row & 7) << 1; }
 
 typedef __attribute__((address_space(3))) unsigned char lds_byte;
+typedef __attribute__((address_space(3))) u32x4 lds_u32x4;
 
 // A lane's places in the K and V tiles (bytes from a tile's start).
 struct Places {
-  uint32_t k[4];  // row n, chunks 2 c + h of c = 0 .. 3 (c + 4: 128 bytes on; rows 32 + n: 32 rows on)
-  uint32_t v[2];  // channels of blocks cb = 0, 1 (cb + 2: 128 bytes on), tokens 4 h + (lane % 16) / 4
+  uint32_t k[4];  // key n of 16, chunks 4 c + q of channel steps c
+  uint32_t v[8];  // channels of groups g of 16, tokens 4 q + n / 4
 };
 __device__ __forceinline__ Places places(int lane) {
   Places p;
-  const int n = lane & 31, h = lane >> 5, i = lane & 15, half = (lane >> 4) & 1;
+  const int n = lane & 15, q = lane >> 4;
 #pragma unroll
-  for (int c = 0; c < 4; ++c) p.k[c] = (uint32_t)(n * kRowBytes + (((2 * c + h) ^ swz_k(n)) << 4));
+  for (int c = 0; c < 4; ++c) p.k[c] = (uint32_t)(n * kRowBytes + (((4 * c + q) ^ swz_k(n)) << 4));
 #pragma unroll
-  for (int cb = 0; cb < 2; ++cb) {
-    const int row = 4 * h + (i >> 2), chunk = 4 * cb + 2 * half + ((i & 3) >> 1);
-    p.v[cb] = (uint32_t)(row * kRowBytes + ((chunk ^ swz_v(row)) << 4) + ((i & 1) << 3));
+  for (int g = 0; g < 8; ++g) {
+    const int row = 4 * q + (n >> 2), chunk = 2 * g + ((n & 3) >> 1);
+    p.v[g] = (uint32_t)(row * kRowBytes + ((chunk ^ swz_v(row)) << 4) + ((n & 1) << 3));
   }
   return p;
 }
-
-// K operand: 32 keys (half t of the block) x 16 channels (step c)
+// K operand: 16 keys (t-th of the block) x 32 channels (step c)
 __device__ __forceinline__ bf16x8 k_frag(const lds_byte* kt, const Places& pl, int t, int c) {
-  return *(const __attribute__((address_space(3))) bf16x8*)(kt + pl.k[c & 3] + (c >> 2) * 128 + t * 32 * kRowBytes);
+  return *(const __attribute__((address_space(3))) bf16x8*)(kt + pl.k[c] + t * 16 * kRowBytes);
 }
-
-// V^T operand: 32 channels (block cb) x 16 tokens (step ks of the block)
-__device__ __forceinline__ bf16x8 v_frag(const lds_byte* vt, const Places& pl, int cb, int ks) {
+// V^T operand: 16 channels (group g) x 32 tokens (step ks of the block)
+__device__ __forceinline__ bf16x8 v_frag(const lds_byte* vt, const Places& pl, int g, int ks) {
   union {
     s16x4 s[2];
     bf16x8 b;
@@ -195,16 +185,27 @@ __device__ __forceinline__ bf16x8 v_frag(const lds_byte* vt, const Places& pl, i
 #pragma unroll
   for (int part = 0; part < 2; ++part)
     u.s[part] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-        (__attribute__((address_space(3))) s16x4*)(vt + pl.v[cb & 1] + (cb >> 1) * 128 + (16 * ks + 8 * part) * kRowBytes));
+        (__attribute__((address_space(3))) s16x4*)(vt + pl.v[g] + (32 * ks + 16 * part) * kRowBytes));
   return u.b;
+}
+
+// f over this lane and those 16, 32 and 48 on: the four that share a row
+template <class F>
+__device__ __forceinline__ float over_quarters(float x, F f) {
+  uint32_t u = __float_as_uint(x);
+  auto sw = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+  x = f(__uint_as_float(sw[0]), __uint_as_float(sw[1]));
+  u = __float_as_uint(x);
+  sw = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+  return f(__uint_as_float(sw[0]), __uint_as_float(sw[1]));
 }
 
 template <int NW>
 __global__ void __launch_bounds__(64 * NW, 2) attn_prefill_kernel(PrefillParams p) {
-  constexpr int BM = 32 * NW;
+  constexpr int WR = 16 * NQ, BM = WR * NW;
   __shared__ __attribute__((aligned(1024))) unsigned char lds[4 * kTileBytes];  // two K tiles, two V tiles
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int n = lane & 31, h = lane >> 5;
+  const int n = lane & 15, q4 = lane >> 4;
 
   // which head and tile
   int hk, rank;
@@ -230,29 +231,27 @@ __global__ void __launch_bounds__(64 * NW, 2) attn_prefill_kernel(PrefillParams 
   packed_rows(p.cu_q, seq, p.Tq, qs, Lq);
   packed_rows(p.cu_k, seq, p.Tk, ks, Lk);
   const int off = Lk - Lq;
-
-  // this lane's row (rows past the last repeat it, and are not stored)
   const int64_t rows = (int64_t)Lq * p.G;
-  const int64_t row0 = (int64_t)tile * BM + wave * 32;
-  const int64_t row = min(row0 + n, rows - 1);
-  const int tok = (int)(row / p.G), g = (int)(row - (int64_t)tok * p.G);
-  const int64_t orow = (int64_t)(qs + tok) * p.Hq + (int64_t)hk * p.G + g;
-  // keys that the row sees; the most over the wave, the least and most over the workgroup
+  const int64_t row0 = (int64_t)tile * BM + wave * WR;
+  // keys that a row sees; the most over the wave, the least and most over the workgroup
   auto limit = [&](int64_t r) { return p.causal ? max(off + (int)(min(r, rows - 1) / p.G) + 1, 0) : Lk; };
-  const int lim = p.causal ? max(off + tok + 1, 0) : Lk;
-  const int lim_hi = __builtin_amdgcn_readfirstlane(limit(row0 + 31));
+  const int lim_hi = __builtin_amdgcn_readfirstlane(limit(row0 + WR - 1));
   const int nblk = (__builtin_amdgcn_readfirstlane(limit((int64_t)tile * BM + BM - 1)) + PN - 1) / PN;
   const int nfull = __builtin_amdgcn_readfirstlane(limit((int64_t)tile * BM)) / PN;  // blocks that every row sees whole
 
-  bf16x8 qf[8];
-  {
-    const uint16_t* qr = p.q + (int64_t)(qs + tok) * p.q_tok + ((int64_t)hk * p.G + g) * p.q_head + 8 * h;
+  // this lane's rows, one of each block of 16 (rows past the last repeat it, and are not stored)
+  bf16x8 qf[NQ][4];
 #pragma unroll
-    for (int s = 0; s < 8; ++s) {
-      u32x4 w = *reinterpret_cast<const u32x4*>(qr + 16 * s);
+  for (int b = 0; b < NQ; ++b) {
+    const int64_t row = min(row0 + 16 * b + n, rows - 1);
+    const int tok = (int)(row / p.G), g = (int)(row - (int64_t)tok * p.G);
+    const uint16_t* qr = p.q + (int64_t)(qs + tok) * p.q_tok + ((int64_t)hk * p.G + g) * p.q_head + 8 * q4;
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+      u32x4 w = *reinterpret_cast<const u32x4*>(qr + 32 * c);
 #pragma unroll
       for (int e = 0; e < 4; ++e) w[e] ^= p.q_flip;
-      qf[s] = __builtin_bit_cast(bf16x8, w);
+      qf[b][c] = __builtin_bit_cast(bf16x8, w);
     }
   }
   const uint16_t* kb = p.k + (int64_t)ks * p.k_tok + (int64_t)hk * p.k_head;
@@ -282,50 +281,74 @@ __global__ void __launch_bounds__(64 * NW, 2) attn_prefill_kernel(PrefillParams 
   auto k_tile = [&](int j) { return (lds_byte*)lds + (j & 1) * kTileBytes; };
   auto v_tile = [&](int j) { return (lds_byte*)lds + (2 + (j & 1)) * kTileBytes; };
 
-  f32x16 o[4];
+  f32x4 o[NQ][8], s[NQ][NT];
+  bf16x8 pf[NQ][NK];
+  float m[NQ], l[NQ];
 #pragma unroll
-  for (int cb = 0; cb < 4; ++cb) o[cb] = f32x16{};
-  float m = -INFINITY, l = 0.f;
-  f32x16 s[2];
-  bf16x8 pf[4];
-
+  for (int b = 0; b < NQ; ++b) {
+    m[b] = -INFINITY;
+    l[b] = 0.f;
+#pragma unroll
+    for (int g = 0; g < 8; ++g) o[b][g] = f32x4{};
+  }
   auto scores = [&](int j) {
     const lds_byte* kt = k_tile(j);
-    s[0] = s[1] = f32x16{};
 #pragma unroll
-    for (int c = 0; c < 8; ++c)
+    for (int t = 0; t < NT; ++t)
 #pragma unroll
-      for (int t = 0; t < 2; ++t) s[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k_frag(kt, pl, t, c), qf[c], s[t], 0, 0, 0);
+      for (int c = 0; c < 4; ++c) {
+        const bf16x8 f = k_frag(kt, pl, t, c);
+#pragma unroll
+        for (int b = 0; b < NQ; ++b)
+          s[b][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f, qf[b][c], c ? s[b][t] : f32x4{}, 0, 0, 0);
+      }
   };
   auto softmax = [&] {
-    const float top = max_halves(fmaxf(max16(s[0]), max16(s[1])));
-    if (__any((top - m) * p.c > 8.f)) {  // (a first finite max: inf; NaN never)
-      const float m_new = fmaxf(m, top);
-      const float alpha = __builtin_amdgcn_exp2f((m - (m_new == -INFINITY ? 0.f : m_new)) * p.c);
-      l *= alpha;
+    bool up = false;
+    float top[NQ];
 #pragma unroll
-      for (int cb = 0; cb < 4; ++cb)
+    for (int b = 0; b < NQ; ++b) {
+      float x = fmaxf(fmaxf(s[b][0][0], s[b][0][1]), s[b][0][2]);
 #pragma unroll
-        for (int r = 0; r < 16; ++r) o[cb][r] *= alpha;
-      m = m_new;
+      for (int i = 3; i + 1 < 4 * NT; i += 2) x = fmaxf(fmaxf(x, s[b][i >> 2][i & 3]), s[b][(i + 1) >> 2][(i + 1) & 3]);
+      x = fmaxf(x, s[b][NT - 1][3]);
+      top[b] = over_quarters(x, [](float a, float c) { return fmaxf(a, c); });
+      up |= (top[b] - m[b]) * p.c > 8.f;  // (a first finite max: inf; NaN never)
     }
-    const float ms = m == -INFINITY ? 0.f : m * p.c;
+    if (__any(up)) {
 #pragma unroll
-    for (int t = 0; t < 2; ++t)
+      for (int b = 0; b < NQ; ++b) {
+        const float m_new = fmaxf(m[b], top[b]);
+        const float alpha = __builtin_amdgcn_exp2f((m[b] - (m_new == -INFINITY ? 0.f : m_new)) * p.c);
+        l[b] *= alpha;
 #pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        const float e = __builtin_amdgcn_exp2f(fmaf(s[t][r], p.c, -ms));
-        l += e;
-        pf[2 * t + (r >> 3)][r & 7] = (__bf16)e;
+        for (int g = 0; g < 8; ++g) o[b][g] *= alpha;
+        m[b] = m_new;
       }
+    }
+#pragma unroll
+    for (int b = 0; b < NQ; ++b) {
+      const float ms = m[b] == -INFINITY ? 0.f : m[b] * p.c;
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const float e = __builtin_amdgcn_exp2f(fmaf(s[b][t][r], p.c, -ms));
+          l[b] += e;
+          pf[b][t >> 1][4 * (t & 1) + r] = (__bf16)e;
+        }
+    }
   };
   auto add_pv = [&](int j) {
     const lds_byte* vt = v_tile(j);
 #pragma unroll
-    for (int kst = 0; kst < 4; ++kst)
+    for (int kst = 0; kst < NK; ++kst)
 #pragma unroll
-      for (int cb = 0; cb < 4; ++cb)
-        o[cb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v_frag(vt, pl, cb, kst), pf[kst], o[cb], 0, 0, 0);
+      for (int g = 0; g < 8; ++g) {
+        const bf16x8 f = v_frag(vt, pl, g, kst);
+#pragma unroll
+        for (int b = 0; b < NQ; ++b) o[b][g] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f, pf[b][kst], o[b][g], 0, 0, 0);
+      }
   };
   auto arrived = [&] {  // this wave's loads, and with them everyone's
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
@@ -368,7 +391,7 @@ __global__ void __launch_bounds__(64 * NW, 2) attn_prefill_kernel(PrefillParams 
 #pragma unroll
       for (int i = 0; i < kTileBytes / 16 / (64 * NW); ++i) {
         const uint32_t at = (uint32_t)(i * 64 * NW + (int)threadIdx.x) * 16;
-        f(at, *(__attribute__((address_space(3))) u32x4*)(v_tile(j) + at));
+        f(at, *(lds_u32x4*)(v_tile(j) + at));
       }
     };
     uint32_t bad = 0;
@@ -378,14 +401,20 @@ __global__ void __launch_bounds__(64 * NW, 2) attn_prefill_kernel(PrefillParams 
         for (int e = 0; e < 4; ++e) bad |= (w[e] & 0x7F807F80u) + 0x00800080u;  // an exponent of all ones carries
       });
     const bool guard = p.causal && __syncthreads_or((bad & 0x80008000u) != 0);
+    int lim[NQ];
+#pragma unroll
+    for (int b = 0; b < NQ; ++b) lim[b] = limit(row0 + 16 * b + n);
     if (mine) {
       scores(j);
-      const int left = lim - j * PN - 4 * h;
 #pragma unroll
-      for (int t = 0; t < 2; ++t)
+      for (int b = 0; b < NQ; ++b) {
+        const int left = lim[b] - j * PN - 4 * q4;
 #pragma unroll
-        for (int r = 0; r < 16; ++r)
-          if (32 * t + (r & 3) + 8 * (r >> 2) >= left) s[t][r] = -INFINITY;
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+            if (16 * t + r >= left) s[b][t][r] = -INFINITY;
+      }
       softmax();
     }
     if (guard) {
@@ -399,57 +428,66 @@ __global__ void __launch_bounds__(64 * NW, 2) attn_prefill_kernel(PrefillParams 
           fin[e] = w[e] & ~mask;
           code[e] = (kind(w[e] & 0xFFFFu) | (kind(w[e] >> 16) << 16)) & mask;
         }
-        *(__attribute__((address_space(3))) u32x4*)(v_tile(j) + at) = fin;
-        *(__attribute__((address_space(3))) u32x4*)(k_tile(j) + at) = code;
+        *(lds_u32x4*)(v_tile(j) + at) = fin;
+        *(lds_u32x4*)(k_tile(j) + at) = code;
       });
       __syncthreads();
       if (mine) {
 #pragma unroll
-        for (int cb = 0; cb < 4; ++cb) {
-          f32x16 seen = {};
+        for (int b = 0; b < NQ; ++b)
 #pragma unroll
-          for (int kst = 0; kst < 4; ++kst) {
-            u32x4 vis;
+          for (int g = 0; g < 8; ++g) {
+            __builtin_amdgcn_sched_barrier(0);  // (one product's registers at a time)
+            f32x4 seen = {};
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const int r = 8 * (kst & 1) + 2 * e, key = j * PN + 32 * (kst >> 1) + (r & 3) + 8 * (r >> 2) + 4 * h;
-              vis[e] = (key < lim ? 0x3F80u : 0u) | (key + 1 < lim ? 0x3F800000u : 0u);
+            for (int kst = 0; kst < NK; ++kst) {
+              u32x4 vis;
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                const int key = j * PN + 32 * kst + 4 * q4 + 16 * (e >> 1) + 2 * (e & 1);
+                vis[e] = (key < lim[b] ? 0x3F80u : 0u) | (key + 1 < lim[b] ? 0x3F800000u : 0u);
+              }
+              seen = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v_frag(k_tile(j), pl, g, kst), __builtin_bit_cast(bf16x8, vis),
+                                                             seen, 0, 0, 0);
             }
-            seen = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v_frag(k_tile(j), pl, cb, kst), __builtin_bit_cast(bf16x8, vis),
-                                                           seen, 0, 0, 0);
-          }
 #pragma unroll
-          for (int r = 0; r < 16; ++r) {
-            const int k = (int)seen[r];
-            o[cb][r] += ((k & 127) ? INFINITY : 0.f) + (((k >> 7) & 127) ? -INFINITY : 0.f) + (k >= 16384 ? NAN : 0.f);
+            for (int r = 0; r < 4; ++r) {
+              const int k = (int)seen[r];
+              o[b][g][r] += ((k & 127) ? INFINITY : 0.f) + (((k >> 7) & 127) ? -INFINITY : 0.f) + (k >= 16384 ? NAN : 0.f);
+            }
           }
-        }
       }
     }
     if (mine) add_pv(j);
   }
 
-  // a lane has 64 of the row's 128 channels: 4 of every 8, the other half's in lane ^ 32
-  l = sum_halves(l);
-  const float inv = l > 0.f ? 1.f / l : (l == 0.f ? 0.f : l);  // (NaN stays)
-  const bool store = row0 + n < rows;
-  uint16_t* dst = p.o + orow * PD;
+  // a lane has 4 of every 16 channels of a row; two groups of them, exchanged between the
+  // quarters, make 16 bytes
 #pragma unroll
-  for (int cb = 0; cb < 4; ++cb)
+  for (int b = 0; b < NQ; ++b) {
+    const float lt = over_quarters(l[b], [](float a, float c) { return a + c; });
+    const float inv = lt > 0.f ? 1.f / lt : (lt == 0.f ? 0.f : lt);  // (NaN stays)
+    const int64_t r = row0 + 16 * b + n, row = min(r, rows - 1);
+    const int tok = (int)(row / p.G);
+    const int64_t orow = (int64_t)(qs + tok) * p.Hq + (int64_t)hk * p.G + (row - (int64_t)tok * p.G);
+    uint16_t* dst = p.o + orow * PD;
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      uint32_t w[4];  // channels 16 i + 4 h + 0 .. 3 and 16 i + 8 + 4 h + 0 .. 3
+    for (int g = 0; g < 8; g += 2) {
+      uint32_t w[4];
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const bf16x2 b = {(__bf16)(o[cb][8 * i + 2 * e] * inv), (__bf16)(o[cb][8 * i + 2 * e + 1] * inv)};
-        w[e] = __builtin_bit_cast(uint32_t, b);
+        const f32x4& x = o[b][g + (e >> 1)];
+        const bf16x2 y = {(__bf16)(x[2 * (e & 1)] * inv), (__bf16)(x[2 * (e & 1) + 1] * inv)};
+        w[e] = __builtin_bit_cast(uint32_t, y);
       }
-      const auto x = __builtin_amdgcn_permlane32_swap(w[0], w[2], false, false);
-      const auto y = __builtin_amdgcn_permlane32_swap(w[1], w[3], false, false);
-      if (store)
-        *reinterpret_cast<u32x4*>(dst + 32 * cb + 16 * i + 8 * h) = u32x4{x[0], y[0], x[1], y[1]};
+      const auto x = __builtin_amdgcn_permlane16_swap(w[0], w[2], false, false);
+      const auto y = __builtin_amdgcn_permlane16_swap(w[1], w[3], false, false);
+      // quarter 0: channels 0 .. 7 of group g, 1: 0 .. 7 of group g + 1, 2: 8 .. 15 of g, 3: of g + 1
+      if (r < rows)
+        *reinterpret_cast<u32x4*>(dst + 16 * (g + (q4 & 1)) + 8 * (q4 >> 1)) = u32x4{x[0], y[0], x[1], y[1]};
     }
-  if (p.lse && store && h == 0) p.lse[orow] = l == 0.f ? -INFINITY : m * p.scale + __logf(l);
+    if (p.lse && r < rows && q4 == 0) p.lse[orow] = lt == 0.f ? -INFINITY : m[b] * p.scale + __logf(lt);
+  }
 }
 
 }  // namespace
@@ -498,9 +536,9 @@ extern "C" int asym_attn_prefill_bf16(int B, int H_q, int H_kv, int D, int T_q, 
   p.c = std::fmax(p.scale * 1.4426950408889634f, 1.17549435e-38f);
   p.q_flip = scale < 0 ? 0x80008000u : 0u;
   // Tiles of 256 rows read the keys half as often and are faster once there is one for
-  // every CU (us, 128 rows first: 16384 tokens, 32 / 8 heads 2031 1953, 4096 tokens 149 137,
-  // two of 4096 with 16 / 16 heads 149 138, eight chunks of 1000 tokens behind
-  // prefixes 329 329); with fewer, CUs would idle (1024 tokens, 32 / 8 heads 25 32).
+  // every CU (us, 128 rows first: 16384 tokens, 32 / 8 heads 1958 1908, 4096 tokens 146 134,
+  // two of 4096 with 16 / 16 heads 147 136; eight chunks of 1000 tokens behind
+  // prefixes 316 321); with fewer, CUs would idle (1024 tokens, 32 / 8 heads 26 34).
   auto count = [&](int rows) { return (int64_t)T_q * p.G / rows + B; };  // sequences end in a part tile each
   const bool wide = count(256) * H_kv >= 256;
   const int64_t tiles = count(wide ? 256 : 128);
