@@ -191,18 +191,27 @@ __global__ void __launch_bounds__(64 * kWaves) kv_read_kernel(KvParams p) {
     kc[t] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rk, 1024 * t + 64 * n + 16 * q, 0, 0));
     vc[t] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rv, 1024 * t + 16 * lane, 0, 0));
   }
-  const uint32_t kscale = __builtin_amdgcn_raw_buffer_load_b16(rk, kFp4ScaleOff + 2 * lane, 0, 0);
+  uint32_t kscale[4];  // of block i, token n of either half, one a byte
+#pragma unroll
+  for (int i = 0; i < 4; ++i) kscale[i] = __builtin_amdgcn_raw_buffer_load_b16(rk, kFp4ScaleOff + 2 * (n + 16 * i), 0, 0);
   uint32_t vscale[2];  // of token n of either half: 4 blocks, one a byte
 #pragma unroll
   for (int t = 0; t < 2; ++t)
     vscale[t] = __builtin_amdgcn_raw_buffer_load_b32(rv, kFp4ScaleOff + 32 * (n >> 2) + 4 * ((n & 3) + 4 * t), 0, 0);
 #pragma unroll
   for (int t = 0; t < 2; ++t) {
+    // codes of 8 channels exchanged between a token's four lanes (a 4 x 4 transpose):
+    // word i of lane q then belongs to channels 32 i + 8 q, and a store fills 64 bytes of a row
+    const auto x = __builtin_amdgcn_permlane16_swap(kc[t][0], kc[t][1], false, false);
+    const auto y = __builtin_amdgcn_permlane16_swap(kc[t][2], kc[t][3], false, false);
+    const auto even = __builtin_amdgcn_permlane32_swap(x[0], y[0], false, false);
+    const auto odd = __builtin_amdgcn_permlane32_swap(x[1], y[1], false, false);
+    const u32x4 c = {even[0], odd[0], even[1], odd[1]};
     const int tok = 16 * t + n;
     if (tok < lo || tok >= hi) continue;
-    u32x4* dst = reinterpret_cast<u32x4*>(p.ko + ((int64_t)(row + tok) * p.H + head) * kKvD + 32 * q);
+    u32x4* dst = reinterpret_cast<u32x4*>(p.ko + ((int64_t)(row + tok) * p.H + head) * kKvD + 8 * q);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) dst[i] = values8(kc[t][i], (kscale >> (8 * t)) & 0xFFu);
+    for (int i = 0; i < 4; ++i) dst[4 * i] = values8(c[i], (kscale[i] >> (8 * t)) & 0xFFu);
   }
   // values: the page has them channel by channel; a matrix product with the tokens' scales
   // on a diagonal turns them (exact: every sum has one term).  Column n is token 16 t + n,
@@ -211,7 +220,7 @@ __global__ void __launch_bounds__(64 * kWaves) kv_read_kernel(KvParams p) {
   for (int t = 0; t < 2; ++t) {
     const int tok = 16 * t + n;
     const bool on = tok >= lo && tok < hi;
-    uint2* dst = reinterpret_cast<uint2*>(p.vo + ((int64_t)(row + tok) * p.H + head) * kKvD + 4 * q);
+    u32x4* dst = reinterpret_cast<u32x4*>(p.vo + ((int64_t)(row + tok) * p.H + head) * kKvD + 16 * (q & 1) + 8 * (q >> 1));
 #pragma unroll
     for (int blk = 0; blk < 4; ++blk) {
       const uint32_t sb = (vscale[t] >> (8 * blk)) & 0xFFu;
@@ -221,14 +230,20 @@ __global__ void __launch_bounds__(64 * kWaves) kv_read_kernel(KvParams p) {
 #pragma unroll
       for (int w = 0; w < 2; ++w)
         d[2 * t + w] = (n & 3) >> 1 == w ? ((n & 1) ? h << 16 : h) : 0u;
+      uint32_t o[4];  // 4 channels of group 2 blk, 4 of group 2 blk + 1
 #pragma unroll
       for (int g2 = 0; g2 < 2; ++g2) {
         const int g = 2 * blk + g2;
         const f32x4 x = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
             __builtin_bit_cast(bf16x8, values8(vc[g >> 2][g & 3], 127u)), __builtin_bit_cast(bf16x8, d), f32x4{}, 0, 0, 0);
         const bf16x2 y0 = {(__bf16)x[0], (__bf16)x[1]}, y1 = {(__bf16)x[2], (__bf16)x[3]};
-        if (on) dst[4 * g] = uint2{__builtin_bit_cast(uint32_t, y0), __builtin_bit_cast(uint32_t, y1)};
+        o[2 * g2] = __builtin_bit_cast(uint32_t, y0);
+        o[2 * g2 + 1] = __builtin_bit_cast(uint32_t, y1);
       }
+      // quarter 0: channels 0 .. 7 of the first group, 1: of the second, 2 and 3: 8 .. 15
+      const auto x = __builtin_amdgcn_permlane16_swap(o[0], o[2], false, false);
+      const auto y = __builtin_amdgcn_permlane16_swap(o[1], o[3], false, false);
+      if (on) dst[4 * blk] = u32x4{x[0], y[0], x[1], y[1]};
     }
   }
 }
