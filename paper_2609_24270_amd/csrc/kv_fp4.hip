@@ -103,63 +103,74 @@ __global__ void __launch_bounds__(64 * kWaves) kv_write_kernel(KvParams p) {
   const size_t entry = ((size_t)seq * p.H + head) * p.pph + page;
   const int kp = __builtin_amdgcn_readfirstlane(p.k_pages[entry]), vp = __builtin_amdgcn_readfirstlane(p.v_pages[entry]);
   const int c16 = lane & 15, t4 = lane >> 4;  // 8 channels, one of four tokens
-  if (kp >= 0 && kp < p.pool_pages) {
-    uint8_t* dst = p.k_pool + (size_t)kp * kFp4PageBytes;
-    for (int t = t4; t < kKvPageTokens; t += 4) {
-      const bool on = t >= lo && t < hi;
-      u32x4 x = {};
-      if (on)
-        x = *reinterpret_cast<const u32x4*>(p.k + (int64_t)(row + t) * p.k_tok + (int64_t)head * p.k_head + 8 * c16);
-      uint32_t top = 0;
+  const bool k_on = kp >= 0 && kp < p.pool_pages, v_on = vp >= 0 && vp < p.pool_pages;
+  uint8_t* kd = p.k_pool + (size_t)(k_on ? kp : 0) * kFp4PageBytes;
+  uint8_t* vd = p.v_pool + (size_t)(v_on ? vp : 0) * kFp4PageBytes;
+  // lane (m, q) of the value page: 8 words, of channels 16 g + m, tokens 4 q + 0 .. 3 and
+  // 16 + 4 q + 0 .. 3; nibbles of tokens that are not written stay
+  uint32_t keep = 0;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) top = max(top, max(x[e] & 0x7FFFu, (x[e] >> 16) & 0x7FFFu));
-      const uint32_t s = scale_byte(max4(top));
-      if (on) {
-        *reinterpret_cast<uint32_t*>(dst + 64 * t + 4 * c16) = codes8(x, s);
-        if ((c16 & 3) == 0) dst[kFp4ScaleOff + 2 * ((t & 15) + 16 * (c16 >> 2)) + (t >> 4)] = (uint8_t)s;
+  for (int j = 0; j < 8; ++j) {
+    const int t = 4 * t4 + (j & 3) + 16 * (j >> 2);
+    if (t < lo || t >= hi) keep |= 0xFu << (4 * j);
+  }
+  const bool some = v_on && keep != 0xFFFFFFFFu;
+  u32x4 old[2] = {};
+  if (some && keep) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) old[i] = *reinterpret_cast<const u32x4*>(vd + 1024 * i + 16 * lane);
+  }
+  auto block_scale = [](u32x4 x) {
+    uint32_t top = 0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) top = max(top, max(x[e] & 0x7FFFu, (x[e] >> 16) & 0x7FFFu));
+    return scale_byte(max4(top));
+  };
+  // 16 tokens at a time, their loads all at once
+#pragma unroll 1
+  for (int t0 = 0; t0 < kKvPageTokens; t0 += 16) {
+    if (t0 + 16 <= lo || t0 >= hi) continue;
+    u32x4 xk[4], xv[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int t = t0 + 4 * i + t4;
+      xk[i] = xv[i] = u32x4{};
+      if (t >= lo && t < hi) {
+        xk[i] = *reinterpret_cast<const u32x4*>(p.k + (int64_t)(row + t) * p.k_tok + (int64_t)head * p.k_head + 8 * c16);
+        xv[i] = *reinterpret_cast<const u32x4*>(p.v + (int64_t)(row + t) * p.v_tok + (int64_t)head * p.v_head + 8 * c16);
       }
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int t = t0 + 4 * i + t4, u = 4 * i + t4;  // u = t % 16
+      const bool on = t >= lo && t < hi;
+      uint32_t s = block_scale(xk[i]);
+      if (on && k_on) {
+        *reinterpret_cast<uint32_t*>(kd + 64 * t + 4 * c16) = codes8(xk[i], s);
+        if ((c16 & 3) == 0) kd[kFp4ScaleOff + 2 * (u + 16 * (c16 >> 2)) + (t0 >> 4)] = (uint8_t)s;
+      }
+      s = block_scale(xv[i]);
+      tile[wave][t][c16] = codes8(xv[i], s);
+      if (on && v_on && (c16 & 3) == 0)
+        vd[kFp4ScaleOff + 32 * (u >> 2) + 4 * ((u & 3) + (t0 >> 2)) + (c16 >> 2)] = (uint8_t)s;
     }
   }
-  if (vp >= 0 && vp < p.pool_pages) {
-    uint8_t* dst = p.v_pool + (size_t)vp * kFp4PageBytes;
-    for (int t = t4; t < kKvPageTokens; t += 4) {
-      const bool on = t >= lo && t < hi;
-      u32x4 x = {};
-      if (on)
-        x = *reinterpret_cast<const u32x4*>(p.v + (int64_t)(row + t) * p.v_tok + (int64_t)head * p.v_head + 8 * c16);
-      uint32_t top = 0;
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+  if (some) {
 #pragma unroll
-      for (int e = 0; e < 4; ++e) top = max(top, max(x[e] & 0x7FFFu, (x[e] >> 16) & 0x7FFFu));
-      const uint32_t s = scale_byte(max4(top));
-      tile[wave][t][c16] = codes8(x, s);
-      if (on && (c16 & 3) == 0)
-        dst[kFp4ScaleOff + 32 * ((t & 15) >> 2) + 4 * ((t & 3) + 4 * (t >> 4)) + (c16 >> 2)] = (uint8_t)s;
-    }
-    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-    // lane (m, q): 8 words, of channels 16 g + m, tokens 4 q + 0 .. 3 and 16 + 4 q + 0 .. 3
-    const int m = lane & 15, q = lane >> 4;
-    uint32_t keep = 0;  // nibbles of tokens that are not written
+    for (int g = 0; g < 8; ++g) {
+      uint32_t w = 0;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const int t = 4 * q + (j & 3) + 16 * (j >> 2);
-      if (t < lo || t >= hi) keep |= 0xFu << (4 * j);
-    }
-    if (keep != 0xFFFFFFFFu) {
-#pragma unroll
-      for (int g = 0; g < 8; ++g) {
-        uint32_t w = 0;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const int t = 4 * q + (j & 3) + 16 * (j >> 2), c = 16 * g + m;
-          w |= ((tile[wave][t][c >> 3] >> (4 * (c & 7))) & 0xFu) << (4 * j);
-        }
-        uint32_t* at = reinterpret_cast<uint32_t*>(dst + 1024 * (g >> 2) + 16 * lane + 4 * (g & 3));
-        if (keep) w = (w & ~keep) | (*at & keep);
-        *at = w;
+      for (int j = 0; j < 8; ++j) {
+        const int t = 4 * t4 + (j & 3) + 16 * (j >> 2), c = 16 * g + c16;
+        w |= ((tile[wave][t][c >> 3] >> (4 * (c & 7))) & 0xFu) << (4 * j);
       }
+      old[g >> 2][g & 3] = (w & ~keep) | (old[g >> 2][g & 3] & keep);
     }
+#pragma unroll
+    for (int i = 0; i < 2; ++i) *reinterpret_cast<u32x4*>(vd + 1024 * i + 16 * lane) = old[i];
   }
 }
 
