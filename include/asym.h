@@ -908,8 +908,11 @@ int asym_mla_decode_plan(const asym_topology* topo, int B, int H_q, int S_k, int
  * falling; held within [0, T_q] and [0, T_k] whatever they say.  Rows of O and lse
  * outside every sequence are left as they are.  D must be 128; q, K, V and O
  * 16-byte aligned.  H_q / H_kv may be any whole number.
- * One launch, no workspace, no host synchronisation; may be captured.  mapping:
- * AWARE keeps the tiles that read one key/value head on one XCD where the head
+ * Few rows over many keys (a verification step, a prompt's last chunk) are cut along the
+ * keys and joined by a second launch; the fp32 pieces lie in the caller's workspace
+ * (16-byte aligned; asym_attn_prefill_workspace's bytes, which depend on the sizes alone
+ * and are 0 for every other call), which calls that may overlap must not share.
+ * No host synchronisation; may be captured.  mapping: AWARE keeps the tiles that read one key/value head on one XCD where the head
  * count divides by the XCDs or the other way round (its keys and values cross
  * into one L2); the oblivious mappings number them head by head.  Longest tiles
  * first in every mapping, and every mapping gives the same bits.  Runs on the
@@ -920,7 +923,9 @@ int asym_attn_prefill_bf16(int B, int H_q, int H_kv, int D, int T_q, int T_k,
                            const void* k, int64_t k_token, int64_t k_head,
                            const void* v, int64_t v_token, int64_t v_head,
                            void* o, float* lse, const int32_t* cu_q, const int32_t* cu_k,
-                           float scale, int causal, int mapping, void* stream);
+                           float scale, int causal, int mapping, void* workspace,
+                           size_t workspace_bytes, void* stream);
+int asym_attn_prefill_workspace(int B, int H_q, int H_kv, int T_q, int T_k, size_t* bytes);
 
 /* ---- paged cache in microscaled 4-bit floating point ---------------------- */
 /* A page (ASYM_FP4_PAGE_BYTES) holds 32 consecutive tokens of one head, keys or

@@ -47,7 +47,8 @@ EXPORTS = (
     "asym_gemm_bf16_trace",
     "asym_gemm_plan", "asym_gemm_set_small_m",
     "asym_attn_decode_bf16", "asym_attn_decode_plan", "asym_attn_decode_paged_bf16", "asym_attn_pages_place", "asym_mla_decode_bf16", "asym_mla_decode_plan", "asym_mla_set_workgroup_form",
-    "asym_attn_prefill_bf16", "asym_kv_write_fp4", "asym_kv_read_fp4", "asym_attn_decode_paged_fp4",
+    "asym_attn_prefill_bf16", "asym_attn_prefill_workspace", "asym_kv_write_fp4", "asym_kv_read_fp4",
+    "asym_attn_decode_paged_fp4",
     "asym_attn_decode_paged_fp4_plan", "asym_kv_pages_workspace", "asym_kv_extend", "asym_kv_fork", "asym_kv_free",
     "asym_kv_compact",
     "asym_copy_bf16", "asym_corun", "asym_last_error", "asym_version",
@@ -282,7 +283,8 @@ def load_library(path: str = LIB_PATH):
                                       ctypes.c_size_t, ip, i, ctypes.POINTER(ctypes.c_int32)]),
         "asym_mla_decode_bf16": (i, [topo_p, i, i, i, vp, vp, vp, vp, ctypes.c_float, i, i, u32, vp]),
         "asym_mla_decode_plan": (i, [topo_p, i, i, i, i, i, u32, vp, ctypes.POINTER(MlaPlanInfo)]),
-        "asym_attn_prefill_bf16": (i, [i] * 6 + [vp, i64, i64] * 3 + [vp] * 4 + [f32, i, i, vp]),
+        "asym_attn_prefill_bf16": (i, [i] * 6 + [vp, i64, i64] * 3 + [vp] * 4 + [f32, i, i, vp, sz, vp]),
+        "asym_attn_prefill_workspace": (i, [i] * 5 + [ctypes.POINTER(sz)]),
         "asym_kv_write_fp4": (i, [i, i, i] + [vp, i64, i64] * 2 + [vp, vp, sz, vp, vp, i, vp, vp, vp]),
         "asym_kv_read_fp4": (i, [i, i, i, vp, vp, sz, vp, vp, i, vp, vp, vp, vp, vp]),
         "asym_attn_decode_paged_fp4": (i, [i] * 5 + [vp, vp, vp, sz, vp, vp, i, vp, vp, vp, f32, i, vp, sz, vp]),
@@ -1139,6 +1141,13 @@ def _workspace(nbytes, device):
     return torch.empty(nbytes, dtype=torch.uint8, device=device)
 
 
+@functools.lru_cache(maxsize=256)
+def _prefill_workspace(B, Hq, Hkv, Tq, Tk) -> int:
+    nbytes = ctypes.c_size_t()
+    _check(load_library().asym_attn_prefill_workspace(B, Hq, Hkv, Tq, Tk, ctypes.byref(nbytes)))
+    return nbytes.value
+
+
 def attn_prefill(q, k, v, cu_q, cu_k=None, o=None, lse=None, scale: Optional[float] = None, causal: bool = True,
                  mapping="aware", stream=None):
     """Attention of packed prompts (or chunks of them behind a prefix): q
@@ -1165,12 +1174,15 @@ def attn_prefill(q, k, v, cu_q, cu_k=None, o=None, lse=None, scale: Optional[flo
     device = _gpu_of("attn_prefill", q, k, v, cu_q, cu_k, *out)
     sc = _SCALE_128 if scale is None else float(scale)
     mp = MAPPINGS[mapping] if isinstance(mapping, str) else int(mapping)
+    nbytes = _prefill_workspace(cu_q.shape[0] - 1, Hq, Hkv, Tq, Tk)
 
     def call(raw):
         r = torch.empty((Tq, Hq, 128), dtype=torch.bfloat16, device=q.device) if o is None else o
+        ws = _workspace(nbytes, q.device) if nbytes else None
         _check(load_library().asym_attn_prefill_bf16(
             cu_q.shape[0] - 1, Hq, Hkv, 128, Tq, Tk, q.data_ptr(), qt, qh, k.data_ptr(), kt, kh, v.data_ptr(), vt, vh,
-            r.data_ptr(), lse_ptr, cu_q.data_ptr(), cu_k.data_ptr(), sc, 1 if causal else 0, mp, raw))
+            r.data_ptr(), lse_ptr, cu_q.data_ptr(), cu_k.data_ptr(), sc, 1 if causal else 0, mp,
+            ws.data_ptr() if nbytes else None, nbytes, raw))
         return r
     return _on(device, stream, call)
 

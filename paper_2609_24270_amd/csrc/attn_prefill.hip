@@ -32,6 +32,7 @@
 // one is needed, 1900: the vector work is not what bounds it.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cmath>
 
 #include "internal.h"
@@ -62,7 +63,8 @@ struct PrefillParams {
   const int *cu_q, *cu_k;
   int64_t q_tok, q_head, k_tok, k_head, v_tok, v_head;  // strides, values
   int B, Hq, Hkv, G, Tq, Tk;
-  int tiles;            // at least the number of tiles of all sequences
+  int tiles;            // at least the number of tiles (cut: of pieces) of all sequences
+  float* part;          // cut: [H_kv * tiles][kCutRows] of O [128], then of max and sum [2]
   int causal, aware;
   float c;              // |scale| * log2(e), positive
   float scale;          // |scale|
@@ -125,6 +127,83 @@ __device__ bool find_tile(const PrefillParams& p, int BM, int k, int& seq, int& 
       return true;
     }
     r -= cnt;
+  }
+  return false;
+}
+
+// Few rows over many keys: the tiles (kCutRows rows) are cut along their keys.  With W the
+// blocks of all tiles and heads, pieces of P blocks take the time of P blocks, and W / P of
+// them have to be written and joined: P = max(W / kPieces, sqrt(kJoinCost * W), kLeastBlocks).
+// A sequence that has at least two pieces' blocks is cut into n = ceil(its key blocks / P),
+// which divide each tile's own blocks evenly.  Pieces are numbered by sequence, tile and place.
+constexpr int kCutRows = 128;
+constexpr int kPieces = 512, kLeastBlocks = 4, kMostPieces = 128;
+constexpr float kJoinCost = 0.03f;  // blocks' time that a piece costs to join
+__host__ __device__ inline int least_blocks(float work) {
+  // (1.001: not less, whatever was rounded)
+  const float x = fmaxf(work * (1.001f / kPieces), sqrtf(kJoinCost * work));
+  return x < 1e9f ? (int)fmaxf(x, kLeastBlocks - 1) + 1 : 1000000000;
+}
+__host__ __device__ inline int pieces_of(int blocks, int least) {
+  if (blocks < 2 * least) return 1;
+  const int n = (blocks + least - 1) / least;
+  return n < kMostPieces ? n : kMostPieces;
+}
+struct Cut {
+  int nc, least;
+  int t0, nb0;  // of sequence `lane`
+};
+__device__ void cut_shape(const PrefillParams& p, int c, int& t, int& nb) {
+  const int b = 64 * c + (int)(threadIdx.x & 63);
+  t = nb = 0;
+  if (b < p.B) {
+    int qs, qn, ks, kn;
+    packed_rows(p.cu_q, b, p.Tq, qs, qn);
+    packed_rows(p.cu_k, b, p.Tk, ks, kn);
+    t = (int)(((int64_t)qn * p.G + kCutRows - 1) / kCutRows);
+    nb = (kn + PN - 1) / PN;
+  }
+}
+__device__ Cut cut_of(const PrefillParams& p) {
+  Cut cut;
+  cut.nc = (p.B + 63) >> 6;
+  cut_shape(p, 0, cut.t0, cut.nb0);
+  float work = 0.f;  // (a wave's sum of 16 + 16 bits: tiles are few, so that neither overflows)
+  for (int c = 0; c < cut.nc; ++c) {
+    int t = cut.t0, nb = cut.nb0;
+    if (c) cut_shape(p, c, t, nb);
+    work += 65536.f * (float)wave_sum(t * (nb >> 16)) + (float)wave_sum(t * (nb & 0xFFFF));
+  }
+  cut.least = least_blocks(work * (float)p.Hkv);
+  return cut;
+}
+// The k-th piece (tiles: the k-th tile): its sequence, tile, place among the tile's n
+// pieces, and the number of the tile's first piece.  One wave.
+template <bool TILES>
+__device__ bool find_piece(const PrefillParams& p, int k, int& seq, int& tile, int& place, int& n, int& first) {
+  const Cut cut = cut_of(p);
+  int before = 0;  // pieces of earlier sequences
+  for (int c = 0; c < cut.nc; ++c) {
+    int t = cut.t0, nb = cut.nb0;
+    if (c) cut_shape(p, c, t, nb);
+    const int each = pieces_of(nb, cut.least), mine = TILES ? t : t * each;
+    const int upto = wave_scan_add(mine);
+    int all = 0;
+    if (TILES) all = wave_scan_add(t * each);
+    const unsigned long long in = __ballot(k < upto);
+    if (in) {
+      const int l = __builtin_ctzll(in);
+      seq = 64 * c + l;
+      n = __builtin_amdgcn_readlane(each, l);
+      k -= __builtin_amdgcn_readlane(upto - mine, l);
+      tile = TILES ? k : k / n;
+      place = TILES ? 0 : k - tile * n;
+      first = before + (TILES ? __builtin_amdgcn_readlane(all - t * each, l) + tile * n
+                              : __builtin_amdgcn_readlane(upto - mine, l) + tile * n);
+      return true;
+    }
+    k -= __builtin_amdgcn_readlane(upto, 63);
+    before += __builtin_amdgcn_readlane(TILES ? all : upto, 63);
   }
   return false;
 }
@@ -200,9 +279,10 @@ __device__ __forceinline__ float over_quarters(float x, F f) {
   return f(__uint_as_float(sw[0]), __uint_as_float(sw[1]));
 }
 
-template <int NW>
+template <int NW, bool CUT>
 __global__ void __launch_bounds__(64 * NW, 2) attn_prefill_kernel(PrefillParams p) {
   constexpr int WR = 16 * NQ, BM = WR * NW;
+  static_assert(!CUT || BM == kCutRows);
   __shared__ __attribute__((aligned(1024))) unsigned char lds[4 * kTileBytes];  // two K tiles, two V tiles
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int n = lane & 15, q4 = lane >> 4;
@@ -226,7 +306,12 @@ __global__ void __launch_bounds__(64 * NW, 2) attn_prefill_kernel(PrefillParams 
     rank = blk / p.Hkv;
   }
   int seq, tile;
-  if (!find_tile(p, BM, rank, seq, tile)) return;
+  int place = 0, pieces = 1, first = 0;
+  if constexpr (CUT) {
+    if (rank >= p.tiles || !find_piece<false>(p, rank, seq, tile, place, pieces, first)) return;
+  } else {
+    if (!find_tile(p, BM, rank, seq, tile)) return;
+  }
   int qs, Lq, ks, Lk;
   packed_rows(p.cu_q, seq, p.Tq, qs, Lq);
   packed_rows(p.cu_k, seq, p.Tk, ks, Lk);
@@ -236,8 +321,14 @@ __global__ void __launch_bounds__(64 * NW, 2) attn_prefill_kernel(PrefillParams 
   // keys that a row sees; the most over the wave, the least and most over the workgroup
   auto limit = [&](int64_t r) { return p.causal ? max(off + (int)(min(r, rows - 1) / p.G) + 1, 0) : Lk; };
   const int lim_hi = __builtin_amdgcn_readfirstlane(limit(row0 + WR - 1));
-  const int nblk = (__builtin_amdgcn_readfirstlane(limit((int64_t)tile * BM + BM - 1)) + PN - 1) / PN;
-  const int nfull = __builtin_amdgcn_readfirstlane(limit((int64_t)tile * BM)) / PN;  // blocks that every row sees whole
+  int nblk = (__builtin_amdgcn_readfirstlane(limit((int64_t)tile * BM + BM - 1)) + PN - 1) / PN;
+  int nfull = __builtin_amdgcn_readfirstlane(limit((int64_t)tile * BM)) / PN;  // blocks that every row sees whole
+  int j0 = 0;
+  if (CUT) {
+    j0 = (int)((int64_t)nblk * place / pieces);
+    nblk = (int)((int64_t)nblk * (place + 1) / pieces);
+    nfull = min(max(nfull, j0), nblk);
+  }
 
   // this lane's rows, one of each block of 16 (rows past the last repeat it, and are not stored)
   bf16x8 qf[NQ][4];
@@ -356,11 +447,11 @@ __global__ void __launch_bounds__(64 * NW, 2) attn_prefill_kernel(PrefillParams 
   };
 
   // Blocks that every row sees whole.
-  if (nfull > 0) {
-    load_k(0);
-    load_v(0);
+  if (nfull > j0) {
+    load_k(j0);
+    load_v(j0);
   }
-  for (int j = 0; j < nfull; ++j) {
+  for (int j = j0; j < nfull; ++j) {
     arrived();
     if (j + 1 < nfull) {
       load_k(j + 1);
@@ -461,6 +552,23 @@ __global__ void __launch_bounds__(64 * NW, 2) attn_prefill_kernel(PrefillParams 
     if (mine) add_pv(j);
   }
 
+  if (CUT && pieces > 1) {  // the piece's unscaled output, max and sum (-1: it is empty) to the joining launch
+    const size_t slot = ((size_t)hk * p.tiles + first + place) * kCutRows;
+    float* po = p.part + slot * PD;
+    float* pm = p.part + (size_t)p.Hkv * p.tiles * kCutRows * PD + slot * 2;
+#pragma unroll
+    for (int b = 0; b < NQ; ++b) {
+      const int r = wave * WR + 16 * b + n;
+      const float lt = over_quarters(l[b], [](float a, float c) { return a + c; });
+      if ((int64_t)tile * BM + r >= rows) continue;
+      if (q4 == 0) *reinterpret_cast<float2*>(pm + 2 * r) = float2{m[b], j0 < nblk ? lt : -1.f};
+      if (j0 < nblk) {
+#pragma unroll
+        for (int g = 0; g < 8; ++g) *reinterpret_cast<f32x4*>(po + (size_t)r * PD + 16 * g + 4 * q4) = o[b][g];
+      }
+    }
+    return;
+  }
   // a lane has 4 of every 16 channels of a row; two groups of them, exchanged between the
   // quarters, make 16 bytes
 #pragma unroll
@@ -490,13 +598,111 @@ __global__ void __launch_bounds__(64 * NW, 2) attn_prefill_kernel(PrefillParams 
   }
 }
 
+// Joins the pieces of the tiles that were cut, in order: a wave has four rows of a tile,
+// a lane eight channels of one.
+constexpr int kJoinRows = 16, kJoinWaves = 4;
+__global__ void __launch_bounds__(64 * kJoinWaves) attn_prefill_join_kernel(PrefillParams p) {
+  constexpr int kParts = kCutRows / kJoinRows;
+  const int hk = (blockIdx.x / kParts) % p.Hkv, rank = blockIdx.x / kParts / p.Hkv;
+  int seq, tile, place, pieces, first;
+  if (!find_piece<true>(p, rank, seq, tile, place, pieces, first)) return;
+  if (pieces == 1 || first + pieces > p.tiles) return;
+  int qs, Lq;
+  packed_rows(p.cu_q, seq, p.Tq, qs, Lq);
+  const int64_t rows = (int64_t)Lq * p.G;
+  const int c = threadIdx.x & 15, r = (int)(blockIdx.x % kParts) * kJoinRows + (int)(threadIdx.x >> 4);
+  const int64_t row = (int64_t)tile * kCutRows + r;
+  if (row >= rows) return;  // (a row's 16 lanes leave together)
+  const size_t slot = ((size_t)hk * p.tiles + first) * kCutRows + r;
+  const float* po = p.part + slot * PD + 8 * c;
+  const float* pm = p.part + (size_t)p.Hkv * p.tiles * kCutRows * PD + slot * 2;
+  float top = -INFINITY;
+  for (int s = c; s < pieces; s += 16) {
+    const float2 x = *reinterpret_cast<const float2*>(pm + (size_t)s * kCutRows * 2);
+    if (!(x.y < 0.f)) top = fmaxf(top, x.x);
+  }
+#pragma unroll
+  for (int d = 1; d < 16; d *= 2) top = fmaxf(top, __shfl_xor(top, d));
+  const float at = top == -INFINITY ? 0.f : top;
+  float lt = 0.f;
+  f32x4 acc[2] = {};
+#pragma unroll 4
+  for (int s = 0; s < pieces; ++s) {
+    const float2 x = *reinterpret_cast<const float2*>(pm + (size_t)s * kCutRows * 2);
+    const f32x4* y = reinterpret_cast<const f32x4*>(po + (size_t)s * kCutRows * PD);
+    const f32x4 y0 = y[0], y1 = y[1];
+    const bool on = !(x.y < 0.f);  // (an empty piece has no output)
+    const float w = __builtin_amdgcn_exp2f((x.x - at) * p.c);
+    lt += on ? x.y * w : 0.f;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      acc[0][e] += on ? y0[e] * w : 0.f;
+      acc[1][e] += on ? y1[e] * w : 0.f;
+    }
+  }
+  const float inv = lt > 0.f ? 1.f / lt : (lt == 0.f ? 0.f : lt);  // (NaN stays)
+  const int tok = (int)(row / p.G);
+  const int64_t orow = (int64_t)(qs + tok) * p.Hq + (int64_t)hk * p.G + (row - (int64_t)tok * p.G);
+  u32x4 out;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const f32x4& a = acc[e >> 1];
+    const bf16x2 y = {(__bf16)(a[2 * (e & 1)] * inv), (__bf16)(a[2 * (e & 1) + 1] * inv)};
+    out[e] = __builtin_bit_cast(uint32_t, y);
+  }
+  *reinterpret_cast<u32x4*>(p.o + orow * PD + 8 * c) = out;
+  if (p.lse && c == 0) p.lse[orow] = lt == 0.f ? -INFINITY : top * p.scale + __logf(lt);
+}
+
+// Which form a call takes, from its sizes alone.
+struct Form {
+  bool wide, cut;
+  int64_t tiles;  // of a head, at least (cut: pieces)
+  int64_t whole;  // cut: tiles of a head, at least
+};
+Form form_of(int B, int Hq, int Hkv, int Tq, int Tk) {
+  const int G = Hq / Hkv;
+  auto count = [&](int rows) { return (int64_t)Tq * G / rows + B; };  // sequences end in a part tile each
+  Form f = {};
+  // Tiles of 256 rows read the keys half as often and are faster once the rows fill two
+  // for every CU (us, 128 rows first: 16384 tokens, 32 / 8 heads 1958 1908, 4096 tokens
+  // 142 132, two of 4096 with 16 / 16 heads 147 136); with fewer the last ones are waited
+  // for (2048 tokens, 32 / 8 heads 51 61, 3000 behind 8000 436 479, 1024 26 34), and
+  // sequences of few rows fill them badly (100 of 8 tokens behind 1000 100 155).
+  f.wide = (int64_t)Tq * G / 256 * Hkv >= 512;
+  f.tiles = f.whole = count(f.wide ? 256 : kCutRows);
+  if (!f.wide && f.tiles * Hkv < 512) {
+    // Cut (us, whole tiles first; 32 / 8 heads): 8 tokens behind 1000 keys 24 14, 4 behind
+    // 4000 76 16, 256 behind 16125 298 92, 4 behind 32000 and 39 times 4 behind 300 569 49.
+    // It costs a launch (12 of 100 behind 700, which it would leave whole: 33 37).
+    const int blocks = Tk / PN / B;  // of the mean sequence; a long batch may hold a long one
+    f.cut = Tk >= 8192 || pieces_of(blocks, least_blocks((float)(f.tiles * Hkv) * (float)blocks)) > 1;
+    if (f.cut) f.tiles += (kPieces + Hkv - 1) / Hkv;
+  }
+  return f;
+}
+size_t part_bytes(const Form& f, int Hkv) {
+  return f.cut ? (size_t)Hkv * (size_t)f.tiles * kCutRows * (PD + 2) * sizeof(float) : 0;
+}
+
 }  // namespace
 }  // namespace asym
+
+extern "C" int asym_attn_prefill_workspace(int B, int H_q, int H_kv, int T_q, int T_k, size_t* bytes) {
+  using namespace asym;
+  if (B < 0 || T_q < 0 || T_k < 0 || H_q < 1 || H_kv < 1)
+    return fail(ASYM_EINVAL, "prefill: B, T_q and T_k must be >= 0, H_q and H_kv >= 1");
+  if (H_q % H_kv) return fail(ASYM_EINVAL, "prefill: H_kv must divide H_q");
+  if (!bytes) return fail(ASYM_EINVAL, "prefill: null pointer");
+  *bytes = B == 0 || T_q == 0 ? 0 : part_bytes(form_of(B, H_q, H_kv, T_q, T_k), H_kv);
+  return ASYM_OK;
+}
 
 extern "C" int asym_attn_prefill_bf16(int B, int H_q, int H_kv, int D, int T_q, int T_k, const void* q, int64_t q_token,
                                       int64_t q_head, const void* k, int64_t k_token, int64_t k_head, const void* v,
                                       int64_t v_token, int64_t v_head, void* o, float* lse, const int32_t* cu_q,
-                                      const int32_t* cu_k, float scale, int causal, int mapping, void* stream) {
+                                      const int32_t* cu_k, float scale, int causal, int mapping, void* workspace,
+                                      size_t workspace_bytes, void* stream) {
   using namespace asym;
   if (B < 0 || T_q < 0 || T_k < 0 || H_q < 1 || H_kv < 1)
     return fail(ASYM_EINVAL, "prefill: B, T_q and T_k must be >= 0, H_q and H_kv >= 1");
@@ -516,7 +722,7 @@ extern "C" int asym_attn_prefill_bf16(int B, int H_q, int H_kv, int D, int T_q, 
   // (64 rows of a block are addressed with 32-bit offsets; a row past a sequence's last must lie past its end)
   for (int64_t s : {k_token, v_token})
     if (s < PD || s > (1 << 23)) return fail(ASYM_EUNSUPPORTED, "prefill: K and V token strides must be in [128, 2^23] values");
-  PrefillParams p;
+  PrefillParams p = {};
   p.q = static_cast<const uint16_t*>(q);
   p.k = static_cast<const uint16_t*>(k);
   p.v = static_cast<const uint16_t*>(v);
@@ -535,13 +741,10 @@ extern "C" int asym_attn_prefill_bf16(int B, int H_q, int H_kv, int D, int T_q, 
   // score (minus infinity) to minus infinity
   p.c = std::fmax(p.scale * 1.4426950408889634f, 1.17549435e-38f);
   p.q_flip = scale < 0 ? 0x80008000u : 0u;
-  // Tiles of 256 rows read the keys half as often and are faster once there is one for
-  // every CU (us, 128 rows first: 16384 tokens, 32 / 8 heads 1958 1908, 4096 tokens 146 134,
-  // two of 4096 with 16 / 16 heads 147 136; eight chunks of 1000 tokens behind
-  // prefixes 316 321); with fewer, CUs would idle (1024 tokens, 32 / 8 heads 26 34).
-  auto count = [&](int rows) { return (int64_t)T_q * p.G / rows + B; };  // sequences end in a part tile each
-  const bool wide = count(256) * H_kv >= 256;
-  const int64_t tiles = count(wide ? 256 : 128);
+  const Form form = form_of(B, H_q, H_kv, T_q, T_k);
+  if (form.cut && (!workspace || ((uintptr_t)workspace & 15u) || workspace_bytes < part_bytes(form, H_kv)))
+    return fail(ASYM_EINVAL, "prefill: workspace null, misaligned or too small");
+  const int64_t tiles = form.tiles;
   int64_t grid = tiles * H_kv;
   if (p.aware && kXcds % H_kv == 0) {
     const int share = kXcds / H_kv;
@@ -551,10 +754,17 @@ extern "C" int asym_attn_prefill_bf16(int B, int H_q, int H_kv, int D, int T_q, 
     return fail(ASYM_EUNSUPPORTED, "prefill: too many rows");
   p.tiles = (int)tiles;
   hipStream_t s = static_cast<hipStream_t>(stream);
-  if (wide)
-    hipLaunchKernelGGL((attn_prefill_kernel<8>), dim3((unsigned)grid), dim3(512), 0, s, p);
-  else
-    hipLaunchKernelGGL((attn_prefill_kernel<4>), dim3((unsigned)grid), dim3(256), 0, s, p);
+  if (form.cut) {
+    p.part = static_cast<float*>(workspace);
+    hipLaunchKernelGGL((attn_prefill_kernel<4, true>), dim3((unsigned)grid), dim3(256), 0, s, p);
+    ASYM_HIP(hipGetLastError());
+    const int64_t rows = form.whole * H_kv * (kCutRows / kJoinRows);
+    hipLaunchKernelGGL(attn_prefill_join_kernel, dim3((unsigned)rows), dim3(64 * kJoinWaves), 0, s, p);
+  } else if (form.wide) {
+    hipLaunchKernelGGL((attn_prefill_kernel<8, false>), dim3((unsigned)grid), dim3(512), 0, s, p);
+  } else {
+    hipLaunchKernelGGL((attn_prefill_kernel<4, false>), dim3((unsigned)grid), dim3(256), 0, s, p);
+  }
   ASYM_HIP(hipGetLastError());
   return ASYM_OK;
 }

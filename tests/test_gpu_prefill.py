@@ -252,3 +252,67 @@ def test_refusals(dev):
     big = torch.zeros(8 * 4 * 128 + 1, dtype=torch.bfloat16, device=dev)
     with pytest.raises(asym.AsymError):  # 2-byte aligned
         asym.attn_prefill(big[1:].view(8, 4, 128), k, v, cu)
+
+
+# Few rows over many keys: tiles cut along the keys and joined.  Joining adds to the bound of
+# the sums (module docstring) two roundings for each piece's weight and product, an exponential
+# (8) and one addition a piece: fewer than the keys that the bound counts.
+CUT = [  # query lengths, key lengths, H_q, H_kv
+    ([1], [700], 4, 1), ([3], [2500], 32, 8), ([40, 1, 9], [600, 2000, 9], 8, 2), ([2], [20000], 2, 1),
+    ([1, 0, 2, 1], [513, 700, 0, 64], 5, 5), ([130], [1000], 3, 1), ([300], [300], 4, 2), ([700, 2], [40, 900], 2, 2),
+    ([5] * 30, [90] * 29 + [1500], 4, 4), ([1] * 70, [11] * 70, 4, 2), ([2] * 70, [11] * 66 + [900, 5, 700, 1], 2, 1)]
+
+
+@pytest.mark.parametrize("lq,lk,Hq,Hkv", CUT)
+@pytest.mark.parametrize("causal", [True, False])
+def test_few_rows_over_many_keys(dev, lq, lk, Hq, Hkv, causal):
+    cu_q, cu_k = offsets(lq), offsets(lk)
+    Tk = max(cu_k[-1], 8192)  # (rows behind the last sequence: any batch with room for a long one may be cut)
+    assert asym._prefill_workspace(len(lq), Hq, Hkv, cu_q[-1], Tk) > 0
+    q, k, v = inputs(dev, cu_q[-1], Tk, Hq, Hkv, seed=sum(lk) + Hq)
+    lse = torch.empty((q.shape[0], Hq), device=dev)
+    o = asym.attn_prefill(q, k, v, i32(cu_q, dev), i32(cu_k, dev), lse=lse, causal=causal)
+    check(q, k, v, cu_q, cu_k, SCALE, causal, o, lse)
+    for mapping in ("oblivious_grouped", "oblivious_rowmajor"):
+        assert torch.equal(o, asym.attn_prefill(q, k, v, i32(cu_q, dev), i32(cu_k, dev), causal=causal, mapping=mapping))
+
+
+def test_cut_rows_outside_are_left_and_unseen_values_do_not_reach(dev):
+    cu_q, cu_k = offsets([5, 0, 9], first=2), offsets([800, 3, 1500], first=7)
+    q, k, v = inputs(dev, 30, 2400, 8, 2, seed=4)
+    o = torch.full((30, 8, 128), 7.0, dtype=torch.bfloat16, device=dev)
+    lse = torch.full((30, 8), 7.0, device=dev)
+    asym.attn_prefill(q, k, v, i32(cu_q, dev), i32(cu_k, dev), o=o, lse=lse)
+    assert torch.all(o[:2] == 7) and torch.all(o[16:] == 7) and torch.all(lse[:2] == 7) and torch.all(lse[16:] == 7)
+    # the last key of a sequence is seen by its last token alone
+    k2, v2 = k.clone(), v.clone()
+    for bad in (float("nan"), float("inf")):
+        k2[:7] = v2[:7] = k2[2310:] = v2[2310:] = bad
+        v2[806, 1, 3] = v2[2309, 0, 9] = bad
+        got = asym.attn_prefill(q, k2, v2, i32(cu_q, dev), i32(cu_k, dev), o=torch.full_like(o, 7.0))
+        hit = torch.zeros_like(o, dtype=torch.bool)
+        hit[6, 4:, 3] = hit[15, :4, 9] = True
+        assert torch.equal(got[~hit], o[~hit])
+        assert not torch.any(torch.isfinite(got[hit].float()))
+
+
+def test_cut_call_captured(dev):
+    cu_q, cu_k = i32(offsets([4, 2]), dev), i32(offsets([900, 1700]), dev)
+    q, k, v = inputs(dev, 6, 2600, 8, 2, seed=9)
+    want = [asym.attn_prefill(q * s, k, v, cu_q, cu_k) for s in (1, -1, 2)]
+    held, o1, o2 = q.clone(), torch.empty_like(q), torch.empty_like(q)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        asym.attn_prefill(held, k, v, cu_q, cu_k, o=o1)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        asym.attn_prefill(held, k, v, cu_q, cu_k, o=o1)
+        asym.attn_prefill(-held, k, v, cu_q, cu_k, o=o2)
+    for s, w in zip((1, -1, 2), want):
+        held.copy_(q * s)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(o1, w)
+        assert torch.equal(o2, asym.attn_prefill(q * -s, k, v, cu_q, cu_k))

@@ -112,7 +112,7 @@ def code(name, *args):
 
 
 PREFILL = dict(B=1, Hq=4, Hkv=2, D=128, Tq=8, Tk=8, q=P, qt=512, qh=128, k=P, kt=256, kh=128, v=P, vt=256, vh=128, o=P,
-               lse=None, cu_q=P, cu_k=P, scale=1.0, causal=1, mapping=0, stream=None)
+               lse=None, cu_q=P, cu_k=P, scale=1.0, causal=1, mapping=0, ws=None, ws_bytes=0, stream=None)
 
 
 @pytest.mark.parametrize("change,want", [
@@ -121,10 +121,25 @@ PREFILL = dict(B=1, Hq=4, Hkv=2, D=128, Tq=8, Tk=8, q=P, qt=512, qh=128, k=P, kt
     (dict(q=None), asym.EINVAL), (dict(k=None), asym.EINVAL), (dict(o=None), asym.EINVAL), (dict(cu_q=None), asym.EINVAL),
     (dict(q=P + 2), asym.EINVAL), (dict(o=P + 8), asym.EINVAL), (dict(lse=P + 2), asym.EINVAL), (dict(cu_k=P + 1), asym.EINVAL),
     (dict(qt=516), asym.EINVAL), (dict(kh=-128), asym.EINVAL), (dict(kt=0), asym.EUNSUPPORTED), (dict(vt=120), asym.EUNSUPPORTED),
-    (dict(kt=1 << 24), asym.EUNSUPPORTED), (dict(Tq=2 ** 31 - 1, Hq=512, Hkv=8), asym.EUNSUPPORTED)])
+    (dict(kt=1 << 24), asym.EUNSUPPORTED), (dict(Tq=2 ** 31 - 1, Hq=512, Hkv=8), asym.EUNSUPPORTED),
+    (dict(Tk=4096), asym.EINVAL), (dict(Tk=4096, ws=P, ws_bytes=4096), asym.EINVAL),
+    (dict(Tk=4096, ws=P + 8, ws_bytes=1 << 30), asym.EINVAL)])
 def test_prefill_refusals(change, want):
     assert code("asym_attn_prefill_bf16", *{**PREFILL, **change}.values()) == want
     assert asym.last_error().startswith("prefill: ")
+
+
+def test_prefill_workspace():
+    import ctypes
+    n = ctypes.c_size_t(7)
+    sizes = lambda *a: (code("asym_attn_prefill_workspace", *a, ctypes.byref(n)), n.value)
+    # a piece is 128 rows of 130 values; few rows over many keys are cut, everything else is not
+    assert sizes(1, 4, 2, 8, 4096) == (asym.OK, (1 + 512 // 2) * 2 * 128 * 130 * 4)
+    assert sizes(1, 4, 2, 8, 8) == sizes(64, 32, 8, 64, 1 << 20) == sizes(1, 32, 8, 16384, 16384) == (asym.OK, 0)
+    assert sizes(0, 4, 2, 8, 4096) == sizes(1, 4, 2, 0, 4096) == (asym.OK, 0)
+    for bad in ((-1, 4, 2, 8, 8), (1, 5, 2, 8, 8), (1, 4, 0, 8, 8), (1, 4, 2, -1, 8), (1, 4, 2, 8, -1)):
+        assert sizes(*bad)[0] == asym.EINVAL
+    assert code("asym_attn_prefill_workspace", 1, 4, 2, 8, 8, None) == asym.EINVAL
 
 
 def test_empty_calls_do_nothing():
