@@ -1010,7 +1010,7 @@ int asym_attn_decode_paged_fp4_plan(int B, int H_q, int H_kv, int S_max, int D, 
  * entries of each head.  A cache whose keys and values share a table has one
  * state and two pools; with a table each it has two states.  Requests of a call
  * (n, device int32 arrays) that name a row outside [0, R), or one that an earlier
- * request of the call names (as a target), are left out.
+ * request of the call names (as a target), are left out.  A table has less than 2^31 entries.
  * status (device int32 [2], nullable): see each call.  Results do not depend on
  * timing.  No host synchronisation; may be captured; asynchronous.  The workspace
  * (asym_kv_pages_workspace bytes, 16-byte aligned) must not be shared by calls that

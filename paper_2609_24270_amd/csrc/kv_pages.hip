@@ -412,6 +412,9 @@ int pages_setup(const char* what, int op, int R, int H, int pph, int32_t* table,
   const std::string w(what);
   if (R < 1 || H < 1 || pph < 1 || n < 0) return fail(ASYM_EINVAL, w + ": R, H and pages_per_head must be >= 1, n >= 0");
   if (pph > (1 << 25)) return fail(ASYM_EUNSUPPORTED, w + ": more than 2^30 tokens a row");
+  // (entries, and with them the pages that a call may need, are counted in 32 bits)
+  if ((int64_t)H * pph > 0x7FFFFFFF || (int64_t)H * pph * R > 0x7FFFFFFF)
+    return fail(ASYM_EUNSUPPORTED, w + ": the table has 2^31 entries or more");
   if (pool_pages < 1 || pool_pages > 0x7FFFFFFFu) return fail(ASYM_EINVAL, w + ": pool_pages must be in [1, 2^31)");
   if ((int64_t)n * H >= (1 << 24))  // (threads of a launch are counted in 32 bits)
     return fail(ASYM_EUNSUPPORTED, w + ": too many requests");

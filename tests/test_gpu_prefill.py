@@ -296,6 +296,15 @@ def test_cut_rows_outside_are_left_and_unseen_values_do_not_reach(dev):
         assert not torch.any(torch.isfinite(got[hit].float()))
 
 
+@pytest.mark.parametrize("Hkv", [1, 4])
+def test_no_keys_at_all(dev, Hkv):
+    q = torch.randn((5, 8, 128), device=dev).to(torch.bfloat16)
+    kv = torch.empty((0, Hkv, 128), dtype=torch.bfloat16, device=dev)
+    lse = torch.empty((5, 8), device=dev)
+    o = asym.attn_prefill(q, kv, kv, i32([0, 5], dev), i32([0, 0], dev), lse=lse)
+    assert torch.all(o == 0) and torch.all(lse == -float("inf"))
+
+
 def test_cut_call_captured(dev):
     cu_q, cu_k = i32(offsets([4, 2]), dev), i32(offsets([900, 1700]), dev)
     q, k, v = inputs(dev, 6, 2600, 8, 2, seed=9)

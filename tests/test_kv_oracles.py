@@ -222,7 +222,8 @@ def test_pages_refusals():
     ext = dict(R=4, H=2, pph=3, table=P, lens=P, refs=P, pool=100, n=5, rows=P, new=P, status=P, ws=P, wsb=big, stream=None)
     for change, want in [(dict(R=0), -1), (dict(n=-1), -1), (dict(table=None), -1), (dict(lens=P + 2), -1), (dict(rows=None), -1),
                          (dict(new=P + 1), -1), (dict(status=P + 2), -1), (dict(ws=None), -1), (dict(wsb=100), -1),
-                         (dict(ws=P + 4), -1), (dict(pool=0), -1), (dict(pph=1 << 26), -3), (dict(n=1 << 24), -3)]:
+                         (dict(ws=P + 4), -1), (dict(pool=0), -1), (dict(pph=1 << 26), -3), (dict(n=1 << 24), -3),
+                         (dict(R=1 << 10, H=1 << 6, pph=1 << 15), -3), (dict(R=2, H=1 << 16, pph=1 << 20), -3)]:
         assert lib.asym_kv_extend(*{**ext, **change}.values()) == want, change
     fork = dict(R=4, H=2, pph=3, table=P, lens=P, refs=P, kp=P, vp=P + 64, page=2176, pool=100, n=5, src=P, dst=P, status=None,
                 ws=P, wsb=big, stream=None)
