@@ -6,8 +6,9 @@
 // The pages of the batch, request by request and head by head, are one list, cut into equal
 // shares, one a wave, whatever the requests' lengths (which only the device knows): a grid
 // of (request, head, split) tasks left waves idle behind the short ones (64 requests of up to
-// 32768 tokens, 1.42 GB: 319 us, in shares 229, 6.2 TB/s).  A wave walks its share; for each (request, key/value head) that it meets it serves the G <= 16
-// query heads that read that head, 32 tokens (a page) at a time:
+// 32768 tokens, 1.41 GB: 319 us, in shares 226, 6.2 TB/s: HBM's rate for reads).  A wave walks
+// its share; for each (request, key/value head) that it meets it serves the G <= 16 query
+// heads that read that head, 32 tokens (a page) at a time:
 //   scores   two v_mfma_scale_f32_16x16x128_f8f6f4 a 16 tokens: the page's codes and scales
 //            are the operand as they lie, with no conversion at all.  The other operand
 //            takes 8 bits at most, so q, whose bf16 has 8 significant bits, goes in as

@@ -23,7 +23,7 @@
 // Scores, max, sum and output are fp32.
 //
 // What bounds it: the matrix cores, at the clock they are left.  16384 causal tokens, 32
-// query and 8 key heads, take 1910 us, 1150 TFLOP/s.  Over that time the clock is 2.1 GHz,
+// query and 8 key heads, take 1870 to 1910 us, 1150 to 1180 TFLOP/s.  Over that time the clock is 2.1 GHz,
 // the matrix cores work in 51 % of the cycles, the vector units (softmax) in 45 %, LDS
 // reads in 25 % and without conflicts: what remains is the overlap of the first two,
 // which two waves a SIMD reach in part.  Blocks of 32 rows (v_mfma_f32_32x32x16_bf16)

@@ -367,9 +367,10 @@ __global__ void __launch_bounds__(kThreads) pages_move(PagesParams p) {
     p.refs[from] = 0;
   }
   // The pages' words as one list, kMoveWords * kThreads a workgroup at a time, so that small
-  // pages fill it as well as large ones.  256 rows, 36000 pairs of 8 KiB pages moved, 1.07 GB: 271
-  // us with a workgroup a pair in 4096 workgroups, 257 to 280 with eight words a thread,
-  // 238 (4.5 TB/s; a plain copy 5.0) with four, non-temporal, a workgroup to almost every pair.
+  // pages fill it as well as large ones.  256 rows, 42734 pairs of 8 KiB pages moved, 1.40 GB:
+  // 271 us with a workgroup a pair in 4096 workgroups, 257 to 280 with eight words a thread,
+  // 238 (5.9 TB/s; a plain copy of 2 GiB 5.0) with four, non-temporal, a workgroup to almost
+  // every pair.
   const uint32_t all = (uint32_t)(p.page_bytes / 16) * (p.v_pool ? 2 : 1);
   const int64_t words = (int64_t)holes * all;
   for (int64_t c = (int64_t)blockIdx.x * (kMoveWords * kThreads); c < words; c += (int64_t)gridDim.x * (kMoveWords * kThreads)) {
