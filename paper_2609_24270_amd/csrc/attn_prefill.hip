@@ -22,15 +22,17 @@
 //                   transposes 16-bit values on the way from LDS.
 // Scores, max, sum and output are fp32.
 //
-// What bounds it: the clock that the power cap leaves, and the matrix cores at it.  16384 causal tokens, 32
-// query and 8 key heads, take 1870 to 1910 us, 1150 to 1180 TFLOP/s.  Over that time the clock is 2.1 of 2.4 GHz;
-// the matrix cores work in 51 % of the cycles, the vector units (softmax) in 45 %, LDS
-// reads in 25 % and without conflicts.  Fewer cycles give little time: with the next
-// block's scores computed beside this block's softmax, and a maximum only where a block's
-// sum asks for one, the launch took 15 % fewer of them, at 1.9 GHz, and 1 to 3 % less time
-// (and more with as many key as query heads), for registers that spill.  Matrix products
-// of 32 rows took 1990 us; 48 rows a wave 2620 (spills); two groups of waves in turn on
-// products and softmax 1950 to 2280.
+// What bounds it: the clock that the power cap leaves, and the matrix cores at it.  16384
+// causal tokens, 32 query and 8 key heads, take 1870 to 1910 us, 1150 to 1180 TFLOP/s.  The
+// clock is 2.1 of 2.4 GHz; the matrix cores work in 51 % of the cycles, the vector units
+// (softmax) in 45 %, LDS reads in 25 % and without conflicts.  Fewer cycles give little
+// time: with the next block's scores computed beside this block's softmax, and a maximum
+// only where a block's sum asks for one, the launch took 15 % fewer of them, at 1.9 GHz, and
+// 1 to 3 % less time (and more with as many key as query heads), for registers that
+// spill.  Matrix products of 32 rows took 1990 us; 48 rows a wave 2620 (spills); two
+// groups of waves in turn on products and softmax 1950 to 2280.
+#include <hip/hip_runtime.h>
+
 #include <algorithm>
 #include <cmath>
 
