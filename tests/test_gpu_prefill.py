@@ -296,6 +296,26 @@ def test_cut_rows_outside_are_left_and_unseen_values_do_not_reach(dev):
         assert not torch.any(torch.isfinite(got[hit].float()))
 
 
+def test_cut_call_on_a_library_stream(dev):
+    cu_q, cu_k = i32(offsets([4, 2]), dev), i32(offsets([900, 1700]), dev)
+    q, k, v = inputs(dev, 6, 2600, 8, 2, seed=9)
+    ref = asym.attn_prefill(q, k, v, cu_q, cu_k)
+    torch.cuda.synchronize()
+    s = asym.stream_create()
+    outs = [asym.attn_prefill(q, k, v, cu_q, cu_k, stream=s) for _ in range(3)]
+    here = [asym.attn_prefill(q, k, v, cu_q, cu_k) for _ in range(3)]  # beside them, on torch's own
+    s.synchronize()
+    torch.cuda.synchronize()
+    assert all(torch.equal(o, ref) for o in outs + here)
+    asym.stream_destroy(s)
+
+
+def test_cut_offsets_that_say_too_much_are_held(dev):
+    q, k, v = inputs(dev, 6, 9000, 8, 2, seed=2)
+    want = asym.attn_prefill(q, k, v, i32([0, 6], dev), i32([0, 9000], dev))
+    assert torch.equal(want, asym.attn_prefill(q, k, v, i32([-5, 100000], dev), i32([-7, 2 ** 31 - 1], dev)))
+
+
 @pytest.mark.parametrize("Hkv", [1, 4])
 def test_no_keys_at_all(dev, Hkv):
     q = torch.randn((5, 8, 128), device=dev).to(torch.bfloat16)
