@@ -220,10 +220,11 @@ __device__ __forceinline__ i32x4 tile_rsrc(const uint16_t* base, int64_t tok, in
   return r;
 }
 
-// 1 KiB from lane addresses voff to LDS bytes dst .. dst + 1023, in lane order
+// 1 KiB from lane addresses voff to LDS bytes dst .. dst + 1023, in lane order (the load takes
+// dst from M0, whose write needs a wait state before it, which the compiler does not add here)
 __device__ __forceinline__ void lds_load_1k(uint32_t dst, i32x4 rs, uint32_t voff) {
-  asm volatile("s_mov_b32 m0, %0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(dst), "v"(voff), "s"(rs)
-               : "memory");
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(dst), "v"(voff), "s"(rs)
+               : "memory", "m0");
 }
 
 // 16-byte chunk c of a tile's row r lies at chunk c ^ swz(r): the rows that one read
