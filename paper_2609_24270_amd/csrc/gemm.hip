@@ -161,10 +161,12 @@ __device__ __forceinline__ i32x4 rsrc_words(const void* base, uint32_t bytes) {
 // `row` (the row block's byte offset) and `kb` (the stage's k byte offset)
 // are added in the scalar unit inside the asm, so no part of the address
 // passes through vector registers.  The add writes SCC, which the compiler
-// must not keep a value in across the asm (declared clobbered), and M0.
+// must not keep a value in across the asm (declared clobbered, as M0 is); it
+// stands between the write of M0 and the load that reads it, which need a
+// wait state between them.
 __device__ __forceinline__ void dma_1k(uint32_t lds_dst, i32x4 rs, uint32_t vo, int row, int kb) {
   int so;
-  asm volatile("s_add_u32 %0, %1, %2\n\ts_mov_b32 m0, %3\n\tbuffer_load_dwordx4 %4, %5, %0 offen lds"
+  asm volatile("s_mov_b32 m0, %3\n\ts_add_u32 %0, %1, %2\n\tbuffer_load_dwordx4 %4, %5, %0 offen lds"
                : "=&s"(so)
                : "s"(row), "s"(kb), "s"(lds_dst), "v"(vo), "s"(rs)
                : "memory", "scc", "m0");

@@ -13,7 +13,7 @@ import pytest
 
 from tests.test_kernel_structure import CSRC, asm_of
 
-SOURCES = ["attn_prefill.hip", "gemm_skinny.hip", "mla_decode.hip"]
+SOURCES = ["attn_prefill.hip", "gemm.hip", "gemm_skinny.hip", "mla_decode.hip"]
 
 
 def instructions(asm: str):
