@@ -1136,6 +1136,13 @@ def _outputs(o, lse, shape, o_shape):
     return lse.data_ptr(), (lse,) if o is None else (o, lse)
 
 
+@functools.lru_cache(maxsize=256)
+def _sizes(*sizes) -> None:
+    """Refuses sizes that the library's 32-bit arguments would cut off."""
+    if max(sizes) >= 1 << 31 or min(sizes) < -(1 << 31):
+        raise ValueError("sizes of 2^31 and more are not supported")
+
+
 def _workspace(nbytes, device):
     import torch
     return torch.empty(nbytes, dtype=torch.uint8, device=device)
@@ -1143,6 +1150,7 @@ def _workspace(nbytes, device):
 
 @functools.lru_cache(maxsize=256)
 def _prefill_workspace(B, Hq, Hkv, Tq, Tk) -> int:
+    _sizes(B, Hq, Hkv, Tq, Tk)
     nbytes = ctypes.c_size_t()
     _check(load_library().asym_attn_prefill_workspace(B, Hq, Hkv, Tq, Tk, ctypes.byref(nbytes)))
     return nbytes.value
@@ -1215,6 +1223,7 @@ def kv_write_fp4(k, v, k_pool, v_pool, k_pages, v_pages, cu, start, stream=None)
     B, Hkv, pph = _fp4_cache(k_pool, v_pool, k_pages, v_pages)
     if vT != T or vH != H or H != Hkv:
         raise ValueError("k and v must be [T, H_kv, 128], H_kv as in the tables")
+    _sizes(B, H, pph, T)
     _index(cu, "cu", (B + 1,))
     _index(start, "start", (B,))
     device = _gpu_of("kv_write_fp4", k, v, k_pool, v_pool, k_pages, v_pages, cu, start)
@@ -1235,6 +1244,7 @@ def kv_read_fp4(k_pool, v_pool, k_pages, v_pages, cu, start, k, v, stream=None):
     if len(shape) != 3 or shape[1] != H or shape[2] != 128 or v.shape != shape or not k.is_contiguous() \
             or not v.is_contiguous():
         raise ValueError("k and v must be contiguous [T, H_kv, 128]")
+    _sizes(B, H, pph, shape[0])
     _index(cu, "cu", (B + 1,))
     _index(start, "start", (B,))
     device = _gpu_of("kv_read_fp4", k, v, k_pool, v_pool, k_pages, v_pages, cu, start)
@@ -1247,9 +1257,7 @@ def kv_read_fp4(k_pool, v_pool, k_pages, v_pages, cu, start, k, v, stream=None):
 @functools.lru_cache(maxsize=256)
 def _fp4_plan_workspace(B, Hq, Hkv, S, split_tokens) -> int:
     """The plan's workspace bytes (a function of the sizes alone)."""
-    plan = AttnPlanInfo()
-    _check(load_library().asym_attn_decode_paged_fp4_plan(B, Hq, Hkv, S, 128, split_tokens, ctypes.byref(plan)))
-    return plan.workspace_bytes
+    return attn_decode_paged_fp4_plan(B, Hq, Hkv, S, 128, split_tokens)["workspace_bytes"]
 
 
 def attn_decode_paged_fp4(q, k_pool, v_pool, k_pages, v_pages, lens, S: Optional[int] = None, o=None, lse=None,
@@ -1274,6 +1282,7 @@ def attn_decode_paged_fp4(q, k_pool, v_pool, k_pages, v_pages, lens, S: Optional
     lse_ptr, out = _outputs(o, lse, shape, "[B, H_q, 128]")
     device = _gpu_of("attn_decode_paged_fp4", q, k_pool, v_pool, k_pages, v_pages, lens, *out)
     sc = _SCALE_128 if scale is None else float(scale)
+    _sizes(pph)
     nbytes = _fp4_plan_workspace(B, Hq, H, S, split_tokens)
 
     def call(raw):
@@ -1288,6 +1297,7 @@ def attn_decode_paged_fp4(q, k_pool, v_pool, k_pages, v_pages, lens, S: Optional
 
 
 def attn_decode_paged_fp4_plan(B: int, Hq: int, Hkv: int, S: int, D: int = 128, split_tokens: int = 0) -> dict:
+    _sizes(B, Hq, Hkv, S, D, split_tokens)
     out = AttnPlanInfo()
     _check(load_library().asym_attn_decode_paged_fp4_plan(B, Hq, Hkv, S, D, split_tokens, ctypes.byref(out)))
     return out.to_dict()
@@ -1334,6 +1344,7 @@ def _status(status):
 
 @functools.lru_cache(maxsize=256)
 def _pages_workspace(op, R, H, pph, pool_pages, n) -> int:
+    _sizes(R, H, pph, n)
     nbytes = ctypes.c_size_t()
     _check(load_library().asym_kv_pages_workspace(op, R, H, pph, pool_pages, n, ctypes.byref(nbytes)))
     return nbytes.value
@@ -1384,6 +1395,7 @@ def kv_free(table, lens, refs, rows, stream=None) -> None:
     """Rows of a paged cache end: their pages' counts fall, their entries become -1."""
     R, H, pph, pool = _pages_state(table, lens, refs)
     n = _requests(rows)
+    _sizes(R, H, pph, n)
     device = _gpu_of("kv_free", table, lens, refs, rows)
     _on(device, stream, lambda raw: _check(load_library().asym_kv_free(
         R, H, pph, table.data_ptr(), lens.data_ptr(), refs.data_ptr(), pool, n, rows.data_ptr(), raw)))

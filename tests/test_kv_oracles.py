@@ -235,3 +235,15 @@ def test_pages_refusals():
     comp = dict(R=4, H=2, pph=3, table=P, refs=P, kp=P, vp=None, page=8192, pool=100, status=None, ws=P, wsb=big, stream=None)
     for change in (dict(refs=None), dict(kp=None), dict(vp=P), dict(page=8), dict(status=P + 1), dict(ws=None), dict(wsb=64)):
         assert lib.asym_kv_compact(*{**comp, **change}.values()) == -1, change
+
+
+@pytest.mark.parametrize("big", [1 << 31, (1 << 32) + 64])
+def test_sizes_past_32_bits_are_refused(big):
+    # (the C ABI's sizes are 32-bit integers: 2^32 + 64 would arrive as 64)
+    for call in (lambda: asym.attn_decode_paged_fp4_plan(1, 8, 8, big), lambda: asym.attn_decode_paged_fp4_plan(big, 8, 8, 64),
+                 lambda: asym.attn_decode_paged_fp4_plan(1, 8, 8, 640, split_tokens=big),
+                 lambda: asym._fp4_plan_workspace(1, 8, 8, big, 0), lambda: asym._prefill_workspace(1, 8, 8, 64, big),
+                 lambda: asym._pages_workspace(asym.KV_EXTEND, big, 1, 1, 100, 5), lambda: asym._sizes(1, big)):
+        for _ in range(2):  # (nothing is kept of a refused call)
+            with pytest.raises(ValueError, match="2\\^31"):
+                call()
