@@ -38,6 +38,7 @@
 
 #include "internal.h"
 #include "kv_fp4.h"
+#include "prefill_form.h"
 
 namespace asym {
 namespace {
@@ -666,12 +667,7 @@ Form form_of(int B, int Hq, int Hkv, int Tq, int Tk) {
   const int G = Hq / Hkv;
   auto count = [&](int rows) { return (int64_t)Tq * G / rows + B; };  // sequences end in a part tile each
   Form f = {};
-  // Tiles of 256 rows read the keys half as often and are faster once the rows fill two
-  // for every CU (us, 128 rows first: 16384 tokens, 32 / 8 heads 1958 1908, 4096 tokens
-  // 142 132, two of 4096 with 16 / 16 heads 147 136); with fewer the last ones are waited
-  // for (2048 tokens, 32 / 8 heads 51 61, 3000 behind 8000 436 479, 1024 26 34), and
-  // sequences of few rows fill them badly (100 of 8 tokens behind 1000 100 155).
-  f.wide = (int64_t)Tq * G / 256 * Hkv >= 512;
+  f.wide = prefill_wide(B, G, Hkv, Tq);
   f.tiles = f.whole = count(f.wide ? 256 : kCutRows);
   if (!f.wide && f.tiles * Hkv < 512) {
     // Cut (us, whole tiles first; 32 / 8 heads): 8 tokens behind 1000 keys 24 14, 4 behind

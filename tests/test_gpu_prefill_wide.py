@@ -16,8 +16,9 @@ from tests.test_gpu_prefill import SCALE, check, dev, i32, inputs, offsets  # no
 pytestmark = pytest.mark.gpu
 
 
-def wide(Tq, Hq, Hkv):
-    return Tq * (Hq // Hkv) // 256 * Hkv >= 512
+def wide(B, Tq, Hq, Hkv):
+    rows = Tq * (Hq // Hkv)
+    return rows // 256 * Hkv >= 512 and rows > 128 * B
 
 
 def same(a, b):
@@ -28,7 +29,7 @@ def alone(q, k, v, cu_q, cu_k, b, causal=True, lse=None):
     """Sequence b in a call of its own (128-row tiles): its rows of O; None if it would be cut."""
     rows, keys = slice(cu_q[b], cu_q[b + 1]), slice(cu_k[b], cu_k[b + 1])
     Lq, Lk = cu_q[b + 1] - cu_q[b], cu_k[b + 1] - cu_k[b]
-    assert not wide(Lq, q.shape[1], k.shape[1])
+    assert not wide(1, Lq, q.shape[1], k.shape[1])
     if asym._prefill_workspace(1, q.shape[1], k.shape[1], Lq, Lk):
         return None
     return asym.attn_prefill(q[rows], k[keys], v[keys], i32([0, Lq], q.device), i32([0, Lk], q.device), lse=lse, causal=causal)
@@ -40,14 +41,16 @@ WIDE = [  # query lengths, key lengths, H_q, H_kv: group sizes that divide 256 a
     ([1000, 31, 1000], [1000, 31, 1111], 72, 24),       # 3 heads a group, 24 key/value heads
     ([1500, 1300, 129], [1500, 1364, 129], 48, 3),      # 3 key/value heads
     ([2000, 40, 2100], [2000, 40, 2100], 32, 1),
-    ([4000, 200, 4000], [4000, 327, 3900], 16, 16)]     # (rows of the last one see nothing)
+    ([4000, 200, 4000], [4000, 327, 3900], 16, 16),     # (rows of the last one see nothing)
+    # more sequences than a wave looks at once, most of them a tile and a bit
+    ([61 + b % 7 for b in range(66)] + [5, 0], [61 + b % 7 + b % 5 * 9 for b in range(66)] + [70, 3], 32, 8)]
 
 
 @pytest.mark.parametrize("lq,lk,Hq,Hkv", WIDE)
 @pytest.mark.parametrize("causal", [True, False])
 def test_a_wide_batch_is_its_sequences(dev, lq, lk, Hq, Hkv, causal):
     cu_q, cu_k = offsets(lq), offsets(lk)
-    assert wide(cu_q[-1], Hq, Hkv)
+    assert wide(len(lq), cu_q[-1], Hq, Hkv)
     q, k, v = inputs(dev, cu_q[-1], cu_k[-1], Hq, Hkv, seed=Hq + len(lq))
     lse = torch.full((cu_q[-1], Hq), 7.0, device=dev)
     o = asym.attn_prefill(q, k, v, i32(cu_q, dev), i32(cu_k, dev), lse=lse, causal=causal)
@@ -78,9 +81,9 @@ def test_a_wide_batch_is_its_sequences(dev, lq, lk, Hq, Hkv, causal):
 
 
 def test_thousands_of_one_token_sequences(dev):
-    # more sequences than a wave looks at once, one row of four heads in each tile
+    # as many rows as a wide call has, but one token (a row of four heads) in each tile: 128-row tiles
     n, Hq, Hkv = 4200, 32, 8
-    assert wide(n, Hq, Hkv)
+    assert not wide(n, n, Hq, Hkv)
     lk = [1 + (7 * b) % 90 for b in range(n)]
     lk[1700] = 900
     cu_q, cu_k = offsets([1] * n), offsets(lk)
@@ -98,7 +101,7 @@ def test_what_a_row_does_not_see_cannot_reach_it(dev, bad):
     lq, lk = [1100, 1300, 800, 1300], [1100, 1427, 800, 1300]
     cu_q, cu_k = offsets(lq), offsets(lk)
     q, k, v = inputs(dev, cu_q[-1], cu_k[-1], 32, 8, seed=21)
-    assert wide(cu_q[-1], 32, 8)
+    assert wide(len(lq), cu_q[-1], 32, 8)
     run = lambda k, v: asym.attn_prefill(q, k, v, i32(cu_q, dev), i32(cu_k, dev))
     clean = run(k, v)
     at = [(0, 63, 0), (0, 700, 3), (1, 127 + 65, 7), (1, 1426, 2), (2, 0, 1), (2, 511, 6), (3, 1023, 4), (3, 1024, 5)]
@@ -132,7 +135,7 @@ def test_opposite_infinities(dev):
     lq = [1500, 1300, 1400]
     cu = offsets(lq)
     q, k, v = inputs(dev, cu[-1], cu[-1], 32, 8, seed=22)
-    assert wide(cu[-1], 32, 8)
+    assert wide(len(lq), cu[-1], 32, 8)
     inf = float("inf")
     v[cu[1] + 70, 2, 3], v[cu[1] + 100, 2, 3], v[cu[1] + 200, 2, 9], v[cu[1] + 900, 2, 9] = inf, -inf, -inf, inf
     o = asym.attn_prefill(q, k, v, i32(cu, dev)).float()
@@ -152,7 +155,7 @@ def test_strided_views_and_rows_outside(dev):
     cu = offsets(lq, first=7)
     qkv[:7], qkv[cu[-1]:] = float("nan"), float("inf")
     q, k, v = qkv[:, :Hq], qkv[:, Hq:Hq + Hkv], qkv[:, Hq + Hkv:]
-    assert wide(T, Hq, Hkv)
+    assert wide(len(lq), T, Hq, Hkv)
     o = torch.full((T, Hq, 128), 7.0, dtype=torch.bfloat16, device=dev)
     lse = torch.full((T, Hq), 7.0, device=dev)
     asym.attn_prefill(q, k, v, i32(cu, dev), o=o, lse=lse)
