@@ -899,7 +899,9 @@ int asym_mla_decode_plan(const asym_topology* topo, int B, int H_q, int S_k, int
  * over all keys j of the sequence, or, if causal is not 0, over j <= i + L_k - L_q
  * (the last query sees the last key).  A row that sees no key has O = 0 and
  * lse = -infinity.  What a row does not see (later keys, other sequences' rows)
- * does not reach it, whatever it holds, infinities and NaN included.
+ * does not reach it, whatever it holds, infinities and NaN included; 32 rows of a
+ * sequence share the moments at which their running maxima are raised, so a key that
+ * some of them see may change how the others are rounded.
  * Layout (caller-owned device memory): q [T_q][H_q][128], K and V [T_k][H_kv][128],
  * bf16, with the given strides in values between tokens and between heads
  * (multiples of 8; K's and V's token strides 128 to 2^23), so that the parts of
@@ -914,9 +916,10 @@ int asym_mla_decode_plan(const asym_topology* topo, int B, int H_q, int S_k, int
  * and are 0 for every other call), which calls that may overlap must not share.
  * No host synchronisation; may be captured.  mapping: AWARE keeps the tiles that read one key/value head on one XCD where the head
  * count divides by the XCDs or the other way round (its keys and values cross
- * into one L2); the oblivious mappings number them head by head.  Longest tiles
- * first in every mapping, and every mapping gives the same bits.  Runs on the
- * stream's CU set; asynchronous.
+ * into one L2); the oblivious mappings number them head by head.  Tiles start longest
+ * first in every mapping, those of a call that may be cut sequence by sequence; every
+ * mapping gives the same bits.  Runs on the stream's CU set; asynchronous.
+ * Sums are fp32 with weights of up to 2^8: results need 2^8 * L_k * max|V| below 2^128.
  * Errors: ASYM_EINVAL, ASYM_EUNSUPPORTED, ASYM_EHIP. */
 int asym_attn_prefill_bf16(int B, int H_q, int H_kv, int D, int T_q, int T_k,
                            const void* q, int64_t q_token, int64_t q_head,
@@ -985,6 +988,7 @@ int asym_kv_read_fp4(int B, int H_kv, int T, const void* k_pool, const void* v_p
  * The fp32 pieces lie in the caller's workspace (16-byte aligned;
  * asym_attn_decode_paged_fp4_plan's workspace_bytes, which may be 0), which calls that may
  * overlap must not share.
+ * Sums are fp32 with weights of up to 2^8: results need 2^8 * S_max * max|V| below 2^128.
  * No host synchronisation; may be captured.  Runs on the stream's CU set;
  * asynchronous.  Errors: ASYM_EINVAL, ASYM_EUNSUPPORTED, ASYM_EHIP. */
 int asym_attn_decode_paged_fp4(int B, int H_q, int H_kv, int S_max, int D, const void* q,

@@ -536,6 +536,9 @@ extern "C" int asym_attn_decode_paged_fp4(int B, int H_q, int H_kv, int S_max, i
   p.q_flip = scale < 0 ? 0x80008000u : 0u;
   hipStream_t s = static_cast<hipStream_t>(stream);
   // (at most: the requests may be shorter than S_max)
+  // (Small CU sets stream too: what costs the 16-bit cache there does not cost this one.  us, ordinary loads first, 64
+  // requests of up to 16384 tokens, 674 MiB: 256 CUs 137 121, 240 162 148, 192 146 133, 128 183 169, 64 302 302; 16 of 8000
+  // with 32 key/value heads, 294 MiB: 65 57, 75 68, 70 65, 87 83, 145 144.)
   const int64_t bytes = 2ll * B * H_kv * ((S_max + (int64_t)kKvPageTokens - 1) / kKvPageTokens) * kFp4PageBytes;
   const bool once = attn_streams_kv(paged_kv_bytes(bytes, (int64_t)pool_pages * kFp4PageBytes, k_pool == v_pool));
   auto kernel = P.rows ? (once ? fp4_decode_share<2, true> : fp4_decode_share<0, true>)

@@ -16,7 +16,7 @@
 //                   the running max is raised only when a row's grows by more than
 //                   2^8 (the sums stay in range, the output is rescaled rarely);
 //   O^T += V^T . P^T: the score registers, rounded to bf16 (the type of the products'
-//                   operands; 2^-9 relative, the output's own rounding), are the
+//                   operands; 2^-8 relative, as the output's own rounding), are the
 //                   operand as they lie, because the order of tokens inside a product
 //                   is free: V^T is read in that order with ds_read_b64_tr_b16, which
 //                   transposes 16-bit values on the way from LDS.
@@ -672,7 +672,10 @@ Form form_of(int B, int Hq, int Hkv, int Tq, int Tk) {
   if (!f.wide && f.tiles * Hkv < 512) {
     // Cut (us, whole tiles first; 32 / 8 heads): 8 tokens behind 1000 keys 24 14, 4 behind
     // 4000 76 16, 256 behind 16125 298 92, 4 behind 32000 and 39 times 4 behind 300 569 49.
-    // It costs a launch (12 of 100 behind 700, which it would leave whole: 33 37).
+    // It costs a launch (12 of 100 behind 700, which it would leave whole: 33 37).  The pieces'
+    // places grow with the tiles, of which each sequence has one at least, so from 512 tiles
+    // over all heads on nothing is cut (56 sequences of 4 tokens, one of them behind 32000 and
+    // the others behind 300: 46 us; 57: 567).
     const int blocks = Tk / PN / B;  // of the mean sequence; a long batch may hold a long one
     f.cut = Tk >= 8192 || pieces_of(blocks, least_blocks((float)(f.tiles * Hkv) * (float)blocks)) > 1;
     if (f.cut) f.tiles += (kPieces + Hkv - 1) / Hkv;
