@@ -23,7 +23,7 @@
 // Scores, max, sum and output are fp32.
 //
 // What bounds it: the clock that the power cap leaves, and the matrix cores at it.  16384
-// causal tokens, 32 query and 8 key heads, take 1870 to 1910 us, 1150 to 1180 TFLOP/s.  The
+// causal tokens, 32 query and 8 key heads, take 1870 to 1920 us, 1145 to 1180 TFLOP/s.  The
 // clock is 2.1 of 2.4 GHz; the matrix cores work in 51 % of the cycles, the vector units
 // (softmax) in 45 %, LDS reads in 25 % and without conflicts.  Fewer cycles give little
 // time: with the next block's scores computed beside this block's softmax, and a maximum
