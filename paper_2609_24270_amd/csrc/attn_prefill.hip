@@ -751,8 +751,7 @@ extern "C" int asym_attn_prefill_bf16(int B, int H_q, int H_kv, int D, int T_q, 
     const int share = kXcds / H_kv;
     grid = (tiles + share - 1) / share * kXcds;
   }
-  if (grid >= (1 << 23))  // (threads of a launch are counted in 32 bits)
-    return fail(ASYM_EUNSUPPORTED, "prefill: too many rows");
+  if (!prefill_fits(grid, form.wide)) return fail(ASYM_EUNSUPPORTED, "prefill: too many rows");
   p.tiles = (int)tiles;
   hipStream_t s = static_cast<hipStream_t>(stream);
   if (form.cut) {

@@ -1,4 +1,4 @@
-// Which row tiles prompt attention takes.  A host rule, a plain function of sizes.
+// Which row tiles prompt attention takes.  Host rules, plain functions of sizes.
 #pragma once
 #include <cstdint>
 
@@ -22,5 +22,8 @@ inline bool prefill_wide(int B, int G, int H_kv, int T_q) {
   const int64_t rows = (int64_t)T_q * G;
   return rows / 256 * H_kv >= 512 && rows > 128ll * B;
 }
+
+// Threads of a launch are counted in 32 bits; a workgroup has two for a row.
+inline bool prefill_fits(int64_t workgroups, bool wide) { return workgroups * (wide ? 512 : 256) < (1ll << 32); }
 
 }  // namespace asym
