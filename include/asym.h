@@ -1048,12 +1048,128 @@ int asym_kv_fork(int R, int H, int pages_per_head, int32_t* table, int32_t* lens
 int asym_kv_free(int R, int H, int pages_per_head, int32_t* table, int32_t* lens, int32_t* refs,
                  size_t pool_pages, int n, const int32_t* rows, void* stream);
 
+/* Rows keep some of their last tokens: of row rows[i]'s last cu[i + 1] - cu[i] tokens (drafted ones)
+ * those at places path[cu[i] .. cu[i] + count[i] - 1] among them (rising) move down, in order, behind
+ * what comes before; the row ends there, and the pages behind its end are given up as in asym_kv_free.  cu:
+ * device int32 [n + 1], not falling, held within [0, T]; path [T] and count [n] as asym_draft_verify
+ * writes them.  A request whose path does not rise or leaves the drafted tokens, or whose row is shorter than
+ * them, is left out.  Pages whose bytes are 32 tokens one after the other (asym_attn_decode_paged_bf16's): page_bytes a
+ * multiple of 512.  v_pool nullable. */
+int asym_kv_keep(int R, int H, int pages_per_head, int32_t* table, int32_t* lens, int32_t* refs,
+                 void* k_pool, void* v_pool, size_t page_bytes, size_t pool_pages, int n,
+                 const int32_t* rows, int T, const int32_t* cu, const int32_t* path,
+                 const int32_t* count, void* stream);
+
 /* With n pages in use, those at or above n move, in order, into the free ones below n, in
  * order; counts and table entries follow.  v_pool nullable.  Pages given up keep
  * their bytes.  status: pages moved, pages in use (all below it now). */
 int asym_kv_compact(int R, int H, int pages_per_head, int32_t* table, int32_t* refs,
                     void* k_pool, void* v_pool, size_t page_bytes, size_t pool_pages,
                     int32_t* status, void* workspace, size_t workspace_bytes, void* stream);
+
+/* ---- rotary positions ------------------------------------------------------ */
+/* The first `rotary` channels of a row are pairs (a, b): channels j and j + rotary / 2
+ * (ASYM_ROPE_HALF) or 2 j and 2 j + 1 (ASYM_ROPE_INTERLEAVED), j < rotary / 2.  With t =
+ * position * freq[j],
+ *   a' = amplitude * (a cos t - b sin t),  b' = amplitude * (b cos t + a sin t);
+ * the other channels are copied.  Long-context scalings are frequencies and an amplitude of
+ * their own.  backward not 0: the gradient, the same with -t (so that with amplitude 1 it undoes
+ * the rotation).  The angle is computed in 64 bits, the rest in fp32.
+ * x and y [T][H][D] bf16 with the given strides in values between tokens and between heads
+ * (multiples of 8), 16-byte aligned; D a multiple of 8, up to 1024.  y may be x, with
+ * x's strides; else the two must not overlap.  rotary even, 0 to D.  positions: device
+ * int32 [T], any values; freq: device double [rotary / 2].  One launch, asynchronous, may be captured.
+ * Errors: ASYM_EINVAL, ASYM_EUNSUPPORTED, ASYM_EHIP. */
+enum asym_rope_layout { ASYM_ROPE_HALF = 0, ASYM_ROPE_INTERLEAVED = 1 };
+int asym_rope_bf16(int T, int H, int D, int rotary, const void* x, int64_t x_token, int64_t x_head,
+                   void* y, int64_t y_token, int64_t y_head, const int32_t* positions,
+                   const double* freq, int layout, float amplitude, int backward, void* stream);
+
+/* ---- 16-bit paged cache: appending tokens ---------------------------------- */
+/* Tokens into a cache of asym_attn_decode_paged_bf16's pages ([32][128] bf16, 8 KiB), their keys
+ * turned on the way: request b's n = cu[b + 1] - cu[b] tokens, rows cu[b] .. of K and V
+ * [T][H_kv][128], become its positions start[b] .. start[b] + n - 1.  K is turned as by asym_rope_bf16
+ * at positions[i] (device int32 [T]; null: the place in the cache; a tree's nodes have the positions of
+ * their depth), V is not; rotary 0 turns nothing.  q [T][H_q][128], if H_q > 0, is turned in the same
+ * way into q_out, which may be q with its strides.  Strides in values, multiples of 8.  cu: device
+ * int32 [B + 1], not falling, held within [0, T]; start: device int32 [B], >= 0 (a request with a
+ * negative one is left out, its q too; keys and values of positions behind the table, and of table
+ * entries outside [0, pool_pages), are not written).  Rows of q_out outside every
+ * request, and all else that the pages hold, stay.  Pages that two requests
+ * of one call write to end up with tokens of both: fork first.  Pools of any size, 16-byte aligned.
+ * Tables: device int32 [B][H_kv][pages_per_head]; k_pages and v_pages may be one table.
+ * One launch, asynchronous, may be captured.  Errors: ASYM_EINVAL, ASYM_EUNSUPPORTED, ASYM_EHIP. */
+int asym_kv_append_bf16(int B, int H_q, int H_kv, int T, const void* q, int64_t q_token, int64_t q_head,
+                        void* q_out, int64_t qo_token, int64_t qo_head,
+                        const void* k, int64_t k_token, int64_t k_head,
+                        const void* v, int64_t v_token, int64_t v_head,
+                        void* k_pool, void* v_pool, size_t pool_pages,
+                        const int32_t* k_pages, const int32_t* v_pages, int pages_per_head,
+                        const int32_t* cu, const int32_t* start, const int32_t* positions,
+                        int rotary, const double* freq, int layout, float amplitude, void* stream);
+
+/* ---- attention of drafted tokens over the 16-bit paged cache ---------------- */
+/* A request's nodes are the rows cu[b] .. cu[b + 1] - 1 of q, n of them, and the last n of its lens[b]
+ * tokens in the cache (node j is token lens[b] - n + j; append them first).  For node i and query head h,
+ * with g = h / (H_q / H_kv),
+ *   O[i][h] = softmax_t(scale * q[i][h] . K[g][t]) . V[g][t]
+ *   lse[i][h] = log sum_t exp(scale * q[i][h] . K[g][t])   (nullable output)
+ * over every token t before the nodes and over those nodes j whose bit j % 64 of word j / 64 of the
+ * mask's row cu[b] + i is set (device uint64 [T][mask_words]; nodes behind the words are not seen); mask null: j <= i, a
+ * chain.  With one node a request this is decode attention with a length per request.  A node that
+ * sees nothing has O = 0 and lse = -infinity.  What a node does not see does not reach it, whatever it holds,
+ * infinities and NaN included; rows that share a wave share the moments at which their running maxima are
+ * raised, so what one of them sees may change how the others are rounded.
+ * q [T][H_q][128] with strides in values (multiples of 8), O [T][H_q][128] bf16 and lse [T][H_q] fp32
+ * contiguous, q, O and the pools 16-byte aligned.  Pages as asym_attn_decode_paged_bf16's, pools of any
+ * size; tables device int32 [B][H_kv][pages_per_head], S_max at most 32 * pages_per_head; an entry
+ * outside [0, pool_pages) reads as zeros.  lens: device int32 [B], held within [0, S_max] (of n nodes
+ * the last lens[b] are there then).  cu: device int32 [B + 1], not falling, held within [0, T].  Rows of O and
+ * lse outside every request are left as they are.  D must be 128, H_q / H_kv any whole number.
+ * The batch's pages are cut into equal shares, one a workgroup (split_tokens tokens of one head, a multiple
+ * of 32 up to 2^20; 0: automatic, from the batch), and a second launch joins what was cut, in the order of
+ * the shares.  The results depend on the sizes, offsets and lengths alone.  The fp32 pieces lie in the caller's
+ * workspace (16-byte aligned; asym_attn_tree_paged_workspace's bytes), which calls that may overlap
+ * must not share.  Sums are fp32 with weights of up to 2^8: results need 2^8 * S_max * max|V| below 2^128.
+ * No host synchronisation; may be captured.  Runs on the stream's CU set; asynchronous.
+ * Errors: ASYM_EINVAL, ASYM_EUNSUPPORTED, ASYM_EHIP. */
+int asym_attn_tree_paged_bf16(int B, int H_q, int H_kv, int T, int S_max, int D,
+                              const void* q, int64_t q_token, int64_t q_head,
+                              const void* k_pool, const void* v_pool, size_t pool_pages,
+                              const int32_t* k_pages, const int32_t* v_pages, int pages_per_head,
+                              const int32_t* cu, const int32_t* lens, const uint64_t* mask, int mask_words,
+                              void* o, float* lse, float scale, int split_tokens,
+                              void* workspace, size_t workspace_bytes, void* stream);
+int asym_attn_tree_paged_workspace(int B, int H_q, int H_kv, int T, int S_max, int split_tokens, size_t* bytes);
+
+/* ---- verification of drafted tokens ----------------------------------------- */
+/* Which drafted tokens a request keeps, and its next token, so that each has the target's distribution.
+ * Request b's nodes are rows cu[b] .. cu[b + 1] - 1: node 0 the root (the last token that was kept
+ * before; its token is not looked at), node i behind it with token tokens[], parent parents[] (a
+ * node before it; null: the one before it, a chain).  target and draft [T][V]: row i holds the two
+ * models' probabilities of the token behind node i (fp32, or bf16 if bf16 is not 0; target_row and
+ * draft_row values apart).  Nodes are taken in order; one whose parent is the current node, with
+ * token t, is accepted, and becomes the current one, if with p and q the current node's rows
+ *   accept[node] * q(t) * m < R(t),  R = max(p - c q, 0),
+ * c = 0 and m = 1 at first; if it is rejected, c becomes c + m and then m the sum of R.  At the end token[b] is the
+ * lowest t with R(0) + .. + R(t) > final[b] * sum R (with p for R if R is 0 throughout; -1 if p is too).
+ * draft null: each token was certain, so that accept[node] * m < p(t) accepts, a rejected
+ * token has no part in R = p any more, nor another chance, and m falls by its p.
+ * All in 64 bits.  What is not a positive finite number counts as 0.  accept [T] and final [B]: fp32 in
+ * [0, 1).  A node whose token lies outside [0, V), or whose parent does not come before it, is passed
+ * over, and so is what hangs on it.
+ * Outputs: path int32 [T], from cu[b] on the nodes kept, the root first, rising, then -1; count
+ * int32 [B], how many; token int32 [B].  A request without nodes: count 0, token -1.  Rows of path outside every
+ * request are left as they are.  cu: device int32 [B + 1], not falling, held within [0, T].
+ * Probabilities are read where they are needed only: a node's own two, and the rows of which sums are taken.
+ * The workspace (16-byte aligned; asym_draft_verify_workspace's bytes) must not be shared by calls that may
+ * overlap.  No host synchronisation; may be captured; asynchronous.  Errors: ASYM_EINVAL, ASYM_EUNSUPPORTED, ASYM_EHIP. */
+int asym_draft_verify(int B, int T, int V, int bf16, const void* target, int64_t target_row,
+                      const void* draft, int64_t draft_row, const int32_t* tokens, const int32_t* parents,
+                      const int32_t* cu, const float* accept, const float* final,
+                      int32_t* path, int32_t* count, int32_t* token,
+                      void* workspace, size_t workspace_bytes, void* stream);
+int asym_draft_verify_workspace(int B, int T, int V, size_t* bytes);
 
 /* ---- streaming copy and co-run (Sections 7.2, 7.3) ---------------------- */
 /* The bandwidth-bound tenant of the co-location study (Section 7.3 runs a

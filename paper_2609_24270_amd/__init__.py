@@ -50,7 +50,9 @@ EXPORTS = (
     "asym_attn_prefill_bf16", "asym_attn_prefill_workspace", "asym_kv_write_fp4", "asym_kv_read_fp4",
     "asym_attn_decode_paged_fp4",
     "asym_attn_decode_paged_fp4_plan", "asym_kv_pages_workspace", "asym_kv_extend", "asym_kv_fork", "asym_kv_free",
-    "asym_kv_compact",
+    "asym_kv_keep", "asym_kv_compact",
+    "asym_rope_bf16", "asym_kv_append_bf16", "asym_attn_tree_paged_bf16", "asym_attn_tree_paged_workspace",
+    "asym_draft_verify", "asym_draft_verify_workspace",
     "asym_copy_bf16", "asym_corun", "asym_last_error", "asym_version",
 )
 
@@ -294,6 +296,14 @@ def load_library(path: str = LIB_PATH):
         "asym_kv_fork": (i, [i, i, i, vp, vp, vp, vp, vp, sz, sz, i, vp, vp, vp, vp, sz, vp]),
         "asym_kv_free": (i, [i, i, i, vp, vp, vp, sz, i, vp, vp]),
         "asym_kv_compact": (i, [i, i, i, vp, vp, vp, vp, sz, sz, vp, vp, sz, vp]),
+        "asym_kv_keep": (i, [i, i, i, vp, vp, vp, vp, vp, sz, sz, i, vp, i, vp, vp, vp, vp]),
+        "asym_rope_bf16": (i, [i] * 4 + [vp, i64, i64] * 2 + [vp, vp, i, f32, i, vp]),
+        "asym_kv_append_bf16": (i, [i] * 4 + [vp, i64, i64] * 4 + [vp, vp, sz, vp, vp, i, vp, vp, vp, i, vp, i, f32, vp]),
+        "asym_attn_tree_paged_bf16": (i, [i] * 6 + [vp, i64, i64, vp, vp, sz, vp, vp, i, vp, vp, vp, i, vp, vp, f32, i, vp,
+                                                    sz, vp]),
+        "asym_attn_tree_paged_workspace": (i, [i] * 6 + [ctypes.POINTER(sz)]),
+        "asym_draft_verify": (i, [i] * 4 + [vp, i64, vp, i64] + [vp] * 9 + [sz, vp]),
+        "asym_draft_verify_workspace": (i, [i] * 3 + [ctypes.POINTER(sz)]),
         "asym_copy_bf16": (i, [topo_p, vp, vp, ctypes.c_size_t, i, vp, u32, vp]),
         "asym_corun": (i, [topo_p, ctypes.POINTER(Task), i, ctypes.POINTER(TaskResult)]),
         "asym_last_error": (cp, []),
@@ -1401,6 +1411,26 @@ def kv_free(table, lens, refs, rows, stream=None) -> None:
         R, H, pph, table.data_ptr(), lens.data_ptr(), refs.data_ptr(), pool, n, rows.data_ptr(), raw)))
 
 
+def kv_keep(k_pool, v_pool, table, lens, refs, rows, cu, path, count, stream=None) -> None:
+    """Rows of a paged cache keep some of their last tokens: of the last cu[i + 1] - cu[i] tokens of row
+    rows[i] those at places path[cu[i] .. cu[i] + count[i] - 1] among them (rising; as draft_verify gives them),
+    in order; the row ends behind them, and the pages behind its end are given up.  Pools [pool_pages, 32,
+    ...] (v_pool None: only one); cu [n + 1], path [T], count [n]; the rest as kv_extend.  All int32."""
+    R, H, pph, pool = _pages_state(table, lens, refs)
+    n = _requests(rows, count)
+    _index(cu, "cu", (n + 1,))
+    T = _requests(path)
+    page = _pools(k_pool, v_pool, pool)
+    if k_pool.shape[1] != PAGE_TOKENS:
+        raise ValueError("pools must be [pool_pages, 32, ...]")
+    _sizes(R, H, pph, n, T)
+    device = _gpu_of("kv_keep", table, lens, refs, rows, cu, path, count, k_pool, k_pool if v_pool is None else v_pool)
+    _on(device, stream, lambda raw: _check(load_library().asym_kv_keep(
+        R, H, pph, table.data_ptr(), lens.data_ptr(), refs.data_ptr(), k_pool.data_ptr(),
+        None if v_pool is None else v_pool.data_ptr(), page, pool, n, rows.data_ptr(), T, cu.data_ptr(), path.data_ptr(),
+        count.data_ptr(), raw)))
+
+
 def kv_compact(k_pool, v_pool, table, lens, refs, status=None, stream=None) -> None:
     """The n pages in use of a paged cache become pages 0 .. n - 1: those at or above n
     move, in order, into the free ones below; refs and table follow (lens does not
@@ -1418,6 +1448,299 @@ def kv_compact(k_pool, v_pool, table, lens, refs, status=None, stream=None) -> N
             R, H, pph, table.data_ptr(), refs.data_ptr(), k_pool.data_ptr(), None if v_pool is None else v_pool.data_ptr(),
             page, pool, st, ws.data_ptr(), nbytes, raw))
     _on(device, stream, call)
+
+
+# ---- rotary positions, the 16-bit paged cache, drafted tokens ---------------------------
+
+ROPE_LAYOUTS = {"half": 0, "interleaved": 1}
+
+
+def rope_freq(rotary: int, base: float = 10000.0, scaling: Optional[str] = None, factor: float = 1.0,
+              original: int = 8192, fast: float = 32.0, slow: float = 1.0):
+    """Frequencies (float64 CPU tensor [rotary / 2]) and amplitude of rotary positions: base^(-2 j / rotary) and 1, or
+    scaled for a context `factor` times as long as the `original` tokens that a model was trained on:
+    "linear" (positions pressed together: every frequency / factor), "base" (base * factor^(rotary / (rotary - 2)):
+    the slowest channel turns `factor` times slower, the fastest as before), "parts" (Peng et al. 2023: channels with
+    more than `fast` turns in `original` tokens as before, with fewer than `slow` / factor, a linear blend in
+    between; amplitude 1 + 0.1 ln factor)."""
+    import math
+
+    import torch
+    if rotary < 0 or rotary % 2:
+        raise ValueError("rotary must be even and not negative")
+    if not base > 0 or not factor >= 1 or not fast > slow or original < 1:
+        raise ValueError("base must be positive, factor >= 1, fast > slow, original >= 1")
+    j = torch.arange(0, rotary, 2, dtype=torch.float64)
+    if scaling == "base":
+        if rotary < 4:
+            raise ValueError("scaling the base needs two pairs or more")
+        base = base * factor ** (rotary / (rotary - 2))
+    freq = base ** (-j / max(rotary, 1))
+    if scaling in (None, "base"):
+        return freq, 1.0
+    if scaling == "linear":
+        return freq / factor, 1.0
+    if scaling != "parts":
+        raise ValueError("scaling must be None, 'linear', 'base' or 'parts'")
+    keep = ((original * freq / (2 * math.pi) - slow) / (fast - slow)).clamp(0, 1)
+    return freq * (keep + (1 - keep) / factor), 1 + 0.1 * math.log(factor)
+
+
+def _freq(freq):
+    """Checks frequencies: (rotary, address, the tensors given)."""
+    import torch
+    if freq is None:
+        return 0, None, ()
+    if freq.dtype is not torch.float64:
+        raise TypeError("freq must be float64")
+    if freq.dim() != 1 or not freq.is_contiguous():
+        raise ValueError("freq must be contiguous [rotary / 2]")
+    return 2 * freq.shape[0], freq.data_ptr(), (freq,)
+
+
+def _rows(t, what):
+    """A bf16 [T, H, D] tensor with unit stride in its last dimension: (T, H, D, token stride, head stride)."""
+    import torch
+    if t.dtype is not torch.bfloat16:
+        raise TypeError(f"{what} must be bfloat16")
+    shape, stride = t.shape, t.stride()
+    if len(shape) != 3 or stride[2] != 1:
+        raise ValueError(f"{what} must be [tokens, heads, channels] with unit stride in its last dimension")
+    T, H, D = shape
+    return T, H, D, (stride[0] if T > 1 else H * D), (stride[1] if H > 1 else D)
+
+
+def rope(x, positions, freq, out=None, layout: str = "half", amplitude: float = 1.0, backward: bool = False, stream=None):
+    """Rotary positions: the first 2 * len(freq) channels of x [T, H, D] (bf16, strided in its first two dimensions as
+    it likes; D a multiple of 8) are turned in pairs by positions[t] * freq[j], times `amplitude`; pairs are channels j
+    and j + rotary / 2 ("half") or 2 j and 2 j + 1 ("interleaved").  positions int32 [T], freq float64 [rotary / 2] (see
+    rope_freq).  backward: the gradient with respect to x, given the output's.  Returns `out` (given: x's
+    shape; x itself is allowed; else a new contiguous tensor)."""
+    import torch
+    T, H, D, xt, xh = _rows(x, "x")
+    _index(positions, "positions", (T,))
+    rotary, freq_ptr, more = _freq(freq)
+    if out is not None:
+        if out.shape != x.shape:
+            raise ValueError("out must have x's shape")
+        _, _, _, ot, oh = _rows(out, "out")
+        more = (*more, out)
+    code = ROPE_LAYOUTS[layout]
+    _sizes(T, H, D)
+    device = _gpu_of("rope", x, positions, *more)
+
+    def call(raw):
+        y = torch.empty((T, H, D), dtype=torch.bfloat16, device=x.device) if out is None else out
+        _check(load_library().asym_rope_bf16(
+            T, H, D, rotary, x.data_ptr(), xt, xh, y.data_ptr(), *((H * D, D) if out is None else (ot, oh)),
+            positions.data_ptr(), freq_ptr, code, amplitude, 1 if backward else 0, raw))
+        return y
+    return _on(device, stream, call)
+
+
+def _paged_cache(k_pool, v_pool, k_pages, v_pages):
+    """Checks a 16-bit cache's pools and tables: (B, H_kv, pages per head)."""
+    import torch
+    if k_pool.dtype is not torch.bfloat16 or v_pool.dtype is not torch.bfloat16:
+        raise TypeError("pools must be bfloat16")
+    pool = k_pool.shape
+    if len(pool) != 3 or pool[1] != PAGE_TOKENS or pool[2] != 128 or v_pool.shape != pool or not k_pool.is_contiguous() \
+            or not v_pool.is_contiguous():
+        raise ValueError("pools must be contiguous [pool_pages, 32, 128]")
+    _index(k_pages, "k_pages")
+    shape = k_pages.shape
+    if len(shape) != 3:
+        raise ValueError("page tables must be [B, H_kv, pages]")
+    if v_pages is not k_pages:
+        _index(v_pages, "v_pages", shape)
+    return shape
+
+
+def kv_append(k, v, k_pool, v_pool, k_pages, v_pages, cu, start, q=None, q_out=None, freq=None, positions=None,
+              layout: str = "half", amplitude: float = 1.0, stream=None):
+    """Append tokens to a 16-bit paged cache: rows cu[b] .. cu[b + 1] - 1 of k and v [T, H_kv, 128] (bf16, strided as
+    in attn_prefill) become request b's positions start[b] onwards, the keys turned on the way as by rope (freq None: not at all)
+    at `positions` (int32 [T]; default: the place in the cache).  q [T, H_q, 128] is turned with them: returns
+    q_out (given, q itself allowed, or a new tensor), None without q.  Pools bf16 [pool_pages, 32, 128]; tables int32 [B, H_kv,
+    pages]; cu int32 [B + 1], start int32 [B].  Pages must not be shared between requests."""
+    import torch
+    T, H, kt, kh = _rows128(k, "k")
+    vT, vH, vt, vh = _rows128(v, "v")
+    B, Hkv, pph = _paged_cache(k_pool, v_pool, k_pages, v_pages)
+    if vT != T or vH != H or H != Hkv:
+        raise ValueError("k and v must be [T, H_kv, 128], H_kv as in the tables")
+    Hq = qt = qh = ot = oh = 0
+    more = ()
+    if q is not None:
+        qT, Hq, qt, qh = _rows128(q, "q")
+        if qT != T:
+            raise ValueError("q, k and v must have as many tokens")
+        more = (q,)
+        if q_out is not None:
+            if q_out.shape != q.shape:
+                raise ValueError("q_out must have q's shape")
+            _, _, ot, oh = _rows128(q_out, "q_out")
+            more = (q, q_out)
+    elif q_out is not None:
+        raise ValueError("q_out without q")
+    _index(cu, "cu", (B + 1,))
+    _index(start, "start", (B,))
+    if positions is not None:
+        _index(positions, "positions", (T,))
+        more = (*more, positions)
+    rotary, freq_ptr, given = _freq(freq)
+    code = ROPE_LAYOUTS[layout]
+    _sizes(B, Hq, H, T, pph)
+    device = _gpu_of("kv_append", k, v, k_pool, v_pool, k_pages, v_pages, cu, start, *more, *given)
+
+    def call(raw):
+        y = q_out
+        if q is not None and y is None:
+            y = torch.empty((T, Hq, 128), dtype=torch.bfloat16, device=q.device)
+        _check(load_library().asym_kv_append_bf16(
+            B, Hq, H, T, None if q is None else q.data_ptr(), qt, qh, None if y is None else y.data_ptr(),
+            *((Hq * 128, 128) if q_out is None else (ot, oh)), k.data_ptr(), kt, kh, v.data_ptr(), vt, vh, k_pool.data_ptr(),
+            v_pool.data_ptr(), k_pool.shape[0], k_pages.data_ptr(), v_pages.data_ptr(), pph, cu.data_ptr(), start.data_ptr(),
+            None if positions is None else positions.data_ptr(), rotary, freq_ptr, code, amplitude, raw))
+        return y
+    return _on(device, stream, call)
+
+
+def draft_tree(parents: Sequence[int]):
+    """Masks (int64 CPU tensor [n, words], bit j % 64 of word j / 64 of row i: node i sees node j, itself and what it hangs
+    on) and depths (a list) of one request's nodes from their parents (node 0 is the root)."""
+    import torch
+    sees, depth = [], []
+    for i, p in enumerate(parents):
+        if i and not 0 <= p < i:
+            raise ValueError("a node's parent must come before it")
+        sees.append((sees[p] if i else 0) | 1 << i)
+        depth.append(depth[p] + 1 if i else 0)
+    words = max(1, (len(depth) + 63) // 64)
+    part = [[s >> 64 * w & (1 << 64) - 1 for w in range(words)] for s in sees]
+    signed = [[x - (1 << 64) if x >> 63 else x for x in row] for row in part]
+    return torch.tensor(signed, dtype=torch.int64).reshape(len(depth), words), depth
+
+
+@functools.lru_cache(maxsize=256)
+def _tree_workspace(B, Hq, Hkv, T, S, split_tokens) -> int:
+    _sizes(B, Hq, Hkv, T, S, split_tokens)
+    nbytes = ctypes.c_size_t()
+    _check(load_library().asym_attn_tree_paged_workspace(B, Hq, Hkv, T, S, split_tokens, ctypes.byref(nbytes)))
+    return nbytes.value
+
+
+def attn_tree_paged(q, k_pool, v_pool, k_pages, v_pages, cu, lens, mask=None, S: Optional[int] = None, o=None, lse=None,
+                    scale: Optional[float] = None, split_tokens: int = 0, stream=None):
+    """Attention of drafted tokens over a 16-bit paged cache: request b's nodes are the rows cu[b] .. cu[b + 1] - 1 of
+    q [T, H_q, 128] (bf16, strided as in attn_prefill) and the last of its lens[b] tokens in the cache (append them
+    first).  A node sees every token before the nodes, and the nodes whose bits are set in its row of mask (int64 [T,
+    words], as draft_tree gives it; None: those up to itself, a chain).  One node a request: decode attention with a length per request.
+    Pools bf16 [pool_pages, 32, 128]; tables int32 [B, H_kv, pages]; cu int32 [B + 1]; lens int32 [B], at most S
+    (default: what the tables hold).  Returns O [T, H_q, 128] bf16 (and fills lse [T, H_q] fp32 when given); rows outside
+    every request are not written.  scale defaults to 1 / sqrt(128)."""
+    import torch
+    T, Hq, qt, qh = _rows128(q, "q")
+    B, H, pph = _paged_cache(k_pool, v_pool, k_pages, v_pages)
+    _index(cu, "cu", (B + 1,))
+    _index(lens, "lens", (B,))
+    words, more = 0, ()
+    if mask is not None:
+        if mask.dtype is not torch.int64:
+            raise TypeError("mask must be int64")
+        if mask.dim() != 2 or mask.shape[0] != T or mask.shape[1] < 1 or not mask.is_contiguous():
+            raise ValueError("mask must be contiguous [T, words]")
+        words, more = mask.shape[1], (mask,)
+    if S is None:
+        S = pph * PAGE_TOKENS
+    lse_ptr, out = _outputs(o, lse, (T, Hq, 128), "[T, H_q, 128]")
+    device = _gpu_of("attn_tree_paged", q, k_pool, v_pool, k_pages, v_pages, cu, lens, *more, *out)
+    sc = _SCALE_128 if scale is None else float(scale)
+    _sizes(pph, words)
+    nbytes = _tree_workspace(B, Hq, H, T, S, split_tokens)
+
+    def call(raw):
+        r = torch.empty((T, Hq, 128), dtype=torch.bfloat16, device=q.device) if o is None else o
+        ws = _workspace(nbytes, q.device) if nbytes else None
+        _check(load_library().asym_attn_tree_paged_bf16(
+            B, Hq, H, T, S, 128, q.data_ptr(), qt, qh, k_pool.data_ptr(), v_pool.data_ptr(), k_pool.shape[0], k_pages.data_ptr(),
+            v_pages.data_ptr(), pph, cu.data_ptr(), lens.data_ptr(), mask.data_ptr() if words else None, words, r.data_ptr(), lse_ptr,
+            sc, split_tokens, ws.data_ptr() if nbytes else None, nbytes, raw))
+        return r
+    return _on(device, stream, call)
+
+
+@functools.lru_cache(maxsize=256)
+def _verify_workspace(B, T, V) -> int:
+    _sizes(B, T, V)
+    nbytes = ctypes.c_size_t()
+    _check(load_library().asym_draft_verify_workspace(B, T, V, ctypes.byref(nbytes)))
+    return nbytes.value
+
+
+def _probabilities(t, what):
+    shape, stride = t.shape, t.stride()
+    if len(shape) != 2 or (stride[1] != 1 and shape[1] > 1):
+        raise ValueError(f"{what} must be [T, V] with unit stride in its last dimension")
+    return stride[0] if shape[0] > 1 else max(stride[0], shape[1])
+
+
+def _random(t, what, n):
+    import torch
+    if t.dtype is not torch.float32:
+        raise TypeError(f"{what} must be float32")
+    if t.shape != (n,) or not t.is_contiguous():
+        raise ValueError(f"{what} must be contiguous [{n}]")
+
+
+def draft_verify(target, draft, tokens, parents, cu, accept, final, path=None, count=None, token=None, stream=None):
+    """Which drafted tokens each request keeps, and its next token, so that each has the target's distribution.
+    Request b's nodes are rows cu[b] .. cu[b + 1] - 1 (cu int32 [B + 1]); node 0 is the root.  target and draft [T, V]
+    (both fp32 or both bf16; draft None: each token was certain): the two models' probabilities of the token behind each
+    node.  tokens int32 [T]; parents int32 [T], each node's parent among its request's nodes (None: chains); accept
+    fp32 [T] and final fp32 [B]: uniform random numbers in [0, 1), one for each node's acceptance and one for the
+    last token.  Returns path int32 [T] (from cu[b] on the nodes kept, the root first, then -1), count int32 [B] (how many),
+    token int32 [B] (the token behind the last of them)."""
+    import torch
+    if target.dtype is not torch.float32 and target.dtype is not torch.bfloat16:
+        raise TypeError("target must be float32 or bfloat16")
+    row = _probabilities(target, "target")
+    T, V = target.shape
+    more, draft_row = (), 0
+    if draft is not None:
+        if draft.dtype is not target.dtype:
+            raise TypeError("draft must have target's type")
+        if draft.shape != target.shape:
+            raise ValueError("draft must have target's shape")
+        draft_row, more = _probabilities(draft, "draft"), (draft,)
+    _index(tokens, "tokens", (T,))
+    if parents is not None:
+        _index(parents, "parents", (T,))
+        more = (*more, parents)
+    _index(cu, "cu")
+    if cu.dim() != 1 or cu.shape[0] < 1:
+        raise ValueError("cu must be [B + 1]")
+    B = cu.shape[0] - 1
+    _random(accept, "accept", T)
+    _random(final, "final", B)
+    for t, what, n in ((path, "path", T), (count, "count", B), (token, "token", B)):
+        if t is not None:
+            _index(t, what, (n,))
+            more = (*more, t)
+    device = _gpu_of("draft_verify", target, tokens, cu, accept, final, *more)
+    nbytes = _verify_workspace(B, T, V)
+
+    def call(raw):
+        new = lambda t, n: torch.empty(n, dtype=torch.int32, device=target.device) if t is None else t
+        r = new(path, T), new(count, B), new(token, B)
+        ws = _workspace(nbytes, target.device)
+        _check(load_library().asym_draft_verify(
+            B, T, V, 0 if target.dtype is torch.float32 else 1, target.data_ptr(), row,
+            None if draft is None else draft.data_ptr(), draft_row, tokens.data_ptr(),
+            None if parents is None else parents.data_ptr(), cu.data_ptr(), accept.data_ptr(), final.data_ptr(),
+            r[0].data_ptr(), r[1].data_ptr(), r[2].data_ptr(), ws.data_ptr(), nbytes, raw))
+        return r
+    return _on(device, stream, call)
 
 
 # ---- copy and co-run --------------------------------------------------------------

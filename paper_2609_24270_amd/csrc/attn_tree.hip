@@ -1,0 +1,662 @@
+// Attention of a tree of drafted tokens over a 16-bit paged cache: a request's n nodes, which
+// are the last n of its len tokens in the cache, against all that each of them sees:
+//
+//   O[i, h] = softmax_t(scale * <q[i, h], K[g, t]>) . V[g, t],  g = h / G, G = H_q / H_kv,
+//
+// over every token t before the nodes (t < base = len - n) and the nodes t = base + j whose
+// bit j is set in node i's mask (without masks: j <= i, a chain; n = 1 is plain decoding with
+// a length per request).
+//
+// A row is a (node, query head of the group) pair, node-major.  A workgroup of four waves serves
+// up to 64 NB (NB 1 or 2) rows of one request and key/value head, a wave NB blocks of 16 rows.  As few
+// waves as the rows need (WR: 1, 2 or 4) share a page of 32 tokens, which each of them
+// loads, from its CU's caches but for the first; the others (WK = 4 / WR groups) take the next
+// pages.  Per page a wave computes
+//   S^T = K . Q^T   v_mfma_f32_16x16x32_bf16, both operands as they lie in memory;
+//   softmax         a row's 32 scores lie in four lanes; its running max is raised only when
+//                   some row's grows by more than 2^8;
+//   O^T += V^T . P^T  with P rounded to bf16 (the type of the products' operands: 2^-9
+//                   relative at most, as the output's own rounding) in the scores' registers,
+//                   V^T through the wave's own part of LDS and ds_read_b64_tr_b16.
+// Scores, max, sum and output are fp32.  No barrier until a segment's pages are done.
+//
+// The pages of the batch, request by request and head by head, are one list, cut into equal
+// shares, one a workgroup, whatever the lengths (which only the device knows).  A segment (what a
+// share has of one request and head) ends with the WK groups' results added up through LDS;
+// whole segments are written, of cut ones the unscaled output, max and sum go to the caller's
+// workspace in fp32 and a second launch joins them in order.
+//
+// Bound by HBM where the rows are few, by the matrix cores and the softmax beside them at 256
+// rows.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+
+#include "internal.h"
+#include "kv_fp4.h"
+#include "read_policy.h"
+
+namespace asym {
+namespace {
+
+constexpr int kWaves = 4;
+constexpr int kRowBytes = kKvD * 2;
+constexpr int kPageBytes = kKvPageTokens * kRowBytes;
+constexpr int kJoinWaves = 4;
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) unsigned char lds_byte;
+typedef __attribute__((address_space(3))) u32x4 lds_u32x4;
+typedef __attribute__((address_space(3))) f32x4 lds_f32x4;
+
+struct TreeParams {
+  const uint16_t* q;
+  int64_t q_tok, q_head;         // strides, values
+  const uint8_t *k_pool, *v_pool;
+  const int *k_pages, *v_pages;  // [B][Hkv][pph]
+  const int *cu, *lens;
+  const uint64_t* mask;          // [T][words], nullable
+  int words;
+  uint16_t* o;                   // [T][Hq][128]
+  float* lse;                    // [T][Hq], nullable
+  float* part_o;                 // [shares][2][rows][128]
+  float* part_ml;                // [shares][2][rows][2]: max (of the raw scores), sum
+  int2* cut;                     // per (unit, key/value head), a unit being the rows of a request that one workgroup
+                                 // serves: of one that was cut, 2 (its first share) + (1: that share's last piece),
+                                 // its last share; -1 of one that was not
+  int B, Hq, Hkv, G, T, S, pph, pool_pages;
+  int rows;                      // of a workgroup: 64 NB
+  int shares, share_pages, least;  // share_pages 0: the batch's pages over the shares, at least `least`
+  float c, scale;                // |scale| * log2(e), |scale|
+  uint32_t q_flip;
+};
+
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t page_of(const uint8_t* pool, int page, int pool_pages) {
+  const bool in = page >= 0 && page < pool_pages;
+  const uint64_t a = (uint64_t)pool + (uint64_t)(uint32_t)(in ? page : 0) * kPageBytes;
+  return __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void*>(a), (short)0, in ? kPageBytes : 0, 0x00020000);
+}
+
+// f over this lane and those 16, 32 and 48 on: the four that share a row
+template <class F>
+__device__ __forceinline__ float over_quarters(float x, F f) {
+  uint32_t u = __float_as_uint(x);
+  auto sw = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+  x = f(__uint_as_float(sw[0]), __uint_as_float(sw[1]));
+  u = __float_as_uint(x);
+  sw = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+  return f(__uint_as_float(sw[0]), __uint_as_float(sw[1]));
+}
+
+// Request b: its first row of q, nodes, tokens, the units that its rows make and its pages
+struct Request {
+  int first, n, len, units, pages;
+};
+__device__ __forceinline__ Request request(const TreeParams& p, int b) {
+  Request r;
+  packed_rows(p.cu, b, p.T, r.first, r.n);
+  r.len = min(max(p.lens[b], 0), p.S);
+  r.units = (int)(((int64_t)r.n * p.G + p.rows - 1) / p.rows);
+  r.pages = (r.len + kKvPageTokens - 1) / kKvPageTokens;
+  return r;
+}
+// The unit's place in `cut` (a request's units follow the rows before it, one more a request)
+__device__ __forceinline__ int64_t unit_id(const TreeParams& p, int b, int first, int unit) {
+  return (int64_t)first * p.G / p.rows + b + unit;
+}
+
+// Where the requests' pages lie in the list, 64 requests at a time: lane l has request base + l.
+struct Batch {
+  int base;
+  int upto;  // pages (of one head) of the batch up to and with the request, each as often as it has units
+  Request r;
+  __device__ __forceinline__ void load(const TreeParams& p, int from, int before, int lane) {
+    base = from;
+    r = Request{};
+    if (from + lane < p.B) r = request(p, from + lane);
+    upto = before + wave_scan_add(r.units * r.pages);
+  }
+  __device__ __forceinline__ int end() const { return __builtin_amdgcn_readlane(upto, 63); }
+};
+
+template <int NB>
+struct Wave {
+  f32x4 o[NB][8];
+  float m[NB], l[NB];
+};
+struct PageRegs {
+  u32x4 k[8], v[8];
+};
+
+template <int POLICY>
+__device__ __forceinline__ void load_page(const TreeParams& p, int kp, int vp, int lane, PageRegs& r) {
+  const __amdgpu_buffer_rsrc_t rk = page_of(p.k_pool, kp, p.pool_pages), rv = page_of(p.v_pool, vp, p.pool_pages);
+  const uint32_t ko = (uint32_t)((lane & 15) * kRowBytes + (lane >> 4) * 16);
+#pragma unroll
+  for (int t = 0; t < 2; ++t)
+#pragma unroll
+    for (int c = 0; c < 4; ++c)
+      r.k[4 * t + c] = __builtin_bit_cast(
+          u32x4, __builtin_amdgcn_raw_buffer_load_b128(rk, ko + (uint32_t)(t * 16 * kRowBytes + 64 * c), 0, POLICY));
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+    r.v[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rv, (uint32_t)(lane * 16 + 1024 * i), 0, POLICY));
+}
+
+// 16-byte chunk c of V's row t lies at chunk c ^ swz(t), so that the rows that one transposing read takes
+// together (8 rows, two chunks of each) lie on different ones of the 64 banks.
+__device__ __forceinline__ int swz(int row) { return (row & 7) << 1; }
+
+// A lane's place of V^T operand g: channels of group g of 16, tokens 4 q + n / 4
+__device__ __forceinline__ uint32_t v_place(int g, int lane) {
+  const int n = lane & 15, q = lane >> 4;
+  const int row = 4 * q + (n >> 2), chunk = 2 * g + ((n & 3) >> 1);
+  return (uint32_t)(row * kRowBytes + ((chunk ^ swz(row)) << 4) + ((n & 1) << 3));
+}
+__device__ __forceinline__ bf16x8 v_frag(const lds_byte* vt, uint32_t at) {
+  union {
+    s16x4 s[2];
+    bf16x8 b;
+  } u;
+#pragma unroll
+  for (int part = 0; part < 2; ++part)
+    u.s[part] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(vt + at + 16 * part * kRowBytes));
+  return u.b;
+}
+// (what one lane writes and others of its wave read)
+__device__ __forceinline__ void wave_lds_order() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+__device__ __forceinline__ void put_v(lds_byte* vt, int lane, const u32x4* v) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const int row = 4 * i + (lane >> 4);
+    *(lds_u32x4*)(vt + row * kRowBytes + (((lane & 15) ^ swz(row)) << 4)) = v[i];
+  }
+}
+
+// Which of tokens 32 page .. + 31 node i sees, a bit each (node 0 is token `base`, which may be negative)
+__device__ __forceinline__ uint32_t seen_bits(const TreeParams& p, const uint64_t* words, int i, int n, int64_t base, int page) {
+  const int64_t j0 = (int64_t)page * kKvPageTokens - base;  // the node at the page's first token
+  if (j0 <= -kKvPageTokens) return 0xFFFFFFFFu;
+  auto up_to = [&](int64_t k) {  // the bits below k
+    return k <= 0 ? 0u : k >= 32 ? 0xFFFFFFFFu : (1u << k) - 1u;
+  };
+  const uint32_t exist = up_to(n - j0), prefix = up_to(-j0);
+  if (!words) return prefix | (up_to((int64_t)i + 1 - j0) & exist);
+  auto word = [&](int64_t w) { return w < p.words ? words[w] : 0ull; };
+  uint64_t bits;
+  if (j0 < 0) {
+    bits = word(0) << (int)-j0;
+  } else {
+    const int off = (int)(j0 & 63);
+    bits = word(j0 >> 6) >> off;
+    if (off > 32) bits |= word((j0 >> 6) + 1) << (64 - off);
+  }
+  return prefix | ((uint32_t)bits & exist);
+}
+
+// 32 tokens.  TAIL: the page holds nodes, or ends behind the request's tokens: `seen` says what each of the lane's rows sees.
+template <int NB, bool TAIL>
+__device__ __forceinline__ void add_page(const TreeParams& p, lds_byte* vt, const bf16x8 (*qf)[4], PageRegs& cur, int lane,
+                                         const uint32_t* seen, int left, Wave<NB>& a) {
+  const int q4 = lane >> 4;
+  if (TAIL && left < kKvPageTokens) {  // (tokens behind the last: no row sees them, whatever lies there)
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (4 * i + q4 >= left) cur.v[i] = u32x4{};
+  }
+  bool guard = false;
+  if constexpr (TAIL) {
+    uint32_t bad = 0;  // an infinity or a NaN among the values: an exponent of all ones carries
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) bad |= (cur.v[i][e] & 0x7F807F80u) + 0x00800080u;
+    guard = __any((bad & 0x80008000u) != 0);
+  }
+  f32x4 s[NB][2];
+#pragma unroll
+  for (int t = 0; t < 2; ++t)
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+      const bf16x8 f = __builtin_bit_cast(bf16x8, cur.k[4 * t + c]);
+#pragma unroll
+      for (int b = 0; b < NB; ++b) s[b][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f, qf[b][c], c ? s[b][t] : f32x4{}, 0, 0, 0);
+    }
+  if constexpr (TAIL) {
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+      const uint32_t w = seen[b] >> (4 * q4);
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        if (!((w >> (16 * (j >> 2) + (j & 3))) & 1)) s[b][j >> 2][j & 3] = -INFINITY;
+    }
+  }
+  bool up = false;
+  float top[NB];
+#pragma unroll
+  for (int b = 0; b < NB; ++b) {
+    const float x = fmaxf(fmaxf(fmaxf(s[b][0][0], s[b][0][1]), fmaxf(s[b][0][2], s[b][0][3])),
+                          fmaxf(fmaxf(s[b][1][0], s[b][1][1]), fmaxf(s[b][1][2], s[b][1][3])));
+    top[b] = over_quarters(x, [](float x, float y) { return fmaxf(x, y); });
+    up |= (top[b] - a.m[b]) * p.c > 8.f;  // (a first finite max: inf; NaN never)
+  }
+  if (__any(up)) {
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+      const float m_new = fmaxf(a.m[b], top[b]);
+      const float alpha = __builtin_amdgcn_exp2f((a.m[b] - (m_new == -INFINITY ? 0.f : m_new)) * p.c);
+      a.l[b] *= alpha;
+#pragma unroll
+      for (int g = 0; g < 8; ++g) a.o[b][g] *= alpha;
+      a.m[b] = m_new;
+    }
+  }
+  bf16x8 pf[NB];
+#pragma unroll
+  for (int b = 0; b < NB; ++b) {
+    const float ms = a.m[b] == -INFINITY ? 0.f : a.m[b];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      // (the difference first: scores of the type's lowest values times c would be infinite)
+      const float e = __builtin_amdgcn_exp2f((s[b][j >> 2][j & 3] - ms) * p.c);
+      a.l[b] += e;
+      pf[b][j] = (__bf16)e;
+    }
+  }
+  if constexpr (TAIL) {
+    // A masked token's probability is 0, but 0 times an infinity or a NaN among its values is NaN, in a row
+    // that does not see it.  Such values are taken out, and a product of the rows' masks with small whole
+    // numbers in their place (1: inf, 128: -inf, 16384: NaN; sums over 32 tokens, exact in fp32) says what
+    // they do to the rows that see them.
+    if (guard) {
+      u32x4 code[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {  // two values a word
+          const uint32_t w = cur.v[i][e];
+          const uint32_t mask = ((((w & 0x7F807F80u) + 0x00800080u) >> 15) & 0x00010001u) * 0xFFFFu;
+          auto kind = [](uint32_t u) { return (u & 0x7Fu) ? 0x4680u : (u & 0x8000u) ? 0x4300u : 0x3F80u; };
+          cur.v[i][e] = w & ~mask;
+          code[i][e] = (kind(w & 0xFFFFu) | (kind(w >> 16) << 16)) & mask;
+        }
+      wave_lds_order();
+      put_v(vt, lane, code);
+      wave_lds_order();
+#pragma unroll
+      for (int b = 0; b < NB; ++b) {
+        const uint32_t w = seen[b] >> (4 * q4);
+        u32x4 vis;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int at = 16 * (e >> 1) + 2 * (e & 1);
+          vis[e] = (((w >> at) & 1) ? 0x3F80u : 0u) | (((w >> (at + 1)) & 1) ? 0x3F800000u : 0u);
+        }
+#pragma unroll
+        for (int g = 0; g < 8; ++g) {
+          __builtin_amdgcn_sched_barrier(0);  // (one product's registers at a time)
+          const f32x4 x = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v_frag(vt, v_place(g, lane)), __builtin_bit_cast(bf16x8, vis),
+                                                                  f32x4{}, 0, 0, 0);
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const int k = (int)x[r];
+            a.o[b][g][r] += ((k & 127) ? INFINITY : 0.f) + (((k >> 7) & 127) ? -INFINITY : 0.f) + (k >= 16384 ? NAN : 0.f);
+          }
+        }
+      }
+    }
+  }
+  wave_lds_order();
+  put_v(vt, lane, cur.v);
+  wave_lds_order();
+#pragma unroll
+  for (int g = 0; g < 8; ++g) {
+    const bf16x8 f = v_frag(vt, v_place(g, lane));
+#pragma unroll
+    for (int b = 0; b < NB; ++b) a.o[b][g] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f, pf[b], a.o[b][g], 0, 0, 0);
+  }
+}
+
+template <int NB, int POLICY>
+__global__ void __launch_bounds__(64 * kWaves, NB == 1 ? 2 : 1) attn_tree_kernel(TreeParams p) {
+  __shared__ __attribute__((aligned(1024))) unsigned char lds[kWaves * kPageBytes];  // a part for each wave
+  __shared__ float2 ml[kWaves][16];                                                  // a row block's max and sum
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int n = lane & 15, q4 = lane >> 4;
+  lds_byte* vt = (lds_byte*)lds + wave * kPageBytes;
+  const int w = blockIdx.x;
+
+  Batch bt;
+  bt.load(p, 0, 0, lane);
+  int total = bt.end();
+  for (int b = 64; b < p.B; b += 64) {
+    int x = 0;
+    if (b + lane < p.B) {
+      const Request r = request(p, b + lane);
+      x = r.units * r.pages;
+    }
+    total += wave_sum(x);
+  }
+  total *= p.Hkv;
+  const int share = p.share_pages ? p.share_pages : max((total + p.shares - 1) / p.shares, p.least);
+  if ((int64_t)w * share >= total) return;
+  int f = w * share;
+  const int f1 = min(f + share, total);
+
+  for (bool start = true; f < f1; start = false) {
+    // the segment: request b, unit, head hk, its pages pg .. pg + count - 1
+    while (bt.end() * p.Hkv <= f) bt.load(p, bt.base + 64, bt.end(), lane);
+    const int at = __builtin_ctzll(__ballot(bt.upto * p.Hkv > f));
+    const int b = bt.base + at;
+    const int first = __builtin_amdgcn_readlane(bt.r.first, at), nodes = __builtin_amdgcn_readlane(bt.r.n, at);
+    const int len = __builtin_amdgcn_readlane(bt.r.len, at), units = __builtin_amdgcn_readlane(bt.r.units, at);
+    const int pages = __builtin_amdgcn_readlane(bt.r.pages, at);
+    const int in = f - (__builtin_amdgcn_readlane(bt.upto, at) - units * pages) * p.Hkv;
+    const int unit = in / (p.Hkv * pages), hk = (in - unit * p.Hkv * pages) / pages, pg = in % pages;
+    const int count = min(pages - pg, f1 - f);
+    const int64_t row0 = (int64_t)unit * p.rows;
+    const int rows = (int)min((int64_t)nodes * p.G - row0, (int64_t)p.rows);  // of the unit
+    // as few waves as hold the rows share a page
+    const int WR = rows <= 16 * NB ? 1 : rows <= 32 * NB ? 2 : 4, WK = kWaves / WR;
+    const int rg = wave & (WR - 1), kg = wave / WR;
+    const int mine = (count - kg + WK - 1) / WK;  // pages pg + kg, + WK, ... of this wave
+    const bool work = rg * 16 * NB < rows;
+    const int64_t base = (int64_t)len - nodes;
+
+    // this lane's rows, one of each block of 16 (rows past the last repeat it, and are not stored)
+    bf16x8 qf[NB][4];
+    int node[NB];
+#pragma unroll
+    for (int k = 0; k < NB; ++k) {
+      const int64_t row = row0 + min(16 * (NB * rg + k) + n, rows - 1);
+      node[k] = (int)(row / p.G);
+      const int g = (int)(row - (int64_t)node[k] * p.G);
+      const uint16_t* qr = p.q + (int64_t)(first + node[k]) * p.q_tok + ((int64_t)hk * p.G + g) * p.q_head + 8 * q4;
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        u32x4 x = *reinterpret_cast<const u32x4*>(qr + 32 * c);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[e] ^= p.q_flip;
+        qf[k][c] = __builtin_bit_cast(bf16x8, x);
+      }
+    }
+    Wave<NB> a;
+#pragma unroll
+    for (int k = 0; k < NB; ++k) {
+      a.m[k] = -INFINITY;
+      a.l[k] = 0.f;
+#pragma unroll
+      for (int g = 0; g < 8; ++g) a.o[k][g] = f32x4{};
+    }
+
+    if (work && mine > 0) {
+      // a lane holds the number of one of the wave's pages of 64, and of one of the next 64
+      const size_t entry = ((size_t)b * p.Hkv + hk) * p.pph + pg + kg;
+      auto numbers = [&](int i, int& k, int& v) {
+        k = v = -1;
+        if (i + lane < mine) {
+          k = p.k_pages[entry + (size_t)(i + lane) * WK];
+          v = p.v_pages[entry + (size_t)(i + lane) * WK];
+        }
+      };
+      int kpg, vpg, kpg2, vpg2;
+      numbers(0, kpg, vpg);
+      PageRegs cur, nxt;
+      load_page<POLICY>(p, __builtin_amdgcn_readlane(kpg, 0), __builtin_amdgcn_readlane(vpg, 0), lane, cur);
+      // pages that every row sees whole, the next one's loads on their way; then those that hold nodes
+      const int64_t plain = base < 0 ? 0 : base / kKvPageTokens - pg - kg;  // (of the pages from the wave's first on)
+      const int nfull = (int)min((int64_t)mine, plain <= 0 ? 0 : (plain + WK - 1) / WK);
+      for (int i = 0; i < nfull; ++i) {
+        const int e = i & 63;
+        if (e == 0) numbers(i + 64, kpg2, vpg2);
+        if (e == 63) {
+          kpg = kpg2;
+          vpg = vpg2;
+        }
+        // (behind the last page: none, which loads nothing)
+        const int ne = (e + 1) & 63, kn = __builtin_amdgcn_readlane(kpg, ne), vn = __builtin_amdgcn_readlane(vpg, ne);
+        load_page<POLICY>(p, i + 1 < mine ? kn : -1, i + 1 < mine ? vn : -1, lane, nxt);
+        add_page<NB, false>(p, vt, qf, cur, lane, nullptr, 0, a);
+        cur = nxt;
+      }
+      for (int i = nfull; i < mine; ++i) {
+        const int page = pg + kg + i * WK;
+        uint32_t seen[NB];
+#pragma unroll
+        for (int k = 0; k < NB; ++k)
+          seen[k] = seen_bits(p, p.mask ? p.mask + (int64_t)(first + node[k]) * p.words : nullptr, node[k], nodes, base, page);
+        add_page<NB, true>(p, vt, qf, cur, lane, seen, len - page * kKvPageTokens, a);
+        if (i + 1 < mine) {
+          const size_t next = entry + (size_t)(i + 1) * WK;
+          load_page<POLICY>(p, __builtin_amdgcn_readfirstlane(p.k_pages[next]), __builtin_amdgcn_readfirstlane(p.v_pages[next]),
+                            lane, cur);
+        }
+      }
+    }
+
+    // The WK groups' results, a row block at a time: each wave leaves its own in its part of LDS
+    // (16-byte chunk i of row r at chunk i ^ r), then adds up a share of the rows.
+    const bool whole = count == pages;
+    const size_t piece = ((size_t)w * 2 + (start ? 0 : 1)) * p.rows;
+#pragma unroll
+    for (int k = 0; k < NB; ++k) {
+      if (16 * k >= rows) break;
+      const float lt = over_quarters(a.l[k], [](float x, float y) { return x + y; });
+      __syncthreads();
+#pragma unroll
+      for (int g = 0; g < 8; ++g) *(lds_f32x4*)(vt + n * 512 + (((4 * g + q4) ^ n) << 4)) = a.o[k][g];
+      if (q4 == 0) ml[wave][n] = float2{a.m[k], lt};
+      __syncthreads();
+      const int per = 16 / WK;
+      for (int i = lane >> 5; i < per; i += 2) {
+        const int r = kg * per + i, in_unit = 16 * (NB * rg + k) + r, ch = lane & 31;
+        if (in_unit >= rows) continue;
+        float top = -INFINITY;
+        for (int s = 0; s < WK; ++s) top = fmaxf(top, ml[rg + s * WR][r].x);
+        const float ref = top == -INFINITY ? 0.f : top;
+        f32x4 acc = {};
+        float sum = 0.f;
+        for (int s = 0; s < WK; ++s) {
+          const int from = rg + s * WR;
+          const float2 x = ml[from][r];
+          const float wt = __builtin_amdgcn_exp2f((x.x - ref) * p.c);
+          const f32x4 y = *(const lds_f32x4*)((lds_byte*)lds + from * kPageBytes + r * 512 + ((ch ^ r) << 4));
+          sum += x.y * wt;
+          // (a group that saw nothing has 0, and weight 0)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) acc[e] += y[e] * wt;
+        }
+        if (whole) {
+          const int64_t row = row0 + in_unit;
+          const int tok = (int)(row / p.G);
+          const int64_t out = (int64_t)(first + tok) * p.Hq + (int64_t)hk * p.G + (row - (int64_t)tok * p.G);
+          const float inv = sum > 0.f ? 1.f / sum : (sum == 0.f ? 0.f : sum);  // (NaN stays)
+          const bf16x2 x = {(__bf16)(acc[0] * inv), (__bf16)(acc[1] * inv)}, y = {(__bf16)(acc[2] * inv), (__bf16)(acc[3] * inv)};
+          *reinterpret_cast<uint2*>(p.o + out * kKvD + 4 * ch) = uint2{__builtin_bit_cast(uint32_t, x), __builtin_bit_cast(uint32_t, y)};
+          if (p.lse && ch == 0) p.lse[out] = sum == 0.f ? -INFINITY : top * p.scale + __logf(sum);
+        } else {
+          *reinterpret_cast<f32x4*>(p.part_o + (piece + in_unit) * kKvD + 4 * ch) = acc;
+          if (ch == 0) *reinterpret_cast<float2*>(p.part_ml + (piece + in_unit) * 2) = float2{top, sum};
+        }
+      }
+    }
+    // (for the join: which shares have a piece of it, and whether the first of them is its share's last)
+    if (pg == 0 && threadIdx.x == 0)
+      p.cut[unit_id(p, b, first, unit) * p.Hkv + hk] = whole ? int2{-1, 0} : int2{2 * w + (start ? 0 : 1), (f + pages - 1) / share};
+    f += count;
+    __syncthreads();  // (the parts of LDS have been read)
+  }
+}
+
+// A wave a (token, query head): one whose request has no tokens is written, one that was cut is joined.
+__global__ void __launch_bounds__(64 * kJoinWaves) attn_tree_join(TreeParams p) {
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t out = (int64_t)blockIdx.x * kJoinWaves + wave;
+  if (out >= (int64_t)p.T * p.Hq) return;
+  const int tok = (int)(out / p.Hq), h = (int)(out - (int64_t)tok * p.Hq);
+  int b = 0;  // requests that end at or before the token
+  for (int j = 0; j < p.B; j += 64) {
+    const bool before = j + lane < p.B && min(max(p.cu[min(j + lane, p.B - 1) + 1], 0), p.T) <= tok;
+    b += __popcll(__ballot(before));
+  }
+  if (b >= p.B) return;
+  const Request r = request(p, b);
+  if (tok < r.first || tok >= r.first + r.n) return;
+  if (r.pages == 0) {
+    *reinterpret_cast<uint32_t*>(p.o + out * kKvD + 2 * lane) = 0;
+    if (p.lse && lane == 0) p.lse[out] = -INFINITY;
+    return;
+  }
+  const int hk = h / p.G;
+  const int64_t row = (int64_t)(tok - r.first) * p.G + (h - hk * p.G);
+  const int unit = (int)(row / p.rows), in_unit = (int)(row - (int64_t)unit * p.rows);
+  const int2 cut = p.cut[unit_id(p, b, r.first, unit) * p.Hkv + hk];
+  if (cut.x < 0) return;
+  const int w0 = cut.x >> 1, w1 = cut.y;
+  auto piece = [&](int w) { return ((size_t)w * 2 + (w == w0 ? cut.x & 1 : 0)) * p.rows + in_unit; };
+  float2 x[8], q[8];
+  auto load = [&](int w) {
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+      const size_t e = piece(min(w + u, w1));
+      x[u] = *reinterpret_cast<const float2*>(p.part_o + e * kKvD + 2 * lane);
+      q[u] = *reinterpret_cast<const float2*>(p.part_ml + e * 2);
+    }
+  };
+  load(w0);
+  float M = -INFINITY;
+  for (int w = w0 + lane; w <= w1; w += 64) M = fmaxf(M, p.part_ml[piece(w) * 2]);
+#pragma unroll
+  for (int d = 32; d >= 1; d >>= 1) M = fmaxf(M, __shfl_xor(M, d));
+  const float ref = M == -INFINITY ? 0.f : M;
+  float a0 = 0.f, a1 = 0.f, L = 0.f;
+  for (int w = w0; w <= w1; w += 8) {
+    if (w != w0) load(w);
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+      if (w + u > w1) break;
+      const float s = __builtin_amdgcn_exp2f((q[u].x - ref) * p.c);
+      L = fmaf(q[u].y, s, L);
+      a0 = fmaf(x[u].x, s, a0);
+      a1 = fmaf(x[u].y, s, a1);
+    }
+  }
+  const float inv = L > 0.f ? 1.f / L : (L == 0.f ? 0.f : L);  // (NaN stays)
+  const bf16x2 y = {(__bf16)(a0 * inv), (__bf16)(a1 * inv)};
+  *reinterpret_cast<uint32_t*>(p.o + out * kKvD + 2 * lane) = __builtin_bit_cast(uint32_t, y);
+  if (p.lse && lane == 0) p.lse[out] = L == 0.f ? -INFINITY : M * p.scale + __logf(L);
+}
+
+struct TreePlan {
+  int nb = 1, rows = 64, shares = 0, share_pages = 0, least = 1;
+  int64_t units = 0;
+  size_t bytes = 0;
+};
+
+int tree_plan(int B, int Hq, int Hkv, int T, int S, int split_tokens, TreePlan* plan) {
+  if (B < 0 || T < 0 || Hq < 1 || Hkv < 1 || S < 1)
+    return fail(ASYM_EINVAL, "tree attention: B and T must be >= 0, H_q, H_kv and S_max >= 1");
+  if (Hq % Hkv) return fail(ASYM_EINVAL, "tree attention: H_kv must divide H_q");
+  if (split_tokens < 0 || split_tokens % kKvPageTokens || split_tokens > (1 << 20))
+    return fail(ASYM_EINVAL, "tree attention: split_tokens must be 0 (automatic) or a multiple of 32 up to 2^20");
+  TreePlan P;
+  if (B == 0 || T == 0) {
+    *plan = P;
+    return ASYM_OK;
+  }
+  const int64_t all = (int64_t)T * (Hq / Hkv), mean = (all + B - 1) / B;
+  P.nb = mean <= 16 ? 1 : 2;
+  P.rows = 64 * P.nb;
+  P.units = all / P.rows + B;
+  const int64_t pages = ((int64_t)S + kKvPageTokens - 1) / kKvPageTokens, heads = P.units * Hkv;
+  if (heads > (1 << 30) || heads * pages > (1 << 30)) return fail(ASYM_EUNSUPPORTED, "tree attention: more than 2^30 pages");
+  if ((int64_t)T * Hq >= (1 << 26)) return fail(ASYM_EUNSUPPORTED, "tree attention: too many rows");  // (threads are counted in 32 bits)
+  P.share_pages = split_tokens / kKvPageTokens;
+  P.least = P.share_pages ? P.share_pages : 4;
+  int64_t shares = (heads * pages + P.least - 1) / P.least;
+  if (!P.share_pages) shares = std::min<int64_t>(shares, P.nb == 1 ? 512 : 256);
+  if (shares >= (1 << 22)) return fail(ASYM_EUNSUPPORTED, "tree attention: too many shares");
+  P.shares = (int)shares;
+  P.bytes = (size_t)shares * 2 * P.rows * (kKvD + 2) * sizeof(float) + (size_t)heads * sizeof(int2);
+  *plan = P;
+  return ASYM_OK;
+}
+
+}  // namespace
+}  // namespace asym
+
+extern "C" int asym_attn_tree_paged_workspace(int B, int H_q, int H_kv, int T, int S_max, int split_tokens, size_t* bytes) {
+  if (!bytes) return asym::fail(ASYM_EINVAL, "tree attention workspace: null output");
+  asym::TreePlan P;
+  const int rc = asym::tree_plan(B, H_q, H_kv, T, S_max, split_tokens, &P);
+  if (rc == ASYM_OK) *bytes = P.bytes;
+  return rc;
+}
+
+extern "C" int asym_attn_tree_paged_bf16(int B, int H_q, int H_kv, int T, int S_max, int D, const void* q, int64_t q_token,
+                                         int64_t q_head, const void* k_pool, const void* v_pool, size_t pool_pages,
+                                         const int32_t* k_pages, const int32_t* v_pages, int pages_per_head, const int32_t* cu,
+                                         const int32_t* lens, const uint64_t* mask, int mask_words, void* o, float* lse,
+                                         float scale, int split_tokens, void* workspace, size_t workspace_bytes, void* stream) {
+  using namespace asym;
+  TreePlan P;
+  int rc = tree_plan(B, H_q, H_kv, T, S_max, split_tokens, &P);
+  if (rc != ASYM_OK) return rc;
+  if (D != kKvD) return fail(ASYM_EUNSUPPORTED, "tree attention: the head dimension must be 128");
+  if (pages_per_head < 1 || (int64_t)pages_per_head * kKvPageTokens < S_max)
+    return fail(ASYM_EINVAL, "tree attention: the page tables end before S_max");
+  if (pool_pages < 1 || pool_pages > 0x7FFFFFFFu) return fail(ASYM_EINVAL, "tree attention: pool_pages must be in [1, 2^31)");
+  if (!std::isfinite(scale)) return fail(ASYM_EINVAL, "tree attention: scale must be finite");
+  if (mask && mask_words < 1) return fail(ASYM_EINVAL, "tree attention: a mask must have a word or more a node");
+  if (B == 0 || T == 0) return ASYM_OK;
+  if (!q || !k_pool || !v_pool || !k_pages || !v_pages || !cu || !lens || !o)
+    return fail(ASYM_EINVAL, "tree attention: null pointer");
+  if (((uintptr_t)q | (uintptr_t)k_pool | (uintptr_t)v_pool | (uintptr_t)o) & 15u)
+    return fail(ASYM_EINVAL, "tree attention: q, the pools and O must be 16-byte aligned");
+  if (((uintptr_t)k_pages | (uintptr_t)v_pages | (uintptr_t)cu | (uintptr_t)lens | (uintptr_t)lse) & 3u || ((uintptr_t)mask & 7u))
+    return fail(ASYM_EINVAL, "tree attention: tables, offsets, lengths and lse must be 4-byte aligned, masks 8-byte aligned");
+  for (int64_t s : {q_token, q_head})
+    if (s < 0 || s % 8) return fail(ASYM_EINVAL, "tree attention: strides must be multiples of 8 values and not negative");
+  if (!workspace || workspace_bytes < P.bytes || ((uintptr_t)workspace & 15u))
+    return fail(ASYM_EINVAL, "tree attention: the workspace must be 16-byte aligned and hold asym_attn_tree_paged_workspace's bytes");
+  TreeParams p = {};
+  p.q = static_cast<const uint16_t*>(q);
+  p.q_tok = q_token; p.q_head = q_head;
+  p.k_pool = static_cast<const uint8_t*>(k_pool);
+  p.v_pool = static_cast<const uint8_t*>(v_pool);
+  p.k_pages = k_pages; p.v_pages = v_pages; p.cu = cu; p.lens = lens;
+  p.mask = mask; p.words = mask_words;
+  p.o = static_cast<uint16_t*>(o);
+  p.lse = lse;
+  const size_t pieces = (size_t)P.shares * 2 * P.rows;
+  p.part_o = static_cast<float*>(workspace);
+  p.part_ml = p.part_o + pieces * kKvD;
+  p.cut = reinterpret_cast<int2*>(p.part_ml + pieces * 2);
+  p.B = B; p.Hq = H_q; p.Hkv = H_kv; p.G = H_q / H_kv; p.T = T; p.S = S_max; p.pph = pages_per_head;
+  p.pool_pages = (int)pool_pages;
+  p.rows = P.rows; p.shares = P.shares; p.share_pages = P.share_pages; p.least = P.least;
+  p.scale = std::fabs(scale);
+  p.c = std::fmax(p.scale * 1.4426950408889634f, 1.17549435e-38f);  // (0 weighs all tokens alike, a masked one not at all)
+  p.q_flip = scale < 0 ? 0x80008000u : 0u;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  // (at most: the requests may be shorter than S_max)
+  const int64_t bytes = 2ll * B * H_kv * ((S_max + (int64_t)kKvPageTokens - 1) / kKvPageTokens) * kPageBytes;
+  const bool once = attn_streams_kv(paged_kv_bytes(bytes, (int64_t)pool_pages * kPageBytes, k_pool == v_pool));
+  auto kernel = P.nb == 1 ? (once ? attn_tree_kernel<1, 2> : attn_tree_kernel<1, 0>)
+                          : (once ? attn_tree_kernel<2, 2> : attn_tree_kernel<2, 0>);
+  hipLaunchKernelGGL(kernel, dim3((unsigned)P.shares), dim3(64 * kWaves), 0, s, p);
+  ASYM_HIP(hipGetLastError());
+  const int64_t out = (int64_t)T * H_q;
+  hipLaunchKernelGGL(attn_tree_join, dim3((unsigned)((out + kJoinWaves - 1) / kJoinWaves)), dim3(64 * kJoinWaves), 0, s, p);
+  ASYM_HIP(hipGetLastError());
+  return ASYM_OK;
+}

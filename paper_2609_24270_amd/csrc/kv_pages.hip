@@ -13,6 +13,7 @@
 //   2. each segment adds up the counts before it and writes its pages' numbers to their
 //      places in a list;
 //   3. the tables, the counts and the pages themselves are changed.
+// (Free and keep need no pages, and are one launch.)
 // Up to 16384 pages and 1024 requests one workgroup does 1 and 2, and all of an extend:
 // short calls are bound by their launches.  Large ones are bound by the copies (each page
 // read and written once).
@@ -407,6 +408,69 @@ __global__ void __launch_bounds__(kThreads) pages_rename(PagesParams p) {
   }
 }
 
+// keep: a workgroup a request.  Of the row's last n tokens (the drafted ones) those that path names move down to
+// their head, in order; the rest and the pages behind them are given up.  A thread has a 16-byte word of a
+// token of one head and pool, and moves it token by token, kKeepTokens loads on their way at a time: path rises, so
+// that the j-th token comes from place path[j] >= j, and what is written, places up to j, is no later token's
+// source (places above j).
+constexpr int kKeepTokens = 8;
+__global__ void __launch_bounds__(kSmallThreads) pages_keep(PagesParams p, int T, const int* cu, const int* path, const int* count) {
+  const int i = blockIdx.x, r = p.a[i];
+  if (r < 0 || r >= p.R) return;
+  bool bad = false;
+  for (int j = threadIdx.x; j < i; j += blockDim.x) bad |= p.a[j] == r;  // (an earlier request of the call has the row,
+  if (__syncthreads_or(bad)) return;                                     // and changes what is read from here on)
+  int at, n;
+  packed_rows(cu, i, T, at, n);
+  const int len = min(p.lens[r], p.pph * kKvPageTokens), keep = count[i], base = len - n;
+  if (base < 0 || keep < 0 || keep > n) return;
+  for (int j = threadIdx.x; j < keep; j += blockDim.x) {
+    const int x = path[at + j];
+    bad |= x < 0 || x >= n || (j > 0 && path[at + j - 1] >= x);
+  }
+  if (__syncthreads_or(bad)) return;
+  const uint32_t words = (uint32_t)(p.page_bytes / (16 * kKvPageTokens));  // of a token
+  const int64_t columns = (int64_t)p.H * words * (p.v_pool ? 2 : 1);
+  for (int64_t c = threadIdx.x; c < columns; c += blockDim.x) {
+    const int64_t head = c / words;
+    const uint32_t w = (uint32_t)(c - head * words);
+    uint8_t* pool = head < p.H ? p.k_pool : p.v_pool;
+    const int* entries = p.table + ((int64_t)r * p.H + (head < p.H ? head : head - p.H)) * p.pph;
+    auto word = [&](int pos) -> u32x4* {
+      const int page = entries[pos / kKvPageTokens];
+      if (page < 0 || page >= p.pool) return nullptr;
+      return reinterpret_cast<u32x4*>(pool + page * p.page_bytes) + (uint32_t)(pos % kKvPageTokens) * words + w;
+    };
+    for (int j0 = 0; j0 < keep; j0 += kKeepTokens) {
+      u32x4 x[kKeepTokens];
+      u32x4* to[kKeepTokens];
+#pragma unroll
+      for (int u = 0; u < kKeepTokens; ++u) {
+        to[u] = nullptr;
+        if (j0 + u >= keep) continue;
+        const int from = path[at + j0 + u];
+        if (from == j0 + u) continue;
+        const u32x4* src = word(base + from);
+        if (src) {
+          x[u] = *src;
+          to[u] = word(base + j0 + u);
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < kKeepTokens; ++u)
+        if (to[u]) *to[u] = x[u];
+    }
+  }
+  __syncthreads();  // (the entries have been read)
+  const int now = base + keep, left = pages_of(now, p.pph), gone = pages_of(len, p.pph) - left;
+  for (int64_t x = threadIdx.x; x < (int64_t)gone * p.H; x += blockDim.x) {
+    int* e = p.table + ((int64_t)r * p.H + x / gone) * p.pph + left + x % gone;
+    if (*e >= 0 && *e < p.pool) atomicSub(&p.refs[*e], 1);
+    *e = -1;
+  }
+  if (threadIdx.x == 0) p.lens[r] = now;
+}
+
 // The checks that every call shares; lays the workspace out (words, counted in `words`).
 int pages_setup(const char* what, int op, int R, int H, int pph, int32_t* table, int32_t* lens, int32_t* refs,
                 size_t pool_pages, int n, void* workspace, size_t workspace_bytes, PagesParams* p) {
@@ -550,6 +614,32 @@ extern "C" int asym_kv_free(int R, int H, int pages_per_head, int32_t* table, in
   if (!rows || ((uintptr_t)rows & 3u)) return fail(ASYM_EINVAL, "kv free: rows must be given, 4-byte aligned");
   p.a = rows;
   hipLaunchKernelGGL(pages_free, dim3(n), dim3(kThreads), 0, static_cast<hipStream_t>(stream), p);
+  ASYM_HIP(hipGetLastError());
+  return ASYM_OK;
+}
+
+extern "C" int asym_kv_keep(int R, int H, int pages_per_head, int32_t* table, int32_t* lens, int32_t* refs, void* k_pool,
+                            void* v_pool, size_t page_bytes, size_t pool_pages, int n, const int32_t* rows, int T,
+                            const int32_t* cu, const int32_t* path, const int32_t* count, void* stream) {
+  PagesParams p;
+  int rc = pages_setup("kv keep", -1, R, H, pages_per_head, table, lens, refs, pool_pages, n, nullptr, 0, &p);
+  if (rc == ASYM_OK) rc = pools_check("kv keep", k_pool, v_pool, page_bytes);
+  if (rc != ASYM_OK) return rc;
+  if (page_bytes % (16 * kKvPageTokens))
+    return fail(ASYM_EUNSUPPORTED, "kv keep: pages must hold 32 tokens one after the other, of a multiple of 16 bytes each");
+  if (T < 0) return fail(ASYM_EINVAL, "kv keep: T must be >= 0");
+  if (n == 0) return ASYM_OK;
+  if (!rows || !cu || !count || (T && !path)) return fail(ASYM_EINVAL, "kv keep: null pointer");
+  if (((uintptr_t)rows | (uintptr_t)cu | (uintptr_t)path | (uintptr_t)count) & 3u)
+    return fail(ASYM_EINVAL, "kv keep: rows, offsets, paths and counts must be 4-byte aligned");
+  p.a = rows;
+  p.k_pool = static_cast<uint8_t*>(k_pool);
+  p.v_pool = static_cast<uint8_t*>(v_pool);
+  p.page_bytes = (int64_t)page_bytes;
+  // a thread a 16-byte word of a token, as far as a workgroup goes
+  const int64_t columns = (int64_t)H * (int64_t)(page_bytes / (16 * kKvPageTokens)) * (v_pool ? 2 : 1);
+  const unsigned threads = (unsigned)std::min<int64_t>((columns + 63) / 64 * 64, kSmallThreads);
+  hipLaunchKernelGGL(pages_keep, dim3(n), dim3(threads), 0, static_cast<hipStream_t>(stream), p, T, cu, path, count);
   ASYM_HIP(hipGetLastError());
   return ASYM_OK;
 }
