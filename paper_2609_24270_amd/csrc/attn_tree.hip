@@ -497,6 +497,363 @@ __global__ void __launch_bounds__(64 * kWaves, NB == 1 ? 2 : 1) attn_tree_kernel
   }
 }
 
+// The wide form: NW waves of 32 rows each, all of one request and key/value head, share blocks of 64 tokens (two
+// pages), which stream through LDS (buffer_load ... lds, kStages blocks on their way or in use): what few
+// rows would read from HBM once, many do too.  Waves past the unit's rows load and wait with the others.
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+constexpr int kTokens = 2 * kKvPageTokens;         // of a block
+constexpr int kTileBytes = kTokens * kRowBytes;    // of its keys, or its values
+constexpr int NT = kTokens / 16, NK = kTokens / 32;  // 16-token and 32-token steps
+
+// (for keys: 16 rows, one chunk of each, are read together)
+__device__ __forceinline__ int swz_k(int row) { return row & 15; }
+
+// 1 KiB from lane addresses voff to LDS bytes dst .. dst + 1023, in lane order (the load takes dst from M0, whose write
+// needs a wait state before it, which the compiler does not add here)
+template <int POLICY>
+__device__ __forceinline__ void lds_load_1k(uint32_t dst, i32x4 rs, uint32_t voff) {
+  if constexpr (POLICY)
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen nt lds" ::"s"(dst), "v"(voff), "s"(rs)
+                 : "memory", "m0");
+  else
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(dst), "v"(voff), "s"(rs)
+                 : "memory", "m0");
+}
+__device__ __forceinline__ i32x4 page_words(const uint8_t* pool, int page, int pool_pages) {
+  const bool in = page >= 0 && page < pool_pages;
+  const uint64_t a = (uint64_t)pool + (uint64_t)(uint32_t)(in ? page : 0) * kPageBytes;
+  i32x4 r;
+  r[0] = __builtin_amdgcn_readfirstlane((int)(uint32_t)a);
+  r[1] = __builtin_amdgcn_readfirstlane((int)(uint32_t)(a >> 32));
+  r[2] = __builtin_amdgcn_readfirstlane(in ? kPageBytes : 0);  // (a page that is none reads zeros)
+  r[3] = 0x00020000;
+  return r;
+}
+
+template <int NW, int STAGES, int POLICY>
+__global__ void __launch_bounds__(64 * NW, 2) attn_tree_wide(TreeParams p) {
+  constexpr int NQ = 2, WR = 16 * NQ;
+  __shared__ __attribute__((aligned(1024))) unsigned char lds[2 * STAGES * kTileBytes];  // K tiles, then V tiles
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int n = lane & 15, q4 = lane >> 4;
+  const int w = blockIdx.x;
+
+  Batch bt;
+  bt.load(p, 0, 0, lane);
+  int total = bt.end();
+  for (int b = 64; b < p.B; b += 64) {
+    int x = 0;
+    if (b + lane < p.B) {
+      const Request r = request(p, b + lane);
+      x = r.units * r.pages;
+    }
+    total += wave_sum(x);
+  }
+  total *= p.Hkv;
+  const int share = p.share_pages ? p.share_pages : max((total + p.shares - 1) / p.shares, p.least);
+  if ((int64_t)w * share >= total) return;
+  int f = w * share;
+  const int f1 = min(f + share, total);
+
+  const uint32_t lds0 = (uint32_t)(size_t)lds;
+  uint32_t ka[4], va[8];  // a lane's places in the tiles: key n of 16, chunks 4 c + q; V^T operand g
+#pragma unroll
+  for (int c = 0; c < 4; ++c) ka[c] = (uint32_t)(n * kRowBytes + (((4 * c + q4) ^ swz_k(n)) << 4));
+#pragma unroll
+  for (int g = 0; g < 8; ++g) va[g] = v_place(g, lane);
+  // 1 KiB is 4 rows of a tile, 16 KiB of keys and 16 of values a block: the wave's pieces lie in one of its two pages
+  constexpr int PIECES = kTileBytes / 1024 / NW;
+  const int half = wave * PIECES / 8;
+  uint32_t ko[PIECES], vo[PIECES];  // from the page's start
+#pragma unroll
+  for (int i = 0; i < PIECES; ++i) {
+    const int r = 4 * (wave * PIECES + i) + (lane >> 4);
+    ko[i] = (uint32_t)((r & 31) * kRowBytes + (((lane & 15) ^ swz_k(r)) << 4));
+    vo[i] = (uint32_t)((r & 31) * kRowBytes + (((lane & 15) ^ swz(r)) << 4));
+  }
+  auto k_tile = [&](int j) { return (lds_byte*)lds + (j % STAGES) * kTileBytes; };
+  auto v_tile = [&](int j) { return (lds_byte*)lds + (STAGES + j % STAGES) * kTileBytes; };
+
+  for (bool start = true; f < f1; start = false) {
+    // the segment: request b, unit, head hk, its pages pg .. pg + count - 1
+    while (bt.end() * p.Hkv <= f) bt.load(p, bt.base + 64, bt.end(), lane);
+    const int at = __builtin_ctzll(__ballot(bt.upto * p.Hkv > f));
+    const int b = bt.base + at;
+    const int first = __builtin_amdgcn_readlane(bt.r.first, at), nodes = __builtin_amdgcn_readlane(bt.r.n, at);
+    const int len = __builtin_amdgcn_readlane(bt.r.len, at), units = __builtin_amdgcn_readlane(bt.r.units, at);
+    const int pages = __builtin_amdgcn_readlane(bt.r.pages, at);
+    const int in = f - (__builtin_amdgcn_readlane(bt.upto, at) - units * pages) * p.Hkv;
+    const int unit = in / (p.Hkv * pages), hk = (in - unit * p.Hkv * pages) / pages, pg = in % pages;
+    const int count = min(pages - pg, f1 - f);
+    const int64_t row0 = (int64_t)unit * p.rows;
+    const int rows = (int)min((int64_t)nodes * p.G - row0, (int64_t)p.rows);  // of the unit
+    const bool work = wave * WR < rows;
+    const int64_t base = (int64_t)len - nodes;
+    const int nblk = (count + 1) / 2;
+    // blocks of two pages of the segment that every row sees whole
+    const int64_t whole_pages = base < 0 ? 0 : base / kKvPageTokens - pg;
+    const int nfull = (int)max<int64_t>(0, min<int64_t>(whole_pages, count) / 2);
+
+    const size_t entry = ((size_t)b * p.Hkv + hk) * p.pph + pg + half;
+    auto numbers = [&](int j, int& k, int& v) {  // of the wave's pages of 64 blocks, one a lane
+      k = v = -1;
+      if (2 * (j + lane) + half < count) {
+        k = p.k_pages[entry + 2 * (size_t)(j + lane)];
+        v = p.v_pages[entry + 2 * (size_t)(j + lane)];
+      }
+    };
+    int kpg, vpg, kpg2, vpg2;
+    numbers(0, kpg, vpg);
+    numbers(64, kpg2, vpg2);
+    auto load = [&](int j) {  // block j (behind the last: none, which loads nothing); j rises by one from call to call
+      const int e = j & 63;
+      if (e == 0 && j) {
+        kpg = kpg2;
+        vpg = vpg2;
+        numbers(j + 64, kpg2, vpg2);
+      }
+      const i32x4 rk = page_words(p.k_pool, __builtin_amdgcn_readlane(kpg, e), p.pool_pages);
+      const i32x4 rv = page_words(p.v_pool, __builtin_amdgcn_readlane(vpg, e), p.pool_pages);
+      const uint32_t dst = lds0 + (uint32_t)(j % STAGES) * kTileBytes + (uint32_t)(wave * PIECES) * 1024;
+#pragma unroll
+      for (int i = 0; i < PIECES; ++i) lds_load_1k<POLICY>(dst + i * 1024, rk, ko[i]);
+#pragma unroll
+      for (int i = 0; i < PIECES; ++i) lds_load_1k<POLICY>(dst + STAGES * kTileBytes + i * 1024, rv, vo[i]);
+    };
+    // this wave's loads of a block, of which STAGES - 1 are on their way, and with them everyone's
+    auto arrived = [&] {
+      asm volatile("s_waitcnt vmcnt(%0)" ::"n"((STAGES - 2) * 2 * PIECES) : "memory");
+      __syncthreads();
+    };
+#pragma unroll
+    for (int j = 0; j < STAGES - 1; ++j) load(j);
+
+    // this lane's rows, one of each block of 16 (rows past the last repeat it, and are not stored)
+    bf16x8 qf[NQ][4];
+#pragma unroll
+    for (int k = 0; k < NQ; ++k) {
+      const int64_t row = row0 + min(wave * WR + 16 * k + n, rows - 1);
+      const int tok = (int)(row / p.G), g = (int)(row - (int64_t)tok * p.G);
+      const uint16_t* qr = p.q + (int64_t)(first + tok) * p.q_tok + ((int64_t)hk * p.G + g) * p.q_head + 8 * q4;
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        u32x4 x = *reinterpret_cast<const u32x4*>(qr + 32 * c);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[e] ^= p.q_flip;
+        qf[k][c] = __builtin_bit_cast(bf16x8, x);
+      }
+    }
+    f32x4 o[NQ][8], s[NQ][NT];
+    bf16x8 pf[NQ][NK];
+    float m[NQ], l[NQ];
+#pragma unroll
+    for (int k = 0; k < NQ; ++k) {
+      m[k] = -INFINITY;
+      l[k] = 0.f;
+#pragma unroll
+      for (int g = 0; g < 8; ++g) o[k][g] = f32x4{};
+    }
+    auto scores = [&](int j) {
+      const lds_byte* kt = k_tile(j);
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          const bf16x8 x = *(const __attribute__((address_space(3))) bf16x8*)(kt + ka[c] + t * 16 * kRowBytes);
+#pragma unroll
+          for (int k = 0; k < NQ; ++k)
+            s[k][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, qf[k][c], c ? s[k][t] : f32x4{}, 0, 0, 0);
+        }
+    };
+    auto softmax = [&] {
+      bool up = false;
+      float top[NQ];
+#pragma unroll
+      for (int k = 0; k < NQ; ++k) {
+        float x = fmaxf(fmaxf(s[k][0][0], s[k][0][1]), s[k][0][2]);
+#pragma unroll
+        for (int i = 3; i + 1 < 4 * NT; i += 2) x = fmaxf(fmaxf(x, s[k][i >> 2][i & 3]), s[k][(i + 1) >> 2][(i + 1) & 3]);
+        x = fmaxf(x, s[k][NT - 1][3]);
+        top[k] = over_quarters(x, [](float x, float y) { return fmaxf(x, y); });
+        up |= (top[k] - m[k]) * p.c > 8.f;  // (a first finite max: inf; NaN never)
+      }
+      if (__any(up)) {
+#pragma unroll
+        for (int k = 0; k < NQ; ++k) {
+          const float m_new = fmaxf(m[k], top[k]);
+          const float alpha = __builtin_amdgcn_exp2f((m[k] - (m_new == -INFINITY ? 0.f : m_new)) * p.c);
+          l[k] *= alpha;
+#pragma unroll
+          for (int g = 0; g < 8; ++g) o[k][g] *= alpha;
+          m[k] = m_new;
+        }
+      }
+#pragma unroll
+      for (int k = 0; k < NQ; ++k) {
+        const float ms = m[k] == -INFINITY ? 0.f : m[k];
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            // (the difference first: scores of the type's lowest values times c would be infinite)
+            const float e = __builtin_amdgcn_exp2f((s[k][t][r] - ms) * p.c);
+            l[k] += e;
+            pf[k][t >> 1][4 * (t & 1) + r] = (__bf16)e;
+          }
+      }
+    };
+    auto v_op = [&](const lds_byte* vt, int g, int ks) { return v_frag(vt, va[g] + (uint32_t)(32 * ks * kRowBytes)); };
+    auto add_pv = [&](int j) {
+      const lds_byte* vt = v_tile(j);
+#pragma unroll
+      for (int ks = 0; ks < NK; ++ks)
+#pragma unroll
+        for (int g = 0; g < 8; ++g) {
+          const bf16x8 x = v_op(vt, g, ks);
+#pragma unroll
+          for (int k = 0; k < NQ; ++k) o[k][g] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, pf[k][ks], o[k][g], 0, 0, 0);
+        }
+    };
+
+    for (int j = 0; j < nfull; ++j) {
+      arrived();
+      load(j + STAGES - 1);
+      if (work) {
+        scores(j);
+        softmax();
+        add_pv(j);
+      }
+    }
+    // Blocks that hold nodes, end behind the tokens or with the segment (see add_page for the infinities and NaN among
+    // masked values; here their whole numbers take the keys' place)
+    for (int j = nfull; j < nblk; ++j) {
+      arrived();
+      load(j + STAGES - 1);
+      auto each_word = [&](auto f) {  // the thread's words of the V tile
+#pragma unroll
+        for (int i = 0; i < kTileBytes / 16 / (64 * NW); ++i) {
+          const uint32_t x = (uint32_t)(i * 64 * NW + (int)threadIdx.x) * 16;
+          f(x, *(lds_u32x4*)(v_tile(j) + x));
+        }
+      };
+      uint32_t bad = 0;
+      each_word([&](uint32_t, u32x4 x) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) bad |= (x[e] & 0x7F807F80u) + 0x00800080u;  // an exponent of all ones carries
+      });
+      const bool guard = __syncthreads_or((bad & 0x80008000u) != 0);
+      uint32_t seen[NQ][2];
+      if (work) {
+#pragma unroll
+        for (int k = 0; k < NQ; ++k) {
+          const int64_t row = row0 + min(wave * WR + 16 * k + n, rows - 1);
+          const int i = (int)(row / p.G);
+          const uint64_t* words = p.mask ? p.mask + (int64_t)(first + i) * p.words : nullptr;
+#pragma unroll
+          for (int h = 0; h < 2; ++h) seen[k][h] = 2 * j + h < count ? seen_bits(p, words, i, nodes, base, pg + 2 * j + h) : 0u;
+        }
+        scores(j);
+#pragma unroll
+        for (int k = 0; k < NQ; ++k)
+#pragma unroll
+          for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+              if (!((seen[k][t >> 1] >> (16 * (t & 1) + 4 * q4 + r)) & 1)) s[k][t][r] = -INFINITY;
+        softmax();
+      }
+      if (guard) {
+        __syncthreads();  // (the K tile has been read)
+        each_word([&](uint32_t at, u32x4 x) {
+          u32x4 fin, code;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {  // two values a word
+            const uint32_t mask = ((((x[e] & 0x7F807F80u) + 0x00800080u) >> 15) & 0x00010001u) * 0xFFFFu;
+            auto kind = [](uint32_t u) { return (u & 0x7Fu) ? 0x4680u : (u & 0x8000u) ? 0x4300u : 0x3F80u; };
+            fin[e] = x[e] & ~mask;
+            code[e] = (kind(x[e] & 0xFFFFu) | (kind(x[e] >> 16) << 16)) & mask;
+          }
+          *(lds_u32x4*)(v_tile(j) + at) = fin;
+          *(lds_u32x4*)(k_tile(j) + at) = code;
+        });
+        __syncthreads();
+        if (work) {
+#pragma unroll
+          for (int k = 0; k < NQ; ++k)
+#pragma unroll
+            for (int g = 0; g < 8; ++g) {
+              __builtin_amdgcn_sched_barrier(0);  // (one product's registers at a time)
+              f32x4 x = {};
+#pragma unroll
+              for (int ks = 0; ks < NK; ++ks) {
+                u32x4 vis;
+                const uint32_t bits = seen[k][ks] >> (4 * q4);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                  const int i = 16 * (e >> 1) + 2 * (e & 1);
+                  vis[e] = (((bits >> i) & 1) ? 0x3F80u : 0u) | (((bits >> (i + 1)) & 1) ? 0x3F800000u : 0u);
+                }
+                x = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v_op(k_tile(j), g, ks), __builtin_bit_cast(bf16x8, vis), x, 0, 0, 0);
+              }
+#pragma unroll
+              for (int r = 0; r < 4; ++r) {
+                const int c = (int)x[r];
+                o[k][g][r] += ((c & 127) ? INFINITY : 0.f) + (((c >> 7) & 127) ? -INFINITY : 0.f) + (c >= 16384 ? NAN : 0.f);
+              }
+            }
+        }
+      }
+      if (work) add_pv(j);
+    }
+
+    const bool whole = count == pages;
+    const size_t piece = ((size_t)w * 2 + (start ? 0 : 1)) * p.rows;
+    if (work) {
+#pragma unroll
+      for (int k = 0; k < NQ; ++k) {
+        const float lt = over_quarters(l[k], [](float x, float y) { return x + y; });
+        const int in_unit = wave * WR + 16 * k + n;
+        const bool on = in_unit < rows;
+        if (!whole) {  // the unscaled output, max and sum to the joining launch
+          if (on) {
+            float* po = p.part_o + (piece + in_unit) * kKvD + 4 * q4;
+#pragma unroll
+            for (int g = 0; g < 8; ++g) *reinterpret_cast<f32x4*>(po + 16 * g) = o[k][g];
+            if (q4 == 0) *reinterpret_cast<float2*>(p.part_ml + (piece + in_unit) * 2) = float2{m[k], lt};
+          }
+          continue;
+        }
+        // a lane has 4 of every 16 channels of a row; two groups of them, exchanged between the quarters, make 16 bytes
+        const float inv = lt > 0.f ? 1.f / lt : (lt == 0.f ? 0.f : lt);  // (NaN stays)
+        const int64_t row = row0 + min(in_unit, rows - 1);
+        const int tok = (int)(row / p.G);
+        const int64_t out = (int64_t)(first + tok) * p.Hq + (int64_t)hk * p.G + (row - (int64_t)tok * p.G);
+#pragma unroll
+        for (int g = 0; g < 8; g += 2) {
+          uint32_t x[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const f32x4& y = o[k][g + (e >> 1)];
+            const bf16x2 z = {(__bf16)(y[2 * (e & 1)] * inv), (__bf16)(y[2 * (e & 1) + 1] * inv)};
+            x[e] = __builtin_bit_cast(uint32_t, z);
+          }
+          const auto y = __builtin_amdgcn_permlane16_swap(x[0], x[2], false, false);
+          const auto z = __builtin_amdgcn_permlane16_swap(x[1], x[3], false, false);
+          // quarter 0: channels 0 .. 7 of group g, 1: 0 .. 7 of group g + 1, 2: 8 .. 15 of g, 3: of g + 1
+          if (on) *reinterpret_cast<u32x4*>(p.o + out * kKvD + 16 * (g + (q4 & 1)) + 8 * (q4 >> 1)) = u32x4{y[0], z[0], y[1], z[1]};
+        }
+        if (p.lse && on && q4 == 0) p.lse[out] = lt == 0.f ? -INFINITY : m[k] * p.scale + __logf(lt);
+      }
+    }
+    if (pg == 0 && threadIdx.x == 0)
+      p.cut[unit_id(p, b, first, unit) * p.Hkv + hk] = whole ? int2{-1, 0} : int2{2 * w + (start ? 0 : 1), (f + pages - 1) / share};
+    f += count;
+    // (the tiles have been read, and no load to them is left)
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+  }
+}
+
 // A wave a (token, query head): one whose request has no tokens is written, one that was cut is joined.
 __global__ void __launch_bounds__(64 * kJoinWaves) attn_tree_join(TreeParams p) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -557,7 +914,8 @@ __global__ void __launch_bounds__(64 * kJoinWaves) attn_tree_join(TreeParams p) 
 }
 
 struct TreePlan {
-  int nb = 1, rows = 64, shares = 0, share_pages = 0, least = 1;
+  int waves = 0;  // of the wide form (0: the narrow one)
+  int rows = 64, shares = 0, share_pages = 0, least = 1;
   int64_t units = 0;
   size_t bytes = 0;
 };
@@ -574,8 +932,8 @@ int tree_plan(int B, int Hq, int Hkv, int T, int S, int split_tokens, TreePlan* 
     return ASYM_OK;
   }
   const int64_t all = (int64_t)T * (Hq / Hkv), mean = (all + B - 1) / B;
-  P.nb = mean <= 16 ? 1 : 2;
-  P.rows = 64 * P.nb;
+  P.waves = mean <= 16 ? 0 : mean <= 128 ? 4 : 8;
+  P.rows = P.waves ? 32 * P.waves : 64;
   P.units = all / P.rows + B;
   const int64_t pages = ((int64_t)S + kKvPageTokens - 1) / kKvPageTokens, heads = P.units * Hkv;
   if (heads > (1 << 30) || heads * pages > (1 << 30)) return fail(ASYM_EUNSUPPORTED, "tree attention: more than 2^30 pages");
@@ -583,7 +941,7 @@ int tree_plan(int B, int Hq, int Hkv, int T, int S, int split_tokens, TreePlan* 
   P.share_pages = split_tokens / kKvPageTokens;
   P.least = P.share_pages ? P.share_pages : 4;
   int64_t shares = (heads * pages + P.least - 1) / P.least;
-  if (!P.share_pages) shares = std::min<int64_t>(shares, P.nb == 1 ? 512 : 256);
+  if (!P.share_pages) shares = std::min<int64_t>(shares, P.waves == 8 ? 256 : 512);
   if (shares >= (1 << 22)) return fail(ASYM_EUNSUPPORTED, "tree attention: too many shares");
   P.shares = (int)shares;
   P.bytes = (size_t)shares * 2 * P.rows * (kKvD + 2) * sizeof(float) + (size_t)heads * sizeof(int2);
@@ -651,9 +1009,10 @@ extern "C" int asym_attn_tree_paged_bf16(int B, int H_q, int H_kv, int T, int S_
   // (at most: the requests may be shorter than S_max)
   const int64_t bytes = 2ll * B * H_kv * ((S_max + (int64_t)kKvPageTokens - 1) / kKvPageTokens) * kPageBytes;
   const bool once = attn_streams_kv(paged_kv_bytes(bytes, (int64_t)pool_pages * kPageBytes, k_pool == v_pool));
-  auto kernel = P.nb == 1 ? (once ? attn_tree_kernel<1, 2> : attn_tree_kernel<1, 0>)
-                          : (once ? attn_tree_kernel<2, 2> : attn_tree_kernel<2, 0>);
-  hipLaunchKernelGGL(kernel, dim3((unsigned)P.shares), dim3(64 * kWaves), 0, s, p);
+  auto kernel = P.waves == 8   ? (once ? attn_tree_wide<8, 4, 2> : attn_tree_wide<8, 4, 0>)
+                : P.waves == 4 ? (once ? attn_tree_wide<4, 2, 2> : attn_tree_wide<4, 2, 0>)
+                               : (once ? attn_tree_kernel<1, 2> : attn_tree_kernel<1, 0>);
+  hipLaunchKernelGGL(kernel, dim3((unsigned)P.shares), dim3(64 * (P.waves ? P.waves : kWaves)), 0, s, p);
   ASYM_HIP(hipGetLastError());
   const int64_t out = (int64_t)T * H_q;
   hipLaunchKernelGGL(attn_tree_join, dim3((unsigned)((out + kJoinWaves - 1) / kJoinWaves)), dim3(64 * kJoinWaves), 0, s, p);
