@@ -530,27 +530,44 @@ __device__ __forceinline__ i32x4 page_words(const uint8_t* pool, int page, int p
   return r;
 }
 
+// f, N times
+template <int N, class F>
+__device__ __forceinline__ void steps(F f) {
+  if constexpr (N > 0) {
+    f();
+    steps<N - 1>(f);
+  }
+}
+
+// The kernel's arguments, read again (scalar loads): what a phase needs of them does not stay in registers through the others
+__device__ __forceinline__ TreeParams arguments() {
+  auto at = (const __attribute__((address_space(4))) TreeParams*)__builtin_amdgcn_kernarg_segment_ptr();
+  asm volatile("" : "+s"(at));
+  return *(const TreeParams*)at;
+}
+
 template <int NW, int STAGES, int POLICY>
-__global__ void __launch_bounds__(64 * NW, 2) attn_tree_wide(TreeParams p) {
+__global__ void __launch_bounds__(64 * NW, 2) attn_tree_wide(TreeParams args) {
   constexpr int NQ = 2, WR = 16 * NQ;
   __shared__ __attribute__((aligned(1024))) unsigned char lds[2 * STAGES * kTileBytes];  // K tiles, then V tiles
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int n = lane & 15, q4 = lane >> 4;
   const int w = blockIdx.x;
 
+  const TreeParams p0 = arguments();
   Batch bt;
-  bt.load(p, 0, 0, lane);
+  bt.load(p0, 0, 0, lane);
   int total = bt.end();
-  for (int b = 64; b < p.B; b += 64) {
+  for (int b = 64; b < p0.B; b += 64) {
     int x = 0;
-    if (b + lane < p.B) {
-      const Request r = request(p, b + lane);
+    if (b + lane < p0.B) {
+      const Request r = request(p0, b + lane);
       x = r.units * r.pages;
     }
     total += wave_sum(x);
   }
-  total *= p.Hkv;
-  const int share = p.share_pages ? p.share_pages : max((total + p.shares - 1) / p.shares, p.least);
+  total *= p0.Hkv;
+  const int share = p0.share_pages ? p0.share_pages : max((total + p0.shares - 1) / p0.shares, p0.least);
   if ((int64_t)w * share >= total) return;
   int f = w * share;
   const int f1 = min(f + share, total);
@@ -575,6 +592,7 @@ __global__ void __launch_bounds__(64 * NW, 2) attn_tree_wide(TreeParams p) {
   auto v_tile = [&](int j) { return (lds_byte*)lds + (STAGES + j % STAGES) * kTileBytes; };
 
   for (bool start = true; f < f1; start = false) {
+    const TreeParams p = arguments();
     // the segment: request b, unit, head hk, its pages pg .. pg + count - 1
     while (bt.end() * p.Hkv <= f) bt.load(p, bt.base + 64, bt.end(), lane);
     const int at = __builtin_ctzll(__ballot(bt.upto * p.Hkv > f));
@@ -602,23 +620,33 @@ __global__ void __launch_bounds__(64 * NW, 2) attn_tree_wide(TreeParams p) {
         v = p.v_pages[entry + 2 * (size_t)(j + lane)];
       }
     };
-    int kpg, vpg, kpg2, vpg2;
+    int kpg, vpg, kpg2, vpg2;  // of blocks chunk .. chunk + 63, and of the next 64
     numbers(0, kpg, vpg);
     numbers(64, kpg2, vpg2);
-    auto load = [&](int j) {  // block j (behind the last: none, which loads nothing); j rises by one from call to call
+    // (waited for here and not, by the compiler, at every use in the loops below, the tiles' loads with them)
+    auto settle = [&] { asm volatile("" : "+v"(kpg), "+v"(vpg), "+v"(kpg2), "+v"(vpg2)); };
+    settle();
+    int chunk = 0;
+    auto load = [&](int j) {  // block j, chunk <= j < chunk + 128 (behind the last: none, which loads nothing)
       const int e = j & 63;
-      if (e == 0 && j) {
-        kpg = kpg2;
-        vpg = vpg2;
-        numbers(j + 64, kpg2, vpg2);
-      }
-      const i32x4 rk = page_words(p.k_pool, __builtin_amdgcn_readlane(kpg, e), p.pool_pages);
-      const i32x4 rv = page_words(p.v_pool, __builtin_amdgcn_readlane(vpg, e), p.pool_pages);
+      const bool next = j >= chunk + 64;
+      const int kn = __builtin_amdgcn_readlane(kpg, e), kn2 = __builtin_amdgcn_readlane(kpg2, e);
+      const int vn = __builtin_amdgcn_readlane(vpg, e), vn2 = __builtin_amdgcn_readlane(vpg2, e);
+      const i32x4 rk = page_words(p.k_pool, next ? kn2 : kn, p.pool_pages);
+      const i32x4 rv = page_words(p.v_pool, next ? vn2 : vn, p.pool_pages);
       const uint32_t dst = lds0 + (uint32_t)(j % STAGES) * kTileBytes + (uint32_t)(wave * PIECES) * 1024;
 #pragma unroll
       for (int i = 0; i < PIECES; ++i) lds_load_1k<POLICY>(dst + i * 1024, rk, ko[i]);
 #pragma unroll
       for (int i = 0; i < PIECES; ++i) lds_load_1k<POLICY>(dst + STAGES * kTileBytes + i * 1024, rv, vo[i]);
+    };
+    auto turn_chunk = [&](int j) {  // before block j: the next 64 blocks' pages
+      if (j < chunk + 64) return;
+      chunk += 64;
+      kpg = kpg2;
+      vpg = vpg2;
+      numbers(chunk + 64, kpg2, vpg2);
+      settle();
     };
     // this wave's loads of a block, of which STAGES - 1 are on their way, and with them everyone's
     auto arrived = [&] {
@@ -640,9 +668,11 @@ __global__ void __launch_bounds__(64 * NW, 2) attn_tree_wide(TreeParams p) {
         u32x4 x = *reinterpret_cast<const u32x4*>(qr + 32 * c);
 #pragma unroll
         for (int e = 0; e < 4; ++e) x[e] ^= p.q_flip;
+        asm volatile("" : "+v"(x));
         qf[k][c] = __builtin_bit_cast(bf16x8, x);
       }
     }
+    const float c = p.c;
     f32x4 o[NQ][8], s[NQ][NT];
     bf16x8 pf[NQ][NK];
     float m[NQ], l[NQ];
@@ -665,7 +695,7 @@ __global__ void __launch_bounds__(64 * NW, 2) attn_tree_wide(TreeParams p) {
             s[k][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, qf[k][c], c ? s[k][t] : f32x4{}, 0, 0, 0);
         }
     };
-    auto softmax = [&] {
+    auto raise = [&] {
       bool up = false;
       float top[NQ];
 #pragma unroll
@@ -675,32 +705,43 @@ __global__ void __launch_bounds__(64 * NW, 2) attn_tree_wide(TreeParams p) {
         for (int i = 3; i + 1 < 4 * NT; i += 2) x = fmaxf(fmaxf(x, s[k][i >> 2][i & 3]), s[k][(i + 1) >> 2][(i + 1) & 3]);
         x = fmaxf(x, s[k][NT - 1][3]);
         top[k] = over_quarters(x, [](float x, float y) { return fmaxf(x, y); });
-        up |= (top[k] - m[k]) * p.c > 8.f;  // (a first finite max: inf; NaN never)
+        up |= (top[k] - m[k]) * c > 8.f;  // (a first finite max: inf; NaN never)
       }
       if (__any(up)) {
 #pragma unroll
         for (int k = 0; k < NQ; ++k) {
           const float m_new = fmaxf(m[k], top[k]);
-          const float alpha = __builtin_amdgcn_exp2f((m[k] - (m_new == -INFINITY ? 0.f : m_new)) * p.c);
+          const float alpha = __builtin_amdgcn_exp2f((m[k] - (m_new == -INFINITY ? 0.f : m_new)) * c);
           l[k] *= alpha;
 #pragma unroll
           for (int g = 0; g < 8; ++g) o[k][g] *= alpha;
           m[k] = m_new;
         }
       }
+    };
+    auto weights = [&](int ks) {
 #pragma unroll
       for (int k = 0; k < NQ; ++k) {
         const float ms = m[k] == -INFINITY ? 0.f : m[k];
 #pragma unroll
-        for (int t = 0; t < NT; ++t)
-#pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            // (the difference first: scores of the type's lowest values times c would be infinite)
-            const float e = __builtin_amdgcn_exp2f((s[k][t][r] - ms) * p.c);
-            l[k] += e;
-            pf[k][t >> 1][4 * (t & 1) + r] = (__bf16)e;
-          }
+        for (int j = 0; j < 8; ++j) {
+          // (the difference first: scores of the type's lowest values times c would be infinite; one instruction for both
+          // took 4 % fewer cycles)
+          const float e = __builtin_amdgcn_exp2f((s[k][2 * ks + (j >> 2)][j & 3] - ms) * c);
+          l[k] += e;
+          pf[k][ks][j] = (__bf16)e;
+        }
       }
+    };
+    // (The order of a block's instructions: operands are read from LDS a few ahead of the products that take them.  Each of these
+    // takes the named number of instructions of a kind: 8 products, 0x100 reads.)
+    auto pace = [](auto reads, auto ahead, auto total) {
+      __builtin_amdgcn_sched_group_barrier(0x100, decltype(reads)::value * decltype(ahead)::value, 0);
+      steps<decltype(total)::value - decltype(ahead)::value>([] {
+        __builtin_amdgcn_sched_group_barrier(8, NQ, 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, decltype(reads)::value, 0);
+      });
+      __builtin_amdgcn_sched_group_barrier(8, NQ * decltype(ahead)::value, 0);
     };
     auto v_op = [&](const lds_byte* vt, int g, int ks) { return v_frag(vt, va[g] + (uint32_t)(32 * ks * kRowBytes)); };
     auto add_pv = [&](int j) {
@@ -715,24 +756,41 @@ __global__ void __launch_bounds__(64 * NW, 2) attn_tree_wide(TreeParams p) {
         }
     };
 
-    for (int j = 0; j < nfull; ++j) {
-      arrived();
-      load(j + STAGES - 1);
-      if (work) {
-        scores(j);
-        softmax();
-        add_pv(j);
+    for (int j0 = 0; j0 < nfull; j0 += 64) {
+      turn_chunk(j0);
+      const int j1 = min(j0 + 64, nfull);
+      for (int j = j0; j < j1; ++j) {
+        arrived();
+        load(j + STAGES - 1);
+        if (work) {
+          // (the waves in step with each other otherwise: one that is at it goes on before the others)
+          __builtin_amdgcn_s_setprio(1);
+          scores(j);
+          pace(std::integral_constant<int, 1>{}, std::integral_constant<int, 4>{}, std::integral_constant<int, 4 * NT>{});
+          raise();
+          weights(0);
+          weights(1);
+          add_pv(j);
+          pace(std::integral_constant<int, 2>{}, std::integral_constant<int, 4>{}, std::integral_constant<int, 8 * NK>{});
+          __builtin_amdgcn_s_setprio(0);
+        }
       }
     }
+    const TreeParams edge = arguments();
     // Blocks that hold nodes, end behind the tokens or with the segment (see add_page for the infinities and NaN among
     // masked values; here their whole numbers take the keys' place)
     for (int j = nfull; j < nblk; ++j) {
+      turn_chunk(j);
       arrived();
       load(j + STAGES - 1);
+      // (what depends on the lane is computed here again: kept through the loop above, it would take registers there)
+      int tid = (int)threadIdx.x;
+      asm volatile("" : "+v"(tid));
+      const int n = tid & 15, q4 = (tid >> 4) & 3;
       auto each_word = [&](auto f) {  // the thread's words of the V tile
 #pragma unroll
         for (int i = 0; i < kTileBytes / 16 / (64 * NW); ++i) {
-          const uint32_t x = (uint32_t)(i * 64 * NW + (int)threadIdx.x) * 16;
+          const uint32_t x = (uint32_t)(i * 64 * NW + tid) * 16;
           f(x, *(lds_u32x4*)(v_tile(j) + x));
         }
       };
@@ -747,10 +805,10 @@ __global__ void __launch_bounds__(64 * NW, 2) attn_tree_wide(TreeParams p) {
 #pragma unroll
         for (int k = 0; k < NQ; ++k) {
           const int64_t row = row0 + min(wave * WR + 16 * k + n, rows - 1);
-          const int i = (int)(row / p.G);
-          const uint64_t* words = p.mask ? p.mask + (int64_t)(first + i) * p.words : nullptr;
+          const int i = (int)(row / edge.G);
+          const uint64_t* words = edge.mask ? edge.mask + (int64_t)(first + i) * edge.words : nullptr;
 #pragma unroll
-          for (int h = 0; h < 2; ++h) seen[k][h] = 2 * j + h < count ? seen_bits(p, words, i, nodes, base, pg + 2 * j + h) : 0u;
+          for (int h = 0; h < 2; ++h) seen[k][h] = 2 * j + h < count ? seen_bits(edge, words, i, nodes, base, pg + 2 * j + h) : 0u;
         }
         scores(j);
 #pragma unroll
@@ -760,7 +818,9 @@ __global__ void __launch_bounds__(64 * NW, 2) attn_tree_wide(TreeParams p) {
 #pragma unroll
             for (int r = 0; r < 4; ++r)
               if (!((seen[k][t >> 1] >> (16 * (t & 1) + 4 * q4 + r)) & 1)) s[k][t][r] = -INFINITY;
-        softmax();
+        raise();
+        weights(0);
+        weights(1);
       }
       if (guard) {
         __syncthreads();  // (the K tile has been read)
@@ -806,8 +866,9 @@ __global__ void __launch_bounds__(64 * NW, 2) attn_tree_wide(TreeParams p) {
       if (work) add_pv(j);
     }
 
+    const TreeParams last = arguments();
     const bool whole = count == pages;
-    const size_t piece = ((size_t)w * 2 + (start ? 0 : 1)) * p.rows;
+    const size_t piece = ((size_t)w * 2 + (start ? 0 : 1)) * last.rows;
     if (work) {
 #pragma unroll
       for (int k = 0; k < NQ; ++k) {
@@ -816,18 +877,18 @@ __global__ void __launch_bounds__(64 * NW, 2) attn_tree_wide(TreeParams p) {
         const bool on = in_unit < rows;
         if (!whole) {  // the unscaled output, max and sum to the joining launch
           if (on) {
-            float* po = p.part_o + (piece + in_unit) * kKvD + 4 * q4;
+            float* po = last.part_o + (piece + in_unit) * kKvD + 4 * q4;
 #pragma unroll
             for (int g = 0; g < 8; ++g) *reinterpret_cast<f32x4*>(po + 16 * g) = o[k][g];
-            if (q4 == 0) *reinterpret_cast<float2*>(p.part_ml + (piece + in_unit) * 2) = float2{m[k], lt};
+            if (q4 == 0) *reinterpret_cast<float2*>(last.part_ml + (piece + in_unit) * 2) = float2{m[k], lt};
           }
           continue;
         }
         // a lane has 4 of every 16 channels of a row; two groups of them, exchanged between the quarters, make 16 bytes
         const float inv = lt > 0.f ? 1.f / lt : (lt == 0.f ? 0.f : lt);  // (NaN stays)
         const int64_t row = row0 + min(in_unit, rows - 1);
-        const int tok = (int)(row / p.G);
-        const int64_t out = (int64_t)(first + tok) * p.Hq + (int64_t)hk * p.G + (row - (int64_t)tok * p.G);
+        const int tok = (int)(row / last.G);
+        const int64_t out = (int64_t)(first + tok) * last.Hq + (int64_t)hk * last.G + (row - (int64_t)tok * last.G);
 #pragma unroll
         for (int g = 0; g < 8; g += 2) {
           uint32_t x[4];
@@ -840,13 +901,13 @@ __global__ void __launch_bounds__(64 * NW, 2) attn_tree_wide(TreeParams p) {
           const auto y = __builtin_amdgcn_permlane16_swap(x[0], x[2], false, false);
           const auto z = __builtin_amdgcn_permlane16_swap(x[1], x[3], false, false);
           // quarter 0: channels 0 .. 7 of group g, 1: 0 .. 7 of group g + 1, 2: 8 .. 15 of g, 3: of g + 1
-          if (on) *reinterpret_cast<u32x4*>(p.o + out * kKvD + 16 * (g + (q4 & 1)) + 8 * (q4 >> 1)) = u32x4{y[0], z[0], y[1], z[1]};
+          if (on) *reinterpret_cast<u32x4*>(last.o + out * kKvD + 16 * (g + (q4 & 1)) + 8 * (q4 >> 1)) = u32x4{y[0], z[0], y[1], z[1]};
         }
-        if (p.lse && on && q4 == 0) p.lse[out] = lt == 0.f ? -INFINITY : m[k] * p.scale + __logf(lt);
+        if (last.lse && on && q4 == 0) last.lse[out] = lt == 0.f ? -INFINITY : m[k] * last.scale + __logf(lt);
       }
     }
     if (pg == 0 && threadIdx.x == 0)
-      p.cut[unit_id(p, b, first, unit) * p.Hkv + hk] = whole ? int2{-1, 0} : int2{2 * w + (start ? 0 : 1), (f + pages - 1) / share};
+      last.cut[unit_id(last, b, first, unit) * last.Hkv + hk] = whole ? int2{-1, 0} : int2{2 * w + (start ? 0 : 1), (f + pages - 1) / share};
     f += count;
     // (the tiles have been read, and no load to them is left)
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
