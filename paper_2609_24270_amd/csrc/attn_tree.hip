@@ -40,7 +40,6 @@
 namespace asym {
 namespace {
 
-constexpr int kWaves = 4;
 constexpr int kRowBytes = kKvD * 2;
 constexpr int kPageBytes = kKvPageTokens * kRowBytes;
 constexpr int kJoinWaves = 4;
@@ -52,7 +51,6 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) unsigned char lds_byte;
 typedef __attribute__((address_space(3))) u32x4 lds_u32x4;
-typedef __attribute__((address_space(3))) f32x4 lds_f32x4;
 
 struct TreeParams {
   const uint16_t* q;
@@ -75,12 +73,6 @@ struct TreeParams {
   float c, scale;                // |scale| * log2(e), |scale|
   uint32_t q_flip;
 };
-
-__device__ __forceinline__ __amdgpu_buffer_rsrc_t page_of(const uint8_t* pool, int page, int pool_pages) {
-  const bool in = page >= 0 && page < pool_pages;
-  const uint64_t a = (uint64_t)pool + (uint64_t)(uint32_t)(in ? page : 0) * kPageBytes;
-  return __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void*>(a), (short)0, in ? kPageBytes : 0, 0x00020000);
-}
 
 // f over this lane and those 16, 32 and 48 on: the four that share a row
 template <class F>
@@ -124,30 +116,6 @@ struct Batch {
   __device__ __forceinline__ int end() const { return __builtin_amdgcn_readlane(upto, 63); }
 };
 
-template <int NB>
-struct Wave {
-  f32x4 o[NB][8];
-  float m[NB], l[NB];
-};
-struct PageRegs {
-  u32x4 k[8], v[8];
-};
-
-template <int POLICY>
-__device__ __forceinline__ void load_page(const TreeParams& p, int kp, int vp, int lane, PageRegs& r) {
-  const __amdgpu_buffer_rsrc_t rk = page_of(p.k_pool, kp, p.pool_pages), rv = page_of(p.v_pool, vp, p.pool_pages);
-  const uint32_t ko = (uint32_t)((lane & 15) * kRowBytes + (lane >> 4) * 16);
-#pragma unroll
-  for (int t = 0; t < 2; ++t)
-#pragma unroll
-    for (int c = 0; c < 4; ++c)
-      r.k[4 * t + c] = __builtin_bit_cast(
-          u32x4, __builtin_amdgcn_raw_buffer_load_b128(rk, ko + (uint32_t)(t * 16 * kRowBytes + 64 * c), 0, POLICY));
-#pragma unroll
-  for (int i = 0; i < 8; ++i)
-    r.v[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rv, (uint32_t)(lane * 16 + 1024 * i), 0, POLICY));
-}
-
 // 16-byte chunk c of V's row t lies at chunk c ^ swz(t), so that the rows that one transposing read takes
 // together (8 rows, two chunks of each) lie on different ones of the 64 banks.
 __device__ __forceinline__ int swz(int row) { return (row & 7) << 1; }
@@ -168,20 +136,6 @@ __device__ __forceinline__ bf16x8 v_frag(const lds_byte* vt, uint32_t at) {
     u.s[part] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(vt + at + 16 * part * kRowBytes));
   return u.b;
 }
-// (what one lane writes and others of its wave read)
-__device__ __forceinline__ void wave_lds_order() {
-  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-  __builtin_amdgcn_wave_barrier();
-  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-}
-__device__ __forceinline__ void put_v(lds_byte* vt, int lane, const u32x4* v) {
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const int row = 4 * i + (lane >> 4);
-    *(lds_u32x4*)(vt + row * kRowBytes + (((lane & 15) ^ swz(row)) << 4)) = v[i];
-  }
-}
-
 // Which of tokens 32 page .. + 31 node i sees, a bit each (node 0 is token `base`, which may be negative)
 __device__ __forceinline__ uint32_t seen_bits(const TreeParams& p, const uint64_t* words, int i, int n, int64_t base, int page) {
   const int64_t j0 = (int64_t)page * kKvPageTokens - base;  // the node at the page's first token
@@ -203,303 +157,6 @@ __device__ __forceinline__ uint32_t seen_bits(const TreeParams& p, const uint64_
   return prefix | ((uint32_t)bits & exist);
 }
 
-// 32 tokens.  TAIL: the page holds nodes, or ends behind the request's tokens: `seen` says what each of the lane's rows sees.
-template <int NB, bool TAIL>
-__device__ __forceinline__ void add_page(const TreeParams& p, lds_byte* vt, const bf16x8 (*qf)[4], PageRegs& cur, int lane,
-                                         const uint32_t* seen, int left, Wave<NB>& a) {
-  const int q4 = lane >> 4;
-  if (TAIL && left < kKvPageTokens) {  // (tokens behind the last: no row sees them, whatever lies there)
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-      if (4 * i + q4 >= left) cur.v[i] = u32x4{};
-  }
-  bool guard = false;
-  if constexpr (TAIL) {
-    uint32_t bad = 0;  // an infinity or a NaN among the values: an exponent of all ones carries
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) bad |= (cur.v[i][e] & 0x7F807F80u) + 0x00800080u;
-    guard = __any((bad & 0x80008000u) != 0);
-  }
-  f32x4 s[NB][2];
-#pragma unroll
-  for (int t = 0; t < 2; ++t)
-#pragma unroll
-    for (int c = 0; c < 4; ++c) {
-      const bf16x8 f = __builtin_bit_cast(bf16x8, cur.k[4 * t + c]);
-#pragma unroll
-      for (int b = 0; b < NB; ++b) s[b][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f, qf[b][c], c ? s[b][t] : f32x4{}, 0, 0, 0);
-    }
-  if constexpr (TAIL) {
-#pragma unroll
-    for (int b = 0; b < NB; ++b) {
-      const uint32_t w = seen[b] >> (4 * q4);
-#pragma unroll
-      for (int j = 0; j < 8; ++j)
-        if (!((w >> (16 * (j >> 2) + (j & 3))) & 1)) s[b][j >> 2][j & 3] = -INFINITY;
-    }
-  }
-  bool up = false;
-  float top[NB];
-#pragma unroll
-  for (int b = 0; b < NB; ++b) {
-    const float x = fmaxf(fmaxf(fmaxf(s[b][0][0], s[b][0][1]), fmaxf(s[b][0][2], s[b][0][3])),
-                          fmaxf(fmaxf(s[b][1][0], s[b][1][1]), fmaxf(s[b][1][2], s[b][1][3])));
-    top[b] = over_quarters(x, [](float x, float y) { return fmaxf(x, y); });
-    up |= (top[b] - a.m[b]) * p.c > 8.f;  // (a first finite max: inf; NaN never)
-  }
-  if (__any(up)) {
-#pragma unroll
-    for (int b = 0; b < NB; ++b) {
-      const float m_new = fmaxf(a.m[b], top[b]);
-      const float alpha = __builtin_amdgcn_exp2f((a.m[b] - (m_new == -INFINITY ? 0.f : m_new)) * p.c);
-      a.l[b] *= alpha;
-#pragma unroll
-      for (int g = 0; g < 8; ++g) a.o[b][g] *= alpha;
-      a.m[b] = m_new;
-    }
-  }
-  bf16x8 pf[NB];
-#pragma unroll
-  for (int b = 0; b < NB; ++b) {
-    const float ms = a.m[b] == -INFINITY ? 0.f : a.m[b];
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      // (the difference first: scores of the type's lowest values times c would be infinite)
-      const float e = __builtin_amdgcn_exp2f((s[b][j >> 2][j & 3] - ms) * p.c);
-      a.l[b] += e;
-      pf[b][j] = (__bf16)e;
-    }
-  }
-  if constexpr (TAIL) {
-    // A masked token's probability is 0, but 0 times an infinity or a NaN among its values is NaN, in a row
-    // that does not see it.  Such values are taken out, and a product of the rows' masks with small whole
-    // numbers in their place (1: inf, 128: -inf, 16384: NaN; sums over 32 tokens, exact in fp32) says what
-    // they do to the rows that see them.
-    if (guard) {
-      u32x4 code[8];
-#pragma unroll
-      for (int i = 0; i < 8; ++i)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {  // two values a word
-          const uint32_t w = cur.v[i][e];
-          const uint32_t mask = ((((w & 0x7F807F80u) + 0x00800080u) >> 15) & 0x00010001u) * 0xFFFFu;
-          auto kind = [](uint32_t u) { return (u & 0x7Fu) ? 0x4680u : (u & 0x8000u) ? 0x4300u : 0x3F80u; };
-          cur.v[i][e] = w & ~mask;
-          code[i][e] = (kind(w & 0xFFFFu) | (kind(w >> 16) << 16)) & mask;
-        }
-      wave_lds_order();
-      put_v(vt, lane, code);
-      wave_lds_order();
-#pragma unroll
-      for (int b = 0; b < NB; ++b) {
-        const uint32_t w = seen[b] >> (4 * q4);
-        u32x4 vis;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int at = 16 * (e >> 1) + 2 * (e & 1);
-          vis[e] = (((w >> at) & 1) ? 0x3F80u : 0u) | (((w >> (at + 1)) & 1) ? 0x3F800000u : 0u);
-        }
-#pragma unroll
-        for (int g = 0; g < 8; ++g) {
-          __builtin_amdgcn_sched_barrier(0);  // (one product's registers at a time)
-          const f32x4 x = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v_frag(vt, v_place(g, lane)), __builtin_bit_cast(bf16x8, vis),
-                                                                  f32x4{}, 0, 0, 0);
-#pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            const int k = (int)x[r];
-            a.o[b][g][r] += ((k & 127) ? INFINITY : 0.f) + (((k >> 7) & 127) ? -INFINITY : 0.f) + (k >= 16384 ? NAN : 0.f);
-          }
-        }
-      }
-    }
-  }
-  wave_lds_order();
-  put_v(vt, lane, cur.v);
-  wave_lds_order();
-#pragma unroll
-  for (int g = 0; g < 8; ++g) {
-    const bf16x8 f = v_frag(vt, v_place(g, lane));
-#pragma unroll
-    for (int b = 0; b < NB; ++b) a.o[b][g] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f, pf[b], a.o[b][g], 0, 0, 0);
-  }
-}
-
-template <int NB, int POLICY>
-__global__ void __launch_bounds__(64 * kWaves, NB == 1 ? 2 : 1) attn_tree_kernel(TreeParams p) {
-  __shared__ __attribute__((aligned(1024))) unsigned char lds[kWaves * kPageBytes];  // a part for each wave
-  __shared__ float2 ml[kWaves][16];                                                  // a row block's max and sum
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int n = lane & 15, q4 = lane >> 4;
-  lds_byte* vt = (lds_byte*)lds + wave * kPageBytes;
-  const int w = blockIdx.x;
-
-  Batch bt;
-  bt.load(p, 0, 0, lane);
-  int total = bt.end();
-  for (int b = 64; b < p.B; b += 64) {
-    int x = 0;
-    if (b + lane < p.B) {
-      const Request r = request(p, b + lane);
-      x = r.units * r.pages;
-    }
-    total += wave_sum(x);
-  }
-  total *= p.Hkv;
-  const int share = p.share_pages ? p.share_pages : max((total + p.shares - 1) / p.shares, p.least);
-  if ((int64_t)w * share >= total) return;
-  int f = w * share;
-  const int f1 = min(f + share, total);
-
-  for (bool start = true; f < f1; start = false) {
-    // the segment: request b, unit, head hk, its pages pg .. pg + count - 1
-    while (bt.end() * p.Hkv <= f) bt.load(p, bt.base + 64, bt.end(), lane);
-    const int at = __builtin_ctzll(__ballot(bt.upto * p.Hkv > f));
-    const int b = bt.base + at;
-    const int first = __builtin_amdgcn_readlane(bt.r.first, at), nodes = __builtin_amdgcn_readlane(bt.r.n, at);
-    const int len = __builtin_amdgcn_readlane(bt.r.len, at), units = __builtin_amdgcn_readlane(bt.r.units, at);
-    const int pages = __builtin_amdgcn_readlane(bt.r.pages, at);
-    const int in = f - (__builtin_amdgcn_readlane(bt.upto, at) - units * pages) * p.Hkv;
-    const int unit = in / (p.Hkv * pages), hk = (in - unit * p.Hkv * pages) / pages, pg = in % pages;
-    const int count = min(pages - pg, f1 - f);
-    const int64_t row0 = (int64_t)unit * p.rows;
-    const int rows = (int)min((int64_t)nodes * p.G - row0, (int64_t)p.rows);  // of the unit
-    // as few waves as hold the rows share a page
-    const int WR = rows <= 16 * NB ? 1 : rows <= 32 * NB ? 2 : 4, WK = kWaves / WR;
-    const int rg = wave & (WR - 1), kg = wave / WR;
-    const int mine = (count - kg + WK - 1) / WK;  // pages pg + kg, + WK, ... of this wave
-    const bool work = rg * 16 * NB < rows;
-    const int64_t base = (int64_t)len - nodes;
-
-    // this lane's rows, one of each block of 16 (rows past the last repeat it, and are not stored)
-    bf16x8 qf[NB][4];
-    int node[NB];
-#pragma unroll
-    for (int k = 0; k < NB; ++k) {
-      const int64_t row = row0 + min(16 * (NB * rg + k) + n, rows - 1);
-      node[k] = (int)(row / p.G);
-      const int g = (int)(row - (int64_t)node[k] * p.G);
-      const uint16_t* qr = p.q + (int64_t)(first + node[k]) * p.q_tok + ((int64_t)hk * p.G + g) * p.q_head + 8 * q4;
-#pragma unroll
-      for (int c = 0; c < 4; ++c) {
-        u32x4 x = *reinterpret_cast<const u32x4*>(qr + 32 * c);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) x[e] ^= p.q_flip;
-        qf[k][c] = __builtin_bit_cast(bf16x8, x);
-      }
-    }
-    Wave<NB> a;
-#pragma unroll
-    for (int k = 0; k < NB; ++k) {
-      a.m[k] = -INFINITY;
-      a.l[k] = 0.f;
-#pragma unroll
-      for (int g = 0; g < 8; ++g) a.o[k][g] = f32x4{};
-    }
-
-    if (work && mine > 0) {
-      // a lane holds the number of one of the wave's pages of 64, and of one of the next 64
-      const size_t entry = ((size_t)b * p.Hkv + hk) * p.pph + pg + kg;
-      auto numbers = [&](int i, int& k, int& v) {
-        k = v = -1;
-        if (i + lane < mine) {
-          k = p.k_pages[entry + (size_t)(i + lane) * WK];
-          v = p.v_pages[entry + (size_t)(i + lane) * WK];
-        }
-      };
-      int kpg, vpg, kpg2, vpg2;
-      numbers(0, kpg, vpg);
-      PageRegs cur, nxt;
-      load_page<POLICY>(p, __builtin_amdgcn_readlane(kpg, 0), __builtin_amdgcn_readlane(vpg, 0), lane, cur);
-      // pages that every row sees whole, the next one's loads on their way; then those that hold nodes
-      const int64_t plain = base < 0 ? 0 : base / kKvPageTokens - pg - kg;  // (of the pages from the wave's first on)
-      const int nfull = (int)min((int64_t)mine, plain <= 0 ? 0 : (plain + WK - 1) / WK);
-      for (int i = 0; i < nfull; ++i) {
-        const int e = i & 63;
-        if (e == 0) numbers(i + 64, kpg2, vpg2);
-        if (e == 63) {
-          kpg = kpg2;
-          vpg = vpg2;
-        }
-        // (behind the last page: none, which loads nothing)
-        const int ne = (e + 1) & 63, kn = __builtin_amdgcn_readlane(kpg, ne), vn = __builtin_amdgcn_readlane(vpg, ne);
-        load_page<POLICY>(p, i + 1 < mine ? kn : -1, i + 1 < mine ? vn : -1, lane, nxt);
-        add_page<NB, false>(p, vt, qf, cur, lane, nullptr, 0, a);
-        cur = nxt;
-      }
-      for (int i = nfull; i < mine; ++i) {
-        const int page = pg + kg + i * WK;
-        uint32_t seen[NB];
-#pragma unroll
-        for (int k = 0; k < NB; ++k)
-          seen[k] = seen_bits(p, p.mask ? p.mask + (int64_t)(first + node[k]) * p.words : nullptr, node[k], nodes, base, page);
-        add_page<NB, true>(p, vt, qf, cur, lane, seen, len - page * kKvPageTokens, a);
-        if (i + 1 < mine) {
-          const size_t next = entry + (size_t)(i + 1) * WK;
-          load_page<POLICY>(p, __builtin_amdgcn_readfirstlane(p.k_pages[next]), __builtin_amdgcn_readfirstlane(p.v_pages[next]),
-                            lane, cur);
-        }
-      }
-    }
-
-    // The WK groups' results, a row block at a time: each wave leaves its own in its part of LDS
-    // (16-byte chunk i of row r at chunk i ^ r), then adds up a share of the rows.
-    const bool whole = count == pages;
-    const size_t piece = ((size_t)w * 2 + (start ? 0 : 1)) * p.rows;
-#pragma unroll
-    for (int k = 0; k < NB; ++k) {
-      if (16 * k >= rows) break;
-      const float lt = over_quarters(a.l[k], [](float x, float y) { return x + y; });
-      __syncthreads();
-#pragma unroll
-      for (int g = 0; g < 8; ++g) *(lds_f32x4*)(vt + n * 512 + (((4 * g + q4) ^ n) << 4)) = a.o[k][g];
-      if (q4 == 0) ml[wave][n] = float2{a.m[k], lt};
-      __syncthreads();
-      const int per = 16 / WK;
-      for (int i = lane >> 5; i < per; i += 2) {
-        const int r = kg * per + i, in_unit = 16 * (NB * rg + k) + r, ch = lane & 31;
-        if (in_unit >= rows) continue;
-        float top = -INFINITY;
-        for (int s = 0; s < WK; ++s) top = fmaxf(top, ml[rg + s * WR][r].x);
-        const float ref = top == -INFINITY ? 0.f : top;
-        f32x4 acc = {};
-        float sum = 0.f;
-        for (int s = 0; s < WK; ++s) {
-          const int from = rg + s * WR;
-          const float2 x = ml[from][r];
-          const float wt = __builtin_amdgcn_exp2f((x.x - ref) * p.c);
-          const f32x4 y = *(const lds_f32x4*)((lds_byte*)lds + from * kPageBytes + r * 512 + ((ch ^ r) << 4));
-          sum += x.y * wt;
-          // (a group that saw nothing has 0, and weight 0)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) acc[e] += y[e] * wt;
-        }
-        if (whole) {
-          const int64_t row = row0 + in_unit;
-          const int tok = (int)(row / p.G);
-          const int64_t out = (int64_t)(first + tok) * p.Hq + (int64_t)hk * p.G + (row - (int64_t)tok * p.G);
-          const float inv = sum > 0.f ? 1.f / sum : (sum == 0.f ? 0.f : sum);  // (NaN stays)
-          const bf16x2 x = {(__bf16)(acc[0] * inv), (__bf16)(acc[1] * inv)}, y = {(__bf16)(acc[2] * inv), (__bf16)(acc[3] * inv)};
-          *reinterpret_cast<uint2*>(p.o + out * kKvD + 4 * ch) = uint2{__builtin_bit_cast(uint32_t, x), __builtin_bit_cast(uint32_t, y)};
-          if (p.lse && ch == 0) p.lse[out] = sum == 0.f ? -INFINITY : top * p.scale + __logf(sum);
-        } else {
-          *reinterpret_cast<f32x4*>(p.part_o + (piece + in_unit) * kKvD + 4 * ch) = acc;
-          if (ch == 0) *reinterpret_cast<float2*>(p.part_ml + (piece + in_unit) * 2) = float2{top, sum};
-        }
-      }
-    }
-    // (for the join: which shares have a piece of it, and whether the first of them is its share's last)
-    if (pg == 0 && threadIdx.x == 0)
-      p.cut[unit_id(p, b, first, unit) * p.Hkv + hk] = whole ? int2{-1, 0} : int2{2 * w + (start ? 0 : 1), (f + pages - 1) / share};
-    f += count;
-    __syncthreads();  // (the parts of LDS have been read)
-  }
-}
-
-// The wide form: NW waves of 32 rows each, all of one request and key/value head, share blocks of 64 tokens (two
-// pages), which stream through LDS (buffer_load ... lds, kStages blocks on their way or in use): what few
-// rows would read from HBM once, many do too.  Waves past the unit's rows load and wait with the others.
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 constexpr int kTokens = 2 * kKvPageTokens;         // of a block
 constexpr int kTileBytes = kTokens * kRowBytes;    // of its keys, or its values
@@ -547,7 +204,7 @@ __device__ __forceinline__ TreeParams arguments() {
 }
 
 template <int NW, int STAGES, int POLICY>
-__global__ void __launch_bounds__(64 * NW, 2) attn_tree_wide(TreeParams args) {
+__global__ void __launch_bounds__(64 * NW, 2) attn_tree_kernel(TreeParams args) {
   constexpr int NQ = 2, WR = 16 * NQ;
   __shared__ __attribute__((aligned(1024))) unsigned char lds[2 * STAGES * kTileBytes];  // K tiles, then V tiles
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -591,86 +248,120 @@ __global__ void __launch_bounds__(64 * NW, 2) attn_tree_wide(TreeParams args) {
   auto k_tile = [&](int j) { return (lds_byte*)lds + (j % STAGES) * kTileBytes; };
   auto v_tile = [&](int j) { return (lds_byte*)lds + (STAGES + j % STAGES) * kTileBytes; };
 
-  for (bool start = true; f < f1; start = false) {
-    const TreeParams p = arguments();
-    // the segment: request b, unit, head hk, its pages pg .. pg + count - 1
+  // A segment: request b, unit, head hk, its pages pg .. pg + count - 1
+  struct Segment {
+    int b, first, nodes, len, pages, unit, hk, pg, count;
+  };
+  auto find = [&](const TreeParams& p, int f) {
     while (bt.end() * p.Hkv <= f) bt.load(p, bt.base + 64, bt.end(), lane);
     const int at = __builtin_ctzll(__ballot(bt.upto * p.Hkv > f));
-    const int b = bt.base + at;
-    const int first = __builtin_amdgcn_readlane(bt.r.first, at), nodes = __builtin_amdgcn_readlane(bt.r.n, at);
-    const int len = __builtin_amdgcn_readlane(bt.r.len, at), units = __builtin_amdgcn_readlane(bt.r.units, at);
-    const int pages = __builtin_amdgcn_readlane(bt.r.pages, at);
-    const int in = f - (__builtin_amdgcn_readlane(bt.upto, at) - units * pages) * p.Hkv;
-    const int unit = in / (p.Hkv * pages), hk = (in - unit * p.Hkv * pages) / pages, pg = in % pages;
-    const int count = min(pages - pg, f1 - f);
-    const int64_t row0 = (int64_t)unit * p.rows;
-    const int rows = (int)min((int64_t)nodes * p.G - row0, (int64_t)p.rows);  // of the unit
-    const bool work = wave * WR < rows;
-    const int64_t base = (int64_t)len - nodes;
-    const int nblk = (count + 1) / 2;
-    // blocks of two pages of the segment that every row sees whole
-    const int64_t whole_pages = base < 0 ? 0 : base / kKvPageTokens - pg;
-    const int nfull = (int)max<int64_t>(0, min<int64_t>(whole_pages, count) / 2);
-
-    const size_t entry = ((size_t)b * p.Hkv + hk) * p.pph + pg + half;
-    auto numbers = [&](int j, int& k, int& v) {  // of the wave's pages of 64 blocks, one a lane
-      k = v = -1;
-      if (2 * (j + lane) + half < count) {
-        k = p.k_pages[entry + 2 * (size_t)(j + lane)];
-        v = p.v_pages[entry + 2 * (size_t)(j + lane)];
-      }
-    };
-    int kpg, vpg, kpg2, vpg2;  // of blocks chunk .. chunk + 63, and of the next 64
-    numbers(0, kpg, vpg);
-    numbers(64, kpg2, vpg2);
-    // (waited for here and not, by the compiler, at every use in the loops below, the tiles' loads with them)
-    auto settle = [&] { asm volatile("" : "+v"(kpg), "+v"(vpg), "+v"(kpg2), "+v"(vpg2)); };
+    Segment x;
+    x.b = bt.base + at;
+    x.first = __builtin_amdgcn_readlane(bt.r.first, at);
+    x.nodes = __builtin_amdgcn_readlane(bt.r.n, at);
+    x.len = __builtin_amdgcn_readlane(bt.r.len, at);
+    x.pages = __builtin_amdgcn_readlane(bt.r.pages, at);
+    const int units = __builtin_amdgcn_readlane(bt.r.units, at);
+    const int in = f - (__builtin_amdgcn_readlane(bt.upto, at) - units * x.pages) * p.Hkv;
+    x.unit = in / (p.Hkv * x.pages);
+    x.hk = (in - x.unit * p.Hkv * x.pages) / x.pages;
+    x.pg = in % x.pages;
+    x.count = min(x.pages - x.pg, f1 - f);
+    return x;
+  };
+  // The numbers of the wave's pages of blocks j .. j + 63 of a segment, one a lane
+  auto numbers = [&](const TreeParams& p, const Segment& x, int j, int& k, int& v) {
+    const size_t entry = ((size_t)x.b * p.Hkv + x.hk) * p.pph + x.pg + half;
+    k = v = -1;
+    if (2 * (j + lane) + half < x.count) {
+      k = p.k_pages[entry + 2 * (size_t)(j + lane)];
+      v = p.v_pages[entry + 2 * (size_t)(j + lane)];
+    }
+  };
+  int kpg, vpg, kpg2, vpg2;  // of blocks chunk .. chunk + 63, and of the next 64
+  // (waited for here and not, by the compiler, at every use in the loops below, the tiles' loads with them)
+  auto settle = [&] { asm volatile("" : "+v"(kpg), "+v"(vpg), "+v"(kpg2), "+v"(vpg2)); };
+  int chunk;
+  auto load = [&](const TreeParams& p, int j) {  // block j, chunk <= j < chunk + 128
+    const int e = j & 63;
+    const bool next = j >= chunk + 64;
+    const int kn = __builtin_amdgcn_readlane(kpg, e), kn2 = __builtin_amdgcn_readlane(kpg2, e);
+    const int vn = __builtin_amdgcn_readlane(vpg, e), vn2 = __builtin_amdgcn_readlane(vpg2, e);
+    const i32x4 rk = page_words(p.k_pool, next ? kn2 : kn, p.pool_pages);
+    const i32x4 rv = page_words(p.v_pool, next ? vn2 : vn, p.pool_pages);
+    const uint32_t dst = lds0 + (uint32_t)(j % STAGES) * kTileBytes + (uint32_t)(wave * PIECES) * 1024;
+#pragma unroll
+    for (int i = 0; i < PIECES; ++i) lds_load_1k<POLICY>(dst + i * 1024, rk, ko[i]);
+#pragma unroll
+    for (int i = 0; i < PIECES; ++i) lds_load_1k<POLICY>(dst + STAGES * kTileBytes + i * 1024, rv, vo[i]);
+  };
+  // A segment's first blocks, and the wave's rows of q, on their way (the tiles are free, its first pages' numbers are there)
+  u32x4 qf[NQ][4];
+  auto begin = [&](const TreeParams& p, const Segment& x) {
     settle();
-    int chunk = 0;
-    auto load = [&](int j) {  // block j, chunk <= j < chunk + 128 (behind the last: none, which loads nothing)
-      const int e = j & 63;
-      const bool next = j >= chunk + 64;
-      const int kn = __builtin_amdgcn_readlane(kpg, e), kn2 = __builtin_amdgcn_readlane(kpg2, e);
-      const int vn = __builtin_amdgcn_readlane(vpg, e), vn2 = __builtin_amdgcn_readlane(vpg2, e);
-      const i32x4 rk = page_words(p.k_pool, next ? kn2 : kn, p.pool_pages);
-      const i32x4 rv = page_words(p.v_pool, next ? vn2 : vn, p.pool_pages);
-      const uint32_t dst = lds0 + (uint32_t)(j % STAGES) * kTileBytes + (uint32_t)(wave * PIECES) * 1024;
+    chunk = 0;
+    const int nblk = (x.count + 1) / 2;
 #pragma unroll
-      for (int i = 0; i < PIECES; ++i) lds_load_1k<POLICY>(dst + i * 1024, rk, ko[i]);
+    for (int j = 0; j < STAGES - 1; ++j)
+      if (j < nblk) load(p, j);
+    const int64_t row0 = (int64_t)x.unit * p.rows;
+    const int rows = (int)min((int64_t)x.nodes * p.G - row0, (int64_t)p.rows);
 #pragma unroll
-      for (int i = 0; i < PIECES; ++i) lds_load_1k<POLICY>(dst + STAGES * kTileBytes + i * 1024, rv, vo[i]);
-    };
+    for (int k = 0; k < NQ; ++k) {
+      const int64_t row = row0 + min(wave * WR + 16 * k + n, rows - 1);
+      const int tok = (int)(row / p.G), g = (int)(row - (int64_t)tok * p.G);
+      const uint16_t* qr = p.q + (int64_t)(x.first + tok) * p.q_tok + ((int64_t)x.hk * p.G + g) * p.q_head + 8 * q4;
+#pragma unroll
+      for (int c = 0; c < 4; ++c) qf[k][c] = *reinterpret_cast<const u32x4*>(qr + 32 * c);
+    }
+  };
+
+  Segment x = find(p0, f);
+  numbers(p0, x, 0, kpg, vpg);
+  numbers(p0, x, 64, kpg2, vpg2);
+  begin(p0, x);
+  for (bool start = true;; start = false) {
+    const TreeParams p = arguments();
+    const int count = x.count, nblk = (count + 1) / 2;
+    const int64_t row0 = (int64_t)x.unit * p.rows;
+    const int rows = (int)min((int64_t)x.nodes * p.G - row0, (int64_t)p.rows);  // of the unit
+    const bool work = wave * WR < rows;
+    const int64_t base = (int64_t)x.len - x.nodes;
+    // blocks of two pages of the segment that every row sees whole
+    const int64_t whole_pages = base < 0 ? 0 : base / kKvPageTokens - x.pg;
+    const int nfull = (int)max<int64_t>(0, min<int64_t>(whole_pages, count) / 2);
     auto turn_chunk = [&](int j) {  // before block j: the next 64 blocks' pages
       if (j < chunk + 64) return;
       chunk += 64;
       kpg = kpg2;
       vpg = vpg2;
-      numbers(chunk + 64, kpg2, vpg2);
+      const TreeParams turn = arguments();
+      numbers(turn, x, chunk + 64, kpg2, vpg2);
       settle();
     };
-    // this wave's loads of a block, of which STAGES - 1 are on their way, and with them everyone's
-    auto arrived = [&] {
-      asm volatile("s_waitcnt vmcnt(%0)" ::"n"((STAGES - 2) * 2 * PIECES) : "memory");
+    // this wave's loads of block j, behind which those of STAGES - 2 are on their way, and with them everyone's
+    auto arrived = [&](int j) {
+      if (j + STAGES - 2 < nblk)
+        asm volatile("s_waitcnt vmcnt(%0)" ::"n"((STAGES - 2) * 2 * PIECES) : "memory");
+      else
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
       __syncthreads();
+      if (j + STAGES - 1 < nblk) load(p, j + STAGES - 1);
     };
 #pragma unroll
-    for (int j = 0; j < STAGES - 1; ++j) load(j);
-
-    // this lane's rows, one of each block of 16 (rows past the last repeat it, and are not stored)
-    bf16x8 qf[NQ][4];
-#pragma unroll
-    for (int k = 0; k < NQ; ++k) {
-      const int64_t row = row0 + min(wave * WR + 16 * k + n, rows - 1);
-      const int tok = (int)(row / p.G), g = (int)(row - (int64_t)tok * p.G);
-      const uint16_t* qr = p.q + (int64_t)(first + tok) * p.q_tok + ((int64_t)hk * p.G + g) * p.q_head + 8 * q4;
+    for (int k = 0; k < NQ; ++k)
 #pragma unroll
       for (int c = 0; c < 4; ++c) {
-        u32x4 x = *reinterpret_cast<const u32x4*>(qr + 32 * c);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) x[e] ^= p.q_flip;
-        asm volatile("" : "+v"(x));
-        qf[k][c] = __builtin_bit_cast(bf16x8, x);
+        for (int e = 0; e < 4; ++e) qf[k][c][e] ^= p.q_flip;
+        asm volatile("" : "+v"(qf[k][c]));  // (waited for here, as the numbers)
       }
+    // the next segment's first numbers, for its loads to begin when this one's are done
+    int kn[2], vn[2];
+    if (f + count < f1) {
+      const Segment next = find(p, f + count);
+      numbers(p, next, 0, kn[0], vn[0]);
+      numbers(p, next, 64, kn[1], vn[1]);
     }
     const float c = p.c;
     f32x4 o[NQ][8], s[NQ][NT];
@@ -692,7 +383,7 @@ __global__ void __launch_bounds__(64 * NW, 2) attn_tree_wide(TreeParams args) {
           const bf16x8 x = *(const __attribute__((address_space(3))) bf16x8*)(kt + ka[c] + t * 16 * kRowBytes);
 #pragma unroll
           for (int k = 0; k < NQ; ++k)
-            s[k][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, qf[k][c], c ? s[k][t] : f32x4{}, 0, 0, 0);
+            s[k][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, __builtin_bit_cast(bf16x8, qf[k][c]), c ? s[k][t] : f32x4{}, 0, 0, 0);
         }
     };
     auto raise = [&] {
@@ -760,8 +451,7 @@ __global__ void __launch_bounds__(64 * NW, 2) attn_tree_wide(TreeParams args) {
       turn_chunk(j0);
       const int j1 = min(j0 + 64, nfull);
       for (int j = j0; j < j1; ++j) {
-        arrived();
-        load(j + STAGES - 1);
+        arrived(j);
         if (work) {
           // (the waves in step with each other otherwise: one that is at it goes on before the others)
           __builtin_amdgcn_s_setprio(1);
@@ -781,8 +471,7 @@ __global__ void __launch_bounds__(64 * NW, 2) attn_tree_wide(TreeParams args) {
     // masked values; here their whole numbers take the keys' place)
     for (int j = nfull; j < nblk; ++j) {
       turn_chunk(j);
-      arrived();
-      load(j + STAGES - 1);
+      arrived(j);
       // (what depends on the lane is computed here again: kept through the loop above, it would take registers there)
       int tid = (int)threadIdx.x;
       asm volatile("" : "+v"(tid));
@@ -790,14 +479,14 @@ __global__ void __launch_bounds__(64 * NW, 2) attn_tree_wide(TreeParams args) {
       auto each_word = [&](auto f) {  // the thread's words of the V tile
 #pragma unroll
         for (int i = 0; i < kTileBytes / 16 / (64 * NW); ++i) {
-          const uint32_t x = (uint32_t)(i * 64 * NW + tid) * 16;
-          f(x, *(lds_u32x4*)(v_tile(j) + x));
+          const uint32_t at = (uint32_t)(i * 64 * NW + tid) * 16;
+          f(at, *(lds_u32x4*)(v_tile(j) + at));
         }
       };
       uint32_t bad = 0;
-      each_word([&](uint32_t, u32x4 x) {
+      each_word([&](uint32_t, u32x4 y) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) bad |= (x[e] & 0x7F807F80u) + 0x00800080u;  // an exponent of all ones carries
+        for (int e = 0; e < 4; ++e) bad |= (y[e] & 0x7F807F80u) + 0x00800080u;  // an exponent of all ones carries
       });
       const bool guard = __syncthreads_or((bad & 0x80008000u) != 0);
       uint32_t seen[NQ][2];
@@ -806,9 +495,9 @@ __global__ void __launch_bounds__(64 * NW, 2) attn_tree_wide(TreeParams args) {
         for (int k = 0; k < NQ; ++k) {
           const int64_t row = row0 + min(wave * WR + 16 * k + n, rows - 1);
           const int i = (int)(row / edge.G);
-          const uint64_t* words = edge.mask ? edge.mask + (int64_t)(first + i) * edge.words : nullptr;
+          const uint64_t* words = edge.mask ? edge.mask + (int64_t)(x.first + i) * edge.words : nullptr;
 #pragma unroll
-          for (int h = 0; h < 2; ++h) seen[k][h] = 2 * j + h < count ? seen_bits(edge, words, i, nodes, base, pg + 2 * j + h) : 0u;
+          for (int h = 0; h < 2; ++h) seen[k][h] = 2 * j + h < count ? seen_bits(edge, words, i, x.nodes, base, x.pg + 2 * j + h) : 0u;
         }
         scores(j);
 #pragma unroll
@@ -824,14 +513,14 @@ __global__ void __launch_bounds__(64 * NW, 2) attn_tree_wide(TreeParams args) {
       }
       if (guard) {
         __syncthreads();  // (the K tile has been read)
-        each_word([&](uint32_t at, u32x4 x) {
+        each_word([&](uint32_t at, u32x4 y) {
           u32x4 fin, code;
 #pragma unroll
           for (int e = 0; e < 4; ++e) {  // two values a word
-            const uint32_t mask = ((((x[e] & 0x7F807F80u) + 0x00800080u) >> 15) & 0x00010001u) * 0xFFFFu;
+            const uint32_t mask = ((((y[e] & 0x7F807F80u) + 0x00800080u) >> 15) & 0x00010001u) * 0xFFFFu;
             auto kind = [](uint32_t u) { return (u & 0x7Fu) ? 0x4680u : (u & 0x8000u) ? 0x4300u : 0x3F80u; };
-            fin[e] = x[e] & ~mask;
-            code[e] = (kind(x[e] & 0xFFFFu) | (kind(x[e] >> 16) << 16)) & mask;
+            fin[e] = y[e] & ~mask;
+            code[e] = (kind(y[e] & 0xFFFFu) | (kind(y[e] >> 16) << 16)) & mask;
           }
           *(lds_u32x4*)(v_tile(j) + at) = fin;
           *(lds_u32x4*)(k_tile(j) + at) = code;
@@ -843,7 +532,7 @@ __global__ void __launch_bounds__(64 * NW, 2) attn_tree_wide(TreeParams args) {
 #pragma unroll
             for (int g = 0; g < 8; ++g) {
               __builtin_amdgcn_sched_barrier(0);  // (one product's registers at a time)
-              f32x4 x = {};
+              f32x4 y = {};
 #pragma unroll
               for (int ks = 0; ks < NK; ++ks) {
                 u32x4 vis;
@@ -853,11 +542,11 @@ __global__ void __launch_bounds__(64 * NW, 2) attn_tree_wide(TreeParams args) {
                   const int i = 16 * (e >> 1) + 2 * (e & 1);
                   vis[e] = (((bits >> i) & 1) ? 0x3F80u : 0u) | (((bits >> (i + 1)) & 1) ? 0x3F800000u : 0u);
                 }
-                x = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v_op(k_tile(j), g, ks), __builtin_bit_cast(bf16x8, vis), x, 0, 0, 0);
+                y = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v_op(k_tile(j), g, ks), __builtin_bit_cast(bf16x8, vis), y, 0, 0, 0);
               }
 #pragma unroll
               for (int r = 0; r < 4; ++r) {
-                const int c = (int)x[r];
+                const int c = (int)y[r];
                 o[k][g][r] += ((c & 127) ? INFINITY : 0.f) + (((c >> 7) & 127) ? -INFINITY : 0.f) + (c >= 16384 ? NAN : 0.f);
               }
             }
@@ -867,12 +556,20 @@ __global__ void __launch_bounds__(64 * NW, 2) attn_tree_wide(TreeParams args) {
     }
 
     const TreeParams last = arguments();
-    const bool whole = count == pages;
+    // the next segment's loads, before this one's results
+    Segment next = x;
+    if (f + count < f1) {
+      next = find(last, f + count);
+      kpg = kn[0], vpg = vn[0], kpg2 = kn[1], vpg2 = vn[1];
+      __syncthreads();  // (the tiles have been read)
+      begin(last, next);
+    }
+    const bool whole = count == x.pages;
     const size_t piece = ((size_t)w * 2 + (start ? 0 : 1)) * last.rows;
     if (work) {
 #pragma unroll
       for (int k = 0; k < NQ; ++k) {
-        const float lt = over_quarters(l[k], [](float x, float y) { return x + y; });
+        const float lt = over_quarters(l[k], [](float a, float b) { return a + b; });
         const int in_unit = wave * WR + 16 * k + n;
         const bool on = in_unit < rows;
         if (!whole) {  // the unscaled output, max and sum to the joining launch
@@ -888,30 +585,30 @@ __global__ void __launch_bounds__(64 * NW, 2) attn_tree_wide(TreeParams args) {
         const float inv = lt > 0.f ? 1.f / lt : (lt == 0.f ? 0.f : lt);  // (NaN stays)
         const int64_t row = row0 + min(in_unit, rows - 1);
         const int tok = (int)(row / last.G);
-        const int64_t out = (int64_t)(first + tok) * last.Hq + (int64_t)hk * last.G + (row - (int64_t)tok * last.G);
+        const int64_t out = (int64_t)(x.first + tok) * last.Hq + (int64_t)x.hk * last.G + (row - (int64_t)tok * last.G);
 #pragma unroll
         for (int g = 0; g < 8; g += 2) {
-          uint32_t x[4];
+          uint32_t u[4];
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             const f32x4& y = o[k][g + (e >> 1)];
             const bf16x2 z = {(__bf16)(y[2 * (e & 1)] * inv), (__bf16)(y[2 * (e & 1) + 1] * inv)};
-            x[e] = __builtin_bit_cast(uint32_t, z);
+            u[e] = __builtin_bit_cast(uint32_t, z);
           }
-          const auto y = __builtin_amdgcn_permlane16_swap(x[0], x[2], false, false);
-          const auto z = __builtin_amdgcn_permlane16_swap(x[1], x[3], false, false);
+          const auto y = __builtin_amdgcn_permlane16_swap(u[0], u[2], false, false);
+          const auto z = __builtin_amdgcn_permlane16_swap(u[1], u[3], false, false);
           // quarter 0: channels 0 .. 7 of group g, 1: 0 .. 7 of group g + 1, 2: 8 .. 15 of g, 3: of g + 1
           if (on) *reinterpret_cast<u32x4*>(last.o + out * kKvD + 16 * (g + (q4 & 1)) + 8 * (q4 >> 1)) = u32x4{y[0], z[0], y[1], z[1]};
         }
         if (last.lse && on && q4 == 0) last.lse[out] = lt == 0.f ? -INFINITY : m[k] * last.scale + __logf(lt);
       }
     }
-    if (pg == 0 && threadIdx.x == 0)
-      last.cut[unit_id(last, b, first, unit) * last.Hkv + hk] = whole ? int2{-1, 0} : int2{2 * w + (start ? 0 : 1), (f + pages - 1) / share};
+    if (x.pg == 0 && threadIdx.x == 0)
+      last.cut[unit_id(last, x.b, x.first, x.unit) * last.Hkv + x.hk] =
+          whole ? int2{-1, 0} : int2{2 * w + (start ? 0 : 1), (f + x.pages - 1) / share};
     f += count;
-    // (the tiles have been read, and no load to them is left)
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    __syncthreads();
+    if (f >= f1) return;
+    x = next;
   }
 }
 
@@ -975,8 +672,7 @@ __global__ void __launch_bounds__(64 * kJoinWaves) attn_tree_join(TreeParams p) 
 }
 
 struct TreePlan {
-  int waves = 0;  // of the wide form (0: the narrow one)
-  int rows = 64, shares = 0, share_pages = 0, least = 1;
+  int waves = 4, rows = 128, shares = 0, share_pages = 0, least = 1;
   int64_t units = 0;
   size_t bytes = 0;
 };
@@ -993,8 +689,8 @@ int tree_plan(int B, int Hq, int Hkv, int T, int S, int split_tokens, TreePlan* 
     return ASYM_OK;
   }
   const int64_t all = (int64_t)T * (Hq / Hkv), mean = (all + B - 1) / B;
-  P.waves = mean <= 16 ? 0 : mean <= 128 ? 4 : 8;
-  P.rows = P.waves ? 32 * P.waves : 64;
+  P.waves = mean <= 128 ? 4 : 8;
+  P.rows = 32 * P.waves;
   P.units = all / P.rows + B;
   const int64_t pages = ((int64_t)S + kKvPageTokens - 1) / kKvPageTokens, heads = P.units * Hkv;
   if (heads > (1 << 30) || heads * pages > (1 << 30)) return fail(ASYM_EUNSUPPORTED, "tree attention: more than 2^30 pages");
@@ -1070,10 +766,9 @@ extern "C" int asym_attn_tree_paged_bf16(int B, int H_q, int H_kv, int T, int S_
   // (at most: the requests may be shorter than S_max)
   const int64_t bytes = 2ll * B * H_kv * ((S_max + (int64_t)kKvPageTokens - 1) / kKvPageTokens) * kPageBytes;
   const bool once = attn_streams_kv(paged_kv_bytes(bytes, (int64_t)pool_pages * kPageBytes, k_pool == v_pool));
-  auto kernel = P.waves == 8   ? (once ? attn_tree_wide<8, 4, 2> : attn_tree_wide<8, 4, 0>)
-                : P.waves == 4 ? (once ? attn_tree_wide<4, 2, 2> : attn_tree_wide<4, 2, 0>)
-                               : (once ? attn_tree_kernel<1, 2> : attn_tree_kernel<1, 0>);
-  hipLaunchKernelGGL(kernel, dim3((unsigned)P.shares), dim3(64 * (P.waves ? P.waves : kWaves)), 0, s, p);
+  auto kernel = P.waves == 8 ? (once ? attn_tree_kernel<8, 4, 2> : attn_tree_kernel<8, 4, 0>)
+                             : (once ? attn_tree_kernel<4, 2, 2> : attn_tree_kernel<4, 2, 0>);
+  hipLaunchKernelGGL(kernel, dim3((unsigned)P.shares), dim3(64 * P.waves), 0, s, p);
   ASYM_HIP(hipGetLastError());
   const int64_t out = (int64_t)T * H_q;
   hipLaunchKernelGGL(attn_tree_join, dim3((unsigned)((out + kJoinWaves - 1) / kJoinWaves)), dim3(64 * kJoinWaves), 0, s, p);
