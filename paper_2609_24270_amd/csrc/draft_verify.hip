@@ -158,15 +158,30 @@ __device__ void walk(const VerifyParams& p, int first, int n, State& s, bool wri
   s.what = kDraw;
 }
 
+// x of the lane that CTRL names (data-parallel primitives), 0 where the row mask leaves a lane out
+template <int CTRL, int ROWS>
+__device__ __forceinline__ double moved(double x) {
+  const uint64_t u = __builtin_bit_cast(uint64_t, x);
+  const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)u, CTRL, ROWS, 0xF, true);
+  const uint32_t hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)(u >> 32), CTRL, ROWS, 0xF, true);
+  return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
+// The sums up to and with each lane (every lane on)
+__device__ __forceinline__ double wave_prefix(double x) {
+  x += moved<0x111, 0xF>(x);  // row_shr 1, 2, 4, 8
+  x += moved<0x112, 0xF>(x);
+  x += moved<0x114, 0xF>(x);
+  x += moved<0x118, 0xF>(x);
+  x += moved<0x142, 0xA>(x);  // row_bcast 15 into rows 1 and 3
+  x += moved<0x143, 0xC>(x);  // row_bcast 31 into rows 2 and 3
+  return x;
+}
+__device__ __forceinline__ double wave_total(double x) { return of_lane(wave_prefix(x), 63); }
+
 // The sum of x over the workgroup, in an order that depends on the number of its threads alone; all threads get it.
 template <int THREADS>
 __device__ double block_sum(double x, double* red) {
-#pragma unroll
-  for (int d = 1; d < 64; d *= 2) {
-    const uint64_t u = __builtin_bit_cast(uint64_t, x);
-    const uint32_t lo = (uint32_t)__shfl_xor((int)(uint32_t)u, d), hi = (uint32_t)__shfl_xor((int)(uint32_t)(u >> 32), d);
-    x += __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
-  }
+  x = wave_total(x);
   __syncthreads();  // (red may still be read from the call before)
   if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = x;
   __syncthreads();
@@ -226,21 +241,19 @@ __device__ void mark_dead(const VerifyParams& p, int first, int n, int cur, int 
   __syncthreads();
 }
 
-// The sum of what is left in one slice, in an order that does not depend on the number of threads: 256 partial sums, of every
-// 256th group of four each, then those.
-template <class T, bool DRAFT, int THREADS>
-__device__ double slice_sum(const VerifyParams& p, const Left& r, int slice, const uint32_t* dead, double* red) {
+// A thread's part of what is left in one slice (thread `id` of 256: every 256th group of four); a slice's sum is that of its four
+// waves' sums, in order.
+template <class T, bool DRAFT>
+__device__ double slice_part(const VerifyParams& p, const Left& r, int slice, int id, const uint32_t* dead) {
   const int from = slice * p.slice, to = min(from + p.slice, p.V);
   double sum = 0.;
-  if (threadIdx.x < kThreads) {
 #pragma unroll 4
-    for (int i = from + (int)threadIdx.x * 4; i < to; i += 4 * kThreads) {
-      double x[4];
-      left4<T, DRAFT>(r, i, to, dead, from, x);
-      sum += (x[0] + x[1]) + (x[2] + x[3]);
-    }
+  for (int i = from + id * 4; i < to; i += 4 * kThreads) {
+    double x[4];
+    left4<T, DRAFT>(r, i, to, dead, from, x);
+    sum += (x[0] + x[1]) + (x[2] + x[3]);
   }
-  return block_sum<THREADS>(sum, red);
+  return sum;
 }
 
 // The state at the start of round `round` (of the launch before, or of the request's beginning) walked on: one wave's work, told to
@@ -296,20 +309,25 @@ __global__ void __launch_bounds__(kThreads) verify_round(VerifyParams p) {
   }
   const int from = slice * p.slice, to = min(from + p.slice, p.V);
   if (!DRAFT) mark_dead<kThreads>(p, first, n, s.cur, from, to, dead);
-  const double sum = slice_sum<T, DRAFT, kThreads>(p, left_of<T, DRAFT>(p, first, s.cur, s.c), slice, dead, red);
+  const double sum = block_sum<kThreads>(slice_part<T, DRAFT>(p, left_of<T, DRAFT>(p, first, s.cur, s.c), slice, threadIdx.x, dead), red);
   if (threadIdx.x == 0) p.sums[now * p.slices + slice] = sum;
 }
 
 // A workgroup a request: the walk's end, the draw, the outputs.
 template <class T, bool DRAFT>
 __global__ void __launch_bounds__(kLast) verify_last(VerifyParams p) {
-  __shared__ double red[kLast / 64];
+  constexpr int kBatch = 64;  // slices that are summed between two barriers
+  __shared__ double red[kLast / 64], part[kBatch][4];
   __shared__ State told;
   __shared__ uint32_t dead[kMaxSlice / 32];
-  __shared__ int found;
-  const int b = blockIdx.x;
+  __shared__ int marks[kLast / 64], found;
+  const int b = blockIdx.x, lane = threadIdx.x & 63;
   int first, n;
   packed_rows(p.cu, b, p.T, first, n);
+  const int prev = (p.round - 1) & 1;
+  double* sums = p.sums + ((size_t)prev * p.B + b) * p.slices;  // (this workgroup's own from here on)
+  const State was = p.state[(size_t)prev * p.B + b];
+  const float draw = p.final[b];
   if (n == 0) {
     if (threadIdx.x == 0) {
       p.count[b] = 0;
@@ -317,24 +335,27 @@ __global__ void __launch_bounds__(kLast) verify_last(VerifyParams p) {
     }
     return;
   }
-  const int prev = (p.round - 1) & 1;
-  double* sums = p.sums + ((size_t)prev * p.B + b) * p.slices;  // (this workgroup's own from here on)
-  State was = p.state[(size_t)prev * p.B + b];
   State s = advance<T, DRAFT, kLast>(p, b, first, n, true, &told, red);
   bool there = s.what == kDraw && s.cur == was.cur && s.c == was.c;  // the sums are those of (cur, c)
-  // every slice's sum (the thread that reads a sum later is not the one that wrote it: the barrier in block_sum and the fence order them)
-  auto all_sums = [&](const Left& r, const uint32_t* bits) {
-    for (int k = 0; k < p.slices; ++k) {
-      if (!DRAFT && bits) mark_dead<kLast>(p, first, n, s.cur, k * p.slice, min((k + 1) * p.slice, p.V), dead);
-      const double x = slice_sum<T, DRAFT, kLast>(p, r, k, bits, red);
-      if (threadIdx.x == 0) sums[k] = x;
+  // Every slice's sum, in the order that the slices' own launches have: 256 threads a slice.
+  auto all_sums = [&](const Left& r) {
+    for (int k0 = 0; k0 < p.slices; k0 += kBatch) {
+      const int end = min(p.slices - k0, kBatch);
+      for (int k = threadIdx.x / kThreads; k < end; k += kLast / kThreads) {
+        const double x = wave_total(slice_part<T, DRAFT>(p, r, k0 + k, threadIdx.x % kThreads, nullptr));
+        if (lane == 0) part[k][threadIdx.x % kThreads / 64] = x;
+      }
+      __syncthreads();
+      if ((int)threadIdx.x < end) {
+        const double* x = part[threadIdx.x];
+        sums[k0 + threadIdx.x] = ((0. + x[0]) + x[1]) + x[2] + x[3];
+      }
+      __threadfence_block();
+      __syncthreads();
     }
-    __threadfence_block();
-    __syncthreads();
   };
-  while (!there) {
-    const Left r = left_of<T, DRAFT>(p, first, s.cur, s.c);
-    all_sums(r, dead);
+  while (!there) {  // (with draft probabilities only: without them the walk ends before the first sum)
+    all_sums(left_of<T, DRAFT>(p, first, s.cur, s.c));
     if (s.what == kDraw) break;
     double x = 0.;
     for (int k = threadIdx.x; k < p.slices; k += kLast) x += sums[k];
@@ -350,35 +371,39 @@ __global__ void __launch_bounds__(kLast) verify_last(VerifyParams p) {
     __syncthreads();
     there = s.what == kDraw && s.cur == cur && s.c == c;
   }
-  // The draw: the slice, by the sums in order, then the token in it
+  // The draw: the slice, by the sums in order (every wave alike), then the token in it
   Left r = left_of<T, DRAFT>(p, first, s.cur, s.c);
   const uint32_t* bits = dead;
   auto mass = [&] {
-    double x = 0.;
-    for (int k = threadIdx.x; k < p.slices; k += kLast) x += sums[k];
-    return block_sum<kLast>(x, red);
+    double all = 0.;
+    for (int k = 0; k < p.slices; k += 64) all += wave_total(k + lane < p.slices ? sums[k + lane] : 0.);
+    return all;
   };
   double M = mass();
   if (!(M > 0.)) {  // nothing is left: from p as it is
     r.c = 0.;
     bits = nullptr;
-    all_sums(r, bits);
+    all_sums(r);
     M = mass();
   }
   int token = -1;
   if (M > 0.) {
-    const double aim = (double)p.final[b] * M;
+    const double aim = (double)draw * M;
     // the first slice whose end lies above the aim (or the last that holds anything)
     double below = 0., upto = 0.;
     int at = -1;
-    for (int k = 0; k < p.slices; ++k) {  // (few, and the same for every thread)
-      const double x = sums[k];
-      if (x > 0.) {
-        at = k;
-        below = upto;
+    bool over = false;
+    for (int k = 0; k < p.slices && !over; k += 64) {
+      const double x = k + lane < p.slices ? sums[k + lane] : 0.;
+      const double here = upto + wave_prefix(x);
+      const unsigned long long some = __ballot(x > 0.), above = __ballot(x > 0. && here > aim);
+      over = above != 0;
+      if (some) {
+        const int l = over ? __builtin_ctzll(above) : 63 - __builtin_clzll(some);
+        at = k + l;
+        below = l ? of_lane(here, l - 1) : upto;
       }
-      upto += x;
-      if (upto > aim) break;
+      upto = of_lane(here, 63);
     }
     const int from = at * p.slice, to = min(from + p.slice, p.V);
     if (!DRAFT && bits) mark_dead<kLast>(p, first, n, s.cur, from, to, dead);
@@ -390,34 +415,31 @@ __global__ void __launch_bounds__(kLast) verify_last(VerifyParams p) {
       left4<T, DRAFT>(r, i, to, bits, from, x);
       // the sums before this thread's four: of the wave's earlier lanes, of the earlier waves
       const double mine = (x[0] + x[1]) + (x[2] + x[3]);
-      double incl = mine;
-      for (int d = 1; d < 64; d *= 2) {
-        const uint64_t u = __builtin_bit_cast(uint64_t, incl);
-        const uint32_t lo = (uint32_t)__shfl_up((int)(uint32_t)u, d), hi = (uint32_t)__shfl_up((int)(uint32_t)(u >> 32), d);
-        if ((threadIdx.x & 63) >= (unsigned)d) incl += __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
-      }
+      const double incl = wave_prefix(mine);
+      __syncthreads();  // (red may still be read from the round before)
+      if (lane == 63) red[threadIdx.x >> 6] = incl;
       __syncthreads();
-      if (threadIdx.x == 0) found = 0x7FFFFFFF;
-      if ((threadIdx.x & 63) == 63) red[threadIdx.x >> 6] = incl;
-      __syncthreads();
-      double at0 = so, all = so;
+      double at0 = so;
       for (int w = 0; w < kLast / 64; ++w) {
         if (w < (int)(threadIdx.x >> 6)) at0 += red[w];
-        all += red[w];
+        so += red[w];
       }
       at0 += incl - mine;
+      int mark = -1;  // the first of the four that lies above the aim
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         at0 += x[e];
         if (x[e] > 0.) {
-          last = max(last, i + e);
-          if (at0 > aim) atomicMin(&found, i + e);
+          last = i + e;
+          if (at0 > aim && mark < 0) mark = i + e;
         }
       }
+      // (of a wave its first such lane has it, of the workgroup the first wave)
+      const unsigned long long above = __ballot(mark >= 0);
+      if (lane == 0) marks[threadIdx.x >> 6] = above ? __builtin_amdgcn_readlane(mark, __builtin_ctzll(above)) : -1;
       __syncthreads();
-      if (found != 0x7FFFFFFF) token = found;
-      so = all;
-      __syncthreads();
+      for (int w = kLast / 64 - 1; w >= 0; --w)
+        if (marks[w] >= 0) token = marks[w];
     }
     if (token < 0) {  // (the aim within a rounding of the slice's end)
       if (threadIdx.x == 0) found = -1;
