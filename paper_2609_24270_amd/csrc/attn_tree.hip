@@ -43,6 +43,7 @@ namespace {
 constexpr int kRowBytes = kKvD * 2;
 constexpr int kPageBytes = kKvPageTokens * kRowBytes;
 constexpr int kJoinWaves = 4;
+constexpr int kLonger = 8;  // pages
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
@@ -98,21 +99,24 @@ __device__ __forceinline__ Request request(const TreeParams& p, int b) {
   return r;
 }
 // The unit's place in `cut` (a request's units follow the rows before it, one more a request)
-__device__ __forceinline__ int64_t unit_id(const TreeParams& p, int b, int first, int unit) {
-  return (int64_t)first * p.G / p.rows + b + unit;
+__device__ __forceinline__ int unit_id(const TreeParams& p, int b, int first, int unit) {
+  return first * p.G / p.rows + b + unit;  // (rows of the call: fewer than 2^26)
 }
 
-// Where the requests' pages lie in the list, 64 requests at a time: lane l has request base + l.
+// Where the requests' pages lie in the list, 64 requests at a time: lane l has request base + l.  A segment of the list is a
+// unit's pages for one head, rounded up to a multiple of `pad`.
 struct Batch {
-  int base;
-  int upto;  // pages (of one head) of the batch up to and with the request, each as often as it has units
+  int base, pad;
+  int upto;  // the list's places (of one head) up to and with the request
   Request r;
+  __device__ __forceinline__ int padded(int pages) const { return (pages + pad - 1) / pad * pad; }
   __device__ __forceinline__ void load(const TreeParams& p, int from, int before, int lane) {
     base = from;
     r = Request{};
     if (from + lane < p.B) r = request(p, from + lane);
-    upto = before + wave_scan_add(r.units * r.pages);
+    place(before);
   }
+  __device__ __forceinline__ void place(int before) { upto = before + wave_scan_add(r.units * padded(r.pages)); }
   __device__ __forceinline__ int end() const { return __builtin_amdgcn_readlane(upto, 63); }
 };
 
@@ -137,20 +141,20 @@ __device__ __forceinline__ bf16x8 v_frag(const lds_byte* vt, uint32_t at) {
   return u.b;
 }
 // Which of tokens 32 page .. + 31 node i sees, a bit each (node 0 is token `base`, which may be negative)
-__device__ __forceinline__ uint32_t seen_bits(const TreeParams& p, const uint64_t* words, int i, int n, int64_t base, int page) {
-  const int64_t j0 = (int64_t)page * kKvPageTokens - base;  // the node at the page's first token
+__device__ __forceinline__ uint32_t seen_bits(const TreeParams& p, const uint64_t* words, int i, int n, int base, int page) {
+  const int j0 = page * kKvPageTokens - base;  // the node at the page's first token
   if (j0 <= -kKvPageTokens) return 0xFFFFFFFFu;
-  auto up_to = [&](int64_t k) {  // the bits below k
+  auto up_to = [&](int k) {  // the bits below k
     return k <= 0 ? 0u : k >= 32 ? 0xFFFFFFFFu : (1u << k) - 1u;
   };
   const uint32_t exist = up_to(n - j0), prefix = up_to(-j0);
-  if (!words) return prefix | (up_to((int64_t)i + 1 - j0) & exist);
-  auto word = [&](int64_t w) { return w < p.words ? words[w] : 0ull; };
+  if (!words) return prefix | (up_to(i + 1 - j0) & exist);
+  auto word = [&](int w) { return w < p.words ? words[w] : 0ull; };
   uint64_t bits;
   if (j0 < 0) {
-    bits = word(0) << (int)-j0;
+    bits = word(0) << -j0;
   } else {
-    const int off = (int)(j0 & 63);
+    const int off = j0 & 63;
     bits = word(j0 >> 6) >> off;
     if (off > 32) bits |= word((j0 >> 6) + 1) << (64 - off);
   }
@@ -213,6 +217,7 @@ __global__ void __launch_bounds__(64 * NW, 2) attn_tree_kernel(TreeParams args) 
 
   const TreeParams p0 = arguments();
   Batch bt;
+  bt.pad = 1;
   bt.load(p0, 0, 0, lane);
   int total = bt.end();
   for (int b = 64; b < p0.B; b += 64) {
@@ -224,10 +229,19 @@ __global__ void __launch_bounds__(64 * NW, 2) attn_tree_kernel(TreeParams args) 
     total += wave_sum(x);
   }
   total *= p0.Hkv;
-  const int share = p0.share_pages ? p0.share_pages : max((total + p0.shares - 1) / p0.shares, p0.least);
+  int share = p0.share_pages ? p0.share_pages : max((total + p0.shares - 1) / p0.shares, p0.least);
+  // A share that goes on in a second segment costs as much as a few pages more would (tree_one); where shares of up to
+  // kLonger more pages suffice with every segment beginning a share of its own, they do.
+  if (!p0.share_pages && p0.B <= 64)
+    for (int longer = (share + 1) & ~1; longer <= share + kLonger; longer += 2)
+      if (wave_sum(bt.r.units * ((bt.r.pages + longer - 1) / longer)) * p0.Hkv <= p0.shares) {
+        share = bt.pad = longer;
+        bt.place(0);
+        total = bt.end() * p0.Hkv;
+        break;
+      }
   if ((int64_t)w * share >= total) return;
-  int f = w * share;
-  const int f1 = min(f + share, total);
+  const int f1 = min((w + 1) * share, total);
 
   const uint32_t lds0 = (uint32_t)(size_t)lds;
   uint32_t ka[4], va[8];  // a lane's places in the tiles: key n of 16, chunks 4 c + q; V^T operand g
@@ -251,6 +265,7 @@ __global__ void __launch_bounds__(64 * NW, 2) attn_tree_kernel(TreeParams args) 
   // A segment: request b, unit, head hk, its pages pg .. pg + count - 1
   struct Segment {
     int b, first, nodes, len, pages, unit, hk, pg, count;
+    int end;  // in the list
   };
   auto find = [&](const TreeParams& p, int f) {
     while (bt.end() * p.Hkv <= f) bt.load(p, bt.base + 64, bt.end(), lane);
@@ -261,12 +276,13 @@ __global__ void __launch_bounds__(64 * NW, 2) attn_tree_kernel(TreeParams args) 
     x.nodes = __builtin_amdgcn_readlane(bt.r.n, at);
     x.len = __builtin_amdgcn_readlane(bt.r.len, at);
     x.pages = __builtin_amdgcn_readlane(bt.r.pages, at);
-    const int units = __builtin_amdgcn_readlane(bt.r.units, at);
-    const int in = f - (__builtin_amdgcn_readlane(bt.upto, at) - units * x.pages) * p.Hkv;
-    x.unit = in / (p.Hkv * x.pages);
-    x.hk = (in - x.unit * p.Hkv * x.pages) / x.pages;
-    x.pg = in % x.pages;
+    const int units = __builtin_amdgcn_readlane(bt.r.units, at), places = bt.padded(x.pages);
+    const int in = f - (__builtin_amdgcn_readlane(bt.upto, at) - units * places) * p.Hkv;
+    x.unit = in / (p.Hkv * places);
+    x.hk = (in - x.unit * p.Hkv * places) / places;
+    x.pg = in % places;
     x.count = min(x.pages - x.pg, f1 - f);
+    x.end = f - x.pg + places;
     return x;
   };
   // The numbers of the wave's pages of blocks j .. j + 63 of a segment, one a lane
@@ -304,32 +320,29 @@ __global__ void __launch_bounds__(64 * NW, 2) attn_tree_kernel(TreeParams args) 
 #pragma unroll
     for (int j = 0; j < STAGES - 1; ++j)
       if (j < nblk) load(p, j);
-    const int64_t row0 = (int64_t)x.unit * p.rows;
-    const int rows = (int)min((int64_t)x.nodes * p.G - row0, (int64_t)p.rows);
+    const int row0 = x.unit * p.rows, rows = min(x.nodes * p.G - row0, p.rows);
 #pragma unroll
     for (int k = 0; k < NQ; ++k) {
-      const int64_t row = row0 + min(wave * WR + 16 * k + n, rows - 1);
-      const int tok = (int)(row / p.G), g = (int)(row - (int64_t)tok * p.G);
+      const int row = row0 + min(wave * WR + 16 * k + n, rows - 1);
+      const int tok = row / p.G, g = row - tok * p.G;
       const uint16_t* qr = p.q + (int64_t)(x.first + tok) * p.q_tok + ((int64_t)x.hk * p.G + g) * p.q_head + 8 * q4;
 #pragma unroll
       for (int c = 0; c < 4; ++c) qf[k][c] = *reinterpret_cast<const u32x4*>(qr + 32 * c);
     }
   };
 
-  Segment x = find(p0, f);
+  Segment x = find(p0, w * share);
   numbers(p0, x, 0, kpg, vpg);
   numbers(p0, x, 64, kpg2, vpg2);
   begin(p0, x);
   for (bool start = true;; start = false) {
     const TreeParams p = arguments();
     const int count = x.count, nblk = (count + 1) / 2;
-    const int64_t row0 = (int64_t)x.unit * p.rows;
-    const int rows = (int)min((int64_t)x.nodes * p.G - row0, (int64_t)p.rows);  // of the unit
+    const int row0 = x.unit * p.rows, rows = min(x.nodes * p.G - row0, p.rows);  // of the unit
     const bool work = wave * WR < rows;
-    const int64_t base = (int64_t)x.len - x.nodes;
+    const int base = x.len - x.nodes;
     // blocks of two pages of the segment that every row sees whole
-    const int64_t whole_pages = base < 0 ? 0 : base / kKvPageTokens - x.pg;
-    const int nfull = (int)max<int64_t>(0, min<int64_t>(whole_pages, count) / 2);
+    const int nfull = max(0, min((base < 0 ? 0 : base / kKvPageTokens) - x.pg, count) / 2);
     auto turn_chunk = [&](int j) {  // before block j: the next 64 blocks' pages
       if (j < chunk + 64) return;
       chunk += 64;
@@ -358,8 +371,8 @@ __global__ void __launch_bounds__(64 * NW, 2) attn_tree_kernel(TreeParams args) 
       }
     // the next segment's first numbers, for its loads to begin when this one's are done
     int kn[2], vn[2];
-    if (f + count < f1) {
-      const Segment next = find(p, f + count);
+    if (x.end < f1) {
+      const Segment next = find(p, x.end);
       numbers(p, next, 0, kn[0], vn[0]);
       numbers(p, next, 64, kn[1], vn[1]);
     }
@@ -470,12 +483,21 @@ __global__ void __launch_bounds__(64 * NW, 2) attn_tree_kernel(TreeParams args) 
     // Blocks that hold nodes, end behind the tokens or with the segment (see add_page for the infinities and NaN among
     // masked values; here their whole numbers take the keys' place)
     for (int j = nfull; j < nblk; ++j) {
-      turn_chunk(j);
-      arrived(j);
       // (what depends on the lane is computed here again: kept through the loop above, it would take registers there)
       int tid = (int)threadIdx.x;
       asm volatile("" : "+v"(tid));
       const int n = tid & 15, q4 = (tid >> 4) & 3;
+      uint32_t seen[NQ][2];
+      if (work)
+#pragma unroll
+        for (int k = 0; k < NQ; ++k) {
+          const int i = (row0 + min(wave * WR + 16 * k + n, rows - 1)) / edge.G;
+          const uint64_t* words = edge.mask ? edge.mask + (int64_t)(x.first + i) * edge.words : nullptr;
+#pragma unroll
+          for (int h = 0; h < 2; ++h) seen[k][h] = 2 * j + h < count ? seen_bits(edge, words, i, x.nodes, base, x.pg + 2 * j + h) : 0u;
+        }
+      turn_chunk(j);
+      arrived(j);
       auto each_word = [&](auto f) {  // the thread's words of the V tile
 #pragma unroll
         for (int i = 0; i < kTileBytes / 16 / (64 * NW); ++i) {
@@ -489,16 +511,7 @@ __global__ void __launch_bounds__(64 * NW, 2) attn_tree_kernel(TreeParams args) 
         for (int e = 0; e < 4; ++e) bad |= (y[e] & 0x7F807F80u) + 0x00800080u;  // an exponent of all ones carries
       });
       const bool guard = __syncthreads_or((bad & 0x80008000u) != 0);
-      uint32_t seen[NQ][2];
       if (work) {
-#pragma unroll
-        for (int k = 0; k < NQ; ++k) {
-          const int64_t row = row0 + min(wave * WR + 16 * k + n, rows - 1);
-          const int i = (int)(row / edge.G);
-          const uint64_t* words = edge.mask ? edge.mask + (int64_t)(x.first + i) * edge.words : nullptr;
-#pragma unroll
-          for (int h = 0; h < 2; ++h) seen[k][h] = 2 * j + h < count ? seen_bits(edge, words, i, x.nodes, base, x.pg + 2 * j + h) : 0u;
-        }
         scores(j);
 #pragma unroll
         for (int k = 0; k < NQ; ++k)
@@ -558,8 +571,8 @@ __global__ void __launch_bounds__(64 * NW, 2) attn_tree_kernel(TreeParams args) 
     const TreeParams last = arguments();
     // the next segment's loads, before this one's results
     Segment next = x;
-    if (f + count < f1) {
-      next = find(last, f + count);
+    if (x.end < f1) {
+      next = find(last, x.end);
       kpg = kn[0], vpg = vn[0], kpg2 = kn[1], vpg2 = vn[1];
       __syncthreads();  // (the tiles have been read)
       begin(last, next);
@@ -583,9 +596,8 @@ __global__ void __launch_bounds__(64 * NW, 2) attn_tree_kernel(TreeParams args) 
         }
         // a lane has 4 of every 16 channels of a row; two groups of them, exchanged between the quarters, make 16 bytes
         const float inv = lt > 0.f ? 1.f / lt : (lt == 0.f ? 0.f : lt);  // (NaN stays)
-        const int64_t row = row0 + min(in_unit, rows - 1);
-        const int tok = (int)(row / last.G);
-        const int64_t out = (int64_t)(x.first + tok) * last.Hq + (int64_t)x.hk * last.G + (row - (int64_t)tok * last.G);
+        const int row = row0 + min(in_unit, rows - 1), tok = row / last.G;
+        const int64_t out = (int64_t)(x.first + tok) * last.Hq + x.hk * last.G + (row - tok * last.G);
 #pragma unroll
         for (int g = 0; g < 8; g += 2) {
           uint32_t u[4];
@@ -605,9 +617,8 @@ __global__ void __launch_bounds__(64 * NW, 2) attn_tree_kernel(TreeParams args) 
     }
     if (x.pg == 0 && threadIdx.x == 0)
       last.cut[unit_id(last, x.b, x.first, x.unit) * last.Hkv + x.hk] =
-          whole ? int2{-1, 0} : int2{2 * w + (start ? 0 : 1), (f + x.pages - 1) / share};
-    f += count;
-    if (f >= f1) return;
+          whole ? int2{-1, 0} : int2{2 * w + (start ? 0 : 1), (x.end - 1) / share};
+    if (x.end >= f1) return;
     x = next;
   }
 }
@@ -632,8 +643,8 @@ __global__ void __launch_bounds__(64 * kJoinWaves) attn_tree_join(TreeParams p) 
     return;
   }
   const int hk = h / p.G;
-  const int64_t row = (int64_t)(tok - r.first) * p.G + (h - hk * p.G);
-  const int unit = (int)(row / p.rows), in_unit = (int)(row - (int64_t)unit * p.rows);
+  const int row = (tok - r.first) * p.G + (h - hk * p.G);
+  const int unit = row / p.rows, in_unit = row - unit * p.rows;
   const int2 cut = p.cut[unit_id(p, b, r.first, unit) * p.Hkv + hk];
   if (cut.x < 0) return;
   const int w0 = cut.x >> 1, w1 = cut.y;
@@ -697,7 +708,7 @@ int tree_plan(int B, int Hq, int Hkv, int T, int S, int split_tokens, TreePlan* 
   if ((int64_t)T * Hq >= (1 << 26)) return fail(ASYM_EUNSUPPORTED, "tree attention: too many rows");  // (threads are counted in 32 bits)
   P.share_pages = split_tokens / kKvPageTokens;
   P.least = P.share_pages ? P.share_pages : 4;
-  int64_t shares = (heads * pages + P.least - 1) / P.least;
+  int64_t shares = heads * pages / P.least + heads;  // (a segment may end in a part of one)
   if (!P.share_pages) shares = std::min<int64_t>(shares, P.waves == 8 ? 256 : 512);
   if (shares >= (1 << 22)) return fail(ASYM_EUNSUPPORTED, "tree attention: too many shares");
   P.shares = (int)shares;

@@ -39,7 +39,6 @@ namespace {
 constexpr int kThreads = 256;   // of a workgroup that sums a slice
 constexpr int kLast = 1024;     // of one that ends a request
 constexpr int kMaxSlice = 8192;
-constexpr int kRounds = 3;      // slice launches of a tree with draft probabilities
 
 // Where a request's walk stands
 struct State {
@@ -522,8 +521,14 @@ extern "C" int asym_draft_verify(int B, int T, int V, int bf16, const void* targ
   p.sums = reinterpret_cast<double*>(p.state + 2 * (size_t)B);
   p.B = B; p.T = T; p.V = V; p.slice = P.slice; p.slices = P.slices;
   hipStream_t s = static_cast<hipStream_t>(stream);
-  // a chain rejects once at most, and without draft probabilities no sum is needed before the last
-  const int rounds = draft && parents ? kRounds : 1;
+  // A chain rejects once at most, and without draft probabilities no sum is needed before the last.  A tree with them
+  // needs a sum a rejection, the last launch takes what is over one by one, and waits for the request that needs the
+  // most.  us at 1, 2, .. 6 launches, trees of 16 nodes and V 128000: 1 request 24 19 23 27 29 32, 4 48 30 22 26 28 30, 16 70
+  // 54 37 30 32 34, 64 of 32 nodes 92 84 72 64 57 60; V 32000: 8 26 24 23 26 28 32, 64 35 33 32 32 33 37; V 5000, which
+  // one workgroup sums as fast as a launch begins: 4 16 19 22 26 30 30, 64 20 22 25 27 31 33.
+  int rounds = 1;
+  if (draft && parents && V > 16384)
+    for (rounds = 2; rounds < 6 && (1 << (2 * (rounds - 1))) <= B;) ++rounds;
   if (bf16)
     draft ? launch_verify<uint16_t, true>(p, rounds, s) : launch_verify<uint16_t, false>(p, rounds, s);
   else
