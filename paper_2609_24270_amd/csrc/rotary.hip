@@ -13,11 +13,11 @@
 // A thread has one unit of a row: two runs of E channels that hold E whole pairs (half: E
 // of either half; interleaved: 2 E neighbours), or 2 E that are copied.  E is 8 (16-byte
 // loads) where rotary and the row are multiples of 16, 4 where they are of 8, else 1.  A
-// workgroup has 256 units of one token (or of a few, where a token has fewer), so that the
+// workgroup has the units of one token (or of a few, where a token has few), so that the
 // cosines of a token are computed once for it, a pair a thread, in LDS, while the rows' loads
 // are on their way.
 //
-// Bound by HBM.
+// Bound by HBM: the gradient of 16384 tokens of 32 heads takes 49 us, 5.4 TB/s, as a plain copy.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -138,38 +138,49 @@ struct AppendParams {
   int tokens, parts;
 };
 
-constexpr int kMostTokens = kThreads / 64;  // of a workgroup: a wave looks one up
+// A workgroup has kAppend units at most, and SLOTS tokens of that many one after the other: a thread's loads of all of them
+// are on their way at once.
+// us at 1, 2 and 4, 32 / 8 heads: 16381 tokens 82.2 78.3 (5.1 TB/s; a plain copy 5.0 to 5.4) 83.6, 2000 tokens 12.9 13.1
+// 13.6; with a token a workgroup of 256 threads, twice where it has more units, 91.8 and 14.0.
+constexpr int kAppend = 512;
+constexpr int kSlots = 2;  // where there are enough tokens for every CU
+constexpr int kMostTokens = 16;  // of a workgroup
 
-template <int E, bool INTER>
-__global__ void __launch_bounds__(kThreads) kv_append_kernel(AppendParams p) {
+template <int E, bool INTER, int SLOTS>
+__global__ void __launch_bounds__(kAppend) kv_append_kernel(AppendParams p) {
   constexpr int units = kKvD / (2 * E);
   __shared__ float2 cs[kMostTokens * (kKvD / 2)];
   __shared__ int seq_of[kMostTokens];      // a token's request (-1: it has none)
   __shared__ int64_t at_of[kMostTokens];  // its place in the cache
-  const int t0 = (int)(blockIdx.x / p.parts) * p.tokens, part = (int)(blockIdx.x % p.parts);
+  const int t0 = (int)(blockIdx.x / p.parts) * p.tokens * SLOTS, part = (int)(blockIdx.x % p.parts);
   const int heads = p.Hq + 2 * p.Hkv, each = heads * units;
-  const int id = part * kThreads + (int)threadIdx.x;
-  const int k = id / each, in = id - k * each;
-  const int t = t0 + k, hh = in / units, c = in - hh * units;
-  const bool on = k < p.tokens && t < p.T;
+  const int id = part * (int)blockDim.x + (int)threadIdx.x;
+  const int k = id / each, in = id - k * each;  // (parts > 1: one token)
+  const int hh = in / units, c = in - hh * units;
   const int kind = hh < p.Hq ? 0 : hh < p.Hq + p.Hkv ? 1 : 2;  // query, key, value
   const int h = kind == 0 ? hh : kind == 1 ? hh - p.Hq : hh - p.Hq - p.Hkv;
-  int a = 0, b = 0;
-  Run<E> u, v;
-  if (on) {
-    runs_of<E, INTER>(c, p.turn.rotary, a, b);
-    const uint16_t* row = kind == 0   ? p.q + (int64_t)t * p.q_tok + (int64_t)h * p.q_head
-                          : kind == 1 ? p.k + (int64_t)t * p.k_tok + (int64_t)h * p.k_head
-                                      : p.v + (int64_t)t * p.v_tok + (int64_t)h * p.v_head;
-    u = *reinterpret_cast<const Run<E>*>(row + a);
-    v = *reinterpret_cast<const Run<E>*>(row + b);
+  int a, b;
+  runs_of<E, INTER>(c, p.turn.rotary, a, b);
+  const uint16_t* from = kind == 0   ? p.q + (int64_t)h * p.q_head
+                         : kind == 1 ? p.k + (int64_t)h * p.k_head
+                                     : p.v + (int64_t)h * p.v_head;
+  const int64_t tok = kind == 0 ? p.q_tok : kind == 1 ? p.k_tok : p.v_tok;
+  Run<E> u[SLOTS], v[SLOTS];
+#pragma unroll
+  for (int s = 0; s < SLOTS; ++s) {
+    const int t = t0 + s * p.tokens + k;
+    if (k < p.tokens && t < p.T) {
+      u[s] = *reinterpret_cast<const Run<E>*>(from + t * tok + a);
+      v[s] = *reinterpret_cast<const Run<E>*>(from + t * tok + b);
+    }
   }
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
-  if (wave < p.tokens) {
-    const int i = t0 + wave;
+  const int all = p.tokens * SLOTS;
+  for (int j = wave; j < all; j += (int)blockDim.x / 64) {  // (a wave looks a token up)
+    const int i = t0 + j;
     int seq = 0;  // requests that end at or before the token
-    for (int j = 0; j < p.B; j += 64) {
-      const bool before = j + lane < p.B && min(max(p.cu[min(j + lane, p.B - 1) + 1], 0), p.T) <= i;
+    for (int r = 0; r < p.B; r += 64) {
+      const bool before = r + lane < p.B && min(max(p.cu[min(r + lane, p.B - 1) + 1], 0), p.T) <= i;
       seq += __popcll(__ballot(before));
     }
     if (lane == 0) {
@@ -180,34 +191,40 @@ __global__ void __launch_bounds__(kThreads) kv_append_kernel(AppendParams p) {
         const int first = p.start[seq];
         if (i >= s && i < s + n && first >= 0) at = (int64_t)first + (i - s);
       }
-      seq_of[wave] = at < 0 ? -1 : seq;
-      at_of[wave] = at;
+      seq_of[j] = at < 0 ? -1 : seq;
+      at_of[j] = at;
     }
   }
   __syncthreads();
   const int pairs = p.turn.rotary / 2;
-  for (int i = threadIdx.x; i < p.tokens * pairs; i += kThreads) {
+  for (int i = threadIdx.x; i < all * pairs; i += (int)blockDim.x) {
     const int q = i / pairs;
     if (seq_of[q] >= 0) cs[i] = cos_sin(p.turn, i - q * pairs, p.pos ? (double)p.pos[t0 + q] : (double)at_of[q]);
   }
-  const int seq = on ? seq_of[k] : -1;
-  const int64_t at = on ? at_of[k] : -1;
-  uint16_t* to = nullptr;
-  if (seq >= 0) {
+  uint16_t* to[SLOTS];
+#pragma unroll
+  for (int s = 0; s < SLOTS; ++s) {
+    to[s] = nullptr;
+    const int j = s * p.tokens + k;
+    if (k >= p.tokens || t0 + j >= p.T || seq_of[j] < 0) continue;
+    const int64_t at = at_of[j];
     if (kind == 0) {
-      to = p.qo + (int64_t)t * p.qo_tok + (int64_t)h * p.qo_head;
+      to[s] = p.qo + (int64_t)(t0 + j) * p.qo_tok + (int64_t)h * p.qo_head;
     } else if (at < p.pph * (int64_t)kKvPageTokens) {
-      const int64_t entry = ((int64_t)seq * p.Hkv + h) * p.pph + at / kKvPageTokens;
+      const int64_t entry = ((int64_t)seq_of[j] * p.Hkv + h) * p.pph + at / kKvPageTokens;
       const int page = (kind == 1 ? p.k_pages : p.v_pages)[entry];
       if (page >= 0 && page < p.pool_pages)
-        to = reinterpret_cast<uint16_t*>((kind == 1 ? p.k_pool : p.v_pool) + page * kPageBytes + at % kKvPageTokens * kPageRow);
+        to[s] = reinterpret_cast<uint16_t*>((kind == 1 ? p.k_pool : p.v_pool) + page * kPageBytes + at % kKvPageTokens * kPageRow);
     }
   }
   __syncthreads();
-  if (!to) return;
-  if (kind < 2 && E * c < pairs) turn_unit<E, INTER>(u, v, cs + k * pairs + E * c);
-  *reinterpret_cast<Run<E>*>(to + a) = u;
-  *reinterpret_cast<Run<E>*>(to + b) = v;
+#pragma unroll
+  for (int s = 0; s < SLOTS; ++s) {
+    if (!to[s]) continue;
+    if (kind < 2 && E * c < pairs) turn_unit<E, INTER>(u[s], v[s], cs + (s * p.tokens + k) * pairs + E * c);
+    *reinterpret_cast<Run<E>*>(to[s] + a) = u[s];
+    *reinterpret_cast<Run<E>*>(to[s] + b) = v[s];
+  }
 }
 
 // Channels of a run: whole runs of pairs, and of what is copied
@@ -226,17 +243,6 @@ bool bad_strides(std::initializer_list<int64_t> strides) {
   for (int64_t s : strides)
     if (s < 0 || s % 8) return true;
   return false;
-}
-
-// A launch of workgroups of `each` units a token
-int unit_grid(const char* what, int T, int64_t each, int most, int* tokens, int* parts, unsigned* grid) {
-  *tokens = (int)std::max<int64_t>(1, std::min<int64_t>(most, kThreads / each));
-  const int64_t n = (each + kThreads - 1) / kThreads;
-  const int64_t all = ((int64_t)T + *tokens - 1) / *tokens * n;
-  if (all >= (1 << 24)) return fail(ASYM_EUNSUPPORTED, std::string(what) + ": too many rows");  // (threads are counted in 32 bits)
-  *parts = (int)n;
-  *grid = (unsigned)all;
-  return ASYM_OK;
 }
 
 template <class F>
@@ -277,11 +283,13 @@ extern "C" int asym_rope_bf16(int T, int H, int D, int rotary, const void* x, in
   p.T = T; p.H = H;
   const int e = run_of(D, rotary);
   p.units = D / (2 * e);
-  unsigned grid;
-  rc = unit_grid("rope", T, (int64_t)H * p.units, 32, &p.tokens, &p.parts, &grid);
-  if (rc != ASYM_OK) return rc;
+  const int64_t each = (int64_t)H * p.units;  // units of a token
+  p.tokens = (int)std::max<int64_t>(1, std::min<int64_t>(32, kThreads / each));
+  p.parts = (int)((each + kThreads - 1) / kThreads);
+  const int64_t grid = ((int64_t)T + p.tokens - 1) / p.tokens * p.parts;
+  if (grid >= (1 << 24)) return fail(ASYM_EUNSUPPORTED, "rope: too many rows");  // (threads are counted in 32 bits)
   with_run(e, layout == ASYM_ROPE_INTERLEAVED, [&](auto E, auto I) {
-    hipLaunchKernelGGL((rope_kernel<decltype(E)::value, decltype(I)::value>), dim3(grid), dim3(kThreads), 0,
+    hipLaunchKernelGGL((rope_kernel<decltype(E)::value, decltype(I)::value>), dim3((unsigned)grid), dim3(kThreads), 0,
                        static_cast<hipStream_t>(stream), p);
   });
   ASYM_HIP(hipGetLastError());
@@ -325,12 +333,19 @@ extern "C" int asym_kv_append_bf16(int B, int H_q, int H_kv, int T, const void* 
   const int e = run_of(kKvD, rotary);
   const int64_t heads = (int64_t)H_q + 2ll * H_kv;
   if (heads > (1 << 20)) return fail(ASYM_EUNSUPPORTED, "kv append: too many heads");
-  unsigned grid;
-  rc = unit_grid("kv append", T, heads * (kKvD / (2 * e)), kMostTokens, &p.tokens, &p.parts, &grid);
-  if (rc != ASYM_OK) return rc;
+  const int64_t each = heads * (kKvD / (2 * e));  // units of a token
+  p.parts = (int)((each + kAppend - 1) / kAppend);
+  const int64_t share = (each + p.parts - 1) / p.parts;
+  p.tokens = (int)std::max<int64_t>(1, std::min<int64_t>(4, 256 / share));
+  const unsigned threads = (unsigned)((share * p.tokens + 63) / 64 * 64);
+  const bool many = (int64_t)T * p.parts >= 4096;
+  const int64_t slots = many ? kSlots : 1;
+  const int64_t grid = ((int64_t)T + p.tokens * slots - 1) / (p.tokens * slots) * p.parts;
+  if (grid >= (1 << 23)) return fail(ASYM_EUNSUPPORTED, "kv append: too many rows");  // (threads are counted in 32 bits)
   with_run(e, layout == ASYM_ROPE_INTERLEAVED, [&](auto E, auto I) {
-    hipLaunchKernelGGL((kv_append_kernel<decltype(E)::value, decltype(I)::value>), dim3(grid), dim3(kThreads), 0,
-                       static_cast<hipStream_t>(stream), p);
+    auto kernel = many ? kv_append_kernel<decltype(E)::value, decltype(I)::value, kSlots>
+                       : kv_append_kernel<decltype(E)::value, decltype(I)::value, 1>;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(threads), 0, static_cast<hipStream_t>(stream), p);
   });
   ASYM_HIP(hipGetLastError());
   return ASYM_OK;
