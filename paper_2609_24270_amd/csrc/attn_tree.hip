@@ -42,7 +42,7 @@ namespace {
 
 constexpr int kRowBytes = kKvD * 2;
 constexpr int kPageBytes = kKvPageTokens * kRowBytes;
-constexpr int kJoinWaves = 4;
+constexpr int kJoinWaves = 4;     // of the joining launch's workgroups
 constexpr int kLonger = 8;  // pages
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
@@ -623,12 +623,19 @@ __global__ void __launch_bounds__(64 * NW, 2) attn_tree_kernel(TreeParams args) 
   }
 }
 
-// A wave a (token, query head): one whose request has no tokens is written, one that was cut is joined.
+// The joining launch: a wave has kJoinHeads query heads of a token, or, where rows are few and have many pieces (SPLIT), a
+// workgroup's waves share one.  Rows of a request without tokens are written, those that were cut are joined in the order
+// of the shares (SPLIT: each wave's every kJoinWaves-th piece, then the waves), the first kJoinPieces of each loaded at once.
+// 32 trees of 24 nodes behind up to 8000 tokens: 12 us, and with a head a wave 20.
+constexpr int kJoinHeads = 2, kJoinPieces = 4;
+template <bool SPLIT>
 __global__ void __launch_bounds__(64 * kJoinWaves) attn_tree_join(TreeParams p) {
+  constexpr int HEADS = SPLIT ? 1 : kJoinHeads, STEP = SPLIT ? kJoinWaves : 1;
+  __shared__ float red[SPLIT ? kJoinWaves : 1][kKvD], red_ml[SPLIT ? kJoinWaves : 1][2];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int64_t out = (int64_t)blockIdx.x * kJoinWaves + wave;
-  if (out >= (int64_t)p.T * p.Hq) return;
-  const int tok = (int)(out / p.Hq), h = (int)(out - (int64_t)tok * p.Hq);
+  const int groups = (p.Hq + HEADS - 1) / HEADS, id = SPLIT ? (int)blockIdx.x : (int)blockIdx.x * kJoinWaves + wave;
+  if (id >= p.T * groups) return;
+  const int tok = id / groups, h0 = (id - tok * groups) * HEADS, sub = SPLIT ? wave : 0;
   int b = 0;  // requests that end at or before the token
   for (int j = 0; j < p.B; j += 64) {
     const bool before = j + lane < p.B && min(max(p.cu[min(j + lane, p.B - 1) + 1], 0), p.T) <= tok;
@@ -637,49 +644,94 @@ __global__ void __launch_bounds__(64 * kJoinWaves) attn_tree_join(TreeParams p) 
   if (b >= p.B) return;
   const Request r = request(p, b);
   if (tok < r.first || tok >= r.first + r.n) return;
+  const int64_t out0 = (int64_t)tok * p.Hq + h0;
   if (r.pages == 0) {
-    *reinterpret_cast<uint32_t*>(p.o + out * kKvD + 2 * lane) = 0;
-    if (p.lse && lane == 0) p.lse[out] = -INFINITY;
+    for (int k = 0; k < HEADS && h0 + k < p.Hq && sub == 0; ++k) {
+      *reinterpret_cast<uint32_t*>(p.o + (out0 + k) * kKvD + 2 * lane) = 0;
+      if (p.lse && lane == 0) p.lse[out0 + k] = -INFINITY;
+    }
     return;
   }
-  const int hk = h / p.G;
+  // lane k < HEADS: head h0 + k
+  const int h = min(h0 + min(lane, HEADS - 1), p.Hq - 1), hk = h / p.G;
   const int row = (tok - r.first) * p.G + (h - hk * p.G);
   const int unit = row / p.rows, in_unit = row - unit * p.rows;
   const int2 cut = p.cut[unit_id(p, b, r.first, unit) * p.Hkv + hk];
-  if (cut.x < 0) return;
-  const int w0 = cut.x >> 1, w1 = cut.y;
-  auto piece = [&](int w) { return ((size_t)w * 2 + (w == w0 ? cut.x & 1 : 0)) * p.rows + in_unit; };
-  float2 x[8], q[8];
-  auto load = [&](int w) {
-#pragma unroll
-    for (int u = 0; u < 8; ++u) {
-      const size_t e = piece(min(w + u, w1));
-      x[u] = *reinterpret_cast<const float2*>(p.part_o + e * kKvD + 2 * lane);
-      q[u] = *reinterpret_cast<const float2*>(p.part_ml + e * 2);
-    }
+  struct Head {
+    int w0, w1, slot, in_unit;
   };
-  load(w0);
-  float M = -INFINITY;
-  for (int w = w0 + lane; w <= w1; w += 64) M = fmaxf(M, p.part_ml[piece(w) * 2]);
+  auto head = [&](int k) {  // (w1 < w0: nothing to join)
+    const int x = __builtin_amdgcn_readlane(cut.x, k), y = __builtin_amdgcn_readlane(cut.y, k);
+    const bool any = h0 + k < p.Hq && x >= 0;
+    return Head{any ? x >> 1 : 0, any ? y : -1, x & 1, __builtin_amdgcn_readlane(in_unit, k)};
+  };
+  auto piece = [&](const Head& d, int w) { return ((size_t)w * 2 + (w == d.w0 ? d.slot : 0)) * p.rows + d.in_unit; };
+  float2 x[HEADS][kJoinPieces], q[HEADS][kJoinPieces];
 #pragma unroll
-  for (int d = 32; d >= 1; d >>= 1) M = fmaxf(M, __shfl_xor(M, d));
-  const float ref = M == -INFINITY ? 0.f : M;
-  float a0 = 0.f, a1 = 0.f, L = 0.f;
-  for (int w = w0; w <= w1; w += 8) {
-    if (w != w0) load(w);
+  for (int k = 0; k < HEADS; ++k) {
+    const Head d = head(k);
 #pragma unroll
-    for (int u = 0; u < 8; ++u) {
-      if (w + u > w1) break;
-      const float s = __builtin_amdgcn_exp2f((q[u].x - ref) * p.c);
-      L = fmaf(q[u].y, s, L);
-      a0 = fmaf(x[u].x, s, a0);
-      a1 = fmaf(x[u].y, s, a1);
+    for (int u = 0; u < kJoinPieces; ++u) {
+      const int w = d.w0 + sub + u * STEP;
+      if (w > d.w1) continue;
+      const size_t e = piece(d, w);
+      x[k][u] = *reinterpret_cast<const float2*>(p.part_o + e * kKvD + 2 * lane);
+      q[k][u] = *reinterpret_cast<const float2*>(p.part_ml + e * 2);
     }
   }
-  const float inv = L > 0.f ? 1.f / L : (L == 0.f ? 0.f : L);  // (NaN stays)
-  const bf16x2 y = {(__bf16)(a0 * inv), (__bf16)(a1 * inv)};
-  *reinterpret_cast<uint32_t*>(p.o + out * kKvD + 2 * lane) = __builtin_bit_cast(uint32_t, y);
-  if (p.lse && lane == 0) p.lse[out] = L == 0.f ? -INFINITY : M * p.scale + __logf(L);
+#pragma unroll
+  for (int k = 0; k < HEADS; ++k) {
+    const Head d = head(k);
+    if (d.w1 < 0) continue;  // (written by its workgroup)
+    const int from = d.w0 + sub;
+    float M = -INFINITY;
+#pragma unroll
+    for (int u = 0; u < kJoinPieces; ++u)
+      if (from + u * STEP <= d.w1) M = fmaxf(M, q[k][u].x);
+    if (from + kJoinPieces * STEP <= d.w1) {
+      for (int w = from + (kJoinPieces + lane) * STEP; w <= d.w1; w += 64 * STEP) M = fmaxf(M, p.part_ml[piece(d, w) * 2]);
+#pragma unroll
+      for (int s = 32; s >= 1; s >>= 1) M = fmaxf(M, __shfl_xor(M, s));
+    }
+    float ref = M == -INFINITY ? 0.f : M;
+    float a0 = 0.f, a1 = 0.f, L = 0.f;
+    auto add = [&](float2 y, float2 z) {
+      const float s = __builtin_amdgcn_exp2f((z.x - ref) * p.c);
+      L = fmaf(z.y, s, L);
+      a0 = fmaf(y.x, s, a0);
+      a1 = fmaf(y.y, s, a1);
+    };
+#pragma unroll
+    for (int u = 0; u < kJoinPieces; ++u)
+      if (from + u * STEP <= d.w1) add(x[k][u], q[k][u]);
+    for (int w = from + kJoinPieces * STEP; w <= d.w1; w += 8 * STEP) {
+      float2 y[8], z[8];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {
+        const size_t e = piece(d, min(w + u * STEP, d.w1));
+        y[u] = *reinterpret_cast<const float2*>(p.part_o + e * kKvD + 2 * lane);
+        z[u] = *reinterpret_cast<const float2*>(p.part_ml + e * 2);
+      }
+#pragma unroll
+      for (int u = 0; u < 8; ++u)
+        if (w + u * STEP <= d.w1) add(y[u], z[u]);
+    }
+    if constexpr (SPLIT) {
+      *reinterpret_cast<float2*>(&red[wave][2 * lane]) = float2{a0, a1};
+      if (lane == 0) *reinterpret_cast<float2*>(red_ml[wave]) = float2{M, L};
+      __syncthreads();  // (the whole workgroup has this row)
+      if (wave) return;
+      M = fmaxf(fmaxf(red_ml[0][0], red_ml[1][0]), fmaxf(red_ml[2][0], red_ml[3][0]));
+      ref = M == -INFINITY ? 0.f : M;
+      a0 = a1 = L = 0.f;
+#pragma unroll
+      for (int j = 0; j < kJoinWaves; ++j) add(*reinterpret_cast<const float2*>(&red[j][2 * lane]), *reinterpret_cast<const float2*>(red_ml[j]));
+    }
+    const float inv = L > 0.f ? 1.f / L : (L == 0.f ? 0.f : L);  // (NaN stays)
+    const bf16x2 y = {(__bf16)(a0 * inv), (__bf16)(a1 * inv)};
+    *reinterpret_cast<uint32_t*>(p.o + (out0 + k) * kKvD + 2 * lane) = __builtin_bit_cast(uint32_t, y);
+    if (p.lse && lane == 0) p.lse[out0 + k] = L == 0.f ? -INFINITY : M * p.scale + __logf(L);
+  }
 }
 
 struct TreePlan {
@@ -699,13 +751,18 @@ int tree_plan(int B, int Hq, int Hkv, int T, int S, int split_tokens, TreePlan* 
     *plan = P;
     return ASYM_OK;
   }
+  if ((int64_t)T * Hq >= (1 << 26)) return fail(ASYM_EUNSUPPORTED, "tree attention: too many rows");  // (threads are counted in 32 bits)
   const int64_t all = (int64_t)T * (Hq / Hkv), mean = (all + B - 1) / B;
-  P.waves = mean <= 128 ? 4 : 8;
+  const int64_t pages = ((int64_t)S + kKvPageTokens - 1) / kKvPageTokens, most = (all / 128 + B) * Hkv;
+  if (most > (1 << 30) || most * pages > (1 << 30)) return fail(ASYM_EUNSUPPORTED, "tree attention: more than 2^30 pages");
+  // Eight waves read the pages of up to 256 rows once, four of 128; but of four there are two workgroups a CU, which hide each
+  // other's starts, ends and waits, and rows past 128 cost a wave what it has of them.  us, four first, lengths from a
+  // quarter of S on, 32 / 8 heads, n nodes in the mean: 16 requests, n 40, S 4000 55 74; 8, n 48, S 32768 184 184; n 64: 4 of 8000 44
+  // 48, 8 of 8000 66 70, 64 of 1000 136 145, 16 of 8000 158 139, 32 of 4000 169 153, 8 of 32768 260 226.
+  P.waves = mean > 192 && (all / 256 + B) * Hkv * pages >= 180 * 256 ? 8 : 4;
   P.rows = 32 * P.waves;
   P.units = all / P.rows + B;
-  const int64_t pages = ((int64_t)S + kKvPageTokens - 1) / kKvPageTokens, heads = P.units * Hkv;
-  if (heads > (1 << 30) || heads * pages > (1 << 30)) return fail(ASYM_EUNSUPPORTED, "tree attention: more than 2^30 pages");
-  if ((int64_t)T * Hq >= (1 << 26)) return fail(ASYM_EUNSUPPORTED, "tree attention: too many rows");  // (threads are counted in 32 bits)
+  const int64_t heads = P.units * Hkv;
   P.share_pages = split_tokens / kKvPageTokens;
   P.least = P.share_pages ? P.share_pages : 4;
   int64_t shares = heads * pages / P.least + heads;  // (a segment may end in a part of one)
@@ -781,8 +838,13 @@ extern "C" int asym_attn_tree_paged_bf16(int B, int H_q, int H_kv, int T, int S_
                              : (once ? attn_tree_kernel<4, 2, 2> : attn_tree_kernel<4, 2, 0>);
   hipLaunchKernelGGL(kernel, dim3((unsigned)P.shares), dim3(64 * P.waves), 0, s, p);
   ASYM_HIP(hipGetLastError());
-  const int64_t out = (int64_t)T * H_q;
-  hipLaunchKernelGGL(attn_tree_join, dim3((unsigned)((out + kJoinWaves - 1) / kJoinWaves)), dim3(64 * kJoinWaves), 0, s, p);
+  // (a row has about as many pieces as there are shares to a unit and head)
+  if (P.shares >= 4 * P.units * H_kv) {
+    hipLaunchKernelGGL(attn_tree_join<true>, dim3((unsigned)(T * H_q)), dim3(64 * kJoinWaves), 0, s, p);
+  } else {
+    const int64_t waves = (int64_t)T * ((H_q + kJoinHeads - 1) / kJoinHeads);
+    hipLaunchKernelGGL(attn_tree_join<false>, dim3((unsigned)((waves + kJoinWaves - 1) / kJoinWaves)), dim3(64 * kJoinWaves), 0, s, p);
+  }
   ASYM_HIP(hipGetLastError());
   return ASYM_OK;
 }
