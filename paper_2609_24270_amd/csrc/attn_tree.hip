@@ -7,27 +7,30 @@
 // bit j is set in node i's mask (without masks: j <= i, a chain; n = 1 is plain decoding with
 // a length per request).
 //
-// A row is a (node, query head of the group) pair, node-major.  A workgroup of four waves serves
-// up to 64 NB (NB 1 or 2) rows of one request and key/value head, a wave NB blocks of 16 rows.  As few
-// waves as the rows need (WR: 1, 2 or 4) share a page of 32 tokens, which each of them
-// loads, from its CU's caches but for the first; the others (WK = 4 / WR groups) take the next
-// pages.  Per page a wave computes
-//   S^T = K . Q^T   v_mfma_f32_16x16x32_bf16, both operands as they lie in memory;
-//   softmax         a row's 32 scores lie in four lanes; its running max is raised only when
+// A row is a (node, query head of the group) pair, node-major.  A workgroup of four or eight waves (tree_plan says when)
+// serves up to 32 rows a wave of one request and key/value head, and takes its tokens 64 at a time, two pages.  K and V
+// come by LDS loads, each wave's part of the block, STAGES - 1 blocks ahead; per block a wave computes
+//   S^T = K . Q^T   v_mfma_f32_16x16x32_bf16, Q in registers, K by ds_read_b128;
+//   softmax         a row's 64 scores lie in four lanes; its running max is raised only when
 //                   some row's grows by more than 2^8;
 //   O^T += V^T . P^T  with P rounded to bf16 (the type of the products' operands: 2^-9
 //                   relative at most, as the output's own rounding) in the scores' registers,
-//                   V^T through the wave's own part of LDS and ds_read_b64_tr_b16.
-// Scores, max, sum and output are fp32.  No barrier until a segment's pages are done.
+//                   V^T by ds_read_b64_tr_b16.
+// Scores, max, sum and output are fp32.  One barrier a block.
 //
 // The pages of the batch, request by request and head by head, are one list, cut into equal
-// shares, one a workgroup, whatever the lengths (which only the device knows).  A segment (what a
-// share has of one request and head) ends with the WK groups' results added up through LDS;
-// whole segments are written, of cut ones the unscaled output, max and sum go to the caller's
-// workspace in fp32 and a second launch joins them in order.
+// shares, one a workgroup, whatever the lengths (which only the device knows).  A segment is what a
+// share has of one request and head.  Whole ones are written; of cut ones the unscaled output, max and sum go to
+// the caller's workspace in fp32 and a second launch joins them in order.
 //
-// Bound by HBM where the rows are few, by the matrix cores and the softmax beside them at 256
-// rows.
+// Bound by HBM where the rows are few: 64 requests of one token behind up to 8000 (32 / 8 heads, 1.40 GB) take 225 us, 6.2
+// TB/s; with 32 trees of 24 nodes behind up to 8000 tokens (96 rows) 159 us, 4.8 TB/s with what a second unit of the larger
+// trees reads again, 12 of them the joining.  At 256 rows, 8 trees of 64 nodes behind 32768 tokens, the matrix cores and
+// the softmax beside them: 257 us a call alone (1.07 PFLOP/s, 46 % of the cycles in matrix instructions), and 322 one
+// after the other, at the clock that the card's power leaves, 1.7 GHz.
+//
+// Each wave with its own pages, K fragments straight from memory and no barrier, took twice as long on trees (348 us
+// for the 32 above): every wave of a unit loaded every page.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -42,8 +45,8 @@ namespace {
 
 constexpr int kRowBytes = kKvD * 2;
 constexpr int kPageBytes = kKvPageTokens * kRowBytes;
-constexpr int kJoinWaves = 4;     // of the joining launch's workgroups
-constexpr int kLonger = 8;  // pages
+constexpr int kJoinWaves = 4;  // of the joining launch's workgroups
+constexpr int kLonger = 8;     // pages
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
@@ -69,8 +72,9 @@ struct TreeParams {
                                  // serves: of one that was cut, 2 (its first share) + (1: that share's last piece),
                                  // its last share; -1 of one that was not
   int B, Hq, Hkv, G, T, S, pph, pool_pages;
-  int rows;                      // of a workgroup: 64 NB
-  int shares, share_pages, least;  // share_pages 0: the batch's pages over the shares, at least `least`
+  int rows;                      // of a workgroup: 32 a wave
+  int shares, least;             // a share has the batch's pages over the shares, at least `least`
+  bool fit;                      // where that makes segments begin with shares, a few more
   float c, scale;                // |scale| * log2(e), |scale|
   uint32_t q_flip;
 };
@@ -108,12 +112,17 @@ __device__ __forceinline__ int unit_id(const TreeParams& p, int b, int first, in
 struct Batch {
   int base, pad;
   int upto;  // the list's places (of one head) up to and with the request
+  bool falls;  // some offset lies below the one before: requests would have rows in common
   Request r;
   __device__ __forceinline__ int padded(int pages) const { return (pages + pad - 1) / pad * pad; }
   __device__ __forceinline__ void load(const TreeParams& p, int from, int before, int lane) {
     base = from;
     r = Request{};
-    if (from + lane < p.B) r = request(p, from + lane);
+    falls = false;
+    if (from + lane < p.B) {
+      r = request(p, from + lane);
+      falls = p.cu[from + lane + 1] < p.cu[from + lane];
+    }
     place(before);
   }
   __device__ __forceinline__ void place(int before) { upto = before + wave_scan_add(r.units * padded(r.pages)); }
@@ -220,19 +229,23 @@ __global__ void __launch_bounds__(64 * NW, 2) attn_tree_kernel(TreeParams args) 
   bt.pad = 1;
   bt.load(p0, 0, 0, lane);
   int total = bt.end();
+  bool falls = bt.falls;
   for (int b = 64; b < p0.B; b += 64) {
     int x = 0;
     if (b + lane < p0.B) {
       const Request r = request(p0, b + lane);
       x = r.units * r.pages;
+      falls |= p0.cu[b + lane + 1] < p0.cu[b + lane];
     }
     total += wave_sum(x);
   }
+  if (__any(falls)) return;  // (the joining launch too)
   total *= p0.Hkv;
-  int share = p0.share_pages ? p0.share_pages : max((total + p0.shares - 1) / p0.shares, p0.least);
-  // A share that goes on in a second segment costs as much as a few pages more would (tree_one); where shares of up to
-  // kLonger more pages suffice with every segment beginning a share of its own, they do.
-  if (!p0.share_pages && p0.B <= 64)
+  int share = max((total + p0.shares - 1) / p0.shares, p0.least);
+  // A share that goes on in a second segment costs as much as a few pages more would; where shares of up to kLonger more
+  // pages suffice with every segment beginning a share of its own, they do: a tree of 8 nodes behind 777 tokens 16.2 ->
+  // 14.6 us, 16 of 16 behind up to 1000 28.8 -> 23.6.
+  if (p0.fit && p0.B <= 64)
     for (int longer = (share + 1) & ~1; longer <= share + kLonger; longer += 2)
       if (wave_sum(bt.r.units * ((bt.r.pages + longer - 1) / longer)) * p0.Hkv <= p0.shares) {
         share = bt.pad = longer;
@@ -480,8 +493,10 @@ __global__ void __launch_bounds__(64 * NW, 2) attn_tree_kernel(TreeParams args) 
       }
     }
     const TreeParams edge = arguments();
-    // Blocks that hold nodes, end behind the tokens or with the segment (see add_page for the infinities and NaN among
-    // masked values; here their whole numbers take the keys' place)
+    // Blocks that hold nodes, end behind the tokens or with the segment: what a row does not see has weight 0, which an
+    // infinity or NaN among the values would make NaN.  Where the block has any, they are taken out of V, and each row's
+    // seen ones added to its output by a product of its own: weights 1, and for a value 1 (infinity), 128 (minus infinity) or
+    // 16384 (NaN), whole numbers whose sums over 64 tokens tell how many there are of each.  They take the keys' place.
     for (int j = nfull; j < nblk; ++j) {
       // (what depends on the lane is computed here again: kept through the loop above, it would take registers there)
       int tid = (int)threadIdx.x;
@@ -637,11 +652,14 @@ __global__ void __launch_bounds__(64 * kJoinWaves) attn_tree_join(TreeParams p) 
   if (id >= p.T * groups) return;
   const int tok = id / groups, h0 = (id - tok * groups) * HEADS, sub = SPLIT ? wave : 0;
   int b = 0;  // requests that end at or before the token
+  bool falls = false;
   for (int j = 0; j < p.B; j += 64) {
-    const bool before = j + lane < p.B && min(max(p.cu[min(j + lane, p.B - 1) + 1], 0), p.T) <= tok;
+    const int at = min(j + lane, p.B - 1), end = p.cu[at + 1];
+    falls |= end < p.cu[at];
+    const bool before = j + lane < p.B && min(max(end, 0), p.T) <= tok;
     b += __popcll(__ballot(before));
   }
-  if (b >= p.B) return;
+  if (b >= p.B || __any(falls)) return;
   const Request r = request(p, b);
   if (tok < r.first || tok >= r.first + r.n) return;
   const int64_t out0 = (int64_t)tok * p.Hq + h0;
@@ -735,7 +753,8 @@ __global__ void __launch_bounds__(64 * kJoinWaves) attn_tree_join(TreeParams p) 
 }
 
 struct TreePlan {
-  int waves = 4, rows = 128, shares = 0, share_pages = 0, least = 1;
+  int waves = 4, rows = 128, shares = 0, least = 1;
+  bool fit = true;
   int64_t units = 0;
   size_t bytes = 0;
 };
@@ -763,10 +782,10 @@ int tree_plan(int B, int Hq, int Hkv, int T, int S, int split_tokens, TreePlan* 
   P.rows = 32 * P.waves;
   P.units = all / P.rows + B;
   const int64_t heads = P.units * Hkv;
-  P.share_pages = split_tokens / kKvPageTokens;
-  P.least = P.share_pages ? P.share_pages : 4;
+  P.fit = split_tokens == 0;
+  P.least = P.fit ? 4 : split_tokens / kKvPageTokens;
   int64_t shares = heads * pages / P.least + heads;  // (a segment may end in a part of one)
-  if (!P.share_pages) shares = std::min<int64_t>(shares, P.waves == 8 ? 256 : 512);
+  if (P.fit) shares = std::min<int64_t>(shares, P.waves == 8 ? 256 : 512);
   if (shares >= (1 << 22)) return fail(ASYM_EUNSUPPORTED, "tree attention: too many shares");
   P.shares = (int)shares;
   P.bytes = (size_t)shares * 2 * P.rows * (kKvD + 2) * sizeof(float) + (size_t)heads * sizeof(int2);
@@ -826,7 +845,7 @@ extern "C" int asym_attn_tree_paged_bf16(int B, int H_q, int H_kv, int T, int S_
   p.cut = reinterpret_cast<int2*>(p.part_ml + pieces * 2);
   p.B = B; p.Hq = H_q; p.Hkv = H_kv; p.G = H_q / H_kv; p.T = T; p.S = S_max; p.pph = pages_per_head;
   p.pool_pages = (int)pool_pages;
-  p.rows = P.rows; p.shares = P.shares; p.share_pages = P.share_pages; p.least = P.least;
+  p.rows = P.rows; p.shares = P.shares; p.least = P.least; p.fit = P.fit;
   p.scale = std::fabs(scale);
   p.c = std::fmax(p.scale * 1.4426950408889634f, 1.17549435e-38f);  // (0 weighs all tokens alike, a masked one not at all)
   p.q_flip = scale < 0 ? 0x80008000u : 0u;
@@ -838,8 +857,9 @@ extern "C" int asym_attn_tree_paged_bf16(int B, int H_q, int H_kv, int T, int S_
                              : (once ? attn_tree_kernel<4, 2, 2> : attn_tree_kernel<4, 2, 0>);
   hipLaunchKernelGGL(kernel, dim3((unsigned)P.shares), dim3(64 * P.waves), 0, s, p);
   ASYM_HIP(hipGetLastError());
-  // (a row has about as many pieces as there are shares to a unit and head)
-  if (P.shares >= 4 * P.units * H_kv) {
+  // (a row has about as many pieces as there are shares to a unit and head; threads are counted in 32 bits.  4 nodes of 8 / 1
+  // heads behind 30000 tokens, 85 pieces a row: 21 us, and 85 with a wave for two heads)
+  if (P.shares >= 4 * P.units * H_kv && T <= (1 << 22) / H_q) {
     hipLaunchKernelGGL(attn_tree_join<true>, dim3((unsigned)(T * H_q)), dim3(64 * kJoinWaves), 0, s, p);
   } else {
     const int64_t waves = (int64_t)T * ((H_q + kJoinHeads - 1) / kJoinHeads);

@@ -123,6 +123,92 @@ def test_shares_of_any_length(dev, split):
     c.check(c.run(split_tokens=split))
 
 
+# Sizes at which a workgroup has eight waves: more than 192 rows a request in the mean, and room in the tables for
+# 180 x 256 pages of units, of which the lengths need not make use.
+MANY_ROWS = [([70, 0, 129, 60], [1000, 5, 700, 64], 8, 2, 2880), ([17, 16, 15, 33], [500, 16, 1000, 90], 16, 1, 5120),
+             ([200, 257], [190, 600], 3, 3, 5120), ([300], [2100], 4, 1, 15360), ([50] * 70, [50 + 13 * i for i in range(70)], 8, 2, 190)]
+
+
+def many_rows(dev, new, lens, Hq, H, room, **kw):
+    c = Case(dev, new, lens, Hq, H, seed=sum(lens), **kw)
+    G = Hq // H
+    assert c.T * G > 192 * len(new) and (c.T * G // 256 + len(new)) * H * room >= 180 * 256
+    c.kt, c.vt = (np.pad(t, ((0, 0), (0, 0), (0, room - c.pph)), constant_values=-1) for t in (c.kt, c.vt))
+    return c
+
+
+@pytest.mark.parametrize("split", [0, 96])
+@pytest.mark.parametrize("tree", [True, False])
+@pytest.mark.parametrize("new,lens,Hq,H,room", MANY_ROWS)
+def test_many_rows_against_oracle(dev, new, lens, Hq, H, room, tree, split):
+    c = many_rows(dev, new, lens, Hq, H, room, tree=tree)
+    c.check(c.run(split_tokens=split), only=[b for b in range(len(new)) if b < 2 or b % 31 < 2 or b == len(new) - 1])
+
+
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
+def test_many_rows_do_not_see_what_they_should_not(dev, bad):
+    n, lens = 130, [475, 300]
+    c = many_rows(dev, [n, 100], lens, 4, 2, 11520)
+    ref = c.run()
+    k0, v0 = c.kp.clone(), c.vp.clone()
+    for b in range(2):
+        for h in range(2):
+            for pool, t in ((c.kp, c.kt), (c.vp, c.vt)):
+                pool[int(t[b, h, lens[b] // 32]), lens[b] % 32:] = bad
+    assert torch.equal(c.run(), ref)
+    c.kp.copy_(k0)
+    j = 5
+    at = 475 - n + j
+    c.vp[int(c.vt[0, 1, at // 32]), at % 32, 100] = bad
+    got = c.run()
+    hit = torch.zeros_like(ref, dtype=torch.bool)
+    for i in range(n):
+        if j in c.sees[0][i]:
+            hit[i, 2:, 100] = True
+    assert hit.any() and torch.equal(got[~hit], ref[~hit])
+    assert torch.all(torch.isnan(got[hit]) if bad != bad else got[hit] == bad)
+    c.vp.copy_(v0)
+
+
+def test_many_rows_captured_and_replayed(dev):
+    c = many_rows(dev, [70, 60], [800, 333], 8, 2, 5760)
+    args = [c.kp, c.vp, i32(c.kt, dev), i32(c.vt, dev), i32(c.cu, dev), i32(c.lens, dev)]
+    eager = lambda q, lens: asym.attn_tree_paged(q, *args[:5], lens, mask=c.mask)
+    held, lens, o = c.q.clone(), args[5].clone(), torch.empty_like(c.q)
+    eager(held, lens)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        asym.attn_tree_paged(held, *args[:5], lens, mask=c.mask, o=o)
+    for s, new in ((1, [800, 333]), (-1, [700, 60]), (2, [71, 320])):
+        held.copy_(c.q * s), lens.copy_(i32(new, dev))
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(o, eager(c.q * s, i32(new, dev)))
+
+
+@pytest.mark.parametrize("G", [1, 5])
+def test_rows_of_very_many_pieces(dev, G):
+    # (joined by a workgroup each)
+    c = Case(dev, [2], [9000], G, 1, seed=12)
+    c.check(c.run(split_tokens=32))
+    c.check(c.run())
+
+
+@pytest.mark.parametrize("B", [3, 130])
+@pytest.mark.parametrize("split", [0, 32])
+def test_offsets_that_fall_write_nothing(dev, B, split):
+    c = Case(dev, [4] * B, [70] * B, 4, 2, seed=B)
+    ref = c.run(split_tokens=split)
+    good, c.cu = c.cu, list(c.cu)
+    c.cu[-2] = c.cu[-3] - 1
+    o = torch.full_like(c.q, 7.0)
+    c.run(o=o, split_tokens=split)
+    assert torch.all(o == 7) and torch.all(c.lse == 3)
+    c.cu = good
+    assert torch.equal(c.run(split_tokens=split), ref)
+
+
 @pytest.mark.parametrize("scale,sigma", [(0.0, 1.0), (-0.11, 1.0), (3.0, 1.0), (SCALE, 8.0), (1e-30, 1.0)])
 def test_scales(dev, scale, sigma):
     c = Case(dev, [9, 2], [70, 300], 6, 2, seed=5, sigma=sigma)
