@@ -1052,8 +1052,9 @@ int asym_kv_free(int R, int H, int pages_per_head, int32_t* table, int32_t* lens
  * those at places path[cu[i] .. cu[i] + count[i] - 1] among them (rising) move down, in order, behind
  * what comes before; the row ends there, and the pages behind its end are given up as in asym_kv_free.  cu:
  * device int32 [n + 1], not falling, held within [0, T]; path [T] and count [n] as asym_draft_verify
- * writes them.  A request whose path does not rise or leaves the drafted tokens, or whose row is shorter than
- * them, is left out.  Pages whose bytes are 32 tokens one after the other (asym_attn_decode_paged_bf16's): page_bytes a
+ * writes them.  A request whose path does not rise or leaves the drafted tokens, whose row is shorter than
+ * them, or whose tokens would move into a page that another row shares, is left out; rows of one call must
+ * share no page that holds drafted tokens (fork rows before the tokens are drafted).  Pages whose bytes are 32 tokens one after the other (asym_attn_decode_paged_bf16's): page_bytes a
  * multiple of 512.  v_pool nullable. */
 int asym_kv_keep(int R, int H, int pages_per_head, int32_t* table, int32_t* lens, int32_t* refs,
                  void* k_pool, void* v_pool, size_t page_bytes, size_t pool_pages, int n,
@@ -1124,8 +1125,8 @@ int asym_kv_append_bf16(int B, int H_q, int H_kv, int T, const void* q, int64_t 
  * contiguous, q, O and the pools 16-byte aligned.  Pages as asym_attn_decode_paged_bf16's, pools of any
  * size; tables device int32 [B][H_kv][pages_per_head], S_max at most 32 * pages_per_head; an entry
  * outside [0, pool_pages) reads as zeros.  lens: device int32 [B], held within [0, S_max] (of n nodes
- * the last lens[b] are there then).  cu: device int32 [B + 1], not falling, held within [0, T].  Rows of O and
- * lse outside every request are left as they are.  D must be 128, H_q / H_kv any whole number.
+ * the last lens[b] are there then).  cu: device int32 [B + 1], held within [0, T]; if it falls
+ * anywhere nothing is written.  Rows of O and lse outside every request are left as they are.  D must be 128, H_q / H_kv any whole number.
  * The batch's pages are cut into equal shares, one a workgroup (split_tokens tokens of one head, a multiple
  * of 32 up to 2^20; 0: automatic, from the batch), and a second launch joins what was cut, in the order of
  * the shares.  The results depend on the sizes, offsets and lengths alone.  The fp32 pieces lie in the caller's

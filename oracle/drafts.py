@@ -89,6 +89,9 @@ def keep(cache, rows, cu, path, count):
         if any(not 0 <= x < n for x in mine) or any(a >= b for a, b in zip(mine, mine[1:])):
             continue
         base = int(cache.lens[r]) - n
+        written = {int(cache.table[r, h, (base + j) // 32]) for j, x in enumerate(mine) if x != j for h in range(cache.H)}
+        if any(0 <= p < len(cache.refs) and cache.refs[p] > 1 for p in written):  # (another row's as well)
+            continue
         for j, x in enumerate(mine):
             for h in range(cache.H):
                 a, b = (cache.table[r, h, (base + y) // 32] for y in (x, j))

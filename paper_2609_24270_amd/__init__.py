@@ -11,8 +11,11 @@ from __future__ import annotations
 import ctypes
 import functools
 import json
+import math
 import os
 from typing import Optional, Sequence
+
+import torch
 
 from . import workloads  # noqa: F401  (seeded inputs; no method arithmetic)
 
@@ -1101,7 +1104,6 @@ def _gpu_of(what, *tensors) -> int:
 def _on(device: int, stream, call):
     """call(raw stream) with the tensors' device as the current one, on `stream` or
     that device's current stream (what the call allocates then belongs to it)."""
-    import torch
     if stream is None:
         if device == torch.cuda.current_device():
             return call(_raw_stream(device))
@@ -1114,7 +1116,6 @@ def _on(device: int, stream, call):
 
 
 def _index(t, what, shape=None):
-    import torch
     if t.dtype is not torch.int32:
         raise TypeError(f"{what} must be int32")
     if not t.is_contiguous() or (shape is not None and t.shape != shape):
@@ -1123,7 +1124,6 @@ def _index(t, what, shape=None):
 
 def _rows128(t, what):
     """A bf16 [T, H, 128] tensor with unit stride in its last dimension: (T, H, token stride, head stride)."""
-    import torch
     if t.dtype is not torch.bfloat16:
         raise TypeError(f"{what} must be bfloat16")
     shape, stride = t.shape, t.stride()
@@ -1136,7 +1136,6 @@ def _rows128(t, what):
 
 def _outputs(o, lse, shape, o_shape):
     """Checks the given outputs of an attention call: (their addresses or None, the tensors given)."""
-    import torch
     if o is not None and (o.dtype is not torch.bfloat16 or o.shape != shape or not o.is_contiguous()):
         raise ValueError(f"o must be a contiguous bf16 {o_shape} tensor")
     if lse is None:
@@ -1154,7 +1153,6 @@ def _sizes(*sizes) -> None:
 
 
 def _workspace(nbytes, device):
-    import torch
     return torch.empty(nbytes, dtype=torch.uint8, device=device)
 
 
@@ -1175,7 +1173,6 @@ def attn_prefill(q, k, v, cu_q, cu_k=None, o=None, lse=None, scale: Optional[flo
     defaults to cu_q).  causal: row i of a sequence sees keys j <= i + L_k - L_q.
     Returns O [T_q, H_q, 128] bf16 (and fills lse [T_q, H_q] fp32 when given); rows
     outside every sequence are not written.  scale defaults to 1 / sqrt(128)."""
-    import torch
     if cu_k is None:
         cu_k = cu_q
     Tq, Hq, qt, qh = _rows128(q, "q")
@@ -1207,7 +1204,6 @@ def attn_prefill(q, k, v, cu_q, cu_k=None, o=None, lse=None, scale: Optional[flo
 
 def _fp4_cache(k_pool, v_pool, k_pages, v_pages):
     """Checks a 4-bit cache's pools and tables: (B, H_kv, pages per head)."""
-    import torch
     if k_pool.dtype is not torch.uint8 or v_pool.dtype is not torch.uint8:
         raise TypeError("pools must be uint8")
     pool = k_pool.shape
@@ -1246,7 +1242,6 @@ def kv_read_fp4(k_pool, v_pool, k_pages, v_pages, cu, start, k, v, stream=None):
     """Read tokens of a 4-bit paged cache back as bf16 (exact): request b's positions
     start[b] onwards into rows cu[b] .. cu[b + 1] - 1 of k and v [T, H_kv, 128]
     (contiguous); returns (k, v)."""
-    import torch
     B, H, pph = _fp4_cache(k_pool, v_pool, k_pages, v_pages)
     if k.dtype is not torch.bfloat16 or v.dtype is not torch.bfloat16:
         raise TypeError("k and v must be bfloat16")
@@ -1276,7 +1271,6 @@ def attn_decode_paged_fp4(q, k_pool, v_pool, k_pages, v_pages, lens, S: Optional
     [pool_pages, 2176]; tables int32 [B, H_kv, pages]; lens int32 [B], each request's
     tokens, at most S (default: what the tables hold).  Returns O [B, H_q, 128] bf16
     (and fills lse [B, H_q] fp32 when given)."""
-    import torch
     if q.dtype is not torch.bfloat16:
         raise TypeError("q must be bfloat16")
     shape = q.shape
@@ -1414,8 +1408,8 @@ def kv_free(table, lens, refs, rows, stream=None) -> None:
 def kv_keep(k_pool, v_pool, table, lens, refs, rows, cu, path, count, stream=None) -> None:
     """Rows of a paged cache keep some of their last tokens: of the last cu[i + 1] - cu[i] tokens of row
     rows[i] those at places path[cu[i] .. cu[i] + count[i] - 1] among them (rising; as draft_verify gives them),
-    in order; the row ends behind them, and the pages behind its end are given up.  Pools [pool_pages, 32,
-    ...] (v_pool None: only one); cu [n + 1], path [T], count [n]; the rest as kv_extend.  All int32."""
+    in order; the row ends behind them, and the pages behind its end are given up.  A row whose tokens would move
+    into a page that another row shares is left as it is.  Pools [pool_pages, 32, ...] (v_pool None: only one); cu [n + 1], path [T], count [n]; the rest as kv_extend.  All int32."""
     R, H, pph, pool = _pages_state(table, lens, refs)
     n = _requests(rows, count)
     _index(cu, "cu", (n + 1,))
@@ -1463,9 +1457,6 @@ def rope_freq(rotary: int, base: float = 10000.0, scaling: Optional[str] = None,
     the slowest channel turns `factor` times slower, the fastest as before), "parts" (Peng et al. 2023: channels with
     more than `fast` turns in `original` tokens as before, with fewer than `slow` / factor, a linear blend in
     between; amplitude 1 + 0.1 ln factor)."""
-    import math
-
-    import torch
     if rotary < 0 or rotary % 2:
         raise ValueError("rotary must be even and not negative")
     if not base > 0 or not factor >= 1 or not fast > slow or original < 1:
@@ -1488,7 +1479,6 @@ def rope_freq(rotary: int, base: float = 10000.0, scaling: Optional[str] = None,
 
 def _freq(freq):
     """Checks frequencies: (rotary, address, the tensors given)."""
-    import torch
     if freq is None:
         return 0, None, ()
     if freq.dtype is not torch.float64:
@@ -1500,7 +1490,6 @@ def _freq(freq):
 
 def _rows(t, what):
     """A bf16 [T, H, D] tensor with unit stride in its last dimension: (T, H, D, token stride, head stride)."""
-    import torch
     if t.dtype is not torch.bfloat16:
         raise TypeError(f"{what} must be bfloat16")
     shape, stride = t.shape, t.stride()
@@ -1516,7 +1505,6 @@ def rope(x, positions, freq, out=None, layout: str = "half", amplitude: float = 
     and j + rotary / 2 ("half") or 2 j and 2 j + 1 ("interleaved").  positions int32 [T], freq float64 [rotary / 2] (see
     rope_freq).  backward: the gradient with respect to x, given the output's.  Returns `out` (given: x's
     shape; x itself is allowed; else a new contiguous tensor)."""
-    import torch
     T, H, D, xt, xh = _rows(x, "x")
     _index(positions, "positions", (T,))
     rotary, freq_ptr, more = _freq(freq)
@@ -1540,7 +1528,6 @@ def rope(x, positions, freq, out=None, layout: str = "half", amplitude: float = 
 
 def _paged_cache(k_pool, v_pool, k_pages, v_pages):
     """Checks a 16-bit cache's pools and tables: (B, H_kv, pages per head)."""
-    import torch
     if k_pool.dtype is not torch.bfloat16 or v_pool.dtype is not torch.bfloat16:
         raise TypeError("pools must be bfloat16")
     pool = k_pool.shape
@@ -1563,7 +1550,6 @@ def kv_append(k, v, k_pool, v_pool, k_pages, v_pages, cu, start, q=None, q_out=N
     at `positions` (int32 [T]; default: the place in the cache).  q [T, H_q, 128] is turned with them: returns
     q_out (given, q itself allowed, or a new tensor), None without q.  Pools bf16 [pool_pages, 32, 128]; tables int32 [B, H_kv,
     pages]; cu int32 [B + 1], start int32 [B].  Pages must not be shared between requests."""
-    import torch
     T, H, kt, kh = _rows128(k, "k")
     vT, vH, vt, vh = _rows128(v, "v")
     B, Hkv, pph = _paged_cache(k_pool, v_pool, k_pages, v_pages)
@@ -1609,7 +1595,6 @@ def kv_append(k, v, k_pool, v_pool, k_pages, v_pages, cu, start, q=None, q_out=N
 def draft_tree(parents: Sequence[int]):
     """Masks (int64 CPU tensor [n, words], bit j % 64 of word j / 64 of row i: node i sees node j, itself and what it hangs
     on) and depths (a list) of one request's nodes from their parents (node 0 is the root)."""
-    import torch
     sees, depth = [], []
     for i, p in enumerate(parents):
         if i and not 0 <= p < i:
@@ -1639,7 +1624,6 @@ def attn_tree_paged(q, k_pool, v_pool, k_pages, v_pages, cu, lens, mask=None, S:
     Pools bf16 [pool_pages, 32, 128]; tables int32 [B, H_kv, pages]; cu int32 [B + 1]; lens int32 [B], at most S
     (default: what the tables hold).  Returns O [T, H_q, 128] bf16 (and fills lse [T, H_q] fp32 when given); rows outside
     every request are not written.  scale defaults to 1 / sqrt(128)."""
-    import torch
     T, Hq, qt, qh = _rows128(q, "q")
     B, H, pph = _paged_cache(k_pool, v_pool, k_pages, v_pages)
     _index(cu, "cu", (B + 1,))
@@ -1686,7 +1670,6 @@ def _probabilities(t, what):
 
 
 def _random(t, what, n):
-    import torch
     if t.dtype is not torch.float32:
         raise TypeError(f"{what} must be float32")
     if t.shape != (n,) or not t.is_contiguous():
@@ -1701,7 +1684,6 @@ def draft_verify(target, draft, tokens, parents, cu, accept, final, path=None, c
     fp32 [T] and final fp32 [B]: uniform random numbers in [0, 1), one for each node's acceptance and one for the
     last token.  Returns path int32 [T] (from cu[b] on the nodes kept, the root first, then -1), count int32 [B] (how many),
     token int32 [B] (the token behind the last of them)."""
-    import torch
     if target.dtype is not torch.float32 and target.dtype is not torch.bfloat16:
         raise TypeError("target must be float32 or bfloat16")
     row = _probabilities(target, "target")

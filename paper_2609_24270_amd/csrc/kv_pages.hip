@@ -428,6 +428,14 @@ __global__ void __launch_bounds__(kSmallThreads) pages_keep(PagesParams p, int T
     const int x = path[at + j];
     bad |= x < 0 || x >= n || (j > 0 && path[at + j - 1] >= x);
   }
+  // (a page that another row has as well is not written to)
+  for (int64_t x = threadIdx.x; x < (int64_t)keep * p.H; x += blockDim.x) {
+    const int64_t head = x / keep;
+    const int j = (int)(x - head * keep);
+    if (path[at + j] == j) continue;
+    const int page = p.table[((int64_t)r * p.H + head) * p.pph + (base + j) / kKvPageTokens];
+    bad |= page >= 0 && page < p.pool && p.refs[page] > 1;
+  }
   if (__syncthreads_or(bad)) return;
   const uint32_t words = (uint32_t)(p.page_bytes / (16 * kKvPageTokens));  // of a token
   const int64_t columns = (int64_t)p.H * words * (p.v_pool ? 2 : 1);

@@ -260,6 +260,25 @@ def test_keep_leaves_out_what_makes_no_sense(dev):
     same(c, [state[0], *state[2:]])
 
 
+def test_keep_writes_to_no_page_of_another_row(dev):
+    # row 3 has row 0's pages, drafted tokens and all, row 4 those of row 1 up to its last 32 tokens; row 2 shares what it does not write to
+    c, state = cache(dev, [90, 96, 70, 0, 0, 0], 2, 4, 3)
+    for to, of, pages in ((3, 0, 2), (4, 1, 2), (5, 2, 1)):
+        c.table[to, :, :pages] = c.table[of, :, :pages]
+        np.add.at(c.refs, c.table[to, :, :pages], 1)
+        c.lens[to] = 32 * pages
+    for x, y in zip(state[2:], (c.table, c.lens, c.refs)):
+        x.copy_(torch.tensor(y))
+    rows, cu, path, count = [0, 1, 2], [0, 40, 60, 80], [-1] * 80, [3, 2, 4]
+    path[:3], path[40:42], path[60:64] = [0, 12, 39], [0, 19], [1, 5, 6, 19]
+    before = [x.copy() for x in c.pools]
+    drafts.keep(c, rows, cu, path, count)
+    # (row 0: 50 tokens and 3 of 40, the moved ones in page 1, which is row 3's too; row 1: 76 and 2 of 20, in page 2; row 2: 50 and 4)
+    assert c.lens.tolist() == [90, 78, 54, 64, 64, 32] and not np.array_equal(before[0], c.pools[0])
+    asym.kv_keep(*state, i32(rows, dev), i32(cu, dev), i32(path, dev), i32(count, dev))
+    same(c, state)
+
+
 def test_keep_captured_and_on_another_stream(dev):
     c, state = cache(dev, [100, 60, 33], 4, 5, 2, 64)
     first = [x.clone() for x in state]
