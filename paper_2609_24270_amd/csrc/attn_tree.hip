@@ -23,11 +23,11 @@
 // share has of one request and head.  Whole ones are written; of cut ones the unscaled output, max and sum go to
 // the caller's workspace in fp32 and a second launch joins them in order.
 //
-// Bound by HBM where the rows are few: 64 requests of one token behind up to 8000 (32 / 8 heads, 1.40 GB) take 225 us, 6.2
-// TB/s; with 32 trees of 24 nodes behind up to 8000 tokens (96 rows) 159 us, 4.8 TB/s with what a second unit of the larger
-// trees reads again, 12 of them the joining.  At 256 rows, 8 trees of 64 nodes behind 32768 tokens, the matrix cores and
-// the softmax beside them: 257 us a call alone (1.07 PFLOP/s, 46 % of the cycles in matrix instructions), and 322 one
-// after the other, at the clock that the card's power leaves, 1.7 GHz.
+// Bound by HBM where the rows are few: 64 requests of one token behind up to 8000 (32 / 8 heads, 1.39 GB) take 223 us, 6.2
+// TB/s.  32 trees of 24 nodes in the mean behind up to 8000 tokens (0.72 GB) take 159 us, 12 of them the joining: 4.5
+// TB/s, and 7 % more is read for the second units of trees past 32 nodes.  With 8 trees of 64 nodes in the mean behind
+// up to 32768 tokens it is the power: 325 us (650 TFLOP/s), 574 thousand cycles at 1.7 to 1.8 GHz of 2.4, of which matrix
+// instructions take 37 % and vector ones 49 %.
 //
 // Each wave with its own pages, K fragments straight from memory and no barrier, took twice as long on trees (348 us
 // for the 32 above): every wave of a unit loaded every page.
