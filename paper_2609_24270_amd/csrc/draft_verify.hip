@@ -20,7 +20,7 @@
 // of the definition but for borders nearer than about 10^-15.  What is not a positive
 // finite number counts as 0.
 //
-// A row is cut into slices; a launch (`round`) sums one each a workgroup, after it has
+// A row is cut into slices; a launch (`round`; none for small vocabularies) sums one each a workgroup, after it has
 // walked the request's nodes as far as the sums so far allow, which all of the request's
 // workgroups do alike (the nodes' p and q, one a lane, are on their way at once).  The last launch has a
 // workgroup a request: it walks to the end (summing slices alone if need be) and draws.
@@ -229,13 +229,15 @@ __device__ __forceinline__ void left4(const Left& r, int i, int to, const uint32
   }
 }
 
-// Marks the tokens of the current node's children (all of them rejected) that lie in [from, to)
+// Marks the tokens of the current node's children (all of them rejected) that lie in [from, to).  The whole workgroup
+// comes here, each THREADS of it with a slice and marks of their own.
 template <int THREADS>
 __device__ void mark_dead(const VerifyParams& p, int first, int n, int cur, int from, int to, uint32_t* dead) {
+  const int id = (int)threadIdx.x % THREADS;
   __syncthreads();
-  for (int i = threadIdx.x; i < kMaxSlice / 32; i += THREADS) dead[i] = 0;
+  for (int i = id; i < kMaxSlice / 32; i += THREADS) dead[i] = 0;
   __syncthreads();
-  for (int i = cur + 1 + (int)threadIdx.x; i < n; i += THREADS) {
+  for (int i = cur + 1 + id; i < n; i += THREADS) {
     const int t = p.tokens[first + i];
     if ((p.parents ? p.parents[first + i] : i - 1) == cur && t >= from && t < to) atomicOr(&dead[(t - from) >> 5], 1u << ((t - from) & 31));
   }
@@ -320,14 +322,14 @@ __global__ void __launch_bounds__(kLast) verify_last(VerifyParams p) {
   constexpr int kBatch = 64;  // slices that are summed between two barriers
   __shared__ double red[kLast / 64], part[kBatch][4];
   __shared__ State told;
-  __shared__ uint32_t dead[kMaxSlice / 32];
+  __shared__ uint32_t dead[kLast / kThreads][kMaxSlice / 32];
   __shared__ int marks[kLast / 64], found;
   const int b = blockIdx.x, lane = threadIdx.x & 63;
   int first, n;
   packed_rows(p.cu, b, p.T, first, n);
   const int prev = (p.round - 1) & 1;
   double* sums = p.sums + ((size_t)prev * p.B + b) * p.slices;  // (this workgroup's own from here on)
-  const State was = p.state[(size_t)prev * p.B + b];
+  const State was = p.round > 0 ? p.state[(size_t)prev * p.B + b] : State{};
   const float draw = p.final[b];
   if (n == 0) {
     if (threadIdx.x == 0) {
@@ -337,13 +339,20 @@ __global__ void __launch_bounds__(kLast) verify_last(VerifyParams p) {
     return;
   }
   State s = advance<T, DRAFT, kLast>(p, b, first, n, true, &told, red);
-  bool there = s.what == kDraw && s.cur == was.cur && s.c == was.c;  // the sums are those of (cur, c)
+  bool there = p.round > 0 && s.what == kDraw && s.cur == was.cur && s.c == was.c;  // the sums are those of (cur, c)
   // Every slice's sum, in the order that the slices' own launches have: 256 threads a slice.
-  auto all_sums = [&](const Left& r) {
+  auto all_sums = [&](const Left& r, bool all) {  // all: rejected tokens too
+    const int group = (int)threadIdx.x / kThreads;
     for (int k0 = 0; k0 < p.slices; k0 += kBatch) {
       const int end = min(p.slices - k0, kBatch);
-      for (int k = threadIdx.x / kThreads; k < end; k += kLast / kThreads) {
-        const double x = wave_total(slice_part<T, DRAFT>(p, r, k0 + k, threadIdx.x % kThreads, nullptr));
+      for (int k1 = 0; k1 < end; k1 += kLast / kThreads) {
+        const int k = k1 + group;
+        if (!DRAFT && !all) {
+          const int from = (k0 + k) * p.slice;
+          mark_dead<kThreads>(p, first, n, s.cur, from, k < end ? min(from + p.slice, p.V) : from, dead[group]);
+        }
+        if (k >= end) continue;
+        const double x = wave_total(slice_part<T, DRAFT>(p, r, k0 + k, threadIdx.x % kThreads, all ? nullptr : dead[group]));
         if (lane == 0) part[k][threadIdx.x % kThreads / 64] = x;
       }
       __syncthreads();
@@ -355,8 +364,8 @@ __global__ void __launch_bounds__(kLast) verify_last(VerifyParams p) {
       __syncthreads();
     }
   };
-  while (!there) {  // (with draft probabilities only: without them the walk ends before the first sum)
-    all_sums(left_of<T, DRAFT>(p, first, s.cur, s.c));
+  while (!there) {  // (without draft probabilities once at most: the walk ends before the first sum)
+    all_sums(left_of<T, DRAFT>(p, first, s.cur, s.c), false);
     if (s.what == kDraw) break;
     double x = 0.;
     for (int k = threadIdx.x; k < p.slices; k += kLast) x += sums[k];
@@ -374,7 +383,7 @@ __global__ void __launch_bounds__(kLast) verify_last(VerifyParams p) {
   }
   // The draw: the slice, by the sums in order (every wave alike), then the token in it
   Left r = left_of<T, DRAFT>(p, first, s.cur, s.c);
-  const uint32_t* bits = dead;
+  uint32_t* bits = dead[0];
   auto mass = [&] {
     double all = 0.;
     for (int k = 0; k < p.slices; k += 64) all += wave_total(k + lane < p.slices ? sums[k + lane] : 0.);
@@ -384,7 +393,7 @@ __global__ void __launch_bounds__(kLast) verify_last(VerifyParams p) {
   if (!(M > 0.)) {  // nothing is left: from p as it is
     r.c = 0.;
     bits = nullptr;
-    all_sums(r);
+    all_sums(r, true);
     M = mass();
   }
   int token = -1;
@@ -407,7 +416,7 @@ __global__ void __launch_bounds__(kLast) verify_last(VerifyParams p) {
       upto = of_lane(here, 63);
     }
     const int from = at * p.slice, to = min(from + p.slice, p.V);
-    if (!DRAFT && bits) mark_dead<kLast>(p, first, n, s.cur, from, to, dead);
+    if (!DRAFT && bits) mark_dead<kLast>(p, first, n, s.cur, from, to, bits);
     double so = below;
     int last = -1;  // the last value that is not 0
     for (int i0 = from; i0 < to && token < 0; i0 += 4 * kLast) {
@@ -523,14 +532,21 @@ extern "C" int asym_draft_verify(int B, int T, int V, int bf16, const void* targ
   p.sums = reinterpret_cast<double*>(p.state + 2 * (size_t)B);
   p.B = B; p.T = T; p.V = V; p.slice = P.slice; p.slices = P.slices;
   hipStream_t s = static_cast<hipStream_t>(stream);
+  // Up to 16384 tokens the last launch sums a row as fast as another begins and does all of it.  us with none, 1 and 2
+  // launches before it, chains of 16 nodes, V 5000: 1 request 12.2 13.6 15.9, 64 12.5 13.7 16.1; trees: 12.7 14.0 16.5, 15.4
+  // 17.7 19.8; V 16000: chains 12.3 13.6 16.1, 12.8 13.6 16.1, trees 12.6 13.7 16.4, 22.0 23.5 24.2; V 64000: chains 17.3 13.7
+  // 16.3, 19.6 16.0 18.4.
   // A chain rejects once at most, and without draft probabilities no sum is needed before the last.  A tree with them
   // needs a sum a rejection, the last launch takes what is over one by one, and waits for the request that needs the
-  // most.  us at 1, 2, .. 6 launches, trees of 16 nodes and V 128000: 1 request 24 19 23 27 29 32, 4 48 30 22 26 28 30, 16 70
-  // 54 37 30 32 34, 64 of 32 nodes 92 84 72 64 57 60; V 32000: 8 26 24 23 26 28 32, 64 35 33 32 32 33 37; V 5000, which
-  // one workgroup sums as fast as a launch begins: 4 16 19 22 26 30 30, 64 20 22 25 27 31 33.
-  int rounds = 1;
-  if (draft && parents && V > 16384)
-    for (rounds = 2; rounds < 6 && (1 << (2 * (rounds - 1))) <= B;) ++rounds;
+  // most.  us with 1, 2, 3 and 4 launches before it, trees of 16 nodes, V 32000: 1 request 15.7 18.0 20.7 24.3, 4 24.8 22.8 22.3
+  // 24.3, 16 30.6 28.8 26.4 26.0, 64 34.0 32.9 31.4 30.7; V 48000: 15.9 17.9 20.6 24.5, 21.0 18.4 21.1 24.2, 33.7 30.2 25.4
+  // 26.1, 39.2 35.9 31.5 31.3; V 128000 (1 to 6): 1 24 19 23 27 29 32, 4 48 30 22 26 28 30, 16 70 54 37 30 32 34, 64 of 32
+  // nodes 92 84 72 64 57 60.
+  int rounds = V > 16384;
+  if (draft && parents && V > 16384) {
+    rounds = V > 65536 ? 2 : 1;
+    for (int64_t requests = 4; requests <= B && rounds < 6; requests *= 4) ++rounds;
+  }
   if (bf16)
     draft ? launch_verify<uint16_t, true>(p, rounds, s) : launch_verify<uint16_t, false>(p, rounds, s);
   else

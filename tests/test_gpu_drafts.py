@@ -95,6 +95,15 @@ def test_many_siblings(dev, seed):
     assert d.run(dev, False) == d.want(False)
 
 
+@pytest.mark.parametrize("new,V", [([24, 17, 40, 2], 16385), ([30], 20000), ([24, 17, 40, 2, 9], 70000), ([20, 5], 140000), ([7] * 20, 33000)])
+@pytest.mark.parametrize("noise", [1.0, 3.0])
+def test_many_siblings_of_a_large_vocabulary(dev, new, V, noise):
+    # rows that are summed by launches of their own, fewer than some request's rejections
+    d = Drafts(new, V, seed=V, noise=noise, peak=2.0, width=12)
+    assert d.run(dev) == d.want()
+    assert d.run(dev, False) == d.want(False)
+
+
 def test_borders(dev):
     # powers of two: every sum exact, every comparison a tie or not at all
     V = 4
@@ -150,8 +159,9 @@ def test_offsets_that_say_too_much_are_held(dev):
     assert d.run(dev) == want
 
 
-def test_streams_and_graphs(dev):
-    a, b = Drafts([6, 9, 1], 5000, seed=5, width=8, noise=2.0), Drafts([6, 9, 1], 5000, seed=6, width=8, noise=2.0)
+@pytest.mark.parametrize("V", [5000, 70000])
+def test_streams_and_graphs(dev, V):
+    a, b = Drafts([6, 9, 1], V, seed=5, width=8, noise=2.0), Drafts([6, 9, 1], V, seed=6, width=8, noise=2.0)
     s = asym.stream_create()
     torch.cuda.synchronize()
     assert a.run(dev, stream=None) == a.want()
