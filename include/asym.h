@@ -1129,9 +1129,10 @@ int asym_kv_append_bf16(int B, int H_q, int H_kv, int T, const void* q, int64_t 
  * anywhere nothing is written.  Rows of O and lse outside every request are left as they are.  D must be 128, H_q / H_kv any whole number.
  * The batch's pages are cut into equal shares, one a workgroup (split_tokens tokens of one head, a multiple
  * of 32 up to 2^20; 0: automatic, from the batch), and a second launch joins what was cut, in the order of
- * the shares.  The results depend on the sizes, offsets and lengths alone.  The fp32 pieces lie in the caller's
- * workspace (16-byte aligned; asym_attn_tree_paged_workspace's bytes), which calls that may overlap
- * must not share.  Sums are fp32 with weights of up to 2^8: results need 2^8 * S_max * max|V| below 2^128.
+ * the shares; automatic calls whose S_max is small for their number of requests and heads are not cut and need no
+ * workspace.  The results depend on the sizes, offsets and lengths alone.  The fp32 pieces lie in the caller's
+ * workspace (16-byte aligned; asym_attn_tree_paged_workspace's bytes; may be null if they are 0), which calls that may
+ * overlap must not share.  Sums are fp32 with weights of up to 2^8: results need 2^8 * S_max * max|V| below 2^128.
  * No host synchronisation; may be captured.  Runs on the stream's CU set; asynchronous.
  * Errors: ASYM_EINVAL, ASYM_EUNSUPPORTED, ASYM_EHIP. */
 int asym_attn_tree_paged_bf16(int B, int H_q, int H_kv, int T, int S_max, int D,

@@ -21,7 +21,8 @@
 // The pages of the batch, request by request and head by head, are one list, cut into equal
 // shares, one a workgroup, whatever the lengths (which only the device knows).  A segment is what a
 // share has of one request and head.  Whole ones are written; of cut ones the unscaled output, max and sum go to
-// the caller's workspace in fp32 and a second launch joins them in order.
+// the caller's workspace in fp32 and a second launch joins them in order.  Where the longest request is short
+// for the number of segments, a share is a segment and one launch does it (tree_plan).
 //
 // Bound by HBM where the rows are few: 64 requests of one token behind up to 8000 (32 / 8 heads, 1.39 GB) take 223 us, 6.2
 // TB/s.  32 trees of 24 nodes in the mean behind up to 8000 tokens (0.72 GB) take 159 us, 12 of them the joining: 4.5
@@ -75,6 +76,7 @@ struct TreeParams {
   int rows;                      // of a workgroup: 32 a wave
   int shares, least;             // a share has the batch's pages over the shares, at least `least`
   bool fit;                      // where that makes segments begin with shares, a few more
+  bool whole;                    // a share is a segment, of up to `least` pages: nothing is cut
   float c, scale;                // |scale| * log2(e), |scale|
   uint32_t q_flip;
 };
@@ -100,6 +102,7 @@ __device__ __forceinline__ Request request(const TreeParams& p, int b) {
   r.len = min(max(p.lens[b], 0), p.S);
   r.units = (int)(((int64_t)r.n * p.G + p.rows - 1) / p.rows);
   r.pages = (r.len + kKvPageTokens - 1) / kKvPageTokens;
+  if (p.whole) r.pages = max(r.pages, 1);  // (no other launch writes the rows that see nothing)
   return r;
 }
 // The unit's place in `cut` (a request's units follow the rows before it, one more a request)
@@ -226,7 +229,7 @@ __global__ void __launch_bounds__(64 * NW, 2) attn_tree_kernel(TreeParams args) 
 
   const TreeParams p0 = arguments();
   Batch bt;
-  bt.pad = 1;
+  bt.pad = p0.whole ? p0.least : 1;
   bt.load(p0, 0, 0, lane);
   int total = bt.end();
   bool falls = bt.falls;
@@ -234,14 +237,14 @@ __global__ void __launch_bounds__(64 * NW, 2) attn_tree_kernel(TreeParams args) 
     int x = 0;
     if (b + lane < p0.B) {
       const Request r = request(p0, b + lane);
-      x = r.units * r.pages;
+      x = r.units * bt.padded(r.pages);
       falls |= p0.cu[b + lane + 1] < p0.cu[b + lane];
     }
     total += wave_sum(x);
   }
   if (__any(falls)) return;  // (the joining launch too)
   total *= p0.Hkv;
-  int share = max((total + p0.shares - 1) / p0.shares, p0.least);
+  int share = p0.whole ? p0.least : max((total + p0.shares - 1) / p0.shares, p0.least);
   // A share that goes on in a second segment costs as much as a few pages more would; where shares of up to kLonger more
   // pages suffice with every segment beginning a share of its own, they do: a tree of 8 nodes behind 777 tokens 16.2 ->
   // 14.6 us, 16 of 16 behind up to 1000 28.8 -> 23.6.
@@ -630,7 +633,7 @@ __global__ void __launch_bounds__(64 * NW, 2) attn_tree_kernel(TreeParams args) 
         if (last.lse && on && q4 == 0) last.lse[out] = lt == 0.f ? -INFINITY : m[k] * last.scale + __logf(lt);
       }
     }
-    if (x.pg == 0 && threadIdx.x == 0)
+    if (x.pg == 0 && threadIdx.x == 0 && !last.whole)
       last.cut[unit_id(last, x.b, x.first, x.unit) * last.Hkv + x.hk] =
           whole ? int2{-1, 0} : int2{2 * w + (start ? 0 : 1), (x.end - 1) / share};
     if (x.end >= f1) return;
@@ -754,7 +757,7 @@ __global__ void __launch_bounds__(64 * kJoinWaves) attn_tree_join(TreeParams p) 
 
 struct TreePlan {
   int waves = 4, rows = 128, shares = 0, least = 1;
-  bool fit = true;
+  bool fit = true, whole = false;
   int64_t units = 0;
   size_t bytes = 0;
 };
@@ -774,21 +777,31 @@ int tree_plan(int B, int Hq, int Hkv, int T, int S, int split_tokens, TreePlan* 
   const int64_t all = (int64_t)T * (Hq / Hkv), mean = (all + B - 1) / B;
   const int64_t pages = ((int64_t)S + kKvPageTokens - 1) / kKvPageTokens, most = (all / 128 + B) * Hkv;
   if (most > (1 << 30) || most * pages > (1 << 30)) return fail(ASYM_EUNSUPPORTED, "tree attention: more than 2^30 pages");
+  // Whole segments need no pieces, no second launch and no workspace, and take as long as the longest request: about 6 us
+  // and 0.58 a page where it is alone.  Cut ones take two launches and what the pieces of T x H_q rows cost to write and
+  // join.  us, cut first, lengths from a quarter of S on, 32 / 8 heads: 1 request of 8 nodes, S 128 13.9 9.7, 256 14.2 10.9, 512
+  // 13.8 15.4; 8 of 8, 512 13.7 15.2; 8 of 32, 256 16.9 11.8, 512 26.1 16.2; 16 of 24, 1000 26.5 27.7; 32 of 4, 1000 22.5 25.4; 24 of
+  // 16, 1000 24.7 26.2; 32 of 24, 1000 35.4 31.0, 2000 48.7 49.7, 8000 155 190; 16 of 64, 500 30.9 22.6, 1000 37.2 35.1, 2000
+  // 48.5 57.7; 64 of 1, 1000 41.6 33.6, 4000 111 112, 8000 206 219; 64 of 32, 64 40.4 17.2, 1000 86 60, 2000 129 97; 64 of 64, 500 99.5
+  // 50.0, 2000 194 145; 256 of 8, 1000 165 140, 4000 473 450; 256 of 1, 8000 786 824.
+  const int64_t units = all / 128 + B;  // of four waves each
+  P.whole = split_tokens == 0 && (pages <= 8 || pages <= units * Hkv / 11 + (int64_t)T * Hq / 1200);
   // Eight waves read the pages of up to 256 rows once, four of 128; but of four there are two workgroups a CU, which hide each
-  // other's starts, ends and waits, and rows past 128 cost a wave what it has of them.  us, four first, lengths from a
-  // quarter of S on, 32 / 8 heads, n nodes in the mean: 16 requests, n 40, S 4000 55 74; 8, n 48, S 32768 184 184; n 64: 4 of 8000 44
-  // 48, 8 of 8000 66 70, 64 of 1000 136 145, 16 of 8000 158 139, 32 of 4000 169 153, 8 of 32768 260 226.
-  P.waves = mean > 192 && (all / 256 + B) * Hkv * pages >= 180 * 256 ? 8 : 4;
+  // other's starts, ends and waits, and rows past 128 cost a wave what it has of them.  us, four first, lengths as above, 32 /
+  // 8 heads, n nodes in the mean: 16 requests, n 40, S 4000 55 74; 8, n 48, S 32768 184 184; n 64: 4 of 8000 44 48, 8 of 8000 66 70,
+  // 16 of 8000 157 138, 32 of 4000 169 156, 8 of 32768 258 217; of n 512: 2 of 4000 64 56, 4 of 8000 174 169.  Whole segments: n
+  // 64, 64 of 2000 145 160, 64 of 4000 269 288, 128 of 1000 166 187, 128 of 4000 569 562.
+  P.waves = !P.whole && mean > 192 && (all / 256 + B) * Hkv * pages >= 180 * 256 ? 8 : 4;
   P.rows = 32 * P.waves;
   P.units = all / P.rows + B;
-  const int64_t heads = P.units * Hkv;
-  P.fit = split_tokens == 0;
-  P.least = P.fit ? 4 : split_tokens / kKvPageTokens;
-  int64_t shares = heads * pages / P.least + heads;  // (a segment may end in a part of one)
+  const int64_t heads = P.units * Hkv;  // segments, where none is cut
+  P.fit = split_tokens == 0 && !P.whole;
+  P.least = P.whole ? (int)pages : P.fit ? 4 : split_tokens / kKvPageTokens;
+  int64_t shares = P.whole ? heads : heads * pages / P.least + heads;  // (a segment may end in a part of one)
   if (P.fit) shares = std::min<int64_t>(shares, P.waves == 8 ? 256 : 512);
   if (shares >= (1 << 22)) return fail(ASYM_EUNSUPPORTED, "tree attention: too many shares");
   P.shares = (int)shares;
-  P.bytes = (size_t)shares * 2 * P.rows * (kKvD + 2) * sizeof(float) + (size_t)heads * sizeof(int2);
+  P.bytes = P.whole ? 0 : (size_t)shares * 2 * P.rows * (kKvD + 2) * sizeof(float) + (size_t)heads * sizeof(int2);
   *plan = P;
   return ASYM_OK;
 }
@@ -828,7 +841,7 @@ extern "C" int asym_attn_tree_paged_bf16(int B, int H_q, int H_kv, int T, int S_
     return fail(ASYM_EINVAL, "tree attention: tables, offsets, lengths and lse must be 4-byte aligned, masks 8-byte aligned");
   for (int64_t s : {q_token, q_head})
     if (s < 0 || s % 8) return fail(ASYM_EINVAL, "tree attention: strides must be multiples of 8 values and not negative");
-  if (!workspace || workspace_bytes < P.bytes || ((uintptr_t)workspace & 15u))
+  if (P.bytes && (!workspace || workspace_bytes < P.bytes || ((uintptr_t)workspace & 15u)))
     return fail(ASYM_EINVAL, "tree attention: the workspace must be 16-byte aligned and hold asym_attn_tree_paged_workspace's bytes");
   TreeParams p = {};
   p.q = static_cast<const uint16_t*>(q);
@@ -845,7 +858,7 @@ extern "C" int asym_attn_tree_paged_bf16(int B, int H_q, int H_kv, int T, int S_
   p.cut = reinterpret_cast<int2*>(p.part_ml + pieces * 2);
   p.B = B; p.Hq = H_q; p.Hkv = H_kv; p.G = H_q / H_kv; p.T = T; p.S = S_max; p.pph = pages_per_head;
   p.pool_pages = (int)pool_pages;
-  p.rows = P.rows; p.shares = P.shares; p.least = P.least; p.fit = P.fit;
+  p.rows = P.rows; p.shares = P.shares; p.least = P.least; p.fit = P.fit; p.whole = P.whole;
   p.scale = std::fabs(scale);
   p.c = std::fmax(p.scale * 1.4426950408889634f, 1.17549435e-38f);  // (0 weighs all tokens alike, a masked one not at all)
   p.q_flip = scale < 0 ? 0x80008000u : 0u;
@@ -857,6 +870,7 @@ extern "C" int asym_attn_tree_paged_bf16(int B, int H_q, int H_kv, int T, int S_
                              : (once ? attn_tree_kernel<4, 2, 2> : attn_tree_kernel<4, 2, 0>);
   hipLaunchKernelGGL(kernel, dim3((unsigned)P.shares), dim3(64 * P.waves), 0, s, p);
   ASYM_HIP(hipGetLastError());
+  if (P.whole) return ASYM_OK;
   // (a row has about as many pieces as there are shares to a unit and head; threads are counted in 32 bits.  4 nodes of 8 / 1
   // heads behind 30000 tokens, 85 pieces a row: 21 us, and 85 with a wave for two heads)
   if (P.shares >= 4 * P.units * H_kv && T <= (1 << 22) / H_q) {

@@ -207,7 +207,9 @@ def test_keep_refusals(change, want):
 
 def test_workspaces():
     n = ctypes.c_size_t()
-    assert code("asym_attn_tree_paged_workspace", 2, 8, 2, 6, 64, 0, ctypes.byref(n)) == asym.OK and n.value > 0
+    assert code("asym_attn_tree_paged_workspace", 2, 8, 2, 6, 6400, 0, ctypes.byref(n)) == asym.OK and n.value > 0
+    assert code("asym_attn_tree_paged_workspace", 2, 8, 2, 6, 64, 32, ctypes.byref(n)) == asym.OK and n.value > 0
+    assert code("asym_attn_tree_paged_workspace", 2, 8, 2, 6, 64, 0, ctypes.byref(n)) == asym.OK and n.value == 0  # one launch
     assert code("asym_attn_tree_paged_workspace", 2, 8, 2, 6, 64, 0, None) == asym.EINVAL
     assert code("asym_attn_tree_paged_workspace", 2, 8, 3, 6, 64, 0, ctypes.byref(n)) == asym.EINVAL
     assert code("asym_attn_tree_paged_workspace", 0, 8, 2, 6, 64, 0, ctypes.byref(n)) == asym.OK and n.value == 0

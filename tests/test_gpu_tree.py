@@ -40,9 +40,9 @@ def offsets(lens, first=0):
 
 
 class Case:
-    """Requests of `new` nodes that are the last of `lens` tokens, in random pages."""
+    """Requests of `new` nodes that are the last of `lens` tokens, in random pages, and tables with room for `room` more."""
 
-    def __init__(self, dev, new, lens, Hq, H, seed=0, sigma=1.0, tree=True, pph=None, spare=3):
+    def __init__(self, dev, new, lens, Hq, H, seed=0, sigma=1.0, tree=True, pph=None, spare=3, room=0):
         self.new, self.lens, self.Hq, self.H, self.dev = new, lens, Hq, H, dev
         g = torch.Generator().manual_seed(seed)
         rng = np.random.default_rng(seed)
@@ -51,6 +51,7 @@ class Case:
         mk = lambda *s: (torch.randn(s, generator=g) * sigma).to(torch.bfloat16).to(dev)
         self.kp, self.vp = mk(n, 32, 128), mk(n, 32, 128)
         self.kt, self.vt = (rng.permutation(n)[:len(new) * H * self.pph].reshape(len(new), H, self.pph).astype(np.int32) for _ in range(2))
+        self.kt, self.vt = (np.pad(t, ((0, 0), (0, 0), (0, room)), constant_values=-1) for t in (self.kt, self.vt))
         self.cu = offsets(new)
         self.T = self.cu[-1]
         self.q = mk(max(self.T, 1), Hq, 128)[:self.T]
@@ -78,7 +79,7 @@ class Case:
 
     def dense(self, b):
         L = self.lens[b]
-        take = lambda pool, t: f64(pool[torch.tensor(t[b].astype(np.int64)).to(self.dev)]).transpose(0, 1, 2, 3).reshape(
+        take = lambda pool, t: f64(pool[torch.tensor(t[b, :, :self.pph].astype(np.int64)).to(self.dev)]).transpose(0, 1, 2, 3).reshape(
             self.H, -1, 128)[:, :L].transpose(1, 0, 2)
         return take(self.kp, self.kt), take(self.vp, self.vt)
 
@@ -110,11 +111,28 @@ CASES = [  # nodes, tokens with them, H_q, H_kv
     ([200], [190], 4, 2), ([6] * 20, [200 + 37 * i for i in range(20)], 10, 2), ([1] * 3, [5000, 1, 3100], 1, 1)]
 
 
+# A call with little room for its number of requests and heads gives every segment a workgroup of its own, one with more
+# cuts them.
+ROOM = [0, 2000]
+
+
 @pytest.mark.parametrize("new,lens,Hq,H", CASES)
 @pytest.mark.parametrize("tree", [True, False])
-def test_against_oracle(dev, new, lens, Hq, H, tree):
-    c = Case(dev, new, lens, Hq, H, seed=sum(lens) + Hq, tree=tree)
+@pytest.mark.parametrize("room", ROOM)
+def test_against_oracle(dev, new, lens, Hq, H, tree, room):
+    c = Case(dev, new, lens, Hq, H, seed=sum(lens) + Hq, tree=tree, room=room)
     c.check(c.run())
+
+
+def test_many_rows_of_a_segment_each(dev):
+    c = Case(dev, [50] * 40, [50 + 6 * i for i in range(40)], 32, 8, seed=13, room=80)
+    assert asym._tree_workspace(40, 32, 8, 2000, c.kt.shape[2] * 32, 0) == 0
+    c.check(c.run(), only=[0, 1, 31, 39])
+
+
+def test_which_calls_are_cut(dev):
+    assert asym._tree_workspace(64, 32, 8, 64 * 32, 2000, 0) == 0 < asym._tree_workspace(8, 32, 8, 8 * 32, 2000, 0)
+    assert asym._tree_workspace(1, 8, 1, 1, 256, 0) == 0 < asym._tree_workspace(1, 8, 1, 1, 257, 0)
 
 
 @pytest.mark.parametrize("split", [32, 64, 96, 4096])
@@ -124,16 +142,16 @@ def test_shares_of_any_length(dev, split):
 
 
 # Sizes at which a workgroup has eight waves: more than 192 rows a request in the mean, and room in the tables for
-# 180 x 256 pages of units, of which the lengths need not make use.
+# 180 x 256 pages of units, of which the lengths need not make use, and too much for a workgroup a segment.
 MANY_ROWS = [([70, 0, 129, 60], [1000, 5, 700, 64], 8, 2, 2880), ([17, 16, 15, 33], [500, 16, 1000, 90], 16, 1, 5120),
              ([200, 257], [190, 600], 3, 3, 5120), ([300], [2100], 4, 1, 15360), ([50] * 70, [50 + 13 * i for i in range(70)], 8, 2, 190)]
 
 
 def many_rows(dev, new, lens, Hq, H, room, **kw):
-    c = Case(dev, new, lens, Hq, H, seed=sum(lens), **kw)
+    c = Case(dev, new, lens, Hq, H, seed=sum(lens), room=room - max(1, -(-max(lens) // 32)), **kw)
     G = Hq // H
-    assert c.T * G > 192 * len(new) and (c.T * G // 256 + len(new)) * H * room >= 180 * 256
-    c.kt, c.vt = (np.pad(t, ((0, 0), (0, 0), (0, room - c.pph)), constant_values=-1) for t in (c.kt, c.vt))
+    assert c.kt.shape[2] == room and c.T * G > 192 * len(new) and (c.T * G // 256 + len(new)) * H * room >= 180 * 256
+    assert asym._tree_workspace(len(new), Hq, H, c.T, room * 32, 0) > 0
     return c
 
 
@@ -197,8 +215,9 @@ def test_rows_of_very_many_pieces(dev, G):
 
 @pytest.mark.parametrize("B", [3, 130])
 @pytest.mark.parametrize("split", [0, 32])
-def test_offsets_that_fall_write_nothing(dev, B, split):
-    c = Case(dev, [4] * B, [70] * B, 4, 2, seed=B)
+@pytest.mark.parametrize("room", ROOM)
+def test_offsets_that_fall_write_nothing(dev, B, split, room):
+    c = Case(dev, [4] * B, [70] * B, 4, 2, seed=B, room=room)
     ref = c.run(split_tokens=split)
     good, c.cu = c.cu, list(c.cu)
     c.cu[-2] = c.cu[-3] - 1
@@ -215,9 +234,10 @@ def test_scales(dev, scale, sigma):
     c.check(c.run(scale=scale), scale)
 
 
-def test_masks_that_are_not_trees(dev):
+@pytest.mark.parametrize("room", ROOM)
+def test_masks_that_are_not_trees(dev, room):
     # any bits: nodes that see later ones, only others, or nothing (behind no token at all)
-    c = Case(dev, [70, 40], [70, 41], 4, 2, seed=3)
+    c = Case(dev, [70, 40], [70, 41], 4, 2, seed=3, room=room)
     bits = torch.rand((110, 128), generator=torch.Generator().manual_seed(1)) < 0.4
     bits[5] = bits[64] = bits[80] = False
     c.sees = [[{j for j in range(128) if bits[i, j]} for i in range(70)], [{j for j in range(128) if bits[70 + i, j]} for i in range(40)]]
@@ -242,8 +262,9 @@ def test_split_and_unsplit_agree_with_prompt_attention(dev):
     assert float((o.float() - p.float()).abs().max()) <= 2 * 2.0 ** -8 * 8
 
 
-def test_strides_and_rows_outside(dev):
-    c = Case(dev, [6, 0, 9], [50, 3, 100], 8, 2, seed=9)
+@pytest.mark.parametrize("room", ROOM)
+def test_strides_and_rows_outside(dev, room):
+    c = Case(dev, [6, 0, 9], [50, 3, 100], 8, 2, seed=9, room=room)
     ref, lse = c.run(), c.lse
     wide = torch.full((c.T + 7, 14, 128), float("nan"), dtype=torch.bfloat16, device=dev)
     wide[4:4 + c.T, 3:11] = c.q
@@ -258,8 +279,9 @@ def test_strides_and_rows_outside(dev):
 
 @pytest.mark.parametrize("G,n", [(1, 3), (4, 12), (4, 40)])
 @pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
-def test_what_a_node_does_not_see_cannot_reach_it(dev, G, n, bad):
-    c = Case(dev, [n, 2], [75, 40], 2 * G, 2, seed=n + G)
+@pytest.mark.parametrize("room", ROOM)
+def test_what_a_node_does_not_see_cannot_reach_it(dev, G, n, bad, room):
+    c = Case(dev, [n, 2], [75, 40], 2 * G, 2, seed=n + G, room=room)
     ref = c.run()
     # behind the requests' tokens, in other pages, and in no node's sight
     k0, v0 = c.kp.clone(), c.vp.clone()
@@ -314,8 +336,9 @@ def test_scores_of_the_lowest_value(dev):
     assert np.all(np.abs(got[:, 0] - np.array(want)) <= 2.0 ** -7 * 4)
 
 
-def test_entries_outside_the_pool_read_zeros(dev):
-    c = Case(dev, [4], [100], 4, 1, seed=2)
+@pytest.mark.parametrize("room", ROOM)
+def test_entries_outside_the_pool_read_zeros(dev, room):
+    c = Case(dev, [4], [100], 4, 1, seed=2, room=room)
     c.kp[int(c.kt[0, 0, 1])] = 0
     c.vp[int(c.vt[0, 0, 2])] = 0
     ref = c.run()
@@ -364,8 +387,9 @@ def test_pages_past_4_gib(dev):
     assert torch.equal(c.run(), ref)
 
 
-def test_streams_and_runs_give_the_same_bits(dev):
-    c = Case(dev, [12, 3, 1], [800, 333, 2100], 8, 2, seed=10)
+@pytest.mark.parametrize("room", ROOM)
+def test_streams_and_runs_give_the_same_bits(dev, room):
+    c = Case(dev, [12, 3, 1] + ([2] * 300 if not room else []), [800, 333, 2100] + ([9] * 300 if not room else []), 8, 2, seed=10, room=room)
     ref = c.run()
     torch.cuda.synchronize()
     s = asym.stream_create()
@@ -379,8 +403,9 @@ def test_streams_and_runs_give_the_same_bits(dev):
     asym.stream_destroy(s)
 
 
-def test_captured_and_replayed(dev):
-    c = Case(dev, [12, 3], [800, 333], 8, 2, seed=11)
+@pytest.mark.parametrize("lens,other", [([800, 333], [700, 40]), ([200, 133], [100, 0])])
+def test_captured_and_replayed(dev, lens, other):
+    c = Case(dev, [12, 3], lens, 8, 2, seed=11)
     args = [c.kp, c.vp, i32(c.kt, dev), i32(c.vt, dev), i32(c.cu, dev), i32(c.lens, dev)]
     eager = lambda q, lens: asym.attn_tree_paged(q, *args[:5], lens, mask=c.mask)
     held, lens, o = c.q.clone(), args[5].clone(), torch.empty_like(c.q)
@@ -391,7 +416,7 @@ def test_captured_and_replayed(dev):
     with torch.cuda.graph(graph):
         asym.attn_tree_paged(held, *args[:5], lens, mask=c.mask, o=o)
         asym.attn_tree_paged(-held, *args[:5], lens, mask=c.mask, o=o2)
-    for s, new in ((1, [800, 333]), (-1, [700, 40]), (2, [12, 320])):
+    for s, new in ((1, c.lens), (-1, other), (2, [12, 3])):
         held.copy_(c.q * s), lens.copy_(i32(new, dev))
         graph.replay()
         torch.cuda.synchronize()
