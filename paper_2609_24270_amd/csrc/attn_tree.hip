@@ -69,14 +69,13 @@ struct TreeParams {
   float* lse;                    // [T][Hq], nullable
   float* part_o;                 // [shares][2][rows][128]
   float* part_ml;                // [shares][2][rows][2]: max (of the raw scores), sum
-  int2* cut;                     // per (unit, key/value head), a unit being the rows of a request that one workgroup
+  int2* cut;                     // null: nothing is cut, a share is a segment of up to `least` pages.  Else per (unit, key/value head), a unit being the rows of a request that one workgroup
                                  // serves: of one that was cut, 2 (its first share) + (1: that share's last piece),
                                  // its last share; -1 of one that was not
   int B, Hq, Hkv, G, T, S, pph, pool_pages;
   int rows;                      // of a workgroup: 32 a wave
-  int shares, least;             // a share has the batch's pages over the shares, at least `least`
-  bool fit;                      // where that makes segments begin with shares, a few more
-  bool whole;                    // a share is a segment, of up to `least` pages: nothing is cut
+  int shares, least;             // a share has `least` pages;
+  bool fit;                      // or the batch's pages over the shares, if they are more, or a few more than that
   float c, scale;                // |scale| * log2(e), |scale|
   uint32_t q_flip;
 };
@@ -102,7 +101,7 @@ __device__ __forceinline__ Request request(const TreeParams& p, int b) {
   r.len = min(max(p.lens[b], 0), p.S);
   r.units = (int)(((int64_t)r.n * p.G + p.rows - 1) / p.rows);
   r.pages = (r.len + kKvPageTokens - 1) / kKvPageTokens;
-  if (p.whole) r.pages = max(r.pages, 1);  // (no other launch writes the rows that see nothing)
+  if (!p.cut) r.pages = max(r.pages, 1);  // (no other launch writes the rows that see nothing)
   return r;
 }
 // The unit's place in `cut` (a request's units follow the rows before it, one more a request)
@@ -229,7 +228,7 @@ __global__ void __launch_bounds__(64 * NW, 2) attn_tree_kernel(TreeParams args) 
 
   const TreeParams p0 = arguments();
   Batch bt;
-  bt.pad = p0.whole ? p0.least : 1;
+  bt.pad = p0.cut ? 1 : p0.least;
   bt.load(p0, 0, 0, lane);
   int total = bt.end();
   bool falls = bt.falls;
@@ -244,7 +243,8 @@ __global__ void __launch_bounds__(64 * NW, 2) attn_tree_kernel(TreeParams args) 
   }
   if (__any(falls)) return;  // (the joining launch too)
   total *= p0.Hkv;
-  int share = p0.whole ? p0.least : max((total + p0.shares - 1) / p0.shares, p0.least);
+  int share = p0.least;
+  if (p0.fit) share = max(share, (total + p0.shares - 1) / p0.shares);
   // A share that goes on in a second segment costs as much as a few pages more would; where shares of up to kLonger more
   // pages suffice with every segment beginning a share of its own, they do: a tree of 8 nodes behind 777 tokens 16.2 ->
   // 14.6 us, 16 of 16 behind up to 1000 28.8 -> 23.6.
@@ -633,7 +633,7 @@ __global__ void __launch_bounds__(64 * NW, 2) attn_tree_kernel(TreeParams args) 
         if (last.lse && on && q4 == 0) last.lse[out] = lt == 0.f ? -INFINITY : m[k] * last.scale + __logf(lt);
       }
     }
-    if (x.pg == 0 && threadIdx.x == 0 && !last.whole)
+    if (x.pg == 0 && threadIdx.x == 0 && last.cut)
       last.cut[unit_id(last, x.b, x.first, x.unit) * last.Hkv + x.hk] =
           whole ? int2{-1, 0} : int2{2 * w + (start ? 0 : 1), (x.end - 1) / share};
     if (x.end >= f1) return;
@@ -855,10 +855,10 @@ extern "C" int asym_attn_tree_paged_bf16(int B, int H_q, int H_kv, int T, int S_
   const size_t pieces = (size_t)P.shares * 2 * P.rows;
   p.part_o = static_cast<float*>(workspace);
   p.part_ml = p.part_o + pieces * kKvD;
-  p.cut = reinterpret_cast<int2*>(p.part_ml + pieces * 2);
+  p.cut = P.whole ? nullptr : reinterpret_cast<int2*>(p.part_ml + pieces * 2);
   p.B = B; p.Hq = H_q; p.Hkv = H_kv; p.G = H_q / H_kv; p.T = T; p.S = S_max; p.pph = pages_per_head;
   p.pool_pages = (int)pool_pages;
-  p.rows = P.rows; p.shares = P.shares; p.least = P.least; p.fit = P.fit; p.whole = P.whole;
+  p.rows = P.rows; p.shares = P.shares; p.least = P.least; p.fit = P.fit;
   p.scale = std::fabs(scale);
   p.c = std::fmax(p.scale * 1.4426950408889634f, 1.17549435e-38f);  // (0 weighs all tokens alike, a masked one not at all)
   p.q_flip = scale < 0 ? 0x80008000u : 0u;
