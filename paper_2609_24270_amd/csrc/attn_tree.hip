@@ -644,8 +644,9 @@ __global__ void __launch_bounds__(64 * NW, 2) attn_tree_kernel(TreeParams args) 
 // The joining launch: a wave has kJoinHeads query heads of a token, or, where rows are few and have many pieces (SPLIT), a
 // workgroup's waves share one.  Rows of a request without tokens are written, those that were cut are joined in the order
 // of the shares (SPLIT: each wave's every kJoinWaves-th piece, then the waves), the first kJoinPieces of each loaded at once.
-// 32 trees of 24 nodes behind up to 8000 tokens: 12 us, and with a head a wave 20.
-constexpr int kJoinHeads = 2, kJoinPieces = 4;
+// us for 32 trees of 24 nodes behind up to 8000 tokens and for 8 of 64 behind up to 32768, at 2 heads a wave and 2, 3, 4, 5,
+// 6 and 8 pieces: 18.3 14.4 11.9 12.2 12.5 13.0, 14.0 13.8 11.2 8.7 9.0 11.6; 4 heads and 4 pieces 12.1 14.7; one head and 6 14.4 10.6.
+constexpr int kJoinHeads = 2, kJoinPieces = 5;
 template <bool SPLIT>
 __global__ void __launch_bounds__(64 * kJoinWaves) attn_tree_join(TreeParams p) {
   constexpr int HEADS = SPLIT ? 1 : kJoinHeads, STEP = SPLIT ? kJoinWaves : 1;

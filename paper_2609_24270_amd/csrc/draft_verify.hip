@@ -26,7 +26,7 @@
 // workgroup a request: it walks to the end (summing slices alone if need be) and draws.
 //
 // Bound by the chain of sums, and each by HBM: only rows that a sum is needed of are read, one a rejection and one for
-// the draw at most.  64 trees of 31 tokens, V 128000, fp32: 56 us in six launches, which read 61, 47, 23, 2, 0 and 2 MB; 16
+// the draw at most.  64 trees of 31 tokens, V 128000, fp32: 50 us in six launches, which read 61, 47, 23, 2, 0 and 2 MB; 16
 // chains of 4, V 32000: 5.0 and 5.5 us in two.
 #include <hip/hip_runtime.h>
 
