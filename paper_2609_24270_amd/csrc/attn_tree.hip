@@ -7,8 +7,8 @@
 // bit j is set in node i's mask (without masks: j <= i, a chain; n = 1 is plain decoding with
 // a length per request).
 //
-// A row is a (node, query head of the group) pair, node-major.  A workgroup of four or eight waves (tree_plan says when)
-// serves up to 32 rows a wave of one request and key/value head, and takes its tokens 64 at a time, two pages.  K and V
+// A row is a (node, query head of the group) pair, node-major.  A workgroup of four or eight waves (tree_plan says when, and NQ)
+// serves up to 16 NQ rows a wave (NQ 1 or 2) of one request and key/value head, and takes its tokens 64 at a time, two pages.  K and V
 // come by LDS loads, each wave's part of the block, STAGES - 1 blocks ahead; per block a wave computes
 //   S^T = K . Q^T   v_mfma_f32_16x16x32_bf16, Q in registers, K by ds_read_b128;
 //   softmax         a row's 64 scores lie in four lanes; its running max is raised only when
@@ -73,7 +73,7 @@ struct TreeParams {
                                  // serves: of one that was cut, 2 (its first share) + (1: that share's last piece),
                                  // its last share; -1 of one that was not
   int B, Hq, Hkv, G, T, S, pph, pool_pages;
-  int rows;                      // of a workgroup: 32 a wave
+  int rows;                      // of a workgroup: 16 NQ a wave
   int shares, least;             // a share has `least` pages;
   bool fit;                      // or the batch's pages over the shares, if they are more, or a few more than that
   float c, scale;                // |scale| * log2(e), |scale|
@@ -218,9 +218,9 @@ __device__ __forceinline__ TreeParams arguments() {
   return *(const TreeParams*)at;
 }
 
-template <int NW, int STAGES, int POLICY>
+template <int NW, int STAGES, int NQ, int POLICY>
 __global__ void __launch_bounds__(64 * NW, 2) attn_tree_kernel(TreeParams args) {
-  constexpr int NQ = 2, WR = 16 * NQ;
+  constexpr int WR = 16 * NQ;
   __shared__ __attribute__((aligned(1024))) unsigned char lds[2 * STAGES * kTileBytes];  // K tiles, then V tiles
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int n = lane & 15, q4 = lane >> 4;
@@ -757,7 +757,7 @@ __global__ void __launch_bounds__(64 * kJoinWaves) attn_tree_join(TreeParams p) 
 }
 
 struct TreePlan {
-  int waves = 4, rows = 128, shares = 0, least = 1;
+  int waves = 4, blocks = 2, rows = 128, shares = 0, least = 1;
   bool fit = true, whole = false;
   int64_t units = 0;
   size_t bytes = 0;
@@ -776,24 +776,39 @@ int tree_plan(int B, int Hq, int Hkv, int T, int S, int split_tokens, TreePlan* 
   }
   if ((int64_t)T * Hq >= (1 << 26)) return fail(ASYM_EUNSUPPORTED, "tree attention: too many rows");  // (threads are counted in 32 bits)
   const int64_t all = (int64_t)T * (Hq / Hkv), mean = (all + B - 1) / B;
-  const int64_t pages = ((int64_t)S + kKvPageTokens - 1) / kKvPageTokens, most = (all / 128 + B) * Hkv;
+  const int64_t pages = ((int64_t)S + kKvPageTokens - 1) / kKvPageTokens, most = (all / 64 + B) * Hkv;
   if (most > (1 << 30) || most * pages > (1 << 30)) return fail(ASYM_EUNSUPPORTED, "tree attention: more than 2^30 pages");
-  // Whole segments need no pieces, no second launch and no workspace, and take as long as the longest request: about 6 us
-  // and 0.58 a page where it is alone.  Cut ones take two launches and what the pieces of T x H_q rows cost to write and
-  // join.  us, cut first, lengths from a quarter of S on, 32 / 8 heads: 1 request of 8 nodes, S 128 13.9 9.7, 256 14.2 10.9, 512
-  // 13.8 15.4; 8 of 8, 512 13.7 15.2; 8 of 32, 256 16.9 11.8, 512 26.1 16.2; 16 of 24, 1000 26.5 27.7; 32 of 4, 1000 22.5 25.4; 24 of
-  // 16, 1000 24.7 26.2; 32 of 24, 1000 35.4 31.0, 2000 48.7 49.7, 8000 155 190; 16 of 64, 500 30.9 22.6, 1000 37.2 35.1, 2000
-  // 48.5 57.7; 64 of 1, 1000 41.6 33.6, 4000 111 112, 8000 206 219; 64 of 32, 64 40.4 17.2, 1000 86 60, 2000 129 97; 64 of 64, 500 99.5
-  // 50.0, 2000 194 145; 256 of 8, 1000 165 140, 4000 473 450; 256 of 1, 8000 786 824.
-  const int64_t units = all / 128 + B;  // of four waves each
-  P.whole = split_tokens == 0 && (pages <= 8 || pages <= units * Hkv / 11 + (int64_t)T * Hq / 1200);
+  const int64_t segments = (all / 128 + B) * Hkv;  // of four waves and two blocks of rows each
+  // One block of 16 rows a wave spreads few rows over more waves, and a wave's chain of products, softmax and products again, which
+  // is what a block of tokens costs where the matrix cores have little to do, is half as long; the pages of more than 64 rows
+  // are read again.  us, two blocks first, 32 / 8 heads, n nodes in the mean, lengths from a quarter of S on, in a graph, S 250,
+  // 777, 2048, 8000: 1 request of 8 nodes 10.5 8.3, 10.0 9.2, 11.2 10.0; 64 of 1 13.7 11.8, 27.1 24.6, 64.1 61.5, 202 201; 64 of 10
+  // 16.1 14.1, 31.3 26.8, 71 62, 234 232; 64 of 16 18.2 19.1, 31.5 32.1, 73 77; 32 of 16 13.0 11.8, 23.1 19.5, 47.8 59.1, 130 163; 8 of
+  // 32 11.4 9.0, 28.9 19.8, 34.5 25.8, 50.9 43.8; 8 of 64 13.0 10.1, 26.6 23.2, 34.1 29.7, 64 96; 32 of 32 16.6 16.3, 29.6 25.2, 64
+  // 57, 183 263; 1 of 512 31.7 24.2 (S 512), 37.0 26.6, 42.8 34.3, 67 100.
+  const bool narrow = mean <= 40 || (segments <= 512 && segments * pages <= 16384);
+  // Whole segments need no pieces, no second launch and no workspace, and take as long as the longest request: about 5 us
+  // and 0.42 a page where it is alone (two blocks of rows: 6 and 0.58).  Cut ones take two launches and what the pieces of T x
+  // H_q rows cost to write and join.  us, cut first, as above: one block of rows: 1 request of 8 nodes, S 300 13.7 9.2, 380 13.7
+  // 10.0, 512 13.7 11.5 (in a graph 9.8 11.6); 16 of 8, 500 15.4 11.8, 1000 20.1 20.4; 8 of 16, 1000 20.4 18.7, 1500 20.4 25.9; 8 of
+  // 64, 1000 23.3 19.6, 1500 25.8 28.4; 24 of 8, 1500 23.3 25.9; 16 of 32, 2000 33.0 37.9; 32 of 10, 2000 36.0 35.7, 3000 54.8
+  // 59.6; 64 of 1, 2000 61.3 56.8, 4000 108 108, 8000 200 211; 64 of 10, 4000 129 111, 5000 155 139; 256 of 1, 8000 777 811.  Two:
+  // 64 of 16, 2000 87.5 72.1; 32 of 24, 1500 41.4 39.7, 2000 48.7 49.7, 4000 92 98, 8000 155 190; 16 of 64, 2000 48.5 57.7; 64 of
+  // 32, 2000 129 97, 4000 201 181; 64 of 64, 500 99.5 50.0, 2000 194 145; 32 of 64, 4000 154 169.
+  const int64_t weight = (int64_t)T * Hq / 1200;
+  const int64_t longest = !narrow           ? segments / 11 + weight
+                          : segments >= 512 ? 128 + weight
+                          : segments >= 256 ? 64
+                                            : std::max<int64_t>(12, std::min<int64_t>(segments * 2 / 5, 32));
+  P.whole = split_tokens == 0 && pages <= longest;
   // Eight waves read the pages of up to 256 rows once, four of 128; but of four there are two workgroups a CU, which hide each
-  // other's starts, ends and waits, and rows past 128 cost a wave what it has of them.  us, four first, lengths as above, 32 /
-  // 8 heads, n nodes in the mean: 16 requests, n 40, S 4000 55 74; 8, n 48, S 32768 184 184; n 64: 4 of 8000 44 48, 8 of 8000 66 70,
-  // 16 of 8000 157 138, 32 of 4000 169 156, 8 of 32768 258 217; of n 512: 2 of 4000 64 56, 4 of 8000 174 169.  Whole segments: n
-  // 64, 64 of 2000 145 160, 64 of 4000 269 288, 128 of 1000 166 187, 128 of 4000 569 562.
-  P.waves = !P.whole && mean > 192 && (all / 256 + B) * Hkv * pages >= 180 * 256 ? 8 : 4;
-  P.rows = 32 * P.waves;
+  // other's starts, ends and waits, and rows past 128 cost a wave what it has of them.  us, four first, as above: 16 requests, n
+  // 40, S 4000 55 74; 8, n 48, S 32768 184 184; n 64: 4 of 8000 44 48, 8 of 8000 66 70, 16 of 8000 157 138, 32 of 4000 169 156, 8 of
+  // 32768 258 217; n 512: 2 of 4000 64 56, 4 of 8000 174 169.  Whole segments: n 64, 64 of 2000 145 160, 64 of 4000 269 288, 128 of
+  // 1000 166 187, 128 of 4000 569 562.
+  P.waves = !narrow && !P.whole && mean > 192 && (all / 256 + B) * Hkv * pages >= 180 * 256 ? 8 : 4;
+  P.blocks = narrow ? 1 : 2;
+  P.rows = 16 * P.blocks * P.waves;
   P.units = all / P.rows + B;
   const int64_t heads = P.units * Hkv;  // segments, where none is cut
   P.fit = split_tokens == 0 && !P.whole;
@@ -867,8 +882,9 @@ extern "C" int asym_attn_tree_paged_bf16(int B, int H_q, int H_kv, int T, int S_
   // (at most: the requests may be shorter than S_max)
   const int64_t bytes = 2ll * B * H_kv * ((S_max + (int64_t)kKvPageTokens - 1) / kKvPageTokens) * kPageBytes;
   const bool once = attn_streams_kv(paged_kv_bytes(bytes, (int64_t)pool_pages * kPageBytes, k_pool == v_pool));
-  auto kernel = P.waves == 8 ? (once ? attn_tree_kernel<8, 4, 2> : attn_tree_kernel<8, 4, 0>)
-                             : (once ? attn_tree_kernel<4, 2, 2> : attn_tree_kernel<4, 2, 0>);
+  auto kernel = P.waves == 8    ? (once ? attn_tree_kernel<8, 4, 2, 2> : attn_tree_kernel<8, 4, 2, 0>)
+                : P.blocks == 2 ? (once ? attn_tree_kernel<4, 2, 2, 2> : attn_tree_kernel<4, 2, 2, 0>)
+                                : (once ? attn_tree_kernel<4, 2, 1, 2> : attn_tree_kernel<4, 2, 1, 0>);
   hipLaunchKernelGGL(kernel, dim3((unsigned)P.shares), dim3(64 * P.waves), 0, s, p);
   ASYM_HIP(hipGetLastError());
   if (P.whole) return ASYM_OK;

@@ -53,7 +53,8 @@ def test_no_registers_in_memory_and_no_packed_fp32(built, src):
     assert not re.search(r"\bs_(store|atomic|buffer_store|scratch_store)", asm)
 
 
-@pytest.mark.parametrize("form,lds", [("Li4ELi2ELi0E", 64), ("Li4ELi2ELi2E", 64), ("Li8ELi4ELi0E", 128), ("Li8ELi4ELi2E", 128)])
+@pytest.mark.parametrize("form,lds", [("Li4ELi2ELi1ELi0E", 64), ("Li4ELi2ELi1ELi2E", 64), ("Li4ELi2ELi2ELi0E", 64), ("Li4ELi2ELi2ELi2E", 64),
+                                      ("Li8ELi4ELi2ELi0E", 128), ("Li8ELi4ELi2ELi2E", 128)])
 def test_the_loop_waits_for_no_more_than_its_tiles(built, form, lds):
     asm = built["attn_tree.hip"]
     name = f"attn_tree_kernelI{form}"
@@ -63,15 +64,16 @@ def test_the_loop_waits_for_no_more_than_its_tiles(built, form, lds):
     assert lds * 1024 <= size <= lds * 1024 + 512
     text = "\n".join(body)
     assert "v_mfma_f32_16x16x32_bf16" in text and "ds_read_b64_tr_b16" in text
-    # the main loop's stretches without a branch: a block's 64 products are two of 32, and between the first
-    # and the last of each nothing waits for all loads on their way
+    # the main loop's stretches without a branch: a block's 64 products (32 of one block of rows) are two halves, and between
+    # the first and the last of each nothing waits for all loads on their way
     runs, now = [], []
     for l in body:
         if re.match(r"^\.LBB", l):
             runs.append(now)
             now = []
         now.append(l)
-    full = [r for r in runs + [now] if sum("v_mfma" in l for l in r) >= 32]
+    half = 16 * int(form[10])
+    full = [r for r in runs + [now] if sum("v_mfma" in l for l in r) >= half]
     assert len(full) >= 2
     for r in full[:2]:
         at = [i for i, l in enumerate(r) if "v_mfma" in l]

@@ -112,8 +112,8 @@ CASES = [  # nodes, tokens with them, H_q, H_kv
 
 
 # A call with little room for its number of requests and heads gives every segment a workgroup of its own, one with more
-# cuts them.
-ROOM = [0, 2000]
+# cuts them, and one with much more, if its requests have more than 40 rows in the mean, has 128 rows a workgroup and not 64.
+ROOM = [0, 2000, 9000]
 
 
 @pytest.mark.parametrize("new,lens,Hq,H", CASES)
@@ -132,7 +132,7 @@ def test_many_rows_of_a_segment_each(dev):
 
 def test_which_calls_are_cut(dev):
     assert asym._tree_workspace(64, 32, 8, 64 * 32, 2000, 0) == 0 < asym._tree_workspace(8, 32, 8, 8 * 32, 2000, 0)
-    assert asym._tree_workspace(1, 8, 1, 1, 256, 0) == 0 < asym._tree_workspace(1, 8, 1, 1, 257, 0)
+    assert asym._tree_workspace(1, 8, 1, 1, 384, 0) == 0 < asym._tree_workspace(1, 8, 1, 1, 385, 0)
 
 
 @pytest.mark.parametrize("split", [32, 64, 96, 4096])
