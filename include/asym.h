@@ -1164,8 +1164,8 @@ int asym_attn_tree_paged_workspace(int B, int H_q, int H_kv, int T, int S_max, i
  * int32 [B], how many; token int32 [B].  A request without nodes: count 0, token -1.  Rows of path outside every
  * request are left as they are.  cu: device int32 [B + 1], not falling, held within [0, T].
  * Probabilities are read where they are needed only: a node's own two, and the rows of which sums are taken.
- * The workspace (16-byte aligned; asym_draft_verify_workspace's bytes) must not be shared by calls that may
- * overlap.  No host synchronisation; may be captured; asynchronous.  Errors: ASYM_EINVAL, ASYM_EUNSUPPORTED, ASYM_EHIP. */
+ * The workspace (16-byte aligned; asym_draft_verify_workspace's bytes; may be null if they are 0) must not be
+ * shared by calls that may overlap.  No host synchronisation; may be captured; asynchronous.  Errors: ASYM_EINVAL, ASYM_EUNSUPPORTED, ASYM_EHIP. */
 int asym_draft_verify(int B, int T, int V, int bf16, const void* target, int64_t target_row,
                       const void* draft, int64_t draft_row, const int32_t* tokens, const int32_t* parents,
                       const int32_t* cu, const float* accept, const float* final,

@@ -1715,12 +1715,12 @@ def draft_verify(target, draft, tokens, parents, cu, accept, final, path=None, c
     def call(raw):
         new = lambda t, n: torch.empty(n, dtype=torch.int32, device=target.device) if t is None else t
         r = new(path, T), new(count, B), new(token, B)
-        ws = _workspace(nbytes, target.device)
+        ws = _workspace(nbytes, target.device) if nbytes else None
         _check(load_library().asym_draft_verify(
             B, T, V, 0 if target.dtype is torch.float32 else 1, target.data_ptr(), row,
             None if draft is None else draft.data_ptr(), draft_row, tokens.data_ptr(),
             None if parents is None else parents.data_ptr(), cu.data_ptr(), accept.data_ptr(), final.data_ptr(),
-            r[0].data_ptr(), r[1].data_ptr(), r[2].data_ptr(), ws.data_ptr(), nbytes, raw))
+            r[0].data_ptr(), r[1].data_ptr(), r[2].data_ptr(), ws.data_ptr() if nbytes else None, nbytes, raw))
         return r
     return _on(device, stream, call)
 

@@ -13,7 +13,7 @@
 //   S^T = K . Q^T   v_mfma_f32_16x16x32_bf16, Q in registers, K by ds_read_b128;
 //   softmax         a row's 64 scores lie in four lanes; its running max is raised only when
 //                   some row's grows by more than 2^8;
-//   O^T += V^T . P^T  with P rounded to bf16 (the type of the products' operands: 2^-9
+//   O^T += V^T . P^T  with P rounded to bf16 (the type of the products' operands: 2^-8
 //                   relative at most, as the output's own rounding) in the scores' registers,
 //                   V^T by ds_read_b64_tr_b16.
 // Scores, max, sum and output are fp32.  One barrier a block.

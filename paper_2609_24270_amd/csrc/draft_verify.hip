@@ -40,7 +40,8 @@ namespace {
 
 constexpr int kThreads = 256;   // of a workgroup that sums a slice
 constexpr int kLast = 1024;     // of one that ends a request
-constexpr int kMaxSlice = 8192;
+constexpr int kMinSlice = 2048, kMaxSlice = 8192;
+constexpr int kOneLaunch = 16384;  // of vocabularies up to this size one launch does everything
 
 // Where a request's walk stands
 struct State {
@@ -323,12 +324,13 @@ __global__ void __launch_bounds__(kLast) verify_last(VerifyParams p) {
   __shared__ double red[kLast / 64], part[kBatch][4];
   __shared__ State told;
   __shared__ uint32_t dead[kLast / kThreads][kMaxSlice / 32];
+  __shared__ double own[kOneLaunch / kMinSlice];
   __shared__ int marks[kLast / 64], found;
   const int b = blockIdx.x, lane = threadIdx.x & 63;
   int first, n;
   packed_rows(p.cu, b, p.T, first, n);
   const int prev = (p.round - 1) & 1;
-  double* sums = p.sums + ((size_t)prev * p.B + b) * p.slices;  // (this workgroup's own from here on)
+  double* sums = p.round > 0 ? p.sums + ((size_t)prev * p.B + b) * p.slices : own;  // (this workgroup's own from here on)
   const State was = p.round > 0 ? p.state[(size_t)prev * p.B + b] : State{};
   const float draw = p.final[b];
   if (n == 0) {
@@ -477,10 +479,10 @@ int verify_plan(int B, int T, int V, VerifyPlan* plan) {
   VerifyPlan P;
   // slices of 2048, 4096 or 8192 values: enough for four workgroups a CU, or the smallest
   P.slice = kMaxSlice;
-  while (P.slice > 2048 && (int64_t)B * ((V + P.slice - 1) / P.slice) < 1024) P.slice /= 2;
+  while (P.slice > kMinSlice && (int64_t)B * ((V + P.slice - 1) / P.slice) < 1024) P.slice /= 2;
   P.slices = (int)(((int64_t)V + P.slice - 1) / P.slice);
   if ((int64_t)B * P.slices >= (1 << 22)) return fail(ASYM_EUNSUPPORTED, "draft verify: too many requests, or too large a vocabulary");
-  P.bytes = (size_t)2 * B * (sizeof(State) + P.slices * sizeof(double));
+  P.bytes = V <= kOneLaunch ? 0 : (size_t)2 * B * (sizeof(State) + P.slices * sizeof(double));
   *plan = P;
   return ASYM_OK;
 }
@@ -520,7 +522,7 @@ extern "C" int asym_draft_verify(int B, int T, int V, int bf16, const void* targ
   if (((uintptr_t)tokens | (uintptr_t)parents | (uintptr_t)cu | (uintptr_t)accept | (uintptr_t)final | (uintptr_t)path |
        (uintptr_t)count | (uintptr_t)token) & 3u)
     return fail(ASYM_EINVAL, "draft verify: nodes, random numbers and outputs must be 4-byte aligned");
-  if (!workspace || workspace_bytes < P.bytes || ((uintptr_t)workspace & 15u))
+  if (P.bytes && (!workspace || workspace_bytes < P.bytes || ((uintptr_t)workspace & 15u)))
     return fail(ASYM_EINVAL, "draft verify: the workspace must be 16-byte aligned and hold asym_draft_verify_workspace's bytes");
   VerifyParams p = {};
   p.target = target; p.draft = draft;
@@ -529,21 +531,21 @@ extern "C" int asym_draft_verify(int B, int T, int V, int bf16, const void* targ
   p.accept = accept; p.final = final;
   p.path = path; p.count = count; p.token = token;
   p.state = static_cast<State*>(workspace);
-  p.sums = reinterpret_cast<double*>(p.state + 2 * (size_t)B);
+  p.sums = P.bytes ? reinterpret_cast<double*>(p.state + 2 * (size_t)B) : nullptr;
   p.B = B; p.T = T; p.V = V; p.slice = P.slice; p.slices = P.slices;
   hipStream_t s = static_cast<hipStream_t>(stream);
-  // Up to 16384 tokens the last launch sums a row as fast as another begins and does all of it.  us with none, 1 and 2
-  // launches before it, chains of 16 nodes, V 5000: 1 request 12.2 13.6 15.9, 64 12.5 13.7 16.1; trees: 12.7 14.0 16.5, 15.4
-  // 17.7 19.8; V 16000: chains 12.3 13.6 16.1, 12.8 13.6 16.1, trees 12.6 13.7 16.4, 22.0 23.5 24.2; V 64000: chains 17.3 13.7
-  // 16.3, 19.6 16.0 18.4.
+  // Up to kOneLaunch tokens the last launch sums a row as fast as another begins, does all of it and needs no workspace.  us
+  // with none, 1 and 2 launches before it, V 5000: chains of 16 nodes, 1 request 10.5 13.6 15.9, 64 10.5 13.7 16.1; trees 10.9 14.0
+  // 16.5, 15.0 17.7 19.8; V 16000: chains 10.7 13.6 16.1, 12.1 13.6 16.1, trees 11.0 13.7 16.4, 22.1 23.5 24.2 (in graphs 9.8 9.6
+  // 11.8, 12.1 13.4 15.5, 10.6 10.8 11.9, 22.0 23.7 24.4); V 64000: chains 17.3 13.7 16.3, 19.6 16.0 18.4.
   // A chain rejects once at most, and without draft probabilities no sum is needed before the last.  A tree with them
   // needs a sum a rejection, the last launch takes what is over one by one, and waits for the request that needs the
   // most.  us with 1, 2, 3 and 4 launches before it, trees of 16 nodes, V 32000: 1 request 15.7 18.0 20.7 24.3, 4 24.8 22.8 22.3
   // 24.3, 16 30.6 28.8 26.4 26.0, 64 34.0 32.9 31.4 30.7; V 48000: 15.9 17.9 20.6 24.5, 21.0 18.4 21.1 24.2, 33.7 30.2 25.4
   // 26.1, 39.2 35.9 31.5 31.3; V 128000 (1 to 6): 1 24 19 23 27 29 32, 4 48 30 22 26 28 30, 16 70 54 37 30 32 34, 64 of 32
   // nodes 92 84 72 64 57 60.
-  int rounds = V > 16384;
-  if (draft && parents && V > 16384) {
+  int rounds = V > kOneLaunch;
+  if (draft && parents && V > kOneLaunch) {
     rounds = V > 65536 ? 2 : 1;
     for (int64_t requests = 4; requests <= B && rounds < 6; requests *= 4) ++rounds;
   }

@@ -181,13 +181,14 @@ def test_tree_refusals(change, want):
 
 VERIFY = dict(B=2, T=6, V=100, bf16=0, target=P, trow=100, draft=P, drow=100, tokens=P, parents=P, cu=P, accept=P, final=P, path=P, count=P,
               token=P, ws=P, wsb=1 << 20, stream=None)
+LONG = dict(V=20000, trow=20000, drow=20000)  # (shorter vocabularies need no workspace)
 
 
 @pytest.mark.parametrize("change,want", [
     (dict(B=-1), asym.EINVAL), (dict(T=-1), asym.EINVAL), (dict(V=0), asym.EINVAL), (dict(V=(1 << 30) + 1), asym.EUNSUPPORTED),
     (dict(trow=99), asym.EINVAL), (dict(drow=99), asym.EINVAL), (dict(target=None), asym.EINVAL), (dict(tokens=None), asym.EINVAL),
     (dict(final=None), asym.EINVAL), (dict(path=None), asym.EINVAL), (dict(target=P + 2), asym.EINVAL), (dict(bf16=1, draft=P + 1), asym.EINVAL),
-    (dict(parents=P + 2), asym.EINVAL), (dict(ws=None), asym.EINVAL), (dict(wsb=8), asym.EINVAL), (dict(ws=P + 8), asym.EINVAL),
+    (dict(parents=P + 2), asym.EINVAL), (dict(LONG, ws=None), asym.EINVAL), (dict(LONG, wsb=8), asym.EINVAL), (dict(LONG, ws=P + 8), asym.EINVAL),
     (dict(B=1 << 22), asym.EUNSUPPORTED), (dict(B=0), asym.OK)])
 def test_verify_refusals(change, want):
     assert code("asym_draft_verify", *{**VERIFY, **change}.values()) == want
@@ -213,7 +214,8 @@ def test_workspaces():
     assert code("asym_attn_tree_paged_workspace", 2, 8, 2, 6, 64, 0, None) == asym.EINVAL
     assert code("asym_attn_tree_paged_workspace", 2, 8, 3, 6, 64, 0, ctypes.byref(n)) == asym.EINVAL
     assert code("asym_attn_tree_paged_workspace", 0, 8, 2, 6, 64, 0, ctypes.byref(n)) == asym.OK and n.value == 0
-    assert code("asym_draft_verify_workspace", 2, 6, 1000, ctypes.byref(n)) == asym.OK and n.value > 0
+    assert code("asym_draft_verify_workspace", 2, 6, 16385, ctypes.byref(n)) == asym.OK and n.value > 0
+    assert code("asym_draft_verify_workspace", 2, 6, 16384, ctypes.byref(n)) == asym.OK and n.value == 0  # one launch
     assert code("asym_draft_verify_workspace", 2, 6, 1000, None) == asym.EINVAL
 
 
