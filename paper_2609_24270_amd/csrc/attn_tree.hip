@@ -812,6 +812,8 @@ int tree_plan(int B, int Hq, int Hkv, int T, int S, int split_tokens, TreePlan* 
   P.units = all / P.rows + B;
   const int64_t heads = P.units * Hkv;  // segments, where none is cut
   P.fit = split_tokens == 0 && !P.whole;
+  // (us in a graph with shares of 2, 4, 6 and 8 pages at least: 1 request of 8 nodes, S 500 9.0 9.9 10.9 12.3, 777 9.3 9.2 9.9 10.6,
+  // 2048 10.8 10.1 10.1 11.5; 16 of 8 with 8 / 1 heads, 777 12.1 11.6 12.4 13.1, 2048 18.0 13.2 13.0 14.1)
   P.least = P.whole ? (int)pages : P.fit ? 4 : split_tokens / kKvPageTokens;
   int64_t shares = P.whole ? heads : heads * pages / P.least + heads;  // (a segment may end in a part of one)
   if (P.fit) shares = std::min<int64_t>(shares, P.waves == 8 ? 256 : 512);
