@@ -69,7 +69,7 @@ struct TreeParams {
   float* lse;                    // [T][Hq], nullable
   float* part_o;                 // [shares][2][rows][128]
   float* part_ml;                // [shares][2][rows][2]: max (of the raw scores), sum
-  int2* cut;                     // null: nothing is cut, a share is a segment of up to `least` pages.  Else per (unit, key/value head), a unit being the rows of a request that one workgroup
+  int2* cut;                     // null: nothing is cut, a workgroup has a segment.  Else per (unit, key/value head), a unit being the rows of a request that one workgroup
                                  // serves: of one that was cut, 2 (its first share) + (1: that share's last piece),
                                  // its last share; -1 of one that was not
   int B, Hq, Hkv, G, T, S, pph, pool_pages;
@@ -95,11 +95,12 @@ __device__ __forceinline__ float over_quarters(float x, F f) {
 struct Request {
   int first, n, len, units, pages;
 };
+__device__ __forceinline__ int units_of(const TreeParams& p, int n) { return (n * p.G + p.rows - 1) / p.rows; }  // (rows of the call: fewer than 2^26)
 __device__ __forceinline__ Request request(const TreeParams& p, int b) {
   Request r;
   packed_rows(p.cu, b, p.T, r.first, r.n);
   r.len = min(max(p.lens[b], 0), p.S);
-  r.units = (int)(((int64_t)r.n * p.G + p.rows - 1) / p.rows);
+  r.units = units_of(p, r.n);
   r.pages = (r.len + kKvPageTokens - 1) / kKvPageTokens;
   if (!p.cut) r.pages = max(r.pages, 1);  // (no other launch writes the rows that see nothing)
   return r;
@@ -226,38 +227,80 @@ __global__ void __launch_bounds__(64 * NW, 2) attn_tree_kernel(TreeParams args) 
   const int n = lane & 15, q4 = lane >> 4;
   const int w = blockIdx.x;
 
+  // A segment: request b, unit, head hk, its pages pg .. pg + count - 1
+  struct Segment {
+    int b, first, nodes, len, pages, unit, hk, pg, count;
+    int end;  // in the list
+  } x;
   const TreeParams p0 = arguments();
   Batch bt;
-  bt.pad = p0.cut ? 1 : p0.least;
-  bt.load(p0, 0, 0, lane);
-  int total = bt.end();
-  bool falls = bt.falls;
-  for (int b = 64; b < p0.B; b += 64) {
-    int x = 0;
-    if (b + lane < p0.B) {
-      const Request r = request(p0, b + lane);
-      x = r.units * bt.padded(r.pages);
-      falls |= p0.cu[b + lane + 1] < p0.cu[b + lane];
+  int share = p0.least, f1 = 0;  // f1: the share's end in the list
+  if (p0.cut) {
+    bt.pad = 1;
+    bt.load(p0, 0, 0, lane);
+    int total = bt.end();
+    bool falls = bt.falls;
+    int more = 0;
+#pragma unroll 4
+    for (int b = 64 + lane; b < p0.B; b += 64) {
+      const Request r = request(p0, b);
+      more += r.units * r.pages;
+      falls |= p0.cu[b + 1] < p0.cu[b];
     }
-    total += wave_sum(x);
-  }
-  if (__any(falls)) return;  // (the joining launch too)
-  total *= p0.Hkv;
-  int share = p0.least;
-  if (p0.fit) share = max(share, (total + p0.shares - 1) / p0.shares);
-  // A share that goes on in a second segment costs as much as a few pages more would; where shares of up to kLonger more
-  // pages suffice with every segment beginning a share of its own, they do: a tree of 8 nodes behind 777 tokens 16.2 ->
-  // 14.6 us, 16 of 16 behind up to 1000 28.8 -> 23.6.
-  if (p0.fit && p0.B <= 64)
-    for (int longer = (share + 1) & ~1; longer <= share + kLonger; longer += 2)
-      if (wave_sum(bt.r.units * ((bt.r.pages + longer - 1) / longer)) * p0.Hkv <= p0.shares) {
-        share = bt.pad = longer;
-        bt.place(0);
-        total = bt.end() * p0.Hkv;
-        break;
+    if (__any(falls)) return;  // (the joining launch too)
+    if (p0.B > 64) total += wave_sum(more);
+    total *= p0.Hkv;
+    if (p0.fit) share = max(share, (total + p0.shares - 1) / p0.shares);
+    // A share that goes on in a second segment costs as much as a few pages more would; where shares of up to kLonger more
+    // pages suffice with every segment beginning a share of its own, they do: a tree of 8 nodes behind 777 tokens 16.2 ->
+    // 14.6 us, 16 of 16 behind up to 1000 28.8 -> 23.6.
+    if (p0.fit && p0.B <= 64)
+      for (int longer = (share + 1) & ~1; longer <= share + kLonger; longer += 2)
+        if (wave_sum(bt.r.units * ((bt.r.pages + longer - 1) / longer)) * p0.Hkv <= p0.shares) {
+          share = bt.pad = longer;
+          bt.place(0);
+          total = bt.end() * p0.Hkv;
+          break;
+        }
+    if ((int64_t)w * share >= total) return;
+    f1 = min((w + 1) * share, total);
+  } else {
+    // Whole segments, unit by unit and head by head: the workgroup's unit among those of requests lo .. hi - 1, a 64th of them
+    // a lane, then of that lane's, until it is one.  1024 requests of 4 nodes behind up to 200 tokens: 281 us by the list, 208 so.
+    x.unit = w / p0.Hkv;
+    x.hk = w - x.unit * p0.Hkv;
+    int lo = 0, hi = p0.B, per;
+    do {
+      per = (hi - lo + 63) / 64;
+      int mine = 0;
+      bool falls = false;
+#pragma unroll 4
+      for (int k = 0; k < per; ++k) {
+        const int b = lo + lane * per + k;
+        if (b < hi) {
+          int first, n;
+          packed_rows(p0.cu, b, p0.T, first, n);
+          mine += units_of(p0, n);
+          falls |= p0.cu[b + 1] < p0.cu[b];
+        }
       }
-  if ((int64_t)w * share >= total) return;
-  const int f1 = min((w + 1) * share, total);
+      if (__any(falls)) return;
+      const int upto = wave_scan_add(mine);
+      const unsigned long long above = __ballot(upto > x.unit);
+      if (!above) return;
+      const int at = __builtin_ctzll(above);
+      x.unit -= __builtin_amdgcn_readlane(upto - mine, at);
+      lo += at * per;
+      hi = min(lo + per, hi);
+    } while (per > 1);
+    const Request r = request(p0, lo);  // (the same for all lanes)
+    x.b = lo;
+    x.first = __builtin_amdgcn_readfirstlane(r.first);
+    x.nodes = __builtin_amdgcn_readfirstlane(r.n);
+    x.len = __builtin_amdgcn_readfirstlane(r.len);
+    x.pages = x.count = __builtin_amdgcn_readfirstlane(r.pages);
+    x.pg = x.end = 0;
+  }
 
   const uint32_t lds0 = (uint32_t)(size_t)lds;
   uint32_t ka[4], va[8];  // a lane's places in the tiles: key n of 16, chunks 4 c + q; V^T operand g
@@ -278,11 +321,6 @@ __global__ void __launch_bounds__(64 * NW, 2) attn_tree_kernel(TreeParams args) 
   auto k_tile = [&](int j) { return (lds_byte*)lds + (j % STAGES) * kTileBytes; };
   auto v_tile = [&](int j) { return (lds_byte*)lds + (STAGES + j % STAGES) * kTileBytes; };
 
-  // A segment: request b, unit, head hk, its pages pg .. pg + count - 1
-  struct Segment {
-    int b, first, nodes, len, pages, unit, hk, pg, count;
-    int end;  // in the list
-  };
   auto find = [&](const TreeParams& p, int f) {
     while (bt.end() * p.Hkv <= f) bt.load(p, bt.base + 64, bt.end(), lane);
     const int at = __builtin_ctzll(__ballot(bt.upto * p.Hkv > f));
@@ -347,7 +385,7 @@ __global__ void __launch_bounds__(64 * NW, 2) attn_tree_kernel(TreeParams args) 
     }
   };
 
-  Segment x = find(p0, w * share);
+  if (p0.cut) x = find(p0, w * share);
   numbers(p0, x, 0, kpg, vpg);
   numbers(p0, x, 64, kpg2, vpg2);
   begin(p0, x);
@@ -811,12 +849,12 @@ int tree_plan(int B, int Hq, int Hkv, int T, int S, int split_tokens, TreePlan* 
   P.rows = 16 * P.blocks * P.waves;
   P.units = all / P.rows + B;
   const int64_t heads = P.units * Hkv;  // segments, where none is cut
-  P.fit = split_tokens == 0 && !P.whole;
+  P.fit = split_tokens == 0;
   // (us in a graph with shares of 2, 4, 6 and 8 pages at least: 1 request of 8 nodes, S 500 9.0 9.9 10.9 12.3, 777 9.3 9.2 9.9 10.6,
   // 2048 10.8 10.1 10.1 11.5; 16 of 8 with 8 / 1 heads, 777 12.1 11.6 12.4 13.1, 2048 18.0 13.2 13.0 14.1)
-  P.least = P.whole ? (int)pages : P.fit ? 4 : split_tokens / kKvPageTokens;
+  P.least = P.fit ? 4 : split_tokens / kKvPageTokens;
   int64_t shares = P.whole ? heads : heads * pages / P.least + heads;  // (a segment may end in a part of one)
-  if (P.fit) shares = std::min<int64_t>(shares, P.waves == 8 ? 256 : 512);
+  if (P.fit && !P.whole) shares = std::min<int64_t>(shares, P.waves == 8 ? 256 : 512);
   if (shares >= (1 << 22)) return fail(ASYM_EUNSUPPORTED, "tree attention: too many shares");
   P.shares = (int)shares;
   P.bytes = P.whole ? 0 : (size_t)shares * 2 * P.rows * (kKvD + 2) * sizeof(float) + (size_t)heads * sizeof(int2);

@@ -130,6 +130,17 @@ def test_many_rows_of_a_segment_each(dev):
     c.check(c.run(), only=[0, 1, 31, 39])
 
 
+@pytest.mark.parametrize("B,room", [(300, 0), (4096, 0), (4500, 0), (300, 700), (4500, 300)])
+def test_very_many_requests(dev, B, room):
+    new = [i % 3 if i % 7 else 0 for i in range(B)]
+    new[-1], new[B // 2] = 2, 40
+    c = Case(dev, new, [max(n, 7 * i % 60) for i, n in enumerate(new)], 2, 1, seed=B, room=room)
+    assert (asym._tree_workspace(B, 2, 1, c.T, c.kt.shape[2] * 32, 0) == 0) == (room == 0)
+    o = torch.full_like(c.q, 7.0)
+    c.check(c.run(o=o), only=[0, 1, 2, 63, 64, 65, B // 2 - 1, B // 2, B // 2 + 1, B - 2, B - 1] + list(range(3, B, B // 17)))
+    assert not torch.any(torch.all(o.flatten(1) == 7, dim=1))  # every row is written
+
+
 def test_which_calls_are_cut(dev):
     assert asym._tree_workspace(64, 32, 8, 64 * 32, 2000, 0) == 0 < asym._tree_workspace(8, 32, 8, 8 * 32, 2000, 0)
     assert asym._tree_workspace(1, 8, 1, 1, 384, 0) == 0 < asym._tree_workspace(1, 8, 1, 1, 385, 0)
