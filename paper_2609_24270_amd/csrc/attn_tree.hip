@@ -13,10 +13,9 @@
 //   S^T = K . Q^T   v_mfma_f32_16x16x32_bf16, Q in registers, K by ds_read_b128;
 //   softmax         a row's 64 scores lie in four lanes; its running max is raised only when
 //                   some row's grows by more than 2^8;
-//   O^T += V^T . P^T  with P rounded to bf16 (the type of the products' operands: 2^-8
-//                   relative at most, as the output's own rounding) in the scores' registers,
-//                   V^T by ds_read_b64_tr_b16.
-// Scores, max, sum and output are fp32.  One barrier a block.
+//   O^T += V^T . P^T  in the scores' registers, V^T by ds_read_b64_tr_b16.  The products take bf16, so a weight is the
+//                   sum of two: itself rounded, and what that left of it, rounded (2^-16 of the weight are lost).
+// Scores, max, sum and output are fp32, and rounded to bf16 once, at the end.  One barrier a block.
 //
 // The pages of the batch, request by request and head by head, are one list, cut into equal
 // shares, one a workgroup, whatever the lengths (which only the device knows).  A segment is what a
@@ -432,7 +431,7 @@ __global__ void __launch_bounds__(64 * NW, 2) attn_tree_kernel(TreeParams args) 
     }
     const float c = p.c;
     f32x4 o[NQ][8], s[NQ][NT];
-    bf16x8 pf[NQ][NK];
+    bf16x8 pf[NQ][NK], pr[NQ][NK];  // the weights rounded to bf16, and what that left of them
     float m[NQ], l[NQ];
 #pragma unroll
     for (int k = 0; k < NQ; ++k) {
@@ -477,29 +476,40 @@ __global__ void __launch_bounds__(64 * NW, 2) attn_tree_kernel(TreeParams args) 
         }
       }
     };
+    // What a pair's rounding left is e - (y0, y1) . (1, 0) and e - (y0, y1) . (0, 1), one instruction each (exact: the difference
+    // has 16 bits at most).  The factors are kept in registers: for a constant (-1, 0) the compiler writes the inline constant
+    // -1.0, which gave other differences.
+    uint32_t minus[2] = {0xBF80u, 0xBF800000u};
+    asm volatile("" : "+s"(minus[0]), "+s"(minus[1]));
     auto weights = [&](int ks) {
 #pragma unroll
       for (int k = 0; k < NQ; ++k) {
         const float ms = m[k] == -INFINITY ? 0.f : m[k];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
+        for (int j = 0; j < 8; j += 2) {
           // (the difference first: scores of the type's lowest values times c would be infinite; one instruction for both
           // took 4 % fewer cycles)
-          const float e = __builtin_amdgcn_exp2f((s[k][2 * ks + (j >> 2)][j & 3] - ms) * c);
-          l[k] += e;
-          pf[k][ks][j] = (__bf16)e;
+          const float e0 = __builtin_amdgcn_exp2f((s[k][2 * ks + (j >> 2)][j & 3] - ms) * c);
+          const float e1 = __builtin_amdgcn_exp2f((s[k][2 * ks + (j >> 2)][(j & 3) + 1] - ms) * c);
+          l[k] += e0;
+          l[k] += e1;
+          const bf16x2 y = {(__bf16)e0, (__bf16)e1};
+          pf[k][ks][j] = y[0];
+          pf[k][ks][j + 1] = y[1];
+          pr[k][ks][j] = (__bf16)__builtin_amdgcn_fdot2_f32_bf16(y, __builtin_bit_cast(bf16x2, minus[0]), e0, false);
+          pr[k][ks][j + 1] = (__bf16)__builtin_amdgcn_fdot2_f32_bf16(y, __builtin_bit_cast(bf16x2, minus[1]), e1, false);
         }
       }
     };
     // (The order of a block's instructions: operands are read from LDS a few ahead of the products that take them.  Each of these
-    // takes the named number of instructions of a kind: 8 products, 0x100 reads.)
-    auto pace = [](auto reads, auto ahead, auto total) {
+    // takes the named number of instructions of a kind: 8 products, 0x100 reads; each: products of an operand.)
+    auto pace = [](auto reads, auto ahead, auto total, auto each) {
       __builtin_amdgcn_sched_group_barrier(0x100, decltype(reads)::value * decltype(ahead)::value, 0);
       steps<decltype(total)::value - decltype(ahead)::value>([] {
-        __builtin_amdgcn_sched_group_barrier(8, NQ, 0);
+        __builtin_amdgcn_sched_group_barrier(8, decltype(each)::value, 0);
         __builtin_amdgcn_sched_group_barrier(0x100, decltype(reads)::value, 0);
       });
-      __builtin_amdgcn_sched_group_barrier(8, NQ * decltype(ahead)::value, 0);
+      __builtin_amdgcn_sched_group_barrier(8, decltype(each)::value * decltype(ahead)::value, 0);
     };
     auto v_op = [&](const lds_byte* vt, int g, int ks) { return v_frag(vt, va[g] + (uint32_t)(32 * ks * kRowBytes)); };
     auto add_pv = [&](int j) {
@@ -509,6 +519,8 @@ __global__ void __launch_bounds__(64 * NW, 2) attn_tree_kernel(TreeParams args) 
 #pragma unroll
         for (int g = 0; g < 8; ++g) {
           const bf16x8 x = v_op(vt, g, ks);
+#pragma unroll
+          for (int k = 0; k < NQ; ++k) o[k][g] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, pr[k][ks], o[k][g], 0, 0, 0);
 #pragma unroll
           for (int k = 0; k < NQ; ++k) o[k][g] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, pf[k][ks], o[k][g], 0, 0, 0);
         }
@@ -523,13 +535,61 @@ __global__ void __launch_bounds__(64 * NW, 2) attn_tree_kernel(TreeParams args) 
           // (the waves in step with each other otherwise: one that is at it goes on before the others)
           __builtin_amdgcn_s_setprio(1);
           scores(j);
-          pace(std::integral_constant<int, 1>{}, std::integral_constant<int, 4>{}, std::integral_constant<int, 4 * NT>{});
+          pace(std::integral_constant<int, 1>{}, std::integral_constant<int, 4>{}, std::integral_constant<int, 4 * NT>{}, std::integral_constant<int, NQ>{});
           raise();
           weights(0);
           weights(1);
           add_pv(j);
-          pace(std::integral_constant<int, 2>{}, std::integral_constant<int, 4>{}, std::integral_constant<int, 8 * NK>{});
+          pace(std::integral_constant<int, 2>{}, std::integral_constant<int, 4>{}, std::integral_constant<int, 8 * NK>{}, std::integral_constant<int, 2 * NQ>{});
           __builtin_amdgcn_s_setprio(0);
+        }
+      }
+    }
+    // An infinity among the values times a weight's second part, which may be 0 or negative, is NaN or has the wrong sign, and
+    // NaN in the sum.  Where a sum is NaN, what the values of its channel hold decides.
+    if (work && nfull > 0) {
+      f32x4 all = o[0][0];
+#pragma unroll
+      for (int i = 1; i < 8 * NQ; ++i) all += o[i >> 3][i & 7];
+      const float odd = (all[0] + all[1]) + (all[2] + all[3]);
+      if (__any(odd != odd)) {
+        const TreeParams at = arguments();
+        const int* entries = at.v_pages + ((size_t)x.b * at.Hkv + x.hk) * at.pph + x.pg;
+        uint32_t none = 0, up = 0, down = 0;  // NaN, infinity, minus infinity: bit 4 g + r, channel 16 g + 4 q4 + r
+        for (int t = n; t < kTokens * nfull; t += 16) {
+          const int page = entries[t / kKvPageTokens];
+          if (page < 0 || page >= at.pool_pages) continue;
+          const uint8_t* row = at.v_pool + (int64_t)page * kPageBytes + t % kKvPageTokens * kRowBytes + 8 * q4;
+#pragma unroll 1
+          for (int g = 0; g < 8; ++g) {
+            const s16x4 y = *reinterpret_cast<const s16x4*>(row + 32 * g);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+              const uint32_t u = (uint16_t)y[r], bit = 1u << (4 * g + r);
+              if ((u & 0x7FFFu) > 0x7F80u) none |= bit;
+              if (u == 0x7F80u) up |= bit;
+              if (u == 0xFF80u) down |= bit;
+            }
+          }
+        }
+#pragma unroll
+        for (int d = 1; d < 16; d <<= 1) {
+          none |= (uint32_t)__shfl_xor((int)none, d);
+          up |= (uint32_t)__shfl_xor((int)up, d);
+          down |= (uint32_t)__shfl_xor((int)down, d);
+        }
+        none = (up ^ down) & ~none;  // (infinities of one sign, and no NaN)
+#pragma unroll
+        for (int g = 0; g < 8; ++g) {
+          __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const uint32_t bit = 1u << (4 * g + r);
+            const float y = up & bit ? INFINITY : -INFINITY;
+#pragma unroll
+            for (int k = 0; k < NQ; ++k)
+              if (o[k][g][r] != o[k][g][r] && (none & bit)) o[k][g][r] = y;
+          }
         }
       }
     }
