@@ -1053,9 +1053,10 @@ int asym_kv_free(int R, int H, int pages_per_head, int32_t* table, int32_t* lens
  * what comes before; the row ends there, and the pages behind its end are given up as in asym_kv_free.  cu:
  * device int32 [n + 1], not falling, held within [0, T]; path [T] and count [n] as asym_draft_verify
  * writes them.  A request whose path does not rise or leaves the drafted tokens, whose row is shorter than
- * them, or whose tokens would move into a page that another row shares, is left out; rows of one call must
- * share no page that holds drafted tokens (fork rows before the tokens are drafted).  Pages whose bytes are 32 tokens one after the other (asym_attn_decode_paged_bf16's): page_bytes a
- * multiple of 512.  v_pool nullable. */
+ * them, whose tokens would move into a page that another row shares, or whose row would come to end inside one
+ * (where its next tokens would overwrite the other's), is left out; rows of one call must
+ * share no page that holds drafted tokens (fork rows before the tokens are drafted).  Pages whose bytes are 32
+ * tokens one after the other (asym_attn_decode_paged_bf16's): page_bytes a multiple of 512.  v_pool nullable. */
 int asym_kv_keep(int R, int H, int pages_per_head, int32_t* table, int32_t* lens, int32_t* refs,
                  void* k_pool, void* v_pool, size_t page_bytes, size_t pool_pages, int n,
                  const int32_t* rows, int T, const int32_t* cu, const int32_t* path,

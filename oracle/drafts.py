@@ -90,6 +90,8 @@ def keep(cache, rows, cu, path, count):
             continue
         base = int(cache.lens[r]) - n
         written = {int(cache.table[r, h, (base + j) // 32]) for j, x in enumerate(mine) if x != j for h in range(cache.H)}
+        if m < n and (base + m) % 32:  # (the page that the row would end inside, and be extended in)
+            written |= {int(cache.table[r, h, (base + m) // 32]) for h in range(cache.H)}
         if any(0 <= p < len(cache.refs) and cache.refs[p] > 1 for p in written):  # (another row's as well)
             continue
         for j, x in enumerate(mine):

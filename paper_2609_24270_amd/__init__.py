@@ -1409,7 +1409,9 @@ def kv_keep(k_pool, v_pool, table, lens, refs, rows, cu, path, count, stream=Non
     """Rows of a paged cache keep some of their last tokens: of the last cu[i + 1] - cu[i] tokens of row
     rows[i] those at places path[cu[i] .. cu[i] + count[i] - 1] among them (rising; as draft_verify gives them),
     in order; the row ends behind them, and the pages behind its end are given up.  A row whose tokens would move
-    into a page that another row shares is left as it is.  Pools [pool_pages, 32, ...] (v_pool None: only one); cu [n + 1], path [T], count [n]; the rest as kv_extend.  All int32."""
+    into a page that another row shares, or that would come to end inside one, is left as it is.  Rows of one call must
+    share no page that holds drafted tokens: fork rows before the tokens are drafted.  Pools [pool_pages, 32, ...]
+    (v_pool None: only one); cu [n + 1], path [T], count [n]; the rest as kv_extend.  All int32."""
     R, H, pph, pool = _pages_state(table, lens, refs)
     n = _requests(rows, count)
     _index(cu, "cu", (n + 1,))

@@ -438,6 +438,13 @@ __global__ void __launch_bounds__(kSmallThreads) pages_keep(PagesParams p, int T
     const int page = p.table[((int64_t)r * p.H + head) * p.pph + (base + j) / kKvPageTokens];
     bad |= page >= 0 && page < p.pool && p.refs[page] > 1;
   }
+  // (nor does the row come to end inside one, where its next tokens would be written)
+  const int now = base + keep;
+  if (now < len && now % kKvPageTokens)
+    for (int head = threadIdx.x; head < p.H; head += blockDim.x) {
+      const int page = p.table[((int64_t)r * p.H + head) * p.pph + now / kKvPageTokens];
+      bad |= page >= 0 && page < p.pool && p.refs[page] > 1;
+    }
   if (__syncthreads_or(bad)) return;
   const uint32_t words = (uint32_t)(p.page_bytes / (16 * kKvPageTokens));  // of a token
   const int64_t columns = (int64_t)p.H * words * (p.v_pool ? 2 : 1);
@@ -472,7 +479,7 @@ __global__ void __launch_bounds__(kSmallThreads) pages_keep(PagesParams p, int T
     }
   }
   __syncthreads();  // (the entries have been read)
-  const int now = base + keep, left = pages_of(now, p.pph), gone = pages_of(len, p.pph) - left;
+  const int left = pages_of(now, p.pph), gone = pages_of(len, p.pph) - left;
   for (int64_t x = threadIdx.x; x < (int64_t)gone * p.H; x += blockDim.x) {
     int* e = p.table + ((int64_t)r * p.H + x / gone) * p.pph + left + x % gone;
     if (*e >= 0 && *e < p.pool) atomicSub(&p.refs[*e], 1);
