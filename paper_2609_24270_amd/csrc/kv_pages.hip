@@ -656,6 +656,8 @@ extern "C" int asym_kv_keep(int R, int H, int pages_per_head, int32_t* table, in
   // a thread a 16-byte word of a token, as far as a workgroup goes
   const int64_t columns = (int64_t)H * (int64_t)(page_bytes / (16 * kKvPageTokens)) * (v_pool ? 2 : 1);
   const unsigned threads = (unsigned)std::min<int64_t>((columns + 63) / 64 * 64, kSmallThreads);
+  if ((int64_t)n * threads > 0xFFFFFFFFll)  // (threads of a launch are counted in 32 bits)
+    return fail(ASYM_EUNSUPPORTED, "kv keep: too many requests for pages of this size");
   hipLaunchKernelGGL(pages_keep, dim3(n), dim3(threads), 0, static_cast<hipStream_t>(stream), p, T, cu, path, count);
   ASYM_HIP(hipGetLastError());
   return ASYM_OK;
