@@ -872,7 +872,10 @@ int tree_plan(int B, int Hq, int Hkv, int T, int S, int split_tokens, TreePlan* 
     *plan = P;
     return ASYM_OK;
   }
-  if ((int64_t)T * Hq >= (1 << 26)) return fail(ASYM_EUNSUPPORTED, "tree attention: too many rows");  // (threads are counted in 32 bits)
+  // (threads are counted in 32 bits: the joining launch has a wave for kJoinHeads heads of a token, kJoinWaves a workgroup)
+  const int64_t joins = ((int64_t)T * ((Hq + kJoinHeads - 1) / kJoinHeads) + kJoinWaves - 1) / kJoinWaves;
+  if ((int64_t)T * Hq >= (1 << 26) || joins * 64 * kJoinWaves > 0xFFFFFFFFll)
+    return fail(ASYM_EUNSUPPORTED, "tree attention: too many rows");
   const int64_t all = (int64_t)T * (Hq / Hkv), mean = (all + B - 1) / B;
   const int64_t pages = ((int64_t)S + kKvPageTokens - 1) / kKvPageTokens, most = (all / 64 + B) * Hkv;
   if (most > (1 << 30) || most * pages > (1 << 30)) return fail(ASYM_EUNSUPPORTED, "tree attention: more than 2^30 pages");
