@@ -1079,7 +1079,7 @@ int asym_kv_compact(int R, int H, int pages_per_head, int32_t* table, int32_t* r
  * the rotation).  The angle is computed in 64 bits, the rest in fp32.
  * x and y [T][H][D] bf16 with the given strides in values between tokens and between heads
  * (multiples of 8), 16-byte aligned; D a multiple of 8, up to 1024.  y may be x, with
- * x's strides; else the two must not overlap.  rotary even, 0 to D.  positions: device
+ * x's strides; else the two must not overlap.  Rows of x may lie on each other (strides of 0), rows of y must not.  rotary even, 0 to D.  positions: device
  * int32 [T], any values; freq: device double [rotary / 2].  One launch, asynchronous, may be captured.
  * Errors: ASYM_EINVAL, ASYM_EUNSUPPORTED, ASYM_EHIP. */
 enum asym_rope_layout { ASYM_ROPE_HALF = 0, ASYM_ROPE_INTERLEAVED = 1 };
@@ -1093,7 +1093,7 @@ int asym_rope_bf16(int T, int H, int D, int rotary, const void* x, int64_t x_tok
  * [T][H_kv][128], become its positions start[b] .. start[b] + n - 1.  K is turned as by asym_rope_bf16
  * at positions[i] (device int32 [T]; null: the place in the cache; a tree's nodes have the positions of
  * their depth), V is not; rotary 0 turns nothing.  q [T][H_q][128], if H_q > 0, is turned in the same
- * way into q_out, which may be q with its strides.  Strides in values, multiples of 8.  cu: device
+ * way into q_out, which may be q with its strides (its rows must not lie on each other).  Strides in values, multiples of 8.  cu: device
  * int32 [B + 1], not falling, held within [0, T]; start: device int32 [B], >= 0 (a request with a
  * negative one is left out, its q too; keys and values of positions behind the table, and of table
  * entries outside [0, pool_pages), are not written).  Rows of q_out outside every

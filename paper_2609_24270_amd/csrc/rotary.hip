@@ -246,6 +246,11 @@ bool bad_strides(std::initializer_list<int64_t> strides) {
   return false;
 }
 
+// Output rows that lie on each other
+bool rows_overlap(int T, int64_t token, int H, int64_t head, int D) {
+  return (T > 1 && token < D) || (H > 1 && head < D) || (T > 1 && H > 1 && token == head);
+}
+
 template <class F>
 void with_run(int e, bool inter, F f) {
   auto go = [&](auto E) { inter ? f(E, std::true_type{}) : f(E, std::false_type{}); };
@@ -275,6 +280,7 @@ extern "C" int asym_rope_bf16(int T, int H, int D, int rotary, const void* x, in
   if ((uintptr_t)positions & 3u) return fail(ASYM_EINVAL, "rope: positions must be 4-byte aligned");
   if (bad_strides({x_token, x_head, y_token, y_head}))
     return fail(ASYM_EINVAL, "rope: strides must be multiples of 8 values and not negative");
+  if (rows_overlap(T, y_token, H, y_head, D)) return fail(ASYM_EINVAL, "rope: rows of y lie on each other");
   RopeParams p = {};
   p.x = static_cast<const uint16_t*>(x);
   p.y = static_cast<uint16_t*>(y);
@@ -319,6 +325,7 @@ extern "C" int asym_kv_append_bf16(int B, int H_q, int H_kv, int T, const void* 
     return fail(ASYM_EINVAL, "kv append: tables, offsets and positions must be 4-byte aligned");
   if (bad_strides({k_token, k_head, v_token, v_head}) || (H_q && bad_strides({q_token, q_head, qo_token, qo_head})))
     return fail(ASYM_EINVAL, "kv append: strides must be multiples of 8 values and not negative");
+  if (H_q && rows_overlap(T, qo_token, H_q, qo_head, kKvD)) return fail(ASYM_EINVAL, "kv append: rows of q_out lie on each other");
   AppendParams p = {};
   p.q = static_cast<const uint16_t*>(q);
   p.k = static_cast<const uint16_t*>(k);
