@@ -33,14 +33,27 @@ def tree_attention(q, k, v, sees, base, scale: float):
     return O, lse, A, N
 
 
-def verify(target, draft, tokens, parents, accept, final):
+class Border(ValueError):
+    """A random number so near to a border that another order of the sums could choose otherwise."""
+
+
+def verify(target, draft, tokens, parents, accept, final, margin=1e-12):
     """One request's nodes: target and draft [n, V] float64 (draft None: each token was certain), tokens, parents
-    (node 0 the root) and random numbers as lists.  Returns (path, the last token)."""
+    (node 0 the root) and random numbers as lists.  Returns (path, the last token).  A comparison whose sides are nearer than
+    `margin` of the probabilities that they are differences of, and not equal (as where powers of two meet on purpose), raises
+    Border; for the last token the share is at least that of V roundings."""
     n, V = target.shape
+
+    def less(a, b, scale):
+        if a != b and abs(a - b) <= margin * scale:
+            raise Border(f"{a} and {b}")
+        return a < b
+
     clean = lambda x: np.where(np.isfinite(x) & (x > 0), x, 0.0)
     path, cur = [0], 0
     r = clean(target[0])
     one = 1.0  # what r sums to: 1 by definition at first, and after each norm()
+    left = 1.0  # what norm() has divided by: r * left is the difference of the rows
     i = 1
     while i < n:
         t = tokens[i]
@@ -48,29 +61,33 @@ def verify(target, draft, tokens, parents, accept, final):
             i += 1
             continue
         if draft is None:
-            took = not (r[t] == 0 and _was_rejected(path, cur, i, tokens, parents)) and accept[i] * one < r[t]
+            took = not (r[t] == 0 and _was_rejected(path, cur, i, tokens, parents)) and less(accept[i] * one, r[t], max(one, r[t]))
             if not took and not _was_rejected(path, cur, i, tokens, parents):
                 one -= r[t]
                 r = r.copy()
                 r[t] = 0
         else:
             q = clean(draft[cur])
-            took = accept[i] * q[t] * one < r[t]
+            took = less(accept[i] * q[t] * one, r[t], max(q[t], float(clean(target[cur])[t]) / left))
             if not took:
                 r = np.maximum(r - q, 0)
                 s = r.sum()
-                r, one = (r / s, 1.0) if s > 0 else (r, 0.0)
+                r, one, left = (r / s, 1.0, left * s) if s > 0 else (r, 0.0, left)
         if took:
             cur = i
             path.append(i)
-            r, one = clean(target[cur]), 1.0
+            r, one, left = clean(target[cur]), 1.0, 1.0
         i += 1
     if r.sum() == 0:
-        r = clean(target[cur])
+        r, left = clean(target[cur]), 1.0
     if r.sum() == 0:
         return path, -1
     cum = np.cumsum(r)
-    over = np.nonzero(cum > final * cum[-1])[0]
+    aim = final * cum[-1]
+    near = np.abs(cum[r > 0] - aim) <= max(margin, V * 2.0 ** -53 * (margin > 0)) * cum[-1] / left
+    if np.any(near & (cum[r > 0] != aim)):
+        raise Border(f"{final} of the last token")
+    over = np.nonzero(cum > aim)[0]
     return path, int(over[0]) if len(over) else int(np.nonzero(r)[0][-1])
 
 
