@@ -16,9 +16,10 @@
 // Without draft probabilities a token counts as certain: R is p without the rejected siblings'
 // tokens, m = 1 - their p.
 //
-// All of it is in 64 bits: products of two fp32 are exact there, and the choices are those
-// of the definition but for borders nearer than about 10^-15.  What is not a positive
-// finite number counts as 0.
+// All of it is in 64 bits.  Before a node's first rejection (c = 0, m = 1) both sides of the comparison are exact; behind it
+// c, m, the product and the difference are rounded, and sums of a row are V roundings: the choices are those of the
+// definition but for borders nearer than about 10^-15 of the probabilities that a difference is of, V 2^-53 of a sum.  What is
+// not a positive finite number counts as 0.
 //
 // A row is cut into slices; a launch (`round`; none for small vocabularies) sums one each a workgroup, after it has
 // walked the request's nodes as far as the sums so far allow, which all of the request's
