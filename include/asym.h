@@ -1091,7 +1091,7 @@ int asym_rope_bf16(int T, int H, int D, int rotary, const void* x, int64_t x_tok
 /* Tokens into a cache of asym_attn_decode_paged_bf16's pages ([32][128] bf16, 8 KiB), their keys
  * turned on the way: request b's n = cu[b + 1] - cu[b] tokens, rows cu[b] .. of K and V
  * [T][H_kv][128], become its positions start[b] .. start[b] + n - 1.  K is turned as by asym_rope_bf16
- * at positions[i] (device int32 [T]; null: the place in the cache; a tree's nodes have the positions of
+ * (to the same bits) at positions[i] (device int32 [T]; null: the place in the cache; a tree's nodes have the positions of
  * their depth), V is not; rotary 0 turns nothing.  q [T][H_q][128], if H_q > 0, is turned in the same
  * way into q_out, which may be q with its strides (its rows must not lie on each other).  Strides in values, multiples of 8.  cu: device
  * int32 [B + 1], not falling, held within [0, T]; start: device int32 [B], >= 0 (a request with a

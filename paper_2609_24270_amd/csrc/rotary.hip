@@ -52,8 +52,8 @@ __device__ __forceinline__ uint16_t down(float x) { return __builtin_bit_cast(ui
 
 // (A cos, A sin) of one pair, the sine's sign that of the direction
 __device__ __forceinline__ float2 cos_sin(const Turn& r, int pair, double pos) {
-  double t = pos * (r.freq[pair] * 0.15915494309189535);  // turns
-  t -= __builtin_rint(t);
+  const double each = r.freq[pair] * 0.15915494309189535;  // turns a position
+  const double t = __builtin_fma(pos, each, -__builtin_rint(pos * each));
   float s, c;
   sincospif(2.f * (float)t, &s, &c);
   return float2{c * r.amp, s * r.amp * r.dir};
@@ -71,7 +71,8 @@ __device__ __forceinline__ void runs_of(int c, int rotary, int& a, int& b) {
     b = a + rotary / 2;
   }
 }
-// cs: of the unit's E pairs
+// cs: of the unit's E pairs.  (Which product is rounded is written out: left to the compiler, it differed between the kernels and
+// between a unit's pairs, and a key appended with 4096 tokens or more from the same one appended alone, 8 of a million.)
 template <int E, bool INTER>
 __device__ __forceinline__ void turn_unit(Run<E>& a, Run<E>& b, const float2* cs) {
 #pragma unroll
@@ -81,8 +82,8 @@ __device__ __forceinline__ void turn_unit(Run<E>& a, Run<E>& b, const float2* cs
     uint16_t& x = i < E ? a.x[i] : b.x[i - E];
     uint16_t& y = j < E ? a.x[j] : b.x[j - E];
     const float u = up(x), v = up(y);
-    x = down(u * cs[e].x - v * cs[e].y);
-    y = down(v * cs[e].x + u * cs[e].y);
+    x = down(fmaf(u, cs[e].x, -(v * cs[e].y)));
+    y = down(fmaf(v, cs[e].x, u * cs[e].y));
   }
 }
 
