@@ -546,13 +546,22 @@ __global__ void __launch_bounds__(64 * NW, 2) attn_tree_kernel(TreeParams args) 
       }
     }
     // An infinity among the values times a weight's second part, which may be 0 or negative, is NaN or has the wrong sign, and
-    // NaN in the sum.  Where a sum is NaN, what the values of its channel hold decides.
+    // NaN in the sum.  Where a sum is NaN and its weights are not, what the values of its channel hold decides.
     if (work && nfull > 0) {
-      f32x4 all = o[0][0];
+      f32x4 all[NQ];
 #pragma unroll
-      for (int i = 1; i < 8 * NQ; ++i) all += o[i >> 3][i & 7];
-      const float odd = (all[0] + all[1]) + (all[2] + all[3]);
-      if (__any(odd != odd)) {
+      for (int k = 0; k < NQ; ++k) {
+        all[k] = o[k][0];
+#pragma unroll
+        for (int g = 1; g < 8; ++g) all[k] += o[k][g];
+      }
+      bool odd = false;
+#pragma unroll
+      for (int k = 0; k < NQ; ++k) {
+        const float y = (all[k][0] + all[k][1]) + (all[k][2] + all[k][3]), lt = over_quarters(l[k], [](float a, float b) { return a + b; });
+        odd |= y != y && lt == lt;
+      }
+      if (__any(odd)) {
         const TreeParams at = arguments();
         const int* entries = at.v_pages + ((size_t)x.b * at.Hkv + x.hk) * at.pph + x.pg;
         uint32_t none = 0, up = 0, down = 0;  // NaN, infinity, minus infinity: bit 4 g + r, channel 16 g + 4 q4 + r
@@ -578,7 +587,7 @@ __global__ void __launch_bounds__(64 * NW, 2) attn_tree_kernel(TreeParams args) 
           up |= (uint32_t)__shfl_xor((int)up, d);
           down |= (uint32_t)__shfl_xor((int)down, d);
         }
-        none = (up ^ down) & ~none;  // (infinities of one sign, and no NaN)
+        const uint32_t one = (up ^ down) & ~none;  // (infinities of one sign)
 #pragma unroll
         for (int g = 0; g < 8; ++g) {
           __builtin_amdgcn_sched_barrier(0);
@@ -588,7 +597,7 @@ __global__ void __launch_bounds__(64 * NW, 2) attn_tree_kernel(TreeParams args) 
             const float y = up & bit ? INFINITY : -INFINITY;
 #pragma unroll
             for (int k = 0; k < NQ; ++k)
-              if (o[k][g][r] != o[k][g][r] && (none & bit)) o[k][g][r] = y;
+              if (o[k][g][r] != o[k][g][r] && (one & bit)) o[k][g][r] = y;
           }
         }
       }

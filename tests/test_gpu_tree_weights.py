@@ -69,6 +69,12 @@ def infinities(c, n0, G):
         else:
             assert torch.all(torch.isnan(got[hit]))
         c.vp.copy_(v0)
+    # a key that is NaN: everything of its head's group
+    c.kp[int(c.kt[0, 0, 2]), 5, 9] = nan
+    got = c.run()
+    hit = torch.zeros_like(ref, dtype=torch.bool)
+    hit[:n0, :G] = True
+    assert torch.all(torch.isnan(got[hit])) and torch.equal(got[~hit], ref[~hit])
 
 
 @pytest.mark.parametrize("n,G,room,split", [(1, 4, 0, 0), (5, 2, 0, 0), (8, 4, 2000, 0), (8, 4, 0, 64), (40, 4, 0, 0), (64, 4, 9000, 0)])
