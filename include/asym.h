@@ -1133,7 +1133,9 @@ int asym_kv_append_bf16(int B, int H_q, int H_kv, int T, const void* q, int64_t 
  * the shares; automatic calls whose S_max is small for their number of requests and heads are not cut and need no
  * workspace.  The results depend on the sizes, offsets and lengths alone.  The fp32 pieces lie in the caller's
  * workspace (16-byte aligned; asym_attn_tree_paged_workspace's bytes; may be null if they are 0), which calls that may
- * overlap must not share.  Sums are fp32 with weights of up to 2^8: results need 2^8 * S_max * max|V| below 2^128.
+ * overlap must not share.  Shares and forms follow S_max and not the lengths: the longest length that the call can meet, where it is
+ * known, is faster than the tables' room.  They are chosen for the whole chip; a stream with fewer CUs gets the same results.
+ * Sums are fp32 with weights of up to 2^8, kept to 2^-16 each: results need 2^8 * S_max * max|V| below 2^128.  O is rounded once.
  * No host synchronisation; may be captured.  Runs on the stream's CU set; asynchronous.
  * Errors: ASYM_EINVAL, ASYM_EUNSUPPORTED, ASYM_EHIP. */
 int asym_attn_tree_paged_bf16(int B, int H_q, int H_kv, int T, int S_max, int D,

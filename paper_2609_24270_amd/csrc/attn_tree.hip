@@ -23,11 +23,17 @@
 // the caller's workspace in fp32 and a second launch joins them in order.  Where the longest request is short
 // for the number of segments, a share is a segment and one launch does it (tree_plan).
 //
-// Bound by HBM where the rows are few: 64 requests of one token behind up to 8000 (32 / 8 heads, 1.39 GB) take 223 us, 6.2
-// TB/s.  32 trees of 24 nodes in the mean behind up to 8000 tokens (0.72 GB) take 159 us, 12 of them the joining: 4.5
-// TB/s, and 7 % more is read for the second units of trees past 32 nodes.  With 8 trees of 64 nodes in the mean behind
-// up to 32768 tokens it is the power: 325 us (650 TFLOP/s), 574 thousand cycles at 1.7 to 1.8 GHz of 2.4, of which matrix
-// instructions take 37 % and vector ones 49 %.
+// Bound by HBM where the rows are few: 64 requests of one token behind up to 8000 (32 / 8 heads, 1.39 GB) take 224 us, 6.2
+// TB/s.  32 trees of 24 nodes in the mean behind up to 8000 tokens (0.72 GB) take 177 us, 12 of them the joining: 4.1
+// TB/s; matrix instructions take 38 % of the cycles and vector ones 42 %, one after the other within a wave.  8 trees of 64
+// nodes in the mean behind up to 32768 tokens: 420 us (503 TFLOP/s of the definition's; the second part of the weights is half as
+// many again), 793 thousand cycles at 1.9 GHz of 2.4 (the power cap), 40 % in matrix instructions and 44 % in vector ones.
+// A unit with few rows costs its pages nearly as much as a full one: 8 trees of 64 nodes exactly 405 us, of 65 657, of 96
+// 700 (200, 314 and 317 million busy cycles), and half of the trees above have such a second unit.
+//
+// The weights' second part costs 1 to 4 % where one block of rows is enough and up to a third where the matrix cores are busy
+// (32 trees of 24 160 -> 177 us, 8 of 64 320 -> 420); with weights of one bf16 value the error against 64 bits was 2.2e-3, and is
+// 1.65e-3, the output's rounding.
 //
 // Each wave with its own pages, K fragments straight from memory and no barrier, took twice as long on trees (348 us
 // for the 32 above): every wave of a unit loaded every page.
@@ -251,8 +257,8 @@ __global__ void __launch_bounds__(64 * NW, 2) attn_tree_kernel(TreeParams args) 
     total *= p0.Hkv;
     if (p0.fit) share = max(share, (total + p0.shares - 1) / p0.shares);
     // A share that goes on in a second segment costs as much as a few pages more would; where shares of up to kLonger more
-    // pages suffice with every segment beginning a share of its own, they do: a tree of 8 nodes behind 777 tokens 16.2 ->
-    // 14.6 us, 16 of 16 behind up to 1000 28.8 -> 23.6.
+    // pages suffice with every segment beginning a share of its own, they do: a tree of 8 nodes behind 777 tokens 14.1 ->
+    // 9.7 us, 4 requests of a token with 8 / 1 heads behind up to 30000 25.9 -> 22.4 (in a graph).
     if (p0.fit && p0.B <= 64)
       for (int longer = (share + 1) & ~1; longer <= share + kLonger; longer += 2)
         if (wave_sum(bt.r.units * ((bt.r.pages + longer - 1) / longer)) * p0.Hkv <= p0.shares) {
@@ -265,7 +271,7 @@ __global__ void __launch_bounds__(64 * NW, 2) attn_tree_kernel(TreeParams args) 
     f1 = min((w + 1) * share, total);
   } else {
     // Whole segments, unit by unit and head by head: the workgroup's unit among those of requests lo .. hi - 1, a 64th of them
-    // a lane, then of that lane's, until it is one.  1024 requests of 4 nodes behind up to 200 tokens: 281 us by the list, 208 so.
+    // a lane, then of that lane's, until it is one.  1024 requests of 4 nodes behind up to 200 tokens 219 us (by the list 73 more).
     x.unit = w / p0.Hkv;
     x.hk = w - x.unit * p0.Hkv;
     int lo = 0, hi = p0.B, per;
@@ -751,7 +757,7 @@ __global__ void __launch_bounds__(64 * NW, 2) attn_tree_kernel(TreeParams args) 
 // The joining launch: a wave has kJoinHeads query heads of a token, or, where rows are few and have many pieces (SPLIT), a
 // workgroup's waves share one.  Rows of a request without tokens are written, those that were cut are joined in the order
 // of the shares (SPLIT: each wave's every kJoinWaves-th piece, then the waves), the first kJoinPieces of each loaded at once.
-// us for 32 trees of 24 nodes behind up to 8000 tokens and for 8 of 64 behind up to 32768, at 2 heads a wave and 2, 3, 4, 5,
+// us for 32 trees of 24 nodes behind up to 8000 tokens and for 8 of 64 behind up to 32768 (the launch alone), at 2 heads a wave and 2, 3, 4, 5,
 // 6 and 8 pieces: 18.3 14.4 11.9 12.2 12.5 13.0, 14.0 13.8 11.2 8.7 9.0 11.6; 4 heads and 4 pieces 12.1 14.7; one head and 6 14.4 10.6.
 constexpr int kJoinHeads = 2, kJoinPieces = 5;
 template <bool SPLIT>
@@ -870,6 +876,8 @@ struct TreePlan {
   size_t bytes = 0;
 };
 
+// The forms, the number of shares and the non-temporal loads are chosen for the whole chip: a stream with fewer CUs gets
+// the same forms (and the same results), whose measurements below do not hold there.
 int tree_plan(int B, int Hq, int Hkv, int T, int S, int split_tokens, TreePlan* plan) {
   if (B < 0 || T < 0 || Hq < 1 || Hkv < 1 || S < 1)
     return fail(ASYM_EINVAL, "tree attention: B and T must be >= 0, H_q, H_kv and S_max >= 1");
@@ -892,19 +900,24 @@ int tree_plan(int B, int Hq, int Hkv, int T, int S, int split_tokens, TreePlan* 
   // One block of 16 rows a wave spreads few rows over more waves, and a wave's chain of products, softmax and products again, which
   // is what a block of tokens costs where the matrix cores have little to do, is half as long; the pages of more than 64 rows
   // are read again.  us, two blocks first, 32 / 8 heads, n nodes in the mean, lengths from a quarter of S on, in a graph, S 250,
-  // 777, 2048, 8000: 1 request of 8 nodes 10.5 8.3, 10.0 9.2, 11.2 10.0; 64 of 1 13.7 11.8, 27.1 24.6, 64.1 61.5, 202 201; 64 of 10
-  // 16.1 14.1, 31.3 26.8, 71 62, 234 232; 64 of 16 18.2 19.1, 31.5 32.1, 73 77; 32 of 16 13.0 11.8, 23.1 19.5, 47.8 59.1, 130 163; 8 of
-  // 32 11.4 9.0, 28.9 19.8, 34.5 25.8, 50.9 43.8; 8 of 64 13.0 10.1, 26.6 23.2, 34.1 29.7, 64 96; 32 of 32 16.6 16.3, 29.6 25.2, 64
-  // 57, 183 263; 1 of 512 31.7 24.2 (S 512), 37.0 26.6, 42.8 34.3, 67 100.
+  // 777, 2048, 8000: 1 request of 8 nodes 13.3 9.3, 11.2 9.8, 12.7 10.8; 64 of 1 15.8 12.8, 30.7 25.7, 70 60, 208 202; 64 of 10
+  // 19.3 15.7, 38.3 28.5, 86 63, 247 235; 64 of 16 21.5 21.7, 39.3 36.6, 87 82; 32 of 16 15.4 13.7, 28.2 22.9, 54 47, 136 165; 8 of
+  // 32 13.7 10.1, 31.5 20.2, 38.6 27.6, 59 49; 8 of 64 15.9 11.5, 29.6 20.6, 39.6 33.1, 81 98; 32 of 32 20.3 18.6, 38.3 28.8, 82
+  // 63, 192 269; 1 of 512 34.0 19.7 (S 512), 39.2 24.6, 48.6 39.3, 84 106.
+  // Near the line either may be a fifth faster.  It gives up 32 of 32 at S 1500 and 2048 (63 46), 8 of 32 at 8000, 16 of 16 at
+  // 4000 (49 39), 32 of 16 at 2048 (also with 8 / 8, 40 / 8 and 64 / 8 heads: 45 39, 58 47, 80 58), 1 of 512 at 6000 (69 83) and 4 of
+  // 256 with 16 / 2 heads at 6000 (63 74); twice the pages would give up 16 of 32 at 3000 (50 58) and 32 of 20 at 2500 (63 72).
   const bool narrow = mean <= 40 || (segments <= 512 && segments * pages <= 16384);
   // Whole segments need no pieces, no second launch and no workspace, and take as long as the longest request: about 5 us
-  // and 0.42 a page where it is alone (two blocks of rows: 6 and 0.58).  Cut ones take two launches and what the pieces of T x
-  // H_q rows cost to write and join.  us, cut first, as above: one block of rows: 1 request of 8 nodes, S 300 13.7 9.2, 380 13.7
-  // 10.0, 512 13.7 11.5 (in a graph 9.8 11.6); 16 of 8, 500 15.4 11.8, 1000 20.1 20.4; 8 of 16, 1000 20.4 18.7, 1500 20.4 25.9; 8 of
-  // 64, 1000 23.3 19.6, 1500 25.8 28.4; 24 of 8, 1500 23.3 25.9; 16 of 32, 2000 33.0 37.9; 32 of 10, 2000 36.0 35.7, 3000 54.8
-  // 59.6; 64 of 1, 2000 61.3 56.8, 4000 108 108, 8000 200 211; 64 of 10, 4000 129 111, 5000 155 139; 256 of 1, 8000 777 811.  Two:
-  // 64 of 16, 2000 87.5 72.1; 32 of 24, 1500 41.4 39.7, 2000 48.7 49.7, 4000 92 98, 8000 155 190; 16 of 64, 2000 48.5 57.7; 64 of
-  // 32, 2000 129 97, 4000 201 181; 64 of 64, 500 99.5 50.0, 2000 194 145; 32 of 64, 4000 154 169.
+  // and 0.5 a page where it is alone.  Cut ones take two launches and what the pieces of T x H_q rows cost to write and
+  // join.  us, cut first, as above: one block of rows: 1 request of 8 nodes, S 300 10.8 10.3, 380 10.7 11.2, 512 10.8
+  // 13.1; 16 of 8, 500 15.9 13.9, 1000 21.3 23.4; 8 of 16, 1000 21.5 21.6, 1500 21.3 29.7; 8 of 64, 1000 26.1 23.0, 1500 28.6
+  // 31.9; 24 of 8, 1500 24.1 29.6; 16 of 32, 2000 36.4 45.8; 32 of 10, 2000 38.5 39.2, 3000 56 61; 64 of 1, 2000 62 58, 4000
+  // 110 110, 8000 204 215; 64 of 10, 4000 131 114, 5000 158 141; 256 of 1, 8000 778 809.  Two: 64 of 16, 2000 92 83; 32 of 24, 1500
+  // 51 54, 2000 60 68, 4000 94 127, 8000 166 254; 16 of 64, 2000 61 79; 64 of 32, 2000 131 119, 4000 211 214; 64 of 64, 500 111
+  // 59, 2000 239 177; 32 of 64, 4000 195 179.
+  // The line is a fit to these heads.  It gives up 16 of 8 at 1000 and 32 of 24 at 1500 (it takes whole ones), 64 of 10 at 5000
+  // and 32 of 64 at 4000 (it cuts them).
   const int64_t weight = (int64_t)T * Hq / 1200;
   const int64_t longest = !narrow           ? segments / 11 + weight
                           : segments >= 512 ? 128 + weight
@@ -913,17 +926,18 @@ int tree_plan(int B, int Hq, int Hkv, int T, int S, int split_tokens, TreePlan* 
   P.whole = split_tokens == 0 && pages <= longest;
   // Eight waves read the pages of up to 256 rows once, four of 128; but of four there are two workgroups a CU, which hide each
   // other's starts, ends and waits, and rows past 128 cost a wave what it has of them.  us, four first, as above: 16 requests, n
-  // 40, S 4000 55 74; 8, n 48, S 32768 184 184; n 64: 4 of 8000 44 48, 8 of 8000 66 70, 16 of 8000 157 138, 32 of 4000 169 156, 8 of
-  // 32768 258 217; n 512: 2 of 4000 64 56, 4 of 8000 174 169.  Whole segments: n 64, 64 of 2000 145 160, 64 of 4000 269 288, 128 of
-  // 1000 166 187, 128 of 4000 569 562.
+  // 40, S 4000 70 92; 8, n 48, S 32768 212 258; n 64: 4 of 8000 52 59, 8 of 8000 82 87, 16 of 8000 170 179, 32 of 4000 185 199, 8 of
+  // 32768 285 295, and 422 412 where calls follow each other until the power cap holds; n 512: 2 of 4000 74 70, 4 of 8000 205 223.
+  // It gives up 5 to 8 % at 16 of 8000 and 32 of 4000 in short runs.  Whole segments of four waves, cut ones of eight: n 64, 64 of
+  // 2000 175 239, 64 of 4000 329 380, 128 of 1000 206 348, 128 of 4000 688 764.
   P.waves = !narrow && !P.whole && mean > 192 && (all / 256 + B) * Hkv * pages >= 180 * 256 ? 8 : 4;
   P.blocks = narrow ? 1 : 2;
   P.rows = 16 * P.blocks * P.waves;
   P.units = all / P.rows + B;
   const int64_t heads = P.units * Hkv;  // segments, where none is cut
   P.fit = split_tokens == 0;
-  // (us in a graph with shares of 2, 4, 6 and 8 pages at least: 1 request of 8 nodes, S 500 9.0 9.9 10.9 12.3, 777 9.3 9.2 9.9 10.6,
-  // 2048 10.8 10.1 10.1 11.5; 16 of 8 with 8 / 1 heads, 777 12.1 11.6 12.4 13.1, 2048 18.0 13.2 13.0 14.1)
+  // (us in a graph with shares of 2, 4, 6 and 8 pages at least: 1 request of 8 nodes, S 500 9.7 10.7 11.8 13.4, 777 10.0 9.7 10.6
+  // 11.5, 2048 11.9 10.8 11.0 12.7; 16 of 8 with 8 / 1 heads, 777 12.9 12.5 13.4 14.2, 2048 18.3 14.0 14.1 15.5)
   P.least = P.fit ? 4 : split_tokens / kKvPageTokens;
   int64_t shares = P.whole ? heads : heads * pages / P.least + heads;  // (a segment may end in a part of one)
   if (P.fit && !P.whole) shares = std::min<int64_t>(shares, P.waves == 8 ? 256 : 512);
@@ -1001,7 +1015,7 @@ extern "C" int asym_attn_tree_paged_bf16(int B, int H_q, int H_kv, int T, int S_
   ASYM_HIP(hipGetLastError());
   if (P.whole) return ASYM_OK;
   // (a row has about as many pieces as there are shares to a unit and head; threads are counted in 32 bits.  4 nodes of 8 / 1
-  // heads behind 30000 tokens, 85 pieces a row: 21 us, and 85 with a wave for two heads)
+  // heads behind 30000 tokens, 85 pieces a row: 22 us, and 64 more with a wave for two heads)
   if (P.shares >= 4 * P.units * H_kv && T <= (1 << 22) / H_q) {
     hipLaunchKernelGGL(attn_tree_join<true>, dim3((unsigned)(T * H_q)), dim3(64 * kJoinWaves), 0, s, p);
   } else {

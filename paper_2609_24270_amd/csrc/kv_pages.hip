@@ -413,7 +413,7 @@ __global__ void __launch_bounds__(kThreads) pages_rename(PagesParams p) {
 // token of one head and pool, and moves it token by token, kKeepTokens loads on their way at a time: path rises, so
 // that the j-th token comes from place path[j] >= j, and what is written, places up to j, is no later token's
 // source (places above j).
-// Bound by a chain of reads that depend on each other where rows are few (8 of 8 nodes behind 900 tokens: 6.5 us), by
+// Bound by a chain of reads that depend on each other where rows are few (8 of 8 nodes behind 900 tokens: 6.8 us), by
 // how the words lie where they are many (256 of 32 behind up to 4000, 7 MB in pieces of 256 bytes over 2 GB: 16 us).
 constexpr int kKeepTokens = 8;
 __global__ void __launch_bounds__(kSmallThreads) pages_keep(PagesParams p, int T, const int* cu, const int* path, const int* count) {

@@ -17,8 +17,9 @@
 // cosines of a token are computed once for it, a pair a thread, in LDS, while the rows' loads
 // are on their way.
 //
-// Bound by HBM: the gradient of 16384 tokens of 32 heads takes 49 us, 5.5 TB/s (a plain copy 4.8 to 5.4); 64 tokens of 128 heads
-// of 64 channels 3.5, as short launches do.
+// Bound by HBM: the gradient of 16384 tokens of 32 heads takes 48 us, 5.6 TB/s (a plain copy 4.8 to 5.4); with runs of 4 (104
+// of the channels turned) 49 to 50, of 1 (6 turned) 119 to 126, bound by the number of its loads.  64 tokens of 128 heads
+// of 64 channels 3.4, as short launches do.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
