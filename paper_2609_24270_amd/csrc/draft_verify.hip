@@ -27,7 +27,7 @@
 // workgroup a request: it walks to the end (summing slices alone if need be) and draws.
 //
 // Bound by the chain of sums, and each by HBM: only rows that a sum is needed of are read, one a rejection and one for
-// the draw at most.  64 trees of 31 tokens, V 128000, fp32: 54 us in six launches, which read 62, 48, 23, 2, 0 and 2 MB;
+// the draw at most.  64 trees of 31 tokens, V 128000, fp32: 54 us in six launches, which read 63, 49, 23, 2, 0 and 2 MB;
 // bf16 48 to 49 (half the bytes: the launches' starts are most of it), without draft probabilities 18 (one sum a request).  16
 // chains of 4, V 32000: 4.7 and 6.2 us in two, fp32 as bf16.
 // The slices' lengths are chosen for the whole chip, whatever the stream's CUs.
